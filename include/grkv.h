@@ -360,6 +360,108 @@ int grkv_carrier_stats(const void* K, int64_t n, int32_t budget, const grkv_prob
                        const int32_t* idx, const float* stats, void* stream, int32_t* assign,
                        int32_t* counts, float* metrics, float* l_common);
 
+/* ------------------------------------------------------------------------
+ * Pages of a cache.  What a call above returns (retained keys, merged values)
+ * is kept, grown by new tokens, branched and thinned in the pages of one pool.
+ * A unit of the pool is one (sequence, layer, KV head) slice of any length L:
+ * its slot s (0 <= s < L) lies in page table[u][s / page_size], row
+ * s % page_size, so units with budgets of their own share one pool.  All memory
+ * is the caller's:
+ *   k, v       dtype [pages][page_size][head_dim], 16-byte aligned
+ *   table      int32 [units][max_pages]: the pages of each unit in slot order,
+ *              -1 behind them
+ *   lens       int32 [units]: L
+ *   refs       int32 [pages]: how many tables hold each page
+ *   free_bits  uint32 [ceil(pages / 32)]: bit p % 32 of word p / 32 is set where
+ *              page p is in no table (refs[p] = 0)
+ * page_size is a power of two, 16 .. 1024.  table .. free_bits are the calls' to
+ * write (after grkv_pages_init); a page that is not full is in one table only,
+ * which every call keeps so.  New pages are the free ones of lowest number,
+ * handed out in the order of the entries and of the slots of each entry, so a
+ * pool's state never depends on timing. */
+typedef struct {
+  void* k;
+  void* v;
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+  uint32_t* free_bits;
+  int32_t pages, page_size, units, max_pages;
+  int32_t head_dim; /* 64 or 128 */
+  int32_t dtype;    /* grkv_dtype of k and v */
+} grkv_pages;
+
+/* Outcome of one entry of a call on pages, in status[i]. */
+#define GRKV_PAGES_OK 0
+#define GRKV_PAGES_FULL 1   /* too few free pages for this entry and those before it */
+#define GRKV_PAGES_LENGTH 2 /* more rows than the unit's table row holds */
+#define GRKV_PAGES_UNIT 3   /* no such unit; the unit is written by an earlier entry of
+                               the call, or read here and written by another entry; or
+                               the destination of a copy is not empty */
+#define GRKV_PAGES_RANGE 4  /* rows outside their source */
+
+/* The units a call works on, one per entry: device arrays of `entries`
+ * elements.  An entry with a status other than GRKV_PAGES_OK leaves its unit as
+ * it was (one exception: grkv_pages_compact); the others go ahead. */
+typedef struct {
+  int32_t entries;       /* >= 0; with 0 a call does nothing */
+  const int32_t* units;  /* unit of each entry, or NULL: entry i is unit i */
+  int32_t rows;          /* rows per entry (the largest, with counts) */
+  const int32_t* counts; /* rows of each entry, taken to 0 .. rows; NULL: rows each */
+  const int64_t* starts; /* first row of each entry in the packed source of
+                            source_rows rows; NULL: i * rows */
+  int64_t source_rows;
+  int32_t* status;       /* out [entries], or NULL */
+} grkv_page_entries;
+
+/* An empty pool: no unit holds a row, every page is free. */
+int grkv_pages_init(const grkv_pages* pages, void* stream);
+
+/* Appends rows to units: row j of entry i, at slot lens[u] + j, is row
+ * starts[i] + j of k and v [source_rows][head_dim], which have types of their
+ * own (k_out is bf16 beside a float v_out) and are rounded to the pool's, to
+ * nearest even.  k and v are 16-byte aligned and not part of the pool.  A unit
+ * may be in a call once. */
+int grkv_pages_append(const grkv_pages* pages, const grkv_page_entries* entries, const void* k,
+                      int32_t k_dtype, const void* v, int32_t v_dtype, void* stream,
+                      void* workspace, size_t workspace_bytes);
+
+/* Unit dst[i] (int32 [entries], device memory; empty before) becomes a copy of
+ * unit units[i]: the full pages are shared, the rows of a last page that is not
+ * full are copied to one of its own.  A unit may be the source of many entries.
+ * rows, counts, starts and source_rows are not read. */
+int grkv_pages_fork(const grkv_pages* pages, const grkv_page_entries* entries, const int32_t* dst,
+                    void* stream, void* workspace, size_t workspace_bytes);
+
+/* The rows of a unit that are to stay: unit dst[i] becomes slots 0 .. keep[i] - 1
+ * of unit units[i], then its slots idx[starts[i]] .. idx[starts[i] + counts[i] - 1]
+ * (int32 [source_rows], any order, repeats allowed).  dst NULL: in place (the pages
+ * that a unit no longer needs are free after the call); else dst[i] is empty before or
+ * equals units[i].  keep NULL: 0.  idx may be NULL where rows is 0 (a cache taken
+ * back to its first keep[i] slots).  The full pages under keep[i] are shared, or
+ * stay in place; the rows behind them go to new pages, which are taken before the
+ * old ones are given up; only slots taken back in place keep a last page that is
+ * not shared.  keep[i] outside 0 .. L gives GRKV_PAGES_RANGE; an index outside
+ * 0 .. L - 1 too, but then the entry is carried out with a row of zeros there. */
+int grkv_pages_compact(const grkv_pages* pages, const grkv_page_entries* entries,
+                       const int32_t* dst, const int32_t* keep, const int32_t* idx, void* stream,
+                       void* workspace, size_t workspace_bytes);
+
+/* Units give up their rows; a page that no table holds any more is free.  A unit
+ * named twice is freed once; GRKV_PAGES_UNIT is the only status. */
+int grkv_pages_free(const grkv_pages* pages, const grkv_page_entries* entries, void* stream);
+
+/* Workspace bytes of grkv_pages_append, _fork and _compact for this many
+ * entries, 256-byte aligned; 0 if invalid. */
+size_t grkv_pages_workspace_bytes(const grkv_pages* pages, int32_t entries);
+
+/* All of these are asynchronous on stream, allocate nothing and may be captured.
+ * Errors: GRKV_ERR_INVALID for null pointers, misaligned k, v or workspace, sizes out of
+ * range (pages, units, max_pages < 1, pages > 2^30, max_pages * page_size > 2^30, entries or
+ * rows < 0, entries * (rows + page_size) >= 2^31), an unknown dtype;
+ * GRKV_ERR_UNSUPPORTED for another head_dim or page_size;
+ * GRKV_ERR_WORKSPACE; GRKV_ERR_HIP. */
+
 /* Workspace bytes grkv_compress needs for this shape; 0 if the shape is
  * invalid or unsupported. */
 size_t grkv_workspace_bytes(const grkv_problem* prob, int64_t n,

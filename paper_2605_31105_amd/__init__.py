@@ -20,7 +20,9 @@ __all__ = [
     "KEY_CONVERGED", "KEY_MAX_ITER", "KEY_SKIPPED", "KEY_BREAKDOWN", "carrier_stats",
     "CARRIER_METRICS", "compress_ragged", "pyramid_budgets", "adaptive_budgets",
     "workspace_bytes_ragged", "compress_noalloc", "NOALLOC_SCRATCH_BYTES", "h2o_scores",
-    "compress_scored", "h2o_workspace_bytes",
+    "compress_scored", "h2o_workspace_bytes", "Pages", "new_pages", "pages_init", "pages_append",
+    "pages_fork", "pages_compact", "pages_free", "pages_workspace_bytes", "PAGES_OK", "PAGES_FULL",
+    "PAGES_LENGTH", "PAGES_UNIT", "PAGES_RANGE",
 ]
 
 GRKV_OK, GRKV_ERR_INVALID, GRKV_ERR_WORKSPACE, GRKV_ERR_UNSUPPORTED, GRKV_ERR_HIP = 0, -1, -2, -3, -4
@@ -33,9 +35,12 @@ EXPORTED_SYMBOLS = ("grkv_compress", "grkv_workspace_bytes", "grkv_workspace_lay
                     "grkv_workspace_bytes_kv", "grkv_default_key_options", "grkv_carrier_stats",
                     "grkv_compress_ragged", "grkv_workspace_bytes_ragged", "grkv_pyramid_budgets",
                     "grkv_adaptive_budgets", "grkv_compress_noalloc", "grkv_h2o_scores",
-                    "grkv_h2o_workspace_bytes", "grkv_compress_scored")
+                    "grkv_h2o_workspace_bytes", "grkv_compress_scored", "grkv_pages_init",
+                    "grkv_pages_append", "grkv_pages_fork", "grkv_pages_compact",
+                    "grkv_pages_free", "grkv_pages_workspace_bytes")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 KEY_CONVERGED, KEY_MAX_ITER, KEY_SKIPPED, KEY_BREAKDOWN = 1, 2, 3, 4
+PAGES_OK, PAGES_FULL, PAGES_LENGTH, PAGES_UNIT, PAGES_RANGE = 0, 1, 2, 3, 4
 CARRIER_METRICS = ("b", "b_eff", "a_max", "gini", "boundary_fraction", "boundary_share",
                    "enrichment", "boundary_interior_load")
 
@@ -77,6 +82,17 @@ class KeyOptions(ctypes.Structure):
 class Layout(ctypes.Structure):
     _fields_ = [(f, ctypes.c_size_t) for f in
                 ("lse", "y", "score", "pooled", "fixed", "resid", "gram", "z", "total")]
+
+
+class _PagesC(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("k", "v", "table", "lens", "refs", "free_bits")] + [
+        (f, ctypes.c_int32) for f in ("pages", "page_size", "units", "max_pages", "head_dim", "dtype")]
+
+
+class _PageEntries(ctypes.Structure):
+    _fields_ = [("entries", ctypes.c_int32), ("units", ctypes.c_void_p), ("rows", ctypes.c_int32),
+                ("counts", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("source_rows", ctypes.c_int64), ("status", ctypes.c_void_p)]
 
 
 _LIB = None
@@ -148,6 +164,18 @@ def lib() -> ctypes.CDLL:
         L.grkv_adaptive_budgets.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
                                             ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
                                             ctypes.c_void_p, ctypes.c_void_p]
+        vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+        pg, en = P(_PagesC), P(_PageEntries)
+        for name, args in (("init", [pg, vp]),
+                           ("append", [pg, en, vp, i32, vp, i32, vp, vp, sz]),
+                           ("fork", [pg, en, vp, vp, vp, sz]),
+                           ("compact", [pg, en, vp, vp, vp, vp, vp, sz]),
+                           ("free", [pg, en, vp])):
+            fn = getattr(L, "grkv_pages_" + name)
+            fn.restype = ctypes.c_int
+            fn.argtypes = args
+        L.grkv_pages_workspace_bytes.restype = sz
+        L.grkv_pages_workspace_bytes.argtypes = [pg, i32]
         L.grkv_status_string.restype = ctypes.c_char_p
         L.grkv_status_string.argtypes = [ctypes.c_int]
         _LIB = L
@@ -551,3 +579,216 @@ def intermediates(res: Result) -> dict:
         "gram": view(lay.gram, torch.float32, (U, mp, mp))[:, :m, :m],
         "z": view(lay.z, torch.float32, (U, d, mp))[:, :, :m],
     }
+
+
+# ------------------------------------------------------- pages of a cache ----
+
+@dataclass
+class Pages:
+    """The pool of pages of grkv.h (``grkv_pages``): contiguous tensors of one
+    device.  ``new_pages`` makes an empty one."""
+    k: "object"       # bfloat16 or float32 [pages, page_size, head_dim]
+    v: "object"       # the same
+    table: "object"   # int32 [units, max_pages]
+    lens: "object"    # int32 [units]
+    refs: "object"    # int32 [pages]
+    free: "object"    # int32 [ceil(pages / 32)], bit p % 32 of word p // 32: page p is free
+
+    def __post_init__(self):
+        import torch
+
+        k, table, i32 = self.k, self.table, torch.int32
+        if not k.is_cuda:
+            raise ValueError("a pool's tensors must be device tensors")
+        if k.dtype != self.v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("k and v must share dtype bfloat16 or float32")
+        if k.dim() != 3 or k.shape != self.v.shape or table.dim() != 2:
+            raise ValueError("k and v must be [pages, page_size, head_dim] and table [units, max_pages]")
+        n = k.shape[0]
+        if (tuple(self.lens.shape) != (table.shape[0],) or tuple(self.refs.shape) != (n,)
+                or tuple(self.free.shape) != ((n + 31) // 32,)):
+            raise ValueError("lens, refs and free must be [units], [pages] and [ceil(pages / 32)]")
+        for t in (k, self.v, table, self.lens, self.refs, self.free):
+            if not t.is_contiguous() or t.device != k.device:
+                raise ValueError("a pool's tensors must be contiguous and on one device")
+        for t in (table, self.lens, self.refs, self.free):
+            if t.dtype != i32:
+                raise ValueError("table, lens, refs and free must be int32")
+
+    @property
+    def device(self):
+        return self.k.device
+
+    def _c(self):
+        import torch
+
+        k = self.k
+        return _PagesC(k.data_ptr(), self.v.data_ptr(), self.table.data_ptr(),
+                       self.lens.data_ptr(), self.refs.data_ptr(), self.free.data_ptr(),
+                       k.shape[0], k.shape[1], self.table.shape[0], self.table.shape[1],
+                       k.shape[2], GRKV_BF16 if k.dtype == torch.bfloat16 else GRKV_F32)
+
+
+def _on(device, stream):
+    """(torch stream, handle, context): the context allocates on that stream, so that a
+    workspace dropped after the call is not handed to another one while it is in use."""
+    import contextlib
+
+    import torch
+
+    if stream is None:
+        if torch.cuda.current_device() == device.index:
+            return torch.cuda.current_stream(device).cuda_stream, contextlib.nullcontext()
+        stream = torch.cuda.current_stream(device)
+    elif not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _vector(t, name, dtype, size, device):
+    """A device vector of a call, as its address; None stays."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or tuple(t.shape) != (size,):
+        raise ValueError("%s must be a contiguous %s vector of %d on %s" % (name, dtype, size, device))
+    return t.data_ptr()
+
+
+def new_pages(units: int, max_pages: int, pages: int, page_size: int, head_dim: int, dtype=None,
+              device=None, *, stream=None) -> Pages:
+    """An empty pool of ``pages`` pages of ``page_size`` rows for ``units`` units of at most
+    ``max_pages`` pages each."""
+    import torch
+
+    dtype = torch.bfloat16 if dtype is None else dtype
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    if min(units, max_pages, pages, page_size, head_dim) < 1:
+        raise ValueError("a pool needs units, pages and rows")
+    i32 = dict(dtype=torch.int32, device=device)
+    pg = Pages(k=torch.empty((pages, page_size, head_dim), dtype=dtype, device=device),
+               v=torch.empty((pages, page_size, head_dim), dtype=dtype, device=device),
+               table=torch.empty((units, max_pages), **i32), lens=torch.empty(units, **i32),
+               refs=torch.empty(pages, **i32), free=torch.empty((pages + 31) // 32, **i32))
+    return pages_init(pg, stream=stream)
+
+
+def pages_init(pages: Pages, *, stream=None) -> Pages:
+    """Empties a pool: no unit holds a row, every page is free."""
+    handle, on = _on(pages.device, stream)
+    with on:
+        _check(lib().grkv_pages_init(pages._c(), handle))
+    return pages
+
+
+def pages_workspace_bytes(pages: Pages, entries: int) -> int:
+    return int(lib().grkv_pages_workspace_bytes(pages._c(), entries))
+
+
+def _page_call(name, pages, entries, args, *, units, rows, counts, starts, source_rows, status,
+               workspace, stream):
+    """One call on pages; ``args`` are those between the entries and the stream."""
+    import torch
+
+    dev, i32 = pages.device, torch.int32
+    c = pages._c()
+    en = _PageEntries(entries, _vector(units, "units", i32, entries, dev), rows,
+                      _vector(counts, "counts", i32, entries, dev),
+                      _vector(starts, "starts", torch.int64, entries, dev), source_rows, None)
+    handle, on = _on(dev, stream)
+    with on:
+        if status is None:
+            status = torch.empty(entries, dtype=i32, device=dev)
+        en.status = _vector(status, "status", i32, entries, dev)
+        fn = getattr(lib(), "grkv_pages_" + name)
+        if name == "free":
+            _check(fn(c, en, handle))
+            return status
+        need = int(lib().grkv_pages_workspace_bytes(c, entries))
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        _check(fn(c, en, *args, handle, workspace.data_ptr(), workspace.numel()))
+    return status
+
+
+def pages_append(pages: Pages, k, v, *, units=None, counts=None, starts=None, rows=None,
+                 status=None, workspace=None, stream=None):
+    """Appends rows to units (grkv_pages_append).
+
+    k, v: contiguous device tensors, bfloat16 or float32 each (rounded to the pool's type):
+    [E, rows, head_dim], ``rows`` for each of E entries, or packed [N, head_dim] with
+    ``starts`` int64 [E] (the first row of each entry) and ``rows``, a bound on the
+    counts.  ``counts`` int32 [E]: the rows of each entry (default: all ``rows``).
+    ``units`` int32 [E]: their units (default 0 .. E - 1).  Returns the status of every
+    entry, int32 [E] (PAGES_OK or why its unit is as it was)."""
+    import torch
+
+    E, rows, n = _packed(k, 3, rows, starts, "k")
+    types = {torch.bfloat16: GRKV_BF16, torch.float32: GRKV_F32}
+    for t in (k, v):
+        if t.device != pages.device or not t.is_contiguous() or t.dtype not in types:
+            raise ValueError("k and v must be contiguous bfloat16 or float32 tensors on the pool's device")
+    if k.shape != v.shape or k.shape[-1] != pages.k.shape[2]:
+        raise ValueError("shape mismatch: k %s v %s head_dim %d"
+                         % (tuple(k.shape), tuple(v.shape), pages.k.shape[2]))
+    return _page_call("append", pages, E, (k.data_ptr(), types[k.dtype], v.data_ptr(), types[v.dtype]),
+                      units=units, rows=rows, counts=counts, starts=starts, source_rows=n,
+                      status=status, workspace=workspace, stream=stream)
+
+
+def _packed(t, dims, rows, starts, name):
+    """(entries, rows, source rows) of [E, rows, ..] or of packed [N, ..] with starts."""
+    if t.dim() == dims and starts is None:
+        if rows is not None and rows != t.shape[1]:
+            raise ValueError("rows is %s's second size" % name)
+        return t.shape[0], t.shape[1], t.shape[0] * t.shape[1]
+    if t.dim() == dims - 1 and starts is not None and rows is not None:
+        return starts.shape[0], int(rows), t.shape[0]
+    raise ValueError("%s must have %d dimensions, or %d with starts and rows" % (name, dims, dims - 1))
+
+
+def pages_fork(pages: Pages, src, dst, *, status=None, workspace=None, stream=None):
+    """Units ``dst`` (int32 [E], empty) become copies of units ``src``, full pages shared
+    (grkv_pages_fork).  Returns the status of every entry."""
+    import torch
+
+    E = src.shape[0]
+    return _page_call("fork", pages, E, (_vector(dst, "dst", torch.int32, E, pages.device),),
+                      units=src, rows=0, counts=None, starts=None, source_rows=0, status=status,
+                      workspace=workspace, stream=stream)
+
+
+def pages_compact(pages: Pages, idx=None, *, units=None, dst=None, keep=None, counts=None,
+                  starts=None, rows=None, status=None, workspace=None, stream=None):
+    """Units keep their first ``keep`` slots and the slots ``idx`` behind them
+    (grkv_pages_compact), in place or, with ``dst`` (int32 [E]), in empty units.
+
+    idx: int32 [E, rows] (the ``idx`` of ``compress``), or packed [N] with ``starts`` int64
+    [E] and ``rows`` (``compress_ragged``, with its budgets as ``counts``); None takes the
+    units back to ``keep``.  ``units`` int32 [E] (default 0 .. E - 1); ``keep`` int32 [E]
+    (default 0).  Returns the status of every entry."""
+    import torch
+
+    dev, i32 = pages.device, torch.int32
+    if idx is None:
+        if counts is not None or starts is not None or rows:
+            raise ValueError("counts, starts and rows belong to idx")
+        known = next((t for t in (units, keep, dst) if t is not None), None)
+        E, rows, n, at = pages.lens.shape[0] if known is None else known.shape[0], 0, 0, None
+    else:
+        if idx.dtype != i32 or idx.device != dev or not idx.is_contiguous():
+            raise ValueError("idx must be a contiguous int32 tensor on the pool's device")
+        E, rows, n = _packed(idx, 2, rows, starts, "idx")
+        at = idx.data_ptr()
+    args = (_vector(dst, "dst", i32, E, dev), _vector(keep, "keep", i32, E, dev), at)
+    return _page_call("compact", pages, E, args, units=units, rows=rows, counts=counts,
+                      starts=starts, source_rows=n, status=status, workspace=workspace,
+                      stream=stream)
+
+
+def pages_free(pages: Pages, units=None, *, status=None, stream=None):
+    """Units (int32 [E]; default all) give up their rows and pages (grkv_pages_free)."""
+    E = pages.lens.shape[0] if units is None else units.shape[0]
+    return _page_call("free", pages, E, (), units=units, rows=0, counts=None, starts=None,
+                      source_rows=0, status=status, workspace=None, stream=stream)

@@ -288,4 +288,24 @@ hipError_t launch_carrier(const void* K, const int32_t* idx, int U, int64_t n, i
                           const float* stats, int32_t* assign, int32_t* counts, float* metrics,
                           float* l_common, hipStream_t s);
 
+// Pages of a cache (pages.hip).
+enum PagesOp { kPagesInit, kPagesAppend, kPagesFork, kPagesCompact, kPagesFree };
+struct PagesCall {
+  PagesOp op;
+  const grkv_pages* pages;
+  const grkv_page_entries* entries;   // (not of kPagesInit)
+  const int32_t* dst;                 // fork, compact
+  const int32_t* keep;                // compact
+  const int32_t* idx;
+  const void* k;                      // append
+  const void* v;
+  int k_dtype, v_dtype;
+  void* workspace;                    // append, fork, compact
+};
+struct PagesLayout {
+  size_t owner, jobs, ids, total;
+};
+PagesLayout pages_layout(const grkv_pages* pg, int entries);
+hipError_t launch_pages(const PagesCall& c, hipStream_t s);
+
 }  // namespace grkv

@@ -1,0 +1,504 @@
+// Pages of a cache: rows stored in, branched over, picked from and released
+// from the pages of one pool (grkv_pages_append, _fork, _compact, _free).
+//
+// A call that needs new pages is a plan and a copy:
+//  * plan_kernel, one block: checks every entry, counts the pages it needs
+//    (a block scan in the order of the entries), takes the free pages of lowest
+//    number from the bitmap (a block scan over the words' bit counts), and
+//    writes one job per entry.  One block, because the pages that an entry
+//    gets depend on all entries before it; a scan over bits, because a stack
+//    of free pages would hold them in the order in which atomics arrived, so
+//    two runs of the same calls would differ.
+//  * append_kernel / move_kernel: the rows, 16 bytes of K and of V per thread
+//    and step; which entry, row and page a thread serves follows from its
+//    index and the entry's job.  What bounds them is HBM (each row read and
+//    written once) or, for the few rows of a decoding step, the launches.
+//  * commit_kernel (fork, compact): the table rows and reference counts, after
+//    the rows that move_kernel reads through the old table are copied.
+#include "grkv_device.h"
+#include "grkv_internal.h"
+
+namespace grkv {
+namespace {
+
+constexpr int kPlanTh = 1024;
+constexpr int kCopyTh = 256;
+constexpr int kNoOwner = 0x7fffffff;
+
+// What an entry of a call does, written by the plan.  n1 < 0: nothing (a
+// refused entry).
+struct PageJob {
+  int32_t src, dst;
+  int32_t n0, n1;      // rows of src before, rows of dst after
+  int32_t keep;        // rows of dst that are the same slots of src (append: n0)
+  int32_t first;       // first page of dst that is new
+  int32_t last;        // pages of dst after
+  int32_t off;         // the new pages are ids[off ..]
+  int64_t start;       // first row (index) in the packed source
+};
+
+struct PagesK {
+  grkv_pages pg;
+  int shift;            // log2 page_size
+  PagesOp op;
+  int entries, rows;
+  const int32_t* units;
+  const int32_t* dst;
+  const int32_t* counts;
+  const int32_t* keep;
+  const int64_t* starts;
+  int64_t source_rows;
+  int32_t* status;
+  int32_t* owner;       // [units] lowest entry that writes the unit
+  PageJob* jobs;        // [entries]
+  int32_t* ids;         // [pages] pages handed out, in order
+};
+
+__device__ __forceinline__ int load_agent(const int32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Exclusive scan over the block in 64 bits (an entry may ask for 2^26 pages).
+__device__ __forceinline__ uint64_t scan64(uint64_t v, uint64_t* scratch, uint64_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t incl = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint64_t t = __shfl_up((unsigned long long)incl, off);
+    if (lane >= off) incl += t;
+  }
+  if (lane == 63) scratch[wave] = incl;
+  __syncthreads();
+  uint64_t before = 0, all = 0;
+  for (int k = 0; k < kPlanTh / 64; ++k) {
+    const uint64_t s = scratch[k];
+    if (k < wave) before += s;
+    all += s;
+  }
+  __syncthreads();
+  *total = all;
+  return before + incl - v;
+}
+
+__global__ __launch_bounds__(kPlanTh) void plan_kernel(PagesK a) {
+  __shared__ uint64_t scratch[kPlanTh / 64];
+  __shared__ uint32_t scratch32[kPlanTh / 64];
+  __shared__ int used_s;
+  const int tid = threadIdx.x;
+  const int ps = 1 << a.shift;
+  const int64_t cap = (int64_t)a.pg.max_pages << a.shift;
+  auto unit_of = [&](int i) { return a.units ? a.units[i] : i; };
+  auto in_pool = [&](int u) { return (unsigned)u < (unsigned)a.pg.units; };
+
+  // owner[u]: the lowest entry that writes unit u
+  for (int i = tid; i < a.entries; i += kPlanTh) {
+    const int u = unit_of(i), w = a.dst ? a.dst[i] : u;
+    if (in_pool(u)) a.owner[u] = kNoOwner;
+    if (in_pool(w)) a.owner[w] = kNoOwner;
+  }
+  if (tid == 0) used_s = 0;
+  __syncthreads();
+  for (int i = tid; i < a.entries; i += kPlanTh) {
+    const int w = a.dst ? a.dst[i] : unit_of(i);
+    if (in_pool(w)) atomicMin(a.owner + w, i);
+  }
+  __syncthreads();
+
+  // each entry's status and job, but for the pages it gets
+  uint64_t need_all = 0;
+  for (int i0 = 0; i0 < a.entries; i0 += kPlanTh) {
+    const int i = i0 + tid;
+    int st = GRKV_PAGES_OK;
+    PageJob j = {};
+    if (i < a.entries) {
+      j.src = unit_of(i);
+      j.dst = a.dst ? a.dst[i] : j.src;
+      const bool moved = j.dst != j.src;
+      if (!in_pool(j.src) || !in_pool(j.dst) || load_agent(a.owner + j.dst) != i ||
+          (moved && load_agent(a.owner + j.src) != kNoOwner)) {
+        st = GRKV_PAGES_UNIT;
+      } else {
+        j.n0 = a.pg.lens[j.src];
+        int count = a.op == kPagesFork ? 0 : a.rows;
+        if (a.counts) count = min(max(a.counts[i], 0), a.rows);
+        j.start = a.starts ? a.starts[i] : (int64_t)i * a.rows;
+        j.keep = a.op != kPagesCompact ? j.n0 : a.keep ? a.keep[i] : 0;
+        const int64_t n1 = (int64_t)j.keep + count;
+        if (j.n0 < 0 || j.n0 > cap || (moved && a.pg.lens[j.dst] != 0)) {
+          st = GRKV_PAGES_UNIT;
+        } else if (j.keep < 0 || j.keep > j.n0 ||
+                   (count > 0 && (j.start < 0 || j.start > a.source_rows - count))) {
+          st = GRKV_PAGES_RANGE;
+        } else if (n1 > cap) {
+          st = GRKV_PAGES_LENGTH;
+        } else {
+          j.n1 = (int)n1;
+          j.last = (int)((n1 + ps - 1) >> a.shift);
+          if (a.op == kPagesAppend) {
+            j.first = (j.n0 + ps - 1) >> a.shift;
+          } else {
+            j.first = j.keep >> a.shift;
+            // slots taken back in place: a last page of the unit's own stays
+            if (!moved && count == 0 && (j.keep & (ps - 1)) != 0) {
+              const int p = a.pg.table[(size_t)j.src * a.pg.max_pages + j.first];
+              if ((unsigned)p < (unsigned)a.pg.pages && a.pg.refs[p] == 1) ++j.first;
+            }
+          }
+        }
+      }
+      if (st != GRKV_PAGES_OK) j.n1 = -1;
+    }
+    const uint64_t need = st == GRKV_PAGES_OK ? (uint64_t)max(j.last - j.first, 0) : 0;
+    uint64_t total;
+    const uint64_t off = need_all + scan64(need, scratch, &total);
+    need_all += total;
+    if (i < a.entries) {
+      // (an entry whose pages end past the pool's last is refused below)
+      j.off = (int)(off < (uint64_t)a.pg.pages ? off : (uint64_t)a.pg.pages);
+      a.jobs[i] = j;
+      if (a.status) a.status[i] = st;
+    }
+  }
+
+  // the lowest free pages, as many as are asked for: thread t of a step takes
+  // four words, so a step covers 131072 pages
+  const int words = (a.pg.pages + 31) / 32;
+  const uint32_t want = (uint32_t)(need_all < (uint64_t)a.pg.pages ? need_all : (uint64_t)a.pg.pages);
+  uint32_t found = 0;
+  for (int w0 = 0; w0 < words && found < want; w0 += 4 * kPlanTh) {
+    uint32_t bits[4], n = 0, total;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int w = w0 + 4 * tid + k;
+      bits[k] = w < words ? a.pg.free_bits[w] : 0u;
+      n += __popc(bits[k]);
+    }
+    uint32_t r = found + block_exclusive_scan(n, scratch32, &total);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      for (uint32_t b = bits[k]; b != 0 && r < want; b &= b - 1)
+        a.ids[r++] = 32 * (w0 + 4 * tid + k) + __ffs((int)b) - 1;
+    found += total;
+  }
+
+  // entries past the free pages are refused; lengths
+  for (int i = tid; i < a.entries; i += kPlanTh) {
+    PageJob* j = a.jobs + i;
+    if (j->n1 < 0) continue;
+    const int need = j->last - j->first;
+    if (need > 0) {
+      if ((uint64_t)j->off + need > found) {
+        j->n1 = -1;
+        if (a.status) a.status[i] = GRKV_PAGES_FULL;
+        continue;
+      }
+      atomicMax(&used_s, j->off + need);
+    }
+    a.pg.lens[j->dst] = j->n1;
+  }
+  __syncthreads();
+
+  // the bits of the pages handed out
+  const uint32_t used = (uint32_t)used_s;
+  uint32_t before = 0;
+  for (int w0 = 0; w0 < words && before < used; w0 += 4 * kPlanTh) {
+    uint32_t bits[4], n = 0, total;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int w = w0 + 4 * tid + k;
+      bits[k] = w < words ? a.pg.free_bits[w] : 0u;
+      n += __popc(bits[k]);
+    }
+    uint32_t r = before + block_exclusive_scan(n, scratch32, &total);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t b = bits[k];
+      for (; b != 0 && r < used; ++r) b &= b - 1;
+      if (b != bits[k]) a.pg.free_bits[w0 + 4 * tid + k] = b;
+    }
+    before += total;
+  }
+}
+
+// The rows of a launch: row g is row (g % tile + tile * ((g / tile) % per)) of
+// entry g / tile / per, so that the rows of one tile are neighbours and a
+// block serves many entries where each has few.  tile is a power of two.
+struct RowMap {
+  int tile_shift;
+  uint32_t per;       // tiles of an entry
+  uint32_t rows;      // rows of the launch, padded: entries * per << tile_shift
+};
+
+__device__ __forceinline__ void map_row(const RowMap& m, uint32_t g, int* entry, int* row) {
+  const uint32_t t = g >> m.tile_shift, e = t / m.per;
+  *entry = (int)e;
+  *row = (int)(((t - e * m.per) << m.tile_shift) | (g & ((1u << m.tile_shift) - 1)));
+}
+
+// 8 values of a source row as 8 of the pool's type (rounded to nearest even).
+template <typename S, typename T>
+__device__ __forceinline__ void copy8(const S* src, T* dst) {
+  if constexpr (sizeof(S) == sizeof(T)) {
+#pragma unroll
+    for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i)
+      reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(src)[i];
+  } else if constexpr (sizeof(S) == 4) {
+    const float4 x = reinterpret_cast<const float4*>(src)[0], y = reinterpret_cast<const float4*>(src)[1];
+    const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    bf16x8 h;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const bf16x2 p = __builtin_convertvector((f32x2){f[i], f[i + 1]}, bf16x2);
+      h[i] = p[0];
+      h[i + 1] = p[1];
+    }
+    *reinterpret_cast<bf16x8*>(dst) = h;
+  } else {
+    const uint4 w = *reinterpret_cast<const uint4*>(src);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      dst[2 * i] = __uint_as_float(u[i] << 16);
+      dst[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+}
+
+// T, KS, VS: u16 (bf16) or float.
+template <typename T, typename KS, typename VS>
+__global__ __launch_bounds__(kCopyTh) void append_kernel(PagesK a, RowMap m, const KS* k,
+                                                         const VS* v) {
+  const int d = a.pg.head_dim, cpr = d / 8;   // 8 or 16 steps of 8 values per row
+  const int c = (threadIdx.x & (cpr - 1)) * 8;
+  const uint32_t stride = gridDim.x * (kCopyTh / cpr);
+  for (uint32_t g = blockIdx.x * (kCopyTh / cpr) + threadIdx.x / cpr; g < m.rows; g += stride) {
+    int e, row;
+    map_row(m, g, &e, &row);
+    const PageJob j = a.jobs[e];
+    if (row >= j.n1 - j.n0) continue;   // (a refused entry's n1 is -1)
+    const int slot = j.n0 + row, ord = slot >> a.shift;
+    int32_t* entry = a.pg.table + (size_t)j.dst * a.pg.max_pages + ord;
+    int page;
+    if (ord < j.first) {
+      page = *entry;
+      if ((unsigned)page >= (unsigned)a.pg.pages) continue;
+    } else {
+      page = a.ids[j.off + ord - j.first];
+      if (c == 0 && (slot & ((1 << a.shift) - 1)) == 0) {
+        *entry = page;
+        a.pg.refs[page] = 1;
+      }
+    }
+    const size_t to = (((size_t)page << a.shift) + (slot & ((1 << a.shift) - 1))) * d + c;
+    const size_t from = (size_t)(j.start + row) * d + c;
+    copy8(k + from, (T*)a.pg.k + to);
+    copy8(v + from, (T*)a.pg.v + to);
+  }
+}
+
+// Rows of the new pages of a fork or a compaction, read through the old table.
+template <typename T>
+__global__ __launch_bounds__(kCopyTh) void move_kernel(PagesK a, RowMap m, const int32_t* idx) {
+  constexpr int V = 16 / sizeof(T);
+  const int d = a.pg.head_dim, cpr = d / V;   // 8, 16 or 32 chunks per row
+  const int c = (threadIdx.x & (cpr - 1)) * V;
+  const int mask = (1 << a.shift) - 1;
+  const uint32_t stride = gridDim.x * (kCopyTh / cpr);
+  for (uint32_t g = blockIdx.x * (kCopyTh / cpr) + threadIdx.x / cpr; g < m.rows; g += stride) {
+    int e, row;
+    map_row(m, g, &e, &row);
+    const PageJob j = a.jobs[e];
+    const int slot = (j.first << a.shift) + row;
+    if (slot >= j.n1) continue;
+    int from = slot;
+    if (slot >= j.keep) from = idx[j.start + (slot - j.keep)];
+    uint4 rk = make_uint4(0, 0, 0, 0), rv = rk;
+    if ((unsigned)from < (unsigned)j.n0) {
+      const int p = a.pg.table[(size_t)j.src * a.pg.max_pages + (from >> a.shift)];
+      if ((unsigned)p < (unsigned)a.pg.pages) {
+        const size_t at = (((size_t)p << a.shift) + (from & mask)) * d + c;
+        rk = *reinterpret_cast<const uint4*>((const T*)a.pg.k + at);
+        rv = *reinterpret_cast<const uint4*>((const T*)a.pg.v + at);
+      }
+    } else if (c == 0 && a.status) {
+      a.status[e] = GRKV_PAGES_RANGE;
+    }
+    const int page = a.ids[j.off + (slot >> a.shift) - j.first];
+    const size_t to = (((size_t)page << a.shift) + (slot & mask)) * d + c;
+    *reinterpret_cast<uint4*>((T*)a.pg.k + to) = rk;
+    *reinterpret_cast<uint4*>((T*)a.pg.v + to) = rv;
+  }
+}
+
+__device__ __forceinline__ void release_page(const grkv_pages& pg, int p) {
+  if ((unsigned)p >= (unsigned)pg.pages) return;
+  if (atomicSub(pg.refs + p, 1) == 1) atomicOr(pg.free_bits + (p >> 5), 1u << (p & 31));
+}
+
+// One block per entry: the destination's table row, and the counts.  A page
+// that is given up here and shared there (two entries, one page) never passes
+// zero in between: the unit it is shared from keeps it.
+__global__ __launch_bounds__(kCopyTh) void commit_kernel(PagesK a) {
+  const PageJob j = a.jobs[blockIdx.x];
+  if (j.n1 < 0) return;
+  const int32_t* from = a.pg.table + (size_t)j.src * a.pg.max_pages;
+  int32_t* to = a.pg.table + (size_t)j.dst * a.pg.max_pages;
+  if (j.src != j.dst) {
+    for (int o = threadIdx.x; o < j.first; o += kCopyTh) {
+      const int p = from[o];
+      to[o] = p;
+      if ((unsigned)p < (unsigned)a.pg.pages) atomicAdd(a.pg.refs + p, 1);
+    }
+  }
+  const int held = j.src == j.dst ? (j.n0 + (1 << a.shift) - 1) >> a.shift : 0;
+  for (int o = j.first + threadIdx.x; o < max(held, j.last); o += kCopyTh) {
+    if (o < held) release_page(a.pg, to[o]);
+    int p = -1;
+    if (o < j.last) {
+      p = a.ids[j.off + o - j.first];
+      a.pg.refs[p] = 1;
+    }
+    to[o] = p;
+  }
+}
+
+// One block per entry.  The first block to take a unit's length frees it.
+__global__ __launch_bounds__(kCopyTh) void free_kernel(PagesK a) {
+  __shared__ int n_s;
+  const int i = blockIdx.x, u = a.units ? a.units[i] : i;
+  const bool ok = (unsigned)u < (unsigned)a.pg.units;
+  if (threadIdx.x == 0) {
+    if (a.status) a.status[i] = ok ? GRKV_PAGES_OK : GRKV_PAGES_UNIT;
+    n_s = ok ? atomicExch(a.pg.lens + u, 0) : 0;
+  }
+  __syncthreads();
+  const int64_t held = ((int64_t)n_s + (1 << a.shift) - 1) >> a.shift;
+  int32_t* row = a.pg.table + (size_t)u * a.pg.max_pages;
+  for (int o = threadIdx.x; o < held && o < a.pg.max_pages; o += kCopyTh) {
+    release_page(a.pg, row[o]);
+    row[o] = -1;
+  }
+}
+
+__global__ __launch_bounds__(kCopyTh) void init_kernel(PagesK a) {
+  const int64_t stride = (int64_t)gridDim.x * kCopyTh;
+  const int64_t at = (int64_t)blockIdx.x * kCopyTh + threadIdx.x;
+  for (int64_t i = at; i < (int64_t)a.pg.units * a.pg.max_pages; i += stride) a.pg.table[i] = -1;
+  for (int64_t i = at; i < a.pg.units; i += stride) a.pg.lens[i] = 0;
+  for (int64_t i = at; i < a.pg.pages; i += stride) a.pg.refs[i] = 0;
+  for (int64_t i = at; i < (a.pg.pages + 31) / 32; i += stride) {
+    const int64_t left = a.pg.pages - 32 * i;
+    a.pg.free_bits[i] = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
+  }
+}
+
+PagesK make_args(const PagesCall& c) {
+  PagesK a = {};
+  a.pg = *c.pages;
+  a.shift = __builtin_ctz((unsigned)c.pages->page_size);
+  a.op = c.op;
+  if (c.entries) {
+    a.entries = c.entries->entries;
+    a.rows = c.op == kPagesFork ? 0 : c.entries->rows;
+    a.units = c.entries->units;
+    a.status = c.entries->status;
+    if (c.op != kPagesFork) {
+      a.counts = c.entries->counts;
+      a.starts = c.entries->starts;
+      a.source_rows = c.entries->source_rows;
+    }
+  }
+  a.dst = c.dst;
+  a.keep = c.keep;
+  if (c.workspace) {
+    char* ws = (char*)c.workspace;
+    const PagesLayout lay = pages_layout(c.pages, a.entries);
+    a.owner = (int32_t*)(ws + lay.owner);
+    a.jobs = (PageJob*)(ws + lay.jobs);
+    a.ids = (int32_t*)(ws + lay.ids);
+  }
+  return a;
+}
+
+// Rows of at most `most` per entry.
+RowMap make_map(int entries, int64_t most) {
+  RowMap m;
+  m.tile_shift = 0;
+  while (m.tile_shift < 6 && (1 << m.tile_shift) < most) ++m.tile_shift;
+  m.per = (uint32_t)((most + (1 << m.tile_shift) - 1) >> m.tile_shift);
+  m.rows = ((uint32_t)entries * m.per) << m.tile_shift;
+  return m;
+}
+
+// Blocks for that many rows, `per_block` at a time: one step per thread until
+// the card is full eight times over, then more steps.
+unsigned copy_blocks(const RowMap& m, int per_block) {
+  const uint32_t b = (m.rows + per_block - 1) / per_block;
+  return b < 16384 ? b : 16384;
+}
+
+template <typename T, typename KS, typename VS>
+void launch_append(const PagesK& a, const PagesCall& c, hipStream_t s) {
+  const RowMap m = make_map(a.entries, a.rows);
+  hipLaunchKernelGGL((append_kernel<T, KS, VS>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim / 8))),
+                     dim3(kCopyTh), 0, s, a, m, (const KS*)c.k, (const VS*)c.v);
+}
+
+template <typename T>
+void launch_append_t(const PagesK& a, const PagesCall& c, hipStream_t s) {
+  if (c.k_dtype == GRKV_BF16)
+    c.v_dtype == GRKV_BF16 ? launch_append<T, u16, u16>(a, c, s) : launch_append<T, u16, float>(a, c, s);
+  else
+    c.v_dtype == GRKV_BF16 ? launch_append<T, float, u16>(a, c, s) : launch_append<T, float, float>(a, c, s);
+}
+
+}  // namespace
+
+PagesLayout pages_layout(const grkv_pages* pg, int entries) {
+  PagesLayout l;
+  auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
+  l.owner = 0;
+  l.jobs = l.owner + up((size_t)pg->units * sizeof(int32_t));
+  l.ids = l.jobs + up((size_t)entries * sizeof(PageJob));
+  l.total = l.ids + up((size_t)pg->pages * sizeof(int32_t));
+  return l;
+}
+
+hipError_t launch_pages(const PagesCall& c, hipStream_t s) {
+  const PagesK a = make_args(c);
+  if (c.op == kPagesInit) {
+    hipLaunchKernelGGL(init_kernel, dim3(1024), dim3(kCopyTh), 0, s, a);
+    return hipGetLastError();
+  }
+  if (a.entries == 0) return hipSuccess;
+  if (c.op == kPagesFree) {
+    hipLaunchKernelGGL(free_kernel, dim3(a.entries), dim3(kCopyTh), 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanTh), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const bool bf16 = a.pg.dtype == GRKV_BF16;
+  if (c.op == kPagesAppend) {
+    if (a.rows == 0) return hipSuccess;
+    bf16 ? launch_append_t<u16>(a, c, s) : launch_append_t<float>(a, c, s);
+    return hipGetLastError();
+  }
+  // the rows under keep in its page (fork: keep is the length), then the picked ones
+  const int64_t most = (int64_t)a.rows + (c.op == kPagesFork || c.keep ? a.pg.page_size - 1 : 0);
+  if (most > 0) {
+    const RowMap m = make_map(a.entries, most);
+    if (bf16)
+      hipLaunchKernelGGL((move_kernel<u16>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim / 8))),
+                         dim3(kCopyTh), 0, s, a, m, c.idx);
+    else
+      hipLaunchKernelGGL((move_kernel<float>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim / 4))),
+                         dim3(kCopyTh), 0, s, a, m, c.idx);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(commit_kernel, dim3(a.entries), dim3(kCopyTh), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace grkv

@@ -1,0 +1,98 @@
+"""Refusals of the calls on pages, on the CPU: every bad argument is found on the host
+before anything is launched."""
+import ctypes
+
+import pytest
+
+import paper_2605_31105_amd as G
+
+INV, UNS, WS = G.GRKV_ERR_INVALID, G.GRKV_ERR_UNSUPPORTED, G.GRKV_ERR_WORKSPACE
+
+
+@pytest.fixture(scope="module")
+def L():
+    import os
+    if not os.path.exists(G.lib_path()):
+        pytest.skip("libgrkv.so not built")
+    return G.lib()
+
+
+def _pool(**kw):
+    a = dict(k=4096, v=4096, table=4096, lens=4096, refs=4096, free_bits=4096, pages=100,
+             page_size=64, units=8, max_pages=16, head_dim=128, dtype=0)
+    a.update(kw)
+    return G._PagesC(*a.values())
+
+
+def _entries(**kw):
+    a = dict(entries=4, units=4096, rows=3, counts=None, starts=None, source_rows=12, status=None)
+    a.update(kw)
+    return G._PageEntries(*a.values())
+
+
+POOL = [(dict(k=None), INV), (dict(v=None), INV), (dict(table=None), INV), (dict(lens=None), INV),
+        (dict(refs=None), INV), (dict(free_bits=None), INV), (dict(k=4104), INV), (dict(v=4100), INV),
+        (dict(pages=0), INV), (dict(pages=(1 << 30) + 1), INV), (dict(units=0), INV),
+        (dict(max_pages=0), INV), (dict(max_pages=1 << 25, page_size=64), INV),
+        (dict(dtype=2), INV), (dict(page_size=8), UNS), (dict(page_size=48), UNS),
+        (dict(page_size=2048), UNS), (dict(head_dim=96), UNS)]
+ENTRIES = [(dict(entries=-1), INV), (dict(rows=-1), INV), (dict(source_rows=-1), INV),
+           (dict(entries=1 << 20, rows=2048), INV)]
+
+
+@pytest.mark.parametrize("kw,code", POOL)
+def test_bad_pool(L, kw, code):
+    pg, en, ws = _pool(**kw), _entries(), 1 << 30
+    assert L.grkv_pages_workspace_bytes(pg, 4) == 0
+    assert L.grkv_pages_init(pg, None) == code
+    assert L.grkv_pages_append(pg, en, 4096, 0, 4096, 0, None, 4096, ws) == code
+    assert L.grkv_pages_fork(pg, en, 4096, None, 4096, ws) == code
+    assert L.grkv_pages_compact(pg, en, None, 4096, 4096, None, 4096, ws) == code
+    assert L.grkv_pages_free(pg, en, None) == code
+
+
+@pytest.mark.parametrize("kw,code", ENTRIES)
+def test_bad_entries(L, kw, code):
+    pg, en, ws = _pool(), _entries(**kw), 1 << 40
+    assert L.grkv_pages_append(pg, en, 4096, 0, 4096, 0, None, 4096, ws) == code
+    assert L.grkv_pages_compact(pg, en, None, 4096, 4096, None, 4096, ws) == code
+
+
+def test_bad_calls(L):
+    pg, en = _pool(), _entries()
+    need = L.grkv_pages_workspace_bytes(pg, 4)
+    assert need > 0 and need % 256 == 0 and L.grkv_pages_workspace_bytes(pg, -1) == 0
+    for k, kt, v, vt, ws, size, code in [
+            (None, 0, 4096, 0, 4096, need, INV), (4096, 0, None, 0, 4096, need, INV),
+            (4104, 0, 4096, 0, 4096, need, INV), (4096, 2, 4096, 0, 4096, need, INV),
+            (4096, 0, 4096, -1, 4096, need, INV), (4096, 0, 4096, 0, None, need, INV),
+            (4096, 0, 4096, 0, 4096 + 16, need, INV), (4096, 0, 4096, 0, 4096, need - 1, WS)]:
+        assert L.grkv_pages_append(pg, en, k, kt, v, vt, None, ws, size) == code
+    assert L.grkv_pages_append(pg, None, 4096, 0, 4096, 0, None, 4096, need) == INV
+    assert L.grkv_pages_fork(pg, en, None, None, 4096, need) == INV
+    assert L.grkv_pages_fork(pg, en, 4096, None, 4096, need - 1) == WS
+    assert L.grkv_pages_fork(pg, _entries(entries=1 << 25), 4096, None, 4096, 1 << 40) == INV
+    assert L.grkv_pages_compact(pg, en, None, None, None, None, 4096, need) == INV
+    assert L.grkv_pages_compact(pg, en, None, None, 4096, None, 4096, need - 1) == WS
+    assert L.grkv_pages_free(pg, None, None) == INV
+
+
+def test_calls_of_no_entries_do_nothing(L):
+    # (no GPU here: a launch would fail)
+    pg, en = _pool(), _entries(entries=0)
+    assert L.grkv_pages_append(pg, en, None, 0, None, 0, None, None, 0) == 0
+    assert L.grkv_pages_fork(pg, en, None, None, None, 0) == 0
+    assert L.grkv_pages_compact(pg, en, None, None, None, None, None, 0) == 0
+    assert L.grkv_pages_free(pg, en, None) == 0
+
+
+def test_binding_refuses_host_tensors():
+    torch = pytest.importorskip("torch")
+    i32 = dict(dtype=torch.int32)
+    with pytest.raises(ValueError):
+        G.Pages(k=torch.zeros(4, 16, 64), v=torch.zeros(4, 16, 64), table=torch.zeros((2, 2), **i32),
+                lens=torch.zeros(2, **i32), refs=torch.zeros(4, **i32), free=torch.zeros(1, **i32))
+    with pytest.raises(ValueError):
+        G.new_pages(1, 1, 1, 16, 64, device="cpu")
+    with pytest.raises(ValueError):
+        G.new_pages(0, 1, 1, 16, 64, device="cpu")
