@@ -462,6 +462,64 @@ size_t grkv_pages_workspace_bytes(const grkv_pages* pages, int32_t entries);
  * GRKV_ERR_UNSUPPORTED for another head_dim or page_size;
  * GRKV_ERR_WORKSPACE; GRKV_ERR_HIP. */
 
+/* Attention over pages: single tokens, or trees of drafted tokens.  Entry e is a
+ * unit of the pool whose last t slots (t = tokens, or counts[e]) are drafted
+ * tokens, stored there by grkv_pages_append; query i of each of the `group`
+ * heads is the i-th of them.  Token i follows drafted token parents[i] < i, or the
+ * cache itself (-1).  It lies at position L - t + depth (depth: its number of
+ * drafted ancestors) and sees the slots j < L - t before the drafted ones, itself
+ * and its ancestors, of these with window > 0 only positions below n_sink or the
+ * last `window` up to its own (slot j < L - t is position j):
+ *   o = sum_j softmax_j(q . k_j / sqrt(d)) v_j,  lse = ln sum_j exp(q . k_j / sqrt(d)).
+ * A query that sees nothing (or whose weights are all zero) gets o = 0, lse =
+ * -infinity.  What a query does not see never reaches it, infinities and NaN
+ * included. */
+typedef struct {
+  int32_t entries;        /* >= 0; with 0 the call does nothing */
+  int32_t group;          /* query heads per KV head, >= 1 */
+  int32_t tokens;         /* queries per head, 1 .. 64 */
+  const int32_t* units;   /* int32 [entries]: unit of each entry, or NULL: entry e is
+                             unit e.  An entry whose unit is not in the pool sees nothing */
+  const int32_t* counts;  /* int32 [entries]: drafted tokens of each entry, taken to
+                             0 .. tokens; o and lse of queries from counts[e] on stay as
+                             they were.  NULL: tokens each */
+  const int32_t* parents; /* int32 [trees][tokens], or NULL: a chain (each token follows
+                             the one before).  Parents outside -1 .. i - 1 count as -1 */
+  int32_t trees;          /* trees: entries e of equal e / (entries / trees) have one tree;
+                             divides entries (not read without parents) */
+  int32_t window;         /* >= 0; 0: none */
+  int32_t n_sink;         /* >= 0 (not read without a window) */
+} grkv_tree;
+
+/* q, o: pages' dtype [entries][group][tokens][head_dim], 16-byte aligned; lse float
+ * [entries][group][tokens] or NULL.  A logit's weight is rounded to bf16 over bf16
+ * values; sums are float32.  The length of a unit is read on the device.  Errors:
+ * those of the calls on pages; GRKV_ERR_INVALID for bad counts in `tree` (also
+ * entries * group * tokens * head_dim >= 2^40); GRKV_ERR_UNSUPPORTED for
+ * tokens > 64. */
+int grkv_tree_attention(const void* q, const grkv_pages* pages, const grkv_tree* tree, void* o,
+                        float* lse, void* stream, void* workspace, size_t workspace_bytes);
+
+size_t grkv_tree_attention_workspace_bytes(const grkv_pages* pages, const grkv_tree* tree);
+
+/* Causal attention with a sliding window and sink tokens over contiguous keys:
+ * query i of nq is position p = n - nq + i (a whole prompt with nq = n, a chunk of
+ * one, a single token) and sees keys j <= p with j > p - window or j < n_sink;
+ * window 0: all j <= p.
+ *   q, o     dtype [U][G][nq][d]
+ *   K, V     dtype [U][n][d]
+ *   lse      float [U][G][nq], or NULL
+ * all 16-byte aligned; o and lse as in grkv_tree_attention.  Errors:
+ * GRKV_ERR_INVALID (null pointers, nq outside 1 .. n, n > 2^30, window or n_sink
+ * < 0, units or group < 1, an unknown dtype, U * G * nq * d >= 2^40),
+ * GRKV_ERR_UNSUPPORTED (head_dim), GRKV_ERR_WORKSPACE, GRKV_ERR_HIP. */
+int grkv_sink_attention(const void* q, const void* K, const void* V, int64_t n, int32_t nq,
+                        int32_t window, int32_t n_sink, void* stream, const grkv_problem* prob,
+                        void* o, float* lse, void* workspace, size_t workspace_bytes);
+
+size_t grkv_sink_attention_workspace_bytes(const grkv_problem* prob, int64_t n, int32_t nq,
+                                           int32_t window, int32_t n_sink);
+
 /* Workspace bytes grkv_compress needs for this shape; 0 if the shape is
  * invalid or unsupported. */
 size_t grkv_workspace_bytes(const grkv_problem* prob, int64_t n,

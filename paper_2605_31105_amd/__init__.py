@@ -22,7 +22,8 @@ __all__ = [
     "workspace_bytes_ragged", "compress_noalloc", "NOALLOC_SCRATCH_BYTES", "h2o_scores",
     "compress_scored", "h2o_workspace_bytes", "Pages", "new_pages", "pages_init", "pages_append",
     "pages_fork", "pages_compact", "pages_free", "pages_workspace_bytes", "PAGES_OK", "PAGES_FULL",
-    "PAGES_LENGTH", "PAGES_UNIT", "PAGES_RANGE",
+    "PAGES_LENGTH", "PAGES_UNIT", "PAGES_RANGE", "tree_attention", "sink_attention",
+    "tree_attention_workspace_bytes", "sink_attention_workspace_bytes",
 ]
 
 GRKV_OK, GRKV_ERR_INVALID, GRKV_ERR_WORKSPACE, GRKV_ERR_UNSUPPORTED, GRKV_ERR_HIP = 0, -1, -2, -3, -4
@@ -37,7 +38,9 @@ EXPORTED_SYMBOLS = ("grkv_compress", "grkv_workspace_bytes", "grkv_workspace_lay
                     "grkv_adaptive_budgets", "grkv_compress_noalloc", "grkv_h2o_scores",
                     "grkv_h2o_workspace_bytes", "grkv_compress_scored", "grkv_pages_init",
                     "grkv_pages_append", "grkv_pages_fork", "grkv_pages_compact",
-                    "grkv_pages_free", "grkv_pages_workspace_bytes")
+                    "grkv_pages_free", "grkv_pages_workspace_bytes", "grkv_tree_attention",
+                    "grkv_tree_attention_workspace_bytes", "grkv_sink_attention",
+                    "grkv_sink_attention_workspace_bytes")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 KEY_CONVERGED, KEY_MAX_ITER, KEY_SKIPPED, KEY_BREAKDOWN = 1, 2, 3, 4
 PAGES_OK, PAGES_FULL, PAGES_LENGTH, PAGES_UNIT, PAGES_RANGE = 0, 1, 2, 3, 4
@@ -93,6 +96,12 @@ class _PageEntries(ctypes.Structure):
     _fields_ = [("entries", ctypes.c_int32), ("units", ctypes.c_void_p), ("rows", ctypes.c_int32),
                 ("counts", ctypes.c_void_p), ("starts", ctypes.c_void_p),
                 ("source_rows", ctypes.c_int64), ("status", ctypes.c_void_p)]
+
+
+class _Tree(ctypes.Structure):
+    _fields_ = [("entries", ctypes.c_int32), ("group", ctypes.c_int32), ("tokens", ctypes.c_int32),
+                ("units", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("parents", ctypes.c_void_p),
+                ("trees", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32)]
 
 
 _LIB = None
@@ -176,6 +185,15 @@ def lib() -> ctypes.CDLL:
             fn.argtypes = args
         L.grkv_pages_workspace_bytes.restype = sz
         L.grkv_pages_workspace_bytes.argtypes = [pg, i32]
+        L.grkv_tree_attention.restype = ctypes.c_int
+        L.grkv_tree_attention.argtypes = [vp, pg, P(_Tree), vp, vp, vp, vp, sz]
+        L.grkv_tree_attention_workspace_bytes.restype = sz
+        L.grkv_tree_attention_workspace_bytes.argtypes = [pg, P(_Tree)]
+        L.grkv_sink_attention.restype = ctypes.c_int
+        L.grkv_sink_attention.argtypes = [vp, vp, vp, ctypes.c_int64, i32, i32, i32, vp,
+                                          P(Problem), vp, vp, vp, sz]
+        L.grkv_sink_attention_workspace_bytes.restype = sz
+        L.grkv_sink_attention_workspace_bytes.argtypes = [P(Problem), ctypes.c_int64, i32, i32, i32]
         L.grkv_status_string.restype = ctypes.c_char_p
         L.grkv_status_string.argtypes = [ctypes.c_int]
         _LIB = L
@@ -792,3 +810,105 @@ def pages_free(pages: Pages, units=None, *, status=None, stream=None):
     E = pages.lens.shape[0] if units is None else units.shape[0]
     return _page_call("free", pages, E, (), units=units, rows=0, counts=None, starts=None,
                       source_rows=0, status=status, workspace=None, stream=stream)
+
+
+# ---------------------------------------------------- attention over a cache ----
+
+def tree_attention_workspace_bytes(pages: Pages, entries, group, tokens, window=0, n_sink=0) -> int:
+    tr = _Tree(entries, group, tokens, None, None, None, 0, window, n_sink)
+    return int(lib().grkv_tree_attention_workspace_bytes(pages._c(), tr))
+
+
+def _attention(fn, need, q, out, lse, workspace, stream):
+    """Outputs, workspace and stream of an attention call: fn(o, lse, handle, ws, bytes)."""
+    import torch
+
+    dev = q.device
+    for t, dtype, shape, name in ((out, q.dtype, q.shape, "out"),
+                                  (lse, torch.float32, q.shape[:3], "lse")):
+        if torch.is_tensor(t) and (t.dtype != dtype or t.shape != shape or t.device != dev
+                                   or not t.is_contiguous()):
+            raise ValueError("%s must be a contiguous %s tensor %s on %s"
+                             % (name, dtype, tuple(shape), dev))
+    handle, on = _on(dev, stream)
+    with on:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        if lse is True:
+            lse = torch.empty(q.shape[:3], dtype=torch.float32, device=dev)
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        _check(fn(out.data_ptr(), None if lse is None else lse.data_ptr(), handle,
+                  workspace.data_ptr(), workspace.numel()))
+    return out, lse
+
+
+def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, window: int = 0,
+                   n_sink: int = 0, return_lse: bool = False, out=None, lse=None, workspace=None,
+                   stream=None):
+    """Attention of drafted tokens over the pages of a cache (grkv_tree_attention).
+
+    q: [E, G, t, d] of the pool's type; its tokens' keys and values are the last t
+    slots of the units (``pages_append``), so decoding one token is t = 1.
+    ``parents``: int32 [trees, t], trees dividing E (consecutive entries share one), or
+    None for a chain.  ``units``: int32 [E] (default 0 .. E - 1).  ``counts``: int32 [E],
+    the drafted tokens of each entry in a padded batch (the rows behind them stay as they
+    were).  ``window`` > 0: only the last ``window`` positions and the first ``n_sink``.
+    Returns o [E, G, t, d], with ``return_lse`` (o, lse float32 [E, G, t])."""
+    import torch
+
+    dev, i32 = pages.device, torch.int32
+    if q.device != dev or q.dtype != pages.k.dtype or q.dim() != 4 or not q.is_contiguous():
+        raise ValueError("q must be a contiguous [E, G, t, d] tensor of the pool's type and device")
+    E, G, t, d = q.shape
+    if d != pages.k.shape[2]:
+        raise ValueError("head_dim %d, the pool's is %d" % (d, pages.k.shape[2]))
+    trees = 0
+    if parents is not None:
+        trees = parents.shape[0]
+        if (parents.dtype != i32 or parents.device != dev or not parents.is_contiguous()
+                or tuple(parents.shape) != (trees, t)):
+            raise ValueError("parents must be a contiguous int32 [trees, %d] tensor on %s" % (t, dev))
+    c = pages._c()
+    tr = _Tree(E, G, t, _vector(units, "units", i32, E, dev), _vector(counts, "counts", i32, E, dev),
+               None if parents is None else parents.data_ptr(), trees, window, n_sink)
+    L = lib()
+    need = int(L.grkv_tree_attention_workspace_bytes(c, tr))
+    o, lse = _attention(lambda o, l, h, ws, n: L.grkv_tree_attention(q.data_ptr(), c, tr, o, l, h, ws, n),
+                        need, q, out, True if lse is None and return_lse else lse, workspace, stream)
+    return (o, lse) if return_lse else o
+
+
+def sink_attention_workspace_bytes(units, group, head_dim, dtype, n, nq, window, n_sink) -> int:
+    prob = Problem(units, group, head_dim, dtype)
+    return int(lib().grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink))
+
+
+def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = False, out=None,
+                   lse=None, workspace=None, stream=None):
+    """Causal attention with a sliding window and sink tokens (grkv_sink_attention).
+
+    q [U, G, nq, d] (the last nq positions), K and V [U, n, d]: contiguous device tensors of
+    one dtype, bfloat16 or float32.  ``window`` 0: none.  Returns o [U, G, nq, d], with
+    ``return_lse`` (o, lse float32 [U, G, nq])."""
+    import torch
+
+    if not (q.is_cuda and K.device == q.device and V.device == q.device):
+        raise ValueError("q, K and V must be tensors of one device")
+    if not (q.dtype == K.dtype == V.dtype) or K.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("q, K, V must share dtype bfloat16 or float32")
+    if not (q.is_contiguous() and K.is_contiguous() and V.is_contiguous()):
+        raise ValueError("inputs must be contiguous")
+    if (q.dim() != 4 or K.dim() != 3 or K.shape != V.shape or q.shape[0] != K.shape[0]
+            or q.shape[3] != K.shape[2]):
+        raise ValueError("shape mismatch: q %s K %s V %s"
+                         % (tuple(q.shape), tuple(K.shape), tuple(V.shape)))
+    U, G, nq, d = q.shape
+    n = K.shape[1]
+    prob = Problem(U, G, d, GRKV_BF16 if q.dtype == torch.bfloat16 else GRKV_F32)
+    L = lib()
+    need = int(L.grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink))
+    o, lse = _attention(lambda o, l, h, ws, b: L.grkv_sink_attention(
+        q.data_ptr(), K.data_ptr(), V.data_ptr(), n, nq, window, n_sink, h, prob, o, l, ws, b),
+        need, q, out, True if lse is None and return_lse else lse, workspace, stream)
+    return (o, lse) if return_lse else o

@@ -1,0 +1,642 @@
+// Attention of a few query rows over many keys: single tokens and trees of
+// drafted tokens over the pages of a cache (grkv_tree_attention), and the short
+// calls of grkv_sink_attention over contiguous keys.
+//
+// For every query row r and the slots j that it sees,
+//   o_r = sum_j 2^(t_rj - m_r) v_j / sum_j 2^(t_rj - m_r),  t = q . k log2(e) / sqrt(d),
+// in one pass over the keys with a running reference m_r.  Rows are the
+// (query, head of the group) pairs, query-major, 16 RT per block; a unit's keys
+// are split over blocks when there are few units, and over the four waves of a
+// block always.
+//
+//  * A wave walks its own key tiles (32 keys of bf16, 16 of float32) with no
+//    barrier: K fragments go from memory to registers in the MFMA A layout and
+//    V tiles to LDS (global_load_lds), both one tile ahead of the products, so a
+//    compute unit keeps 8 waves x 16 KB in flight.
+//  * S^T = K Q^T puts a query row in each lane column: the four lanes of a row
+//    hold its logits as P^T already lies in the B operand of O^T = V^T P^T (the
+//    order of the keys inside a tile is free as long as V^T uses the same), so P
+//    never leaves the registers.  V^T comes from the row-major tile by the LDS
+//    transpose read.
+//  * The reference of a row moves only when a logit exceeds it by 2^40: float32
+//    sums (and bf16 P) lose nothing by a reference that is too low, so most
+//    tiles need no exchange between lanes.
+//  * P is rounded to bf16 for the product with bf16 values, and o divided by the
+//    sum of the rounded weights (an MFMA with ones), so the weights of a row add
+//    up to one and a row of a single key is exact; the sum behind lse is of the
+//    weights before the rounding.
+//  * Tiles that every row sees whole skip the masks.  In the others an entry
+//    that a row does not see has weight zero, and a tile with an infinity or
+//    NaN among its values adds them by plain multiplications to the rows that
+//    see them only (0 x inf is NaN in a product).
+// Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
+#include "grkv_device.h"
+#include "grkv_internal.h"
+
+#include <type_traits>
+
+namespace grkv {
+namespace {
+
+constexpr int kAtWaves = 4;
+constexpr int kAtTh = 64 * kAtWaves;
+constexpr float kUnset = 3e38f;      // minus the reference of a row without one
+constexpr float kMoveAt = 40.f;      // log2 of the largest weight before a move
+constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
+constexpr float kLn2 = 0.6931471805599453f;
+
+// 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform).
+__device__ __forceinline__ void load_lds16(const char* from, char* lds) {
+  __builtin_amdgcn_global_load_lds(from, (lds_void*)lds, 16, 0, 0);
+}
+
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+template <typename E>
+struct Tile {
+  static constexpr int KEYS = sizeof(E) == 2 ? 32 : 16;   // keys of a wave's tile
+  static constexpr int KT = KEYS / 16;
+};
+
+// The slots a block's rows may see, in tiles of TK: tiles 0 .. at - 1 (sinks)
+// and bt .. (the window), `nt` in all; `full` slots before `lim` and from `lo` on
+// (or among the sinks) are seen by every row.
+struct Span {
+  int at, bt, nt;
+  int kend;        // slots that any row may see end here
+  int lim, lo;
+  int chunk, ns;   // tiles per split, splits in use
+};
+
+__device__ __forceinline__ Span make_span(const AttendK& a, int len, int base, int t, int i0, int i1,
+                                          int tk) {
+  Span s;
+  if (a.lens) {   // drafted tokens i0 .. i1 lie at positions base .. base + t - 1
+    s.kend = t > 0 ? len : 0;
+    s.lim = base;
+    s.lo = base + t - a.window;
+  } else {        // query i is position base + i
+    s.kend = base + i1 + 1;
+    s.lim = base + i0 + 1;
+    s.lo = base + i1 + 1 - a.window;
+  }
+  s.at = s.bt = 0;
+  if (a.window > 0) {
+    const int first = (a.lens ? base : base + i0) + 1 - a.window;
+    s.at = (min(a.n_sink, s.kend) + tk - 1) / tk;
+    s.bt = max(first > 0 ? first / tk : 0, s.at);
+  } else {
+    s.lo = 0;
+  }
+  const int end = (s.kend + tk - 1) / tk;
+  s.nt = s.at + max(0, end - s.bt);
+  // (a sink tile past the end: a.n_sink was cut to kend)
+  s.chunk = max(a.min_tiles, (s.nt + a.splits - 1) / a.splits);
+  s.ns = (s.nt + s.chunk - 1) / s.chunk;
+  return s;
+}
+
+// Block b's entry, row group and split: the row groups of one split follow one
+// another on one XCD (blocks go round the 8 XCDs in turn), which reads its
+// keys from HBM once.
+__device__ __forceinline__ bool block_work(const AttendK& a, int* e, int* rg, int* sp) {
+  const uint32_t b = blockIdx.x, c = b >> 3;
+  const uint32_t w = (c / a.row_groups) * 8 + (b & 7);
+  *rg = (int)(c % a.row_groups);
+  *sp = (int)(w % a.splits);
+  const uint32_t ee = w / a.splits;
+  *e = (int)ee;
+  return ee < (uint32_t)a.entries;
+}
+
+// The length, drafted tokens and table row of entry e.
+__device__ __forceinline__ void entry_shape(const AttendK& a, int e, int* len, int* t,
+                                            const int32_t** row) {
+  if (a.lens) {
+    const int u = a.units ? a.units[e] : e;
+    const bool ok = (unsigned)u < (unsigned)a.pool_units;
+    *len = ok ? min(max(a.lens[u], 0), a.max_pages << a.shift) : 0;
+    *row = a.table + (size_t)(ok ? u : 0) * a.max_pages;
+    *t = a.counts ? min(max(a.counts[e], 0), a.tokens) : a.tokens;
+  } else {
+    *len = a.n;
+    *t = a.tokens;
+    *row = nullptr;
+  }
+}
+
+// Four values of output row `at`: x / l; lse from the reference m and the sum
+// lx of the weights before their rounding.
+template <typename E, int D>
+__device__ __forceinline__ void write_out(const AttendK& a, size_t at, int ch, f32x4 x, float m,
+                                          float l, float lx) {
+  x *= l == 0.f ? 0.f : 1.f / l;
+  if constexpr (sizeof(E) == 2) {
+    uint2 w;
+    w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[0], x[1]}, bf16x2));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2], x[3]}, bf16x2));
+    *reinterpret_cast<uint2*>((E*)a.o + at * D + 4 * ch) = w;
+  } else {
+    *reinterpret_cast<f32x4*>((E*)a.o + at * D + 4 * ch) = x;
+  }
+  if (ch == 0 && a.lse) a.lse[at] = lx == 0.f ? -__builtin_huge_valf() : (m + __log2f(lx)) * kLn2;
+}
+
+template <typename E, int D, int RT, bool PAGED>
+__global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_kernel(AttendK a) {
+  constexpr bool BF = sizeof(E) == 2;
+  constexpr int TK = Tile<E>::KEYS, KT = Tile<E>::KT;
+  constexpr int RB = D * (int)sizeof(E);          // bytes of a row
+  constexpr int CPR = RB / 16;                    // 16-byte chunks of a row
+  constexpr int VB = TK * RB;                     // bytes of a wave's V tile
+  constexpr int NV = VB / 1024;                   // its load instructions
+  constexpr int RPI = 64 / CPR;                   // rows of one of them
+  constexpr int DS = BF ? D / 32 : D / 16;        // 16-byte K fragments of a key
+  constexpr int DT = D / 16;
+  static_assert(2 * VB == 16 * 2 * D * 4, "two stages hold the partial rows of a wave");
+  typedef typename std::conditional<BF, bf16x8, float4>::type Frag;
+
+  __shared__ __attribute__((aligned(16))) char v0_s[kAtWaves * VB];
+  __shared__ __attribute__((aligned(16))) char v1_s[kAtWaves * VB];
+  __shared__ float m_s[kAtWaves][16 * RT], l_s[kAtWaves][16 * RT], x_s[kAtWaves][16 * RT];
+
+  int e, rg, sp;
+  if (!block_work(a, &e, &rg, &sp)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, gq = lane >> 4;
+  const int R = a.group * a.tokens, r0 = rg * 16 * RT;
+  int len, t;
+  const int32_t* trow;
+  entry_shape(a, e, &len, &t, &trow);
+  const int base = len - t;
+  const int i0 = r0 / a.group, i1 = min(r0 + 16 * RT - 1, R - 1) / a.group;
+  const Span sn = make_span(a, len, base, t, i0, i1, TK);
+  const int vt0 = sp * sn.chunk, vt1 = min(sn.nt, vt0 + sn.chunk);
+  if (sp > 0 && vt0 >= sn.nt) return;
+
+  // ancestors (a bit per drafted token) and depth of each drafted token, by
+  // doubling the step from a token to its parent; lane i holds token i
+  uint64_t family = 1ull << lane;
+  int depth = 0;
+  if (PAGED && a.tokens > 1) {
+    const int up = lane >= t ? -1
+                   : a.parents ? a.parents[(size_t)(e / a.per_tree) * a.tokens + lane] : lane - 1;
+    int at = up >= 0 && up < lane ? up : -1;   // (any other parent counts as none)
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+      const uint64_t f = __shfl((unsigned long long)family, at & 63);
+      const int next = __shfl(at, at & 63);
+      if (at >= 0) {
+        family |= f;
+        at = next;
+      }
+    }
+    depth = __popcll(family) - 1;
+    if (a.window > 0 && a.window < t) {
+      // ancestors that have left the window (and are not sinks)
+      uint64_t in = 0;
+      for (int j = 0; j < t; ++j) {
+        const int dj = __builtin_amdgcn_readlane(depth, j);
+        if (depth - dj < a.window || base + dj < a.n_sink) in |= 1ull << j;
+      }
+      family &= in;
+    }
+  }
+
+  // this lane's rows (one per 16-row tile): the slots before lim and from lo
+  // on, or below n_sink, and the drafted ones of `bits`
+  Frag qf[RT][DS];
+  int lim[RT], lo[RT];
+  uint64_t bits[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = r0 + 16 * rt + l16;
+    const int i = r / a.group, g = r - i * a.group;
+    const bool on = r < R && i < t;
+    int pos = base + i;
+    bits[rt] = 0;
+    if (PAGED) {
+      const uint64_t f = __shfl((unsigned long long)family, i & 63);
+      pos = base + __shfl(depth, i & 63);
+      if (on) bits[rt] = f;
+    }
+    lim[rt] = on ? (PAGED ? base : pos + 1) : 0;
+    lo[rt] = a.window > 0 ? pos + 1 - a.window : 0;
+    const E* q = (const E*)a.q + (((size_t)e * a.group + g) * a.tokens + i) * D;
+#pragma unroll
+    for (int ks = 0; ks < DS; ++ks) {
+      if (on) qf[rt][ks] = *reinterpret_cast<const Frag*>(q + (BF ? 32 * ks + 8 * gq : 16 * ks + 4 * gq));
+      else qf[rt][ks] = Frag{};
+    }
+  }
+
+  // lane offsets inside a tile
+  uint32_t ko[KT], vo[NV];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) ko[kt] = l16 * RB + gq * 16;
+  auto swz = [](int row) {
+    return BF ? (D == 128 ? row & 15 : (row >> 1) & 7) : ((row >> 2) & 3) << 2;
+  };
+#pragma unroll
+  for (int it = 0; it < NV; ++it) {
+    const int row = it * RPI + lane / CPR;
+    vo[it] = ((row & 15) * CPR + ((lane % CPR) ^ swz(row))) * 16;
+  }
+  const char* kb = (const char*)a.k;
+  const char* vb = (const char*)a.v;
+  const int last = sn.kend - 1;
+  auto slot_of = [&](int vt) { return (vt < sn.at ? vt : vt - sn.at + sn.bt) * TK; };
+  // byte offset of the 16 rows around `slot` (uniform)
+  auto rows16 = [&](int slot) -> size_t {
+    if (PAGED) {
+      int p = trow[slot >> a.shift];
+      p = (unsigned)p < (unsigned)a.pages ? p : 0;
+      return (((size_t)p << a.shift) + ((slot & ((1 << a.shift) - 1)) & ~15)) * RB;
+    }
+    return ((size_t)e * a.n + (slot & ~15)) * RB;
+  };
+
+  f32x4 acc[DT][RT], accl[RT];
+  float nref[RT], sum[RT];   // sum: this lane's weights before their rounding
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    nref[rt] = kUnset;
+    sum[rt] = 0.f;
+    accl[rt] = zero4();
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt][rt] = zero4();
+  }
+
+  // loads of tile vt: V into the stage `vs`, then K into registers (in that
+  // order: the K fragments' arrival says that V has arrived too).  Rows past the
+  // last slot read the last one again.
+  auto load = [&](int vt, char* vs, Frag (&kf)[KT][DS]) __attribute__((always_inline)) {
+    const int slot0 = slot_of(vt);
+    size_t rb[KT];
+#pragma unroll
+    for (int h = 0; h < KT; ++h)
+      rb[h] = rows16(__builtin_amdgcn_readfirstlane(min(slot0 + 16 * h, last)));
+    const bool whole = slot0 + TK - 1 <= last;
+    auto lane_row = [&](int row) { return min(slot0 + row, last) & 15; };
+    // the stage's last reads are done before its refill is asked for
+    wait_lds();
+#pragma unroll
+    for (int it = 0; it < NV; ++it) {
+      const int h = (it * RPI) / 16;
+      uint32_t o = vo[it];
+      if (!whole) {
+        const int row = it * RPI + lane / CPR;
+        o = (lane_row(row) * CPR + ((lane % CPR) ^ swz(row))) * 16;
+      }
+      load_lds16(vb + rb[h] + o, vs + it * 1024);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      uint32_t o = ko[kt];
+      if (!whole) o = lane_row(16 * kt + l16) * RB + gq * 16;
+#pragma unroll
+      for (int ks = 0; ks < DS; ++ks)
+        kf[kt][ks] = *reinterpret_cast<const Frag*>(kb + rb[kt] + o + ks * 64);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // whether row tile rt's row of this lane sees slot j
+  auto sees = [&](int rt, int j) {
+    bool on = j < lim[rt] && (j >= lo[rt] || j < a.n_sink);
+    if (PAGED) {
+      const int n = j - base;   // drafted token
+      on |= n >= 0 && n < 64 && j < len && (bits[rt] >> (n & 63) & 1) != 0;
+    }
+    return on;
+  };
+  auto step = [&](int vt, char* vs, char* nxt, const Frag (&kf)[KT][DS], Frag (&kn)[KT][DS])
+                  __attribute__((always_inline)) {
+    load(min(vt + kAtWaves, vt1 - 1), nxt, kn);   // (past the end: the last tile again)
+    const int slot0 = slot_of(vt);
+    const bool full = slot0 + TK <= sn.lim && (slot0 >= sn.lo || slot0 + TK <= a.n_sink);
+    // s[kt][rt][i]: slot slot0 + 16 kt + 4 gq + i of row l16
+    f32x4 s[KT][RT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        s[kt][rt] = zero4();
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks) {
+          if constexpr (BF) {
+            s[kt][rt] = mfma_bf16(kf[kt][ks], qf[rt][ks], s[kt][rt]);
+          } else {
+            s[kt][rt] = mfma_f32(kf[kt][ks].x, qf[rt][ks].x, s[kt][rt]);
+            s[kt][rt] = mfma_f32(kf[kt][ks].y, qf[rt][ks].y, s[kt][rt]);
+            s[kt][rt] = mfma_f32(kf[kt][ks].z, qf[rt][ks].z, s[kt][rt]);
+            s[kt][rt] = mfma_f32(kf[kt][ks].w, qf[rt][ks].w, s[kt][rt]);
+          }
+        }
+      }
+    if (!full) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!sees(rt, slot0 + 16 * kt + 4 * gq + i)) s[kt][rt][i] = -__builtin_huge_valf();
+    }
+    bool moved = false;
+    float mx[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      mx[rt] = s[0][rt][0];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[rt] = fmaxf(mx[rt], s[kt][rt][i]);
+      moved |= !(fmaf(mx[rt], a.scale_log2, nref[rt]) <= kMoveAt);
+    }
+    if (__any(moved)) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float m4 = max_over_groups(mx[rt]);
+        if (!(fmaf(m4, a.scale_log2, nref[rt]) <= kMoveAt) && m4 > -__builtin_huge_valf()) {
+          const float f = __builtin_amdgcn_exp2f(-nref[rt] - m4 * a.scale_log2);
+          nref[rt] = -(m4 * a.scale_log2);
+          accl[rt] *= f;
+          sum[rt] *= f;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) acc[dt][rt] *= f;
+        }
+      }
+    }
+    // the weights; a slot that is not seen has logit -inf and weight 0
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[kt][rt][i] = __builtin_amdgcn_exp2f(fmaf(s[kt][rt][i], a.scale_log2, nref[rt]));
+          sum[rt] += s[kt][rt][i];
+        }
+
+    // V^T operand of output columns 16 dt ..: bf16 by the transpose read (lane
+    // 4e + q of a group supplies row 4 gq + e, columns 4q .. 4q + 3), float32 one
+    // value of row 4 gq + i
+    const int row_t = 4 * gq + (l16 >> 2);
+    const int at_t = row_t * RB + ((((l16 >> 1) & 1) ^ swz(row_t)) << 4) + ((l16 & 1) << 3);
+    auto frag = [&](int dt) {
+      const char* p0 = vs + (at_t ^ (dt << 5));
+      // (the chunk order of rows 16 .. 31 is that of rows 0 .. 15)
+      const v4i16 x = ds_read_tr16(p0), y = ds_read_tr16(p0 + 16 * RB);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto elem = [&](int dt, int i) {
+      const int row = 4 * gq + i, ch = 4 * dt + (l16 >> 2);
+      return *reinterpret_cast<const float*>(vs + (row * CPR + (ch ^ swz(row))) * 16 + 4 * (l16 & 3));
+    };
+    bf16x8 p[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      if constexpr (BF) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const bf16x2 h = __builtin_convertvector((f32x2){s[kt][rt][i], s[kt][rt][i + 1]}, bf16x2);
+            p[rt][4 * kt + i] = h[0];
+            p[rt][4 * kt + i + 1] = h[1];
+          }
+        accl[rt] = mfma_bf16(as_bf16x8(make_uint4(kOnes, kOnes, kOnes, kOnes)), p[rt], accl[rt]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) accl[rt] = mfma_f32(1.f, s[0][rt][i], accl[rt]);
+      }
+    }
+    if (!full) {
+      bool odd = false;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        if constexpr (BF) {
+          const uint4 w = __builtin_bit_cast(uint4, frag(dt));
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            odd |= (u[c] & 0x7f80u) == 0x7f80u || (u[c] & 0x7f800000u) == 0x7f800000u;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            odd |= (__float_as_uint(elem(dt, i)) & 0x7f800000u) == 0x7f800000u;
+        }
+      }
+      if (__any(odd)) {   // values that are not finite: key by key, to the rows that see it
+#pragma unroll 1
+        for (int k = 0; k < TK; ++k) {
+          const int own = (k >> 4) * 4 + (k & 3), from = 16 * ((k >> 2) & 3) + l16;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            float w = s[0][rt][0];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (own == 4 * kt + i) w = s[kt][rt][i];
+            if constexpr (BF) w = (float)(__bf16)w;   // as in the product
+            w = __shfl(w, from);
+            const bool on = sees(rt, slot0 + k);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const int byte = (16 * dt + 4 * gq + c) * (int)sizeof(E);
+                const E x = *reinterpret_cast<const E*>(
+                    vs + (k * CPR + ((byte >> 4) ^ swz(k))) * 16 + (byte & 15));
+                float v;
+                if constexpr (BF) v = bf16_to_f32(x);
+                else v = x;
+                if (on) acc[dt][rt][c] = fmaf(w, v, acc[dt][rt][c]);
+              }
+          }
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      if constexpr (BF) {
+        const bf16x8 vf = frag(dt);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[dt][rt] = mfma_bf16(vf, p[rt], acc[dt][rt]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float vf = elem(dt, i);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[dt][rt] = mfma_f32(vf, s[0][rt][i], acc[dt][rt]);
+        }
+      }
+    }
+  };
+  char* va = v0_s + wave * VB;
+  char* vc = v1_s + wave * VB;
+  int vt = vt0 + wave;
+  if (vt < vt1) {
+    Frag ka[KT][DS], kc[KT][DS];
+    load(vt, va, ka);
+    for (;;) {
+      step(vt, va, vc, ka, kc);
+      vt += kAtWaves;
+      if (vt >= vt1) break;
+      step(vt, vc, va, kc, ka);
+      vt += kAtWaves;
+      if (vt >= vt1) break;
+    }
+  }
+
+  // the waves' parts: references, then rows scaled to the largest, summed over
+  // the waves in order.  Every load in flight has to land before its stage is
+  // written here.
+  wait_vmcnt<0>();
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    sum[rt] += __shfl_xor(sum[rt], 16);
+    sum[rt] += __shfl_xor(sum[rt], 32);
+    if (gq == 0) {
+      m_s[wave][16 * rt + l16] = -nref[rt];
+      l_s[wave][16 * rt + l16] = accl[rt][0];
+      x_s[wave][16 * rt + l16] = sum[rt];
+    }
+  }
+  __syncthreads();
+  char* part = (wave < 2 ? v0_s : v1_s) + (wave & 1) * 2 * VB;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = 16 * rt + l16;
+    float m = m_s[0][row];
+#pragma unroll
+    for (int w = 1; w < kAtWaves; ++w) m = fmaxf(m, m_s[w][row]);
+    const float f = __builtin_amdgcn_exp2f(-nref[rt] - m);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      *reinterpret_cast<f32x4*>(part + row * D * 4 + (((4 * dt + gq) ^ l16) << 4)) = acc[dt][rt] * f;
+  }
+  __syncthreads();
+  constexpr int CR = D / 4;   // 4-value chunks of a row
+  for (int c = tid; c < 16 * RT * CR; c += kAtTh) {
+    const int row = c / CR, ch = c % CR, r = r0 + row;
+    const int i = r / a.group, g = r - i * a.group;
+    if (r >= R || i >= t) continue;
+    float m = m_s[0][row], l = 0.f, lx = 0.f;
+#pragma unroll
+    for (int w = 1; w < kAtWaves; ++w) m = fmaxf(m, m_s[w][row]);
+    f32x4 x = zero4();
+#pragma unroll
+    for (int w = 0; w < kAtWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(m_s[w][row] - m);
+      l += l_s[w][row] * f;
+      lx += x_s[w][row] * f;
+      x += *reinterpret_cast<const f32x4*>((w < 2 ? v0_s : v1_s) + (w & 1) * 2 * VB + row * D * 4 +
+                                           ((ch ^ (row & 15)) << 4));
+    }
+    if (sn.ns > 1) {
+      const size_t at = ((size_t)e * a.splits + sp) * R + r;
+      *reinterpret_cast<f32x4*>(a.opart + at * D + 4 * ch) = x;
+      if (ch == 0) a.mpart[at] = make_float4(m, l, lx, 0.f);
+    } else {
+      const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
+      write_out<E, D>(a, at, ch, x, m, l, lx);
+    }
+  }
+}
+
+// The splits of a row in order; one thread per 4 values.
+template <typename E, int D, int RT>
+__global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
+  constexpr int CR = D / 4;
+  const int R = a.group * a.tokens;
+  const int64_t c = (int64_t)blockIdx.x * kAtTh + threadIdx.x;
+  const int64_t row = c / CR;
+  const int ch = (int)(c % CR);
+  const int e = (int)(row / R), r = (int)(row % R);
+  if (e >= a.entries) return;
+  int len, t;
+  const int32_t* trow;
+  entry_shape(a, e, &len, &t, &trow);
+  const int i = r / a.group, g = r - i * a.group;
+  if (i >= t) return;
+  const int r0 = r / (16 * RT) * (16 * RT);
+  const Span sn = make_span(a, len, len - t, t, r0 / a.group, min(r0 + 16 * RT - 1, R - 1) / a.group,
+                            Tile<E>::KEYS);
+  if (sn.ns <= 1) return;
+  const size_t at0 = (size_t)e * a.splits * R + r;
+  float m = -kUnset;
+  for (int s = 0; s < sn.ns; ++s) m = fmaxf(m, a.mpart[at0 + (size_t)s * R].x);
+  float l = 0.f, lx = 0.f;
+  f32x4 x = zero4();
+#pragma unroll 4
+  for (int s = 0; s < sn.ns; ++s) {
+    const float4 ml = a.mpart[at0 + (size_t)s * R];
+    const float f = __builtin_amdgcn_exp2f(ml.x - m);
+    l += ml.y * f;
+    lx += ml.z * f;
+    x += *reinterpret_cast<const f32x4*>(a.opart + (at0 + (size_t)s * R) * D + 4 * ch) * f;
+  }
+  const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
+  write_out<E, D>(a, at, ch, x, m, l, lx);
+}
+
+template <typename E, int D, int RT, bool PAGED>
+hipError_t launch_t(const AttendK& a, hipStream_t s) {
+  const unsigned w = (unsigned)(((int64_t)a.entries * a.splits + 7) / 8 * 8);
+  hipLaunchKernelGGL((attend_kernel<E, D, RT, PAGED>), dim3(w * a.row_groups), dim3(kAtTh), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t n = (int64_t)a.entries * a.group * a.tokens * (D / 4);
+  hipLaunchKernelGGL((combine_kernel<E, D, RT>), dim3((unsigned)((n + kAtTh - 1) / kAtTh)),
+                     dim3(kAtTh), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename E, int D>
+hipError_t launch_d(const AttendK& a, int rt, hipStream_t s) {
+  if (a.lens) return rt == 1 ? launch_t<E, D, 1, true>(a, s) : launch_t<E, D, 2, true>(a, s);
+  return rt == 1 ? launch_t<E, D, 1, false>(a, s) : launch_t<E, D, 2, false>(a, s);
+}
+
+}  // namespace
+
+// Row tiles per block, splits and workspace of a call whose rows see at most
+// `slots` slots each.
+AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots) {
+  AttendPlan p;
+  const int64_t R = (int64_t)group * tokens;
+  p.rt = R <= 16 ? 1 : 2;
+  p.row_groups = (int)((R + 16 * p.rt - 1) / (16 * p.rt));
+  const int tk = dtype == GRKV_BF16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
+  p.min_tiles = 8;
+  const int64_t tiles = (slots + tk - 1) / tk, most = (tiles + p.min_tiles - 1) / p.min_tiles;
+  int64_t s = 1024 / ((int64_t)entries * p.row_groups);
+  s = s < most ? s : most;
+  p.splits = (int)(s < 1 ? 1 : s > 256 ? 256 : s);
+  p.blocks = ((int64_t)entries * p.splits + 7) / 8 * 8 * p.row_groups;
+  auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
+  const size_t rows = p.splits > 1 ? (size_t)entries * p.splits * R : 0;
+  p.opart = 0;
+  p.mpart = up(rows * d * sizeof(float));
+  p.total = p.mpart + up(rows * sizeof(float4));
+  return p;
+}
+
+hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void* workspace,
+                         hipStream_t s) {
+  a.row_groups = p.row_groups;
+  a.splits = p.splits;
+  a.min_tiles = p.min_tiles;
+  a.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
+  a.opart = (float*)((char*)workspace + p.opart);
+  a.mpart = (float4*)((char*)workspace + p.mpart);
+  if (dtype == GRKV_BF16) return d == 64 ? launch_d<u16, 64>(a, p.rt, s) : launch_d<u16, 128>(a, p.rt, s);
+  return d == 64 ? launch_d<float, 64>(a, p.rt, s) : launch_d<float, 128>(a, p.rt, s);
+}
+
+}  // namespace grkv

@@ -308,4 +308,36 @@ struct PagesLayout {
 PagesLayout pages_layout(const grkv_pages* pg, int entries);
 hipError_t launch_pages(const PagesCall& c, hipStream_t s);
 
+// Attention over pages or over contiguous keys (attend.hip).
+struct AttendK {
+  const void* q;      // [entries][group][tokens][d]
+  const void* k;      // pages, or [entries][n][d]
+  const void* v;
+  void* o;            // as q
+  float* lse;         // [entries][group][tokens] or null
+  float* opart;       // [entries][splits][group * tokens][d]
+  float4* mpart;      // [entries][splits][group * tokens] reference, sums
+  int entries, group, tokens;
+  int row_groups, splits, min_tiles;
+  int window, n_sink; // window 0: none
+  float scale_log2;
+  // pages (lens null: contiguous, query i at position n - tokens + i)
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* units;
+  const int32_t* counts;
+  const int32_t* parents;
+  int per_tree;       // entries of a tree
+  int max_pages, shift, pages, pool_units;
+  int n;
+};
+struct AttendPlan {
+  int rt, row_groups, splits, min_tiles;
+  int64_t blocks;
+  size_t opart, mpart, total;
+};
+AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots);
+hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void* workspace,
+                         hipStream_t s);
+
 }  // namespace grkv

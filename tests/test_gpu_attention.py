@@ -1,0 +1,365 @@
+"""Attention over pages (tree_attention) and with a window and sinks over contiguous keys
+(sink_attention) against float64 rows, within the bounds of tests/attention_ref.py."""
+import math
+
+import pytest
+
+from tests.attention_ref import check, rows, sink_seen, tree_seen
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _pool(lens, ps, d, dtype, gen, scale=1.0):
+    """A pool of NaN whose units hold random rows, its pages scattered; rows on the host."""
+    import paper_2605_31105_amd as G
+    held = [-(-n // ps) for n in lens]
+    pages = 2 * sum(held) + 3
+    pg = G.new_pages(len(lens) + 1, max(held + [1]) + 1, pages, ps, d, dtype)
+    pg.k.fill_(math.nan)
+    pg.v.fill_(math.nan)
+    ids = torch.randperm(pages, generator=gen)
+    K, V, at = [], [], 0
+    for u, n in enumerate(lens):
+        K.append((torch.randn((n, d), generator=gen) * scale).to(dtype))
+        V.append(torch.randn((n, d), generator=gen).to(dtype))
+        for j in range(held[u]):
+            p = int(ids[at])
+            at += 1
+            rows_ = slice(j * ps, min(n, (j + 1) * ps))
+            m = rows_.stop - rows_.start
+            pg.k[p, :m] = K[u][rows_].cuda()
+            pg.v[p, :m] = V[u][rows_].cuda()
+            pg.table[u, j] = p
+        pg.lens[u] = n
+    return pg, K, V
+
+
+def _parents(kind, trees, t, gen):
+    if kind == "chain":
+        return None, [list(range(-1, t - 1))] * trees
+    if kind == "flat":
+        p = [[-1] * t] * trees
+    elif kind == "bad":    # not earlier tokens: they count as none
+        p = [[(-5, i, 100, i - 1)[i % 4] for i in range(t)] for _ in range(trees)]
+    else:
+        p = [[int(torch.randint(-1, i, (1,), generator=gen)) if i else -1 for i in range(t)]
+             for _ in range(trees)]
+    return _i32(p), p
+
+
+TREE_CASES = [
+    # dtype, d, page, group, tokens, lens, parents, window, sinks
+    (BF, 128, 64, 4, 1, [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 1000, 5000], "chain", 0, 0),
+    (BF, 64, 16, 1, 5, [0, 3, 5, 6, 20, 33, 200, 4097], "tree", 0, 0),
+    (BF, 128, 32, 5, 33, [33, 34, 100, 2049], "tree", 0, 0),
+    (BF, 128, 256, 8, 64, [64, 70, 700], "tree", 0, 0),
+    (BF, 64, 128, 3, 9, [9, 400, 1300], "bad", 0, 0),
+    (BF, 128, 16, 2, 4, [4, 50, 900, 3000], "flat", 37, 4),
+    (BF, 64, 64, 7, 2, [2, 640, 641, 2100], "chain", 500, 70),
+    (BF, 128, 64, 4, 33, [40, 77, 1000], "tree", 1, 0),
+    (BF, 128, 64, 4, 12, [12, 13, 400], "chain", 5, 14),
+    (BF, 128, 1024, 1, 1, [1, 1023, 1024, 1025, 9000], "chain", 100, 0),
+    (F32, 128, 32, 3, 7, [3, 7, 8, 100, 1500], "tree", 50, 4),
+    (F32, 64, 256, 8, 64, [64, 65, 300, 1025], "chain", 10, 2),
+    (F32, 64, 16, 1, 1, [0, 1, 15, 16, 17, 500], "chain", 0, 0),
+    (F32, 128, 64, 6, 6, [6, 2000], "tree", 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", TREE_CASES, ids=lambda c: "%s-d%d-p%d-g%d-t%d-%s-w%d" % (
+    "bf16" if c[0] == BF else "f32", c[1], c[2], c[3], c[4], c[6], c[7]))
+def test_tree_attention(case):
+    import paper_2605_31105_amd as G
+    dtype, d, ps, group, t, lens, kind, window, n_sink = case
+    gen = torch.Generator().manual_seed(d + ps + t)
+    pg, K, V = _pool(lens, ps, d, dtype, gen)
+    E = len(lens)
+    trees = 2 if E % 2 == 0 else 1
+    parents, plist = _parents(kind, trees, t, gen)
+    q = torch.randn((E, group, t, d), generator=gen).to(dtype)
+    units = torch.randperm(E, generator=gen).tolist()
+    o, lse = G.tree_attention(q.cuda(), pg, parents, units=_i32(units), window=window, n_sink=n_sink,
+                              return_lse=True)
+    torch.cuda.synchronize()
+    for e, u in enumerate(units):
+        seen = tree_seen(lens[u], t, plist[e // (E // trees)], window, n_sink)
+        for g in range(group):
+            check("len %d head %d" % (lens[u], g), o[e, g].cpu(), lse[e, g].cpu(), q[e, g], K[u], V[u], seen)
+
+
+def test_tree_attention_padded_batch_and_bad_units():
+    # ragged drafted tokens: rows behind counts stay as they were; a unit twice; no such unit
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(9)
+    lens = [100, 37, 3, 64]
+    pg, K, V = _pool(lens, 16, 64, BF, gen)
+    t, group = 6, 3
+    units, counts = [0, 1, 1, 3, 2, -1, 99, 4], [6, 0, 2, 9, 5, 2, 3, 1]
+    parents, plist = _parents("tree", 1, t, gen)
+    q = torch.randn((8, group, t, 64), generator=gen).to(BF)
+    o = torch.full(q.shape, 5.0, dtype=BF, device="cuda")
+    lse = torch.full(q.shape[:3], 6.0, device="cuda")
+    G.tree_attention(q.cuda(), pg, parents, units=_i32(units), counts=_i32(counts), out=o, lse=lse)
+    torch.cuda.synchronize()
+    o, lse = o.cpu(), lse.cpu()
+    empty = torch.zeros((0, 64), dtype=BF)
+    for e, (u, c) in enumerate(zip(units, counts)):
+        c = min(c, t)
+        assert (o[e, :, c:] == 5).all() and (lse[e, :, c:] == 6).all()
+        n, Ku, Vu = (lens[u], K[u], V[u]) if 0 <= u < 4 else (0, empty, empty)
+        for g in range(group):
+            check("entry %d" % e, o[e, g, :c], lse[e, g, :c], q[e, g, :c], Ku, Vu,
+                  tree_seen(n, c, plist[0], 0, 0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_what_a_query_does_not_see_never_reaches_it(dtype):
+    # NaN and infinities in the keys and values of a sibling: the rows that do not see it are
+    # those of the finite cache, bit for bit; those that do are not finite
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(3)
+    parents, plist = _i32([[-1, 0, 0, 1, 2, 4]]), [[-1, 0, 0, 1, 2, 4]]
+    pg, K, V = _pool([70], 16, 64, dtype, gen)
+    q = torch.randn((1, 2, 6, 64), generator=gen).to(dtype).cuda()
+    want = G.tree_attention(q, pg, parents, units=_i32([0])).cpu()
+    for where, value in ((2, math.nan), (2, math.inf), (5, -math.inf), (3, math.nan)):
+        slot = 64 + where
+        page, row = int(pg.table[0, slot // 16]), slot % 16
+        for t in (pg.k, pg.v):
+            keep = t[page, row].clone()
+            t[page, row] = value
+            o = G.tree_attention(q, pg, parents, units=_i32([0])).cpu()
+            t[page, row] = keep
+            see = tree_seen(70, 6, plist[0], 0, 0)[:, slot]
+            # (the finite rows may be summed by another instruction: within two steps)
+            near = (o.double() - want.double()).abs() <= 2 * torch.finfo(dtype).eps * want.double().abs() + 1e-6
+            print(where, value, see.tolist(), flush=True)
+            assert near[:, :, ~see].all()
+            if t is pg.v or math.isnan(value):
+                assert not torch.isfinite(o[:, :, see]).all()
+
+
+def test_large_logits_move_the_reference():
+    # logits that grow along the cache by thousands, and a key far above all others
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(5)
+    for dtype in (BF, F32):
+        pg, K, V = _pool([2000], 64, 128, dtype, gen)
+        q = torch.randn((1, 4, 2, 128), generator=gen)
+        q[0, 0, 0] = 0
+        q[0, 0, 0, 0] = 64.0
+        ramp = torch.linspace(-400, 400, 2000)
+        K[0][:, 0] = ramp.to(dtype)
+        K[0][777] = (K[0][777].float() * 300).to(dtype)
+        q = q.to(dtype)
+        pages = pg.table[0, torch.arange(2000, device="cuda") // 64].long()
+        pg.k[pages, torch.arange(2000, device="cuda") % 64] = K[0].cuda()
+        o, lse = G.tree_attention(q.cuda(), pg, units=_i32([0]), return_lse=True)
+        torch.cuda.synchronize()
+        seen = tree_seen(2000, 2, [-1, 0], 0, 0)
+        for g in range(4):
+            check("head %d" % g, o[0, g].cpu(), lse[0, g].cpu(), q[0, g], K[0], V[0], seen)
+
+
+SINK_CASES = [
+    # dtype, d, U, G, n, nq, window, sinks
+    (BF, 128, 1, 1, 1, 1, 0, 0), (BF, 64, 2, 3, 17, 17, 4, 1), (BF, 128, 2, 4, 300, 300, 64, 4),
+    (BF, 128, 1, 4, 1000, 1000, 0, 0), (BF, 128, 2, 5, 700, 37, 100, 9), (BF, 64, 3, 8, 2500, 1, 500, 4),
+    (BF, 128, 1, 2, 513, 513, 1, 0), (BF, 64, 1, 1, 400, 399, 37, 50), (BF, 128, 1, 7, 200, 130, 1000, 4),
+    (BF, 128, 1, 1, 1500, 1500, 256, 300), (BF, 64, 2, 16, 130, 70, 33, 2), (BF, 128, 3, 4, 4100, 2, 0, 0),
+    (F32, 128, 1, 3, 259, 259, 50, 4), (F32, 64, 2, 5, 700, 101, 77, 9), (F32, 128, 2, 4, 1200, 1, 100, 0),
+    (F32, 64, 1, 1, 600, 600, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", SINK_CASES, ids=lambda c: "%s-d%d-u%d-g%d-n%d-q%d-w%d-s%d" % (
+    ("bf16" if c[0] == BF else "f32",) + c[1:]))
+def test_sink_attention(case):
+    import paper_2605_31105_amd as G
+    dtype, d, U, group, n, nq, window, n_sink = case
+    gen = torch.Generator().manual_seed(n + nq + d)
+    q = torch.randn((U, group, nq, d), generator=gen).to(dtype)
+    K, V = (torch.randn((U, n, d), generator=gen).to(dtype) for _ in range(2))
+    o, lse = G.sink_attention(q.cuda(), K.cuda(), V.cuda(), window, n_sink, return_lse=True)
+    torch.cuda.synchronize()
+    seen = sink_seen(n, nq, window, n_sink)
+    for u in range(U):
+        for g in range(group):
+            check("unit %d head %d" % (u, g), o[u, g].cpu(), lse[u, g].cpu(), q[u, g], K[u], V[u], seen)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_later_keys_that_are_not_finite_do_not_reach_earlier_queries(dtype):
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(8)
+    n = 200
+    q = torch.randn((1, 2, n, 64), generator=gen).to(dtype).cuda()
+    K, V = (torch.randn((1, n, 64), generator=gen).to(dtype).cuda() for _ in range(2))
+    want = G.sink_attention(q, K, V, 50, 3)
+    bad = V.clone()
+    bad[0, 101] = math.nan
+    bad[0, 103, 5] = math.inf
+    got = G.sink_attention(q, K, bad, 50, 3)
+    near = (got.double() - want.double()).abs() <= 2 * torch.finfo(dtype).eps * want.double().abs() + 1e-6
+    assert near[0, :, :101].all() and near[0, :, 153:].all()
+    assert torch.isnan(got[0, :, 101:151]).all()
+    assert torch.isinf(got[0, :, 151:153, 5]).all()
+
+
+def test_window_calls_agree_with_each_other():
+    # the last queries of a prompt, a chunk of it and single tokens give the prompt's rows
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(2)
+    q = torch.randn((2, 4, 777, 128), generator=gen).cuda()
+    K, V = (torch.randn((2, 777, 128), generator=gen).cuda() for _ in range(2))
+    whole = G.sink_attention(q, K, V, 100, 4)
+    part = G.sink_attention(q[:, :, 700:].contiguous(), K, V, 100, 4)
+    assert (whole[:, :, 700:] - part).abs().max() < 1e-5
+    for p in (0, 3, 4, 99, 104, 500):
+        one = G.sink_attention(q[:, :, p:p + 1].contiguous(), K[:, :p + 1].contiguous(),
+                               V[:, :p + 1].contiguous(), 100, 4)
+        assert (whole[:, :, p:p + 1] - one).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("units,group,tokens", [(8, 4, 1), (300, 2, 1), (700, 1, 3), (4, 8, 64)])
+def test_long_units_with_and_without_splits(units, group, tokens):
+    # splits are a matter of the call's size: against torch in float64 on the GPU
+    import paper_2605_31105_amd as G
+    g = torch.Generator(device="cuda").manual_seed(units)
+    n, ps, d = 1500 if units > 100 else 9000, 64, 128
+    held = -(-n // ps)
+    pg = G.new_pages(units, held, units * held, ps, d)
+    k = torch.randn((units, n, d), device="cuda", generator=g).to(BF)
+    v = torch.randn((units, n, d), device="cuda", generator=g).to(BF)
+    assert not G.pages_append(pg, k, v).any().item()
+    q = torch.randn((units, group, tokens, d), device="cuda", generator=g).to(BF)
+    o, lse = G.tree_attention(q, pg, return_lse=True)
+    again, _ = G.tree_attention(q, pg, return_lse=True)
+    assert torch.equal(o, again)
+    for u in (0, units // 2, units - 1):
+        seen = tree_seen(n, tokens, list(range(-1, tokens - 1)), 0, 0)
+        for h in range(0, group, 3):
+            check("unit %d" % u, o[u, h].cpu(), lse[u, h].cpu(), q[u, h].cpu(), k[u].cpu(), v[u].cpu(), seen)
+
+
+def test_captured_calls_and_another_stream():
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(4)
+    pg, K, V = _pool([900, 50], 64, 128, BF, gen)
+    q = torch.randn((2, 4, 3, 128), generator=gen).to(BF).cuda()
+    Kc, Vc = (torch.randn((2, 300, 128), generator=gen).to(BF).cuda() for _ in range(2))
+    units = _i32([0, 1])
+    want = G.tree_attention(q, pg, units=units), G.sink_attention(q, Kc, Vc, 64)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = G.tree_attention(q, pg, units=units, stream=side), G.sink_attention(q, Kc, Vc, 64, stream=side)
+    handle = G.tree_attention(q, pg, units=units, stream=side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and torch.equal(handle, want[0])
+    outs = torch.empty_like(q), torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G.tree_attention(q, pg, units=units, out=outs[0])
+        G.sink_attention(q, Kc, Vc, 64, out=outs[1])
+    for _ in range(3):
+        outs[0].zero_()
+        outs[1].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs))
+        assert torch.equal(G.tree_attention(q, pg, units=units), want[0])
+    # a length that grew since the capture is the one read
+    pg.lens[1] = 49
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], G.tree_attention(q, pg, units=units))
+
+
+def test_compress_store_attend_and_draft():
+    """The path as it is used: a cache is compressed, stored, attended to by its window (which
+    gives the discrepancy that the compression reported), extended by drafted tokens, and taken
+    down to the accepted ones."""
+    import paper_2605_31105_amd as G
+    import workloads as W
+    from tests.parity import to_device
+    cfg = W.config(2, layers=1, kv_heads=2, n=2048, budget=256)
+    q, K, V = (to_device(a, cfg.dtype) for a in W.make_batch(cfg))
+    U, c, d, w = cfg.units, cfg.budget, cfg.head_dim, cfg.window
+    res = G.compress(q, K, V, w, c, cfg.pool_kernel, cfg.lam)
+    pg = G.new_pages(U + 2, 12, 60, 32, d, F32)
+    assert not G.pages_append(pg, res.k_out, res.v_out).any().item()
+    # the window's queries are the last w slots as a chain: o = X V*
+    o = G.tree_attention(q.float(), pg, units=_i32([0, 1]))
+    Y = G.intermediates(res)["y"].view(U, cfg.group, w, d)
+    D = ((Y - o).double().square().sum((1, 2, 3)) / Y.double().square().sum((1, 2, 3))).cpu()
+    want = res.stats[:, 2].double().cpu()
+    print("D", D.tolist(), "reported", want.tolist(), flush=True)
+    assert ((D - want).abs() <= 2e-3 * want + 1e-9).all()
+    # ragged results go in packed, by their budgets and offsets
+    idx, k_out, v_out, _, offs = G.compress_ragged(q, K, V, w, [200, 77], cfg.pool_kernel, cfg.lam)
+    st = G.pages_append(pg, k_out, v_out, units=_i32([2, 3]), counts=_i32([200, 77]),
+                        starts=torch.from_numpy(offs).cuda(), rows=200)
+    assert not st.any().item() and pg.lens.tolist() == [256, 256, 200, 77]
+    o2 = G.tree_attention(q.float(), pg, units=_i32([2, 3]))
+    for u, (n, at) in enumerate(((200, 0), (77, 200))):
+        seen = tree_seen(n, w, list(range(-1, w - 1)), 0, 0)
+        for g in range(cfg.group):
+            want = rows(q[u, g].float().cpu(), k_out[at:at + n].float().cpu(), v_out[at:at + n].cpu(),
+                        seen, False)
+            assert ((o2[u, g].cpu().double() - want[0]).abs() <= want[2]).all()
+    # four drafted tokens, a tree; tokens 0, 2 and 3 are accepted
+    gen = torch.Generator().manual_seed(1)
+    kd, vd, qd = (torch.randn(s, generator=gen).cuda() for s in ((2, 4, d), (2, 4, d), (2, 4, 4, d)))
+    tree = _i32([[-1, 0, 0, 2]])
+    u01 = _i32([0, 1])
+    G.pages_append(pg, kd, vd, units=u01)
+    tree_o = G.tree_attention(qd, pg, tree, units=u01)
+    st = G.pages_compact(pg, _i32([[256, 258, 259]] * 2), units=u01, keep=_i32([256, 256]))
+    assert not st.any().item() and pg.lens[:2].tolist() == [259, 259]
+    chain_o = G.tree_attention(qd[:, :, [0, 2, 3]].contiguous(), pg, units=u01)
+    assert (chain_o - tree_o[:, :, [0, 2, 3]]).abs().max() < 1e-5
+    G.pages_free(pg)
+    assert pg.free.tolist() == [-1, (1 << 28) - 1]
+
+
+def test_binding_checks():
+    import paper_2605_31105_amd as G
+    pg = G.new_pages(4, 4, 8, 16, 64)
+    q = torch.zeros(4, 2, 3, 64, dtype=BF, device="cuda")
+    K = torch.zeros(4, 5, 64, dtype=BF, device="cuda")
+    for call in (lambda: G.tree_attention(q.float(), pg), lambda: G.tree_attention(q.cpu(), pg),
+                 lambda: G.tree_attention(q.transpose(1, 2), pg), lambda: G.tree_attention(q[0], pg),
+                 lambda: G.tree_attention(q[..., :32].contiguous(), pg),
+                 lambda: G.tree_attention(q, pg, _i32([-1, 0, 1])),
+                 lambda: G.tree_attention(q, pg, _i32([[-1, 0]])),
+                 lambda: G.tree_attention(q, pg, counts=_i32([1])),
+                 lambda: G.tree_attention(q, pg, units=torch.zeros(4, device="cuda")),
+                 lambda: G.tree_attention(q, pg, out=torch.zeros_like(K)),
+                 lambda: G.tree_attention(q, pg, lse=torch.zeros(4, device="cuda")),
+                 lambda: G.sink_attention(q, K, K.float(), 4), lambda: G.sink_attention(q, K, K.cpu(), 4),
+                 lambda: G.sink_attention(q, K[:2], K[:2], 4), lambda: G.sink_attention(q, K[0], K[0], 4),
+                 lambda: G.sink_attention(q, K.transpose(0, 1), K, 4),
+                 lambda: G.sink_attention(q, K, K, 4, out=q.float())):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: G.tree_attention(torch.zeros(4, 1, 65, 64, dtype=BF, device="cuda"), pg),
+                 lambda: G.tree_attention(q, pg, window=-1),
+                 lambda: G.tree_attention(q, pg, _i32([[-1] * 3] * 3)),
+                 lambda: G.sink_attention(q, K[:, :2].contiguous(), K[:, :2].contiguous(), 4),
+                 lambda: G.sink_attention(q, K, K, -1)):
+        with pytest.raises(G.GrkvError):
+            call()
