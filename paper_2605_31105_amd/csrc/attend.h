@@ -1,0 +1,261 @@
+// What the attention kernels share: which slots a block's rows see, how blocks
+// map to work, and the outputs.
+#pragma once
+
+#include "grkv_device.h"
+#include "grkv_internal.h"
+
+namespace grkv {
+
+constexpr float kUnset = 3e38f;      // minus the reference of a row without one
+constexpr float kMoveAt = 40.f;      // log2 of the largest weight before a move
+constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
+constexpr float kLn2 = 0.6931471805599453f;
+
+// The slots a block's rows may see, in tiles of TK: tiles 0 .. at - 1 (sinks)
+// and bt .. (the window), `nt` in all; `full` slots before `lim` and from `lo` on
+// (or among the sinks) are seen by every row.
+struct Span {
+  int at, bt, nt;
+  int kend;        // slots that any row may see end here
+  int lim, lo;
+  int chunk, ns;   // tiles per split, splits in use
+};
+
+__device__ __forceinline__ Span make_span(const AttendK& a, int len, int base, int t, int i0, int i1,
+                                          int tk) {
+  Span s;
+  if (a.lens) {   // drafted tokens i0 .. i1 lie at positions base .. base + t - 1
+    s.kend = t > 0 ? len : 0;
+    s.lim = base;
+    s.lo = base + t - a.window;
+  } else {        // query i is position base + i
+    s.kend = base + i1 + 1;
+    s.lim = base + i0 + 1;
+    s.lo = base + i1 + 1 - a.window;
+  }
+  s.at = s.bt = 0;
+  if (a.window > 0) {
+    const int first = (a.lens ? base : base + i0) + 1 - a.window;
+    s.at = (min(a.n_sink, s.kend) + tk - 1) / tk;
+    s.bt = max(first > 0 ? first / tk : 0, s.at);
+  } else {
+    s.lo = 0;
+  }
+  const int end = (s.kend + tk - 1) / tk;
+  s.nt = s.at + max(0, end - s.bt);
+  // (a sink tile past the end: a.n_sink was cut to kend)
+  s.chunk = max(a.min_tiles, (s.nt + a.splits - 1) / a.splits);
+  s.ns = (s.nt + s.chunk - 1) / s.chunk;
+  return s;
+}
+
+// Block b's entry, row group and split.  Blocks go round the 8 XCDs in turn: with
+// `grouped` the row groups of one split follow one another on one XCD, whose L2
+// then reads the keys once (entries x splits rounded up to 8); fewer splits than
+// that are dealt out row group by row group, so that no XCD is left idle.
+__device__ __forceinline__ bool block_work(const AttendK& a, int* e, int* rg, int* sp) {
+  const uint32_t b = blockIdx.x;
+  uint32_t w;
+  if (a.grouped) {
+    const uint32_t c = b >> 3;
+    w = (c / a.row_groups) * 8 + (b & 7);
+    *rg = (int)(c % a.row_groups);
+  } else {
+    const uint32_t all = (uint32_t)a.entries * a.splits;
+    w = b % all;
+    *rg = (int)(b / all);
+  }
+  *sp = (int)(w % a.splits);
+  const uint32_t ee = w / a.splits;
+  *e = (int)ee;
+  return ee < (uint32_t)a.entries;
+}
+
+// The length, drafted tokens and table row of entry e.
+__device__ __forceinline__ void entry_shape(const AttendK& a, int e, int* len, int* t,
+                                            const int32_t** row) {
+  if (a.lens) {
+    const int u = a.units ? a.units[e] : e;
+    const bool ok = (unsigned)u < (unsigned)a.pool_units;
+    *len = ok ? min(max(a.lens[u], 0), a.max_pages << a.shift) : 0;
+    *row = a.table + (size_t)(ok ? u : 0) * a.max_pages;
+    *t = a.counts ? min(max(a.counts[e], 0), a.tokens) : a.tokens;
+  } else {
+    *len = a.n;
+    *t = a.tokens;
+    *row = nullptr;
+  }
+}
+
+// Four values of output row `at`: x / l; lse from the reference m and the sum
+// lx of the weights before their rounding.
+template <typename E, int D>
+__device__ __forceinline__ void write_out(const AttendK& a, size_t at, int ch, f32x4 x, float m,
+                                          float l, float lx) {
+  x *= l == 0.f ? 0.f : 1.f / l;
+  if constexpr (sizeof(E) == 2) {
+    uint2 w;
+    w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[0], x[1]}, bf16x2));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2], x[3]}, bf16x2));
+    *reinterpret_cast<uint2*>((E*)a.o + at * D + 4 * ch) = w;
+  } else {
+    *reinterpret_cast<f32x4*>((E*)a.o + at * D + 4 * ch) = x;
+  }
+  if (ch == 0 && a.lse) a.lse[at] = lx == 0.f ? -__builtin_huge_valf() : (m + __log2f(lx)) * kLn2;
+}
+
+// What this lane's row sees: slots before lim from lo on or below n_sink, and
+// with pages the drafted tokens of `bits` (slot base + n is bit n).
+struct RowSight {
+  int lim, lo;
+  uint64_t bits;
+};
+
+template <bool PAGED>
+__device__ __forceinline__ bool sees(const RowSight& s, int j, int n_sink, int base, int len) {
+  bool on = j < s.lim && (j >= s.lo || j < n_sink);
+  if (PAGED) {
+    const int n = j - base;
+    on |= n >= 0 && n < 64 && j < len && (s.bits >> (n & 63) & 1) != 0;
+  }
+  return on;
+}
+
+// Drafted token `lane` of entry e: its ancestors and itself (a bit per token) as
+// far as it sees them, and its depth, by doubling the step from a token to its
+// parent.  Every lane of the wave takes part.
+__device__ __forceinline__ void draft_family(const AttendK& a, int e, int t, int base, int lane,
+                                             uint64_t* bits, int* depth) {
+  uint64_t family = 1ull << lane;
+  *depth = 0;
+  if (a.tokens > 1) {
+    const int up = lane >= t ? -1
+                   : a.parents ? a.parents[(size_t)(e / a.per_tree) * a.tokens + lane] : lane - 1;
+    int at = up >= 0 && up < lane ? up : -1;   // (any other parent counts as none)
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+      const uint64_t f = __shfl((unsigned long long)family, at & 63);
+      const int next = __shfl(at, at & 63);
+      if (at >= 0) {
+        family |= f;
+        at = next;
+      }
+    }
+    *depth = __popcll(family) - 1;
+    if (a.window > 0 && a.window < t) {
+      // ancestors that have left the window (and are not sinks)
+      uint64_t in = 0;
+      for (int j = 0; j < t; ++j) {
+        const int dj = __builtin_amdgcn_readlane(*depth, j);
+        if (*depth - dj < a.window || base + dj < a.n_sink) in |= 1ull << j;
+      }
+      family &= in;
+    }
+  }
+  *bits = family;
+}
+
+// The row of (query i, head) with drafted token i's family and depth held by
+// lane i.
+template <bool PAGED>
+__device__ __forceinline__ RowSight row_sight(const AttendK& a, int base, int i, bool on,
+                                              uint64_t family, int depth) {
+  RowSight s;
+  int pos = base + i;
+  s.bits = 0;
+  if (PAGED) {
+    const uint64_t f = __shfl((unsigned long long)family, i & 63);
+    pos = base + __shfl(depth, i & 63);
+    if (on) s.bits = f;
+  }
+  s.lim = on ? (PAGED ? base : pos + 1) : 0;
+  s.lo = a.window > 0 ? pos + 1 - a.window : 0;
+  return s;
+}
+
+// Rows of a split once more, key by key: taken where a tile that some rows see
+// only part of holds an infinity or NaN among its values, since 0 x inf in a
+// product would reach the rows that do not see it.  One wave; rows first ..
+// first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn.  A lane forms the
+// weight of one key of 64, then sums D / 64 columns.
+template <typename E, int D, bool PAGED>
+__device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, int e, int sp, int first,
+                                            int count, int vt0, int vt1, int tk, int len, int t,
+                                            const int32_t* trow, uint64_t family, int depth) {
+  constexpr bool BF = sizeof(E) == 2;
+  constexpr int C = D / 64;
+  const int lane = threadIdx.x & 63, R = a.group * a.tokens, base = len - t;
+  auto value = [](E x) -> float {
+    if constexpr (sizeof(E) == 2) return bf16_to_f32(x);
+    else return x;
+  };
+  auto slot_row = [&](int slot) -> size_t {
+    if (!PAGED) return (size_t)e * a.n + slot;
+    const int p = trow[slot >> a.shift];
+    return ((size_t)((unsigned)p < (unsigned)a.pages ? p : 0) << a.shift) + (slot & ((1 << a.shift) - 1));
+  };
+  for (int n = 0; n < count; ++n) {
+    const int r = first + n, i = r / a.group, g = r - i * a.group;
+    if (r >= R) return;
+    const RowSight sight = row_sight<PAGED>(a, base, i, i < t, family, depth);
+    const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
+    if (i >= t) continue;
+    const E* q = (const E*)a.q + at * D;
+    float m = -kUnset, l = 0.f, lx = 0.f, o[C] = {};
+    for (int vt = vt0; vt < vt1; ++vt) {
+      const int slot0 = (vt < sn.at ? vt : vt - sn.at + sn.bt) * tk;
+      for (int j0 = slot0; j0 < slot0 + tk; j0 += 64) {
+        const int j = j0 + lane;
+        const bool on = j < slot0 + tk && j < sn.kend && sees<PAGED>(sight, j, a.n_sink, base, len);
+        float x = -__builtin_huge_valf();
+        if (on) {
+          const E* k = (const E*)a.k + slot_row(j) * D;
+          x = 0.f;
+          for (int c = 0; c < D; ++c) x = fmaf(value(q[c]), value(k[c]), x);
+          x *= a.scale_log2;
+        }
+        float mx = x;
+        for (int k = 1; k < 64; k <<= 1) mx = fmaxf(mx, __shfl_xor(mx, k));
+        if (mx > m) {
+          const float f = __builtin_amdgcn_exp2f(m - mx);
+          m = mx;
+          l *= f;
+          lx *= f;
+          for (int c = 0; c < C; ++c) o[c] *= f;
+        }
+        const float w = on ? __builtin_amdgcn_exp2f(x - m) : 0.f;
+        float wr = w;
+        if constexpr (BF) wr = (float)(__bf16)w;
+        float s = w, sr = wr;
+        for (int k = 1; k < 64; k <<= 1) {
+          s += __shfl_xor(s, k);
+          sr += __shfl_xor(sr, k);
+        }
+        lx += s;
+        l += sr;
+        for (int k = 0; k < 64; ++k) {
+          const float wk = __shfl(wr, k);
+          if (!__shfl((int)on, k)) continue;
+          const E* v = (const E*)a.v + slot_row(j0 + k) * D;
+          for (int c = 0; c < C; ++c) o[c] = fmaf(wk, value(v[64 * c + lane]), o[c]);
+        }
+      }
+    }
+    if (sn.ns > 1) {
+      const size_t to = ((size_t)e * a.splits + sp) * R + r;
+      for (int c = 0; c < C; ++c) a.opart[to * D + 64 * c + lane] = o[c];
+      if (lane == 0) a.mpart[to] = make_float4(m, l, lx, 0.f);
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      for (int c = 0; c < C; ++c) {
+        E* to = (E*)a.o + at * D + 64 * c + lane;
+        if constexpr (BF) *reinterpret_cast<__bf16*>(to) = (__bf16)(o[c] * inv);
+        else *to = o[c] * inv;
+      }
+      if (lane == 0 && a.lse) a.lse[at] = lx == 0.f ? -__builtin_huge_valf() : (m + __log2f(lx)) * kLn2;
+    }
+  }
+}
+
+}  // namespace grkv

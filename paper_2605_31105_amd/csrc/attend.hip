@@ -26,12 +26,11 @@
 //    up to one and a row of a single key is exact; the sum behind lse is of the
 //    weights before the rounding.
 //  * Tiles that every row sees whole skip the masks.  In the others an entry
-//    that a row does not see has weight zero, and a tile with an infinity or
-//    NaN among its values adds them by plain multiplications to the rows that
-//    see them only (0 x inf is NaN in a product).
+//    that a row does not see has weight zero; where such a tile holds an infinity or
+//    NaN among its values (0 x inf is NaN in a product), the block does its rows
+//    again key by key.
 // Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
-#include "grkv_device.h"
-#include "grkv_internal.h"
+#include "attend.h"
 
 #include <type_traits>
 
@@ -40,11 +39,6 @@ namespace {
 
 constexpr int kAtWaves = 4;
 constexpr int kAtTh = 64 * kAtWaves;
-constexpr float kUnset = 3e38f;      // minus the reference of a row without one
-constexpr float kMoveAt = 40.f;      // log2 of the largest weight before a move
-constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
-constexpr float kLn2 = 0.6931471805599453f;
-
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform).
 __device__ __forceinline__ void load_lds16(const char* from, char* lds) {
   __builtin_amdgcn_global_load_lds(from, (lds_void*)lds, 16, 0, 0);
@@ -57,90 +51,6 @@ struct Tile {
   static constexpr int KEYS = sizeof(E) == 2 ? 32 : 16;   // keys of a wave's tile
   static constexpr int KT = KEYS / 16;
 };
-
-// The slots a block's rows may see, in tiles of TK: tiles 0 .. at - 1 (sinks)
-// and bt .. (the window), `nt` in all; `full` slots before `lim` and from `lo` on
-// (or among the sinks) are seen by every row.
-struct Span {
-  int at, bt, nt;
-  int kend;        // slots that any row may see end here
-  int lim, lo;
-  int chunk, ns;   // tiles per split, splits in use
-};
-
-__device__ __forceinline__ Span make_span(const AttendK& a, int len, int base, int t, int i0, int i1,
-                                          int tk) {
-  Span s;
-  if (a.lens) {   // drafted tokens i0 .. i1 lie at positions base .. base + t - 1
-    s.kend = t > 0 ? len : 0;
-    s.lim = base;
-    s.lo = base + t - a.window;
-  } else {        // query i is position base + i
-    s.kend = base + i1 + 1;
-    s.lim = base + i0 + 1;
-    s.lo = base + i1 + 1 - a.window;
-  }
-  s.at = s.bt = 0;
-  if (a.window > 0) {
-    const int first = (a.lens ? base : base + i0) + 1 - a.window;
-    s.at = (min(a.n_sink, s.kend) + tk - 1) / tk;
-    s.bt = max(first > 0 ? first / tk : 0, s.at);
-  } else {
-    s.lo = 0;
-  }
-  const int end = (s.kend + tk - 1) / tk;
-  s.nt = s.at + max(0, end - s.bt);
-  // (a sink tile past the end: a.n_sink was cut to kend)
-  s.chunk = max(a.min_tiles, (s.nt + a.splits - 1) / a.splits);
-  s.ns = (s.nt + s.chunk - 1) / s.chunk;
-  return s;
-}
-
-// Block b's entry, row group and split: the row groups of one split follow one
-// another on one XCD (blocks go round the 8 XCDs in turn), which reads its
-// keys from HBM once.
-__device__ __forceinline__ bool block_work(const AttendK& a, int* e, int* rg, int* sp) {
-  const uint32_t b = blockIdx.x, c = b >> 3;
-  const uint32_t w = (c / a.row_groups) * 8 + (b & 7);
-  *rg = (int)(c % a.row_groups);
-  *sp = (int)(w % a.splits);
-  const uint32_t ee = w / a.splits;
-  *e = (int)ee;
-  return ee < (uint32_t)a.entries;
-}
-
-// The length, drafted tokens and table row of entry e.
-__device__ __forceinline__ void entry_shape(const AttendK& a, int e, int* len, int* t,
-                                            const int32_t** row) {
-  if (a.lens) {
-    const int u = a.units ? a.units[e] : e;
-    const bool ok = (unsigned)u < (unsigned)a.pool_units;
-    *len = ok ? min(max(a.lens[u], 0), a.max_pages << a.shift) : 0;
-    *row = a.table + (size_t)(ok ? u : 0) * a.max_pages;
-    *t = a.counts ? min(max(a.counts[e], 0), a.tokens) : a.tokens;
-  } else {
-    *len = a.n;
-    *t = a.tokens;
-    *row = nullptr;
-  }
-}
-
-// Four values of output row `at`: x / l; lse from the reference m and the sum
-// lx of the weights before their rounding.
-template <typename E, int D>
-__device__ __forceinline__ void write_out(const AttendK& a, size_t at, int ch, f32x4 x, float m,
-                                          float l, float lx) {
-  x *= l == 0.f ? 0.f : 1.f / l;
-  if constexpr (sizeof(E) == 2) {
-    uint2 w;
-    w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[0], x[1]}, bf16x2));
-    w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2], x[3]}, bf16x2));
-    *reinterpret_cast<uint2*>((E*)a.o + at * D + 4 * ch) = w;
-  } else {
-    *reinterpret_cast<f32x4*>((E*)a.o + at * D + 4 * ch) = x;
-  }
-  if (ch == 0 && a.lse) a.lse[at] = lx == 0.f ? -__builtin_huge_valf() : (m + __log2f(lx)) * kLn2;
-}
 
 template <typename E, int D, int RT, bool PAGED>
 __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_kernel(AttendK a) {
@@ -174,54 +84,19 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   const int vt0 = sp * sn.chunk, vt1 = min(sn.nt, vt0 + sn.chunk);
   if (sp > 0 && vt0 >= sn.nt) return;
 
-  // ancestors (a bit per drafted token) and depth of each drafted token, by
-  // doubling the step from a token to its parent; lane i holds token i
-  uint64_t family = 1ull << lane;
+  uint64_t family = 0;
   int depth = 0;
-  if (PAGED && a.tokens > 1) {
-    const int up = lane >= t ? -1
-                   : a.parents ? a.parents[(size_t)(e / a.per_tree) * a.tokens + lane] : lane - 1;
-    int at = up >= 0 && up < lane ? up : -1;   // (any other parent counts as none)
-#pragma unroll
-    for (int k = 0; k < 6; ++k) {
-      const uint64_t f = __shfl((unsigned long long)family, at & 63);
-      const int next = __shfl(at, at & 63);
-      if (at >= 0) {
-        family |= f;
-        at = next;
-      }
-    }
-    depth = __popcll(family) - 1;
-    if (a.window > 0 && a.window < t) {
-      // ancestors that have left the window (and are not sinks)
-      uint64_t in = 0;
-      for (int j = 0; j < t; ++j) {
-        const int dj = __builtin_amdgcn_readlane(depth, j);
-        if (depth - dj < a.window || base + dj < a.n_sink) in |= 1ull << j;
-      }
-      family &= in;
-    }
-  }
+  if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);
 
-  // this lane's rows (one per 16-row tile): the slots before lim and from lo
-  // on, or below n_sink, and the drafted ones of `bits`
+  // this lane's rows, one per 16-row tile
   Frag qf[RT][DS];
-  int lim[RT], lo[RT];
-  uint64_t bits[RT];
+  RowSight sight[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = r0 + 16 * rt + l16;
     const int i = r / a.group, g = r - i * a.group;
     const bool on = r < R && i < t;
-    int pos = base + i;
-    bits[rt] = 0;
-    if (PAGED) {
-      const uint64_t f = __shfl((unsigned long long)family, i & 63);
-      pos = base + __shfl(depth, i & 63);
-      if (on) bits[rt] = f;
-    }
-    lim[rt] = on ? (PAGED ? base : pos + 1) : 0;
-    lo[rt] = a.window > 0 ? pos + 1 - a.window : 0;
+    sight[rt] = row_sight<PAGED>(a, base, i, on, family, depth);
     const E* q = (const E*)a.q + (((size_t)e * a.group + g) * a.tokens + i) * D;
 #pragma unroll
     for (int ks = 0; ks < DS; ++ks) {
@@ -258,6 +133,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
 
   f32x4 acc[DT][RT], accl[RT];
   float nref[RT], sum[RT];   // sum: this lane's weights before their rounding
+  bool odd = false;          // a value that is not finite in a tile that is not seen whole
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     nref[rt] = kUnset;
@@ -302,15 +178,6 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // whether row tile rt's row of this lane sees slot j
-  auto sees = [&](int rt, int j) {
-    bool on = j < lim[rt] && (j >= lo[rt] || j < a.n_sink);
-    if (PAGED) {
-      const int n = j - base;   // drafted token
-      on |= n >= 0 && n < 64 && j < len && (bits[rt] >> (n & 63) & 1) != 0;
-    }
-    return on;
-  };
   auto step = [&](int vt, char* vs, char* nxt, const Frag (&kf)[KT][DS], Frag (&kn)[KT][DS])
                   __attribute__((always_inline)) {
     load(min(vt + kAtWaves, vt1 - 1), nxt, kn);   // (past the end: the last tile again)
@@ -342,7 +209,8 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!sees(rt, slot0 + 16 * kt + 4 * gq + i)) s[kt][rt][i] = -__builtin_huge_valf();
+            if (!sees<PAGED>(sight[rt], slot0 + 16 * kt + 4 * gq + i, a.n_sink, base, len))
+              s[kt][rt][i] = -__builtin_huge_valf();
     }
     bool moved = false;
     float mx[RT];
@@ -413,8 +281,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
         for (int i = 0; i < 4; ++i) accl[rt] = mfma_f32(1.f, s[0][rt][i], accl[rt]);
       }
     }
-    if (!full) {
-      bool odd = false;
+    if (!full) {   // values that are not finite?
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         if constexpr (BF) {
@@ -428,37 +295,6 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
           for (int i = 0; i < 4; ++i)
             odd |= (__float_as_uint(elem(dt, i)) & 0x7f800000u) == 0x7f800000u;
         }
-      }
-      if (__any(odd)) {   // values that are not finite: key by key, to the rows that see it
-#pragma unroll 1
-        for (int k = 0; k < TK; ++k) {
-          const int own = (k >> 4) * 4 + (k & 3), from = 16 * ((k >> 2) & 3) + l16;
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            float w = s[0][rt][0];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (own == 4 * kt + i) w = s[kt][rt][i];
-            if constexpr (BF) w = (float)(__bf16)w;   // as in the product
-            w = __shfl(w, from);
-            const bool on = sees(rt, slot0 + k);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const int byte = (16 * dt + 4 * gq + c) * (int)sizeof(E);
-                const E x = *reinterpret_cast<const E*>(
-                    vs + (k * CPR + ((byte >> 4) ^ swz(k))) * 16 + (byte & 15));
-                float v;
-                if constexpr (BF) v = bf16_to_f32(x);
-                else v = x;
-                if (on) acc[dt][rt][c] = fmaf(w, v, acc[dt][rt][c]);
-              }
-          }
-        }
-        return;
       }
     }
 #pragma unroll
@@ -497,6 +333,11 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
   wait_vmcnt<0>();
+  if (__syncthreads_or(odd)) {
+    rows_by_key<E, D, PAGED>(a, sn, e, sp, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
+                             family, depth);
+    return;
+  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16);
@@ -550,7 +391,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
 }
 
 // The splits of a row in order; one thread per 4 values.
-template <typename E, int D, int RT>
+template <typename E, int D>
 __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   constexpr int CR = D / 4;
   const int R = a.group * a.tokens;
@@ -564,9 +405,9 @@ __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   entry_shape(a, e, &len, &t, &trow);
   const int i = r / a.group, g = r - i * a.group;
   if (i >= t) return;
-  const int r0 = r / (16 * RT) * (16 * RT);
-  const Span sn = make_span(a, len, len - t, t, r0 / a.group, min(r0 + 16 * RT - 1, R - 1) / a.group,
-                            Tile<E>::KEYS);
+  const int r0 = r / a.rows * a.rows;
+  const Span sn = make_span(a, len, len - t, t, r0 / a.group, min(r0 + a.rows - 1, R - 1) / a.group,
+                            a.tile_keys);
   if (sn.ns <= 1) return;
   const size_t at0 = (size_t)e * a.splits * R + r;
   float m = -kUnset;
@@ -585,42 +426,65 @@ __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   write_out<E, D>(a, at, ch, x, m, l, lx);
 }
 
-template <typename E, int D, int RT, bool PAGED>
-hipError_t launch_t(const AttendK& a, hipStream_t s) {
-  const unsigned w = (unsigned)(((int64_t)a.entries * a.splits + 7) / 8 * 8);
-  hipLaunchKernelGGL((attend_kernel<E, D, RT, PAGED>), dim3(w * a.row_groups), dim3(kAtTh), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t n = (int64_t)a.entries * a.group * a.tokens * (D / 4);
-  hipLaunchKernelGGL((combine_kernel<E, D, RT>), dim3((unsigned)((n + kAtTh - 1) / kAtTh)),
-                     dim3(kAtTh), 0, s, a);
+template <typename E, int D>
+hipError_t launch_d(const AttendK& a, int rt, hipStream_t s) {
+  const dim3 grid((unsigned)a.blocks), th(kAtTh);
+  if constexpr (sizeof(E) == 2) {
+    if (rt == 0) return launch_attend_wide(a, D, s);
+  }
+  if (a.lens) {
+    if (rt == 1) hipLaunchKernelGGL((attend_kernel<E, D, 1, true>), grid, th, 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<E, D, 2, true>), grid, th, 0, s, a);
+  } else {
+    if (rt == 1) hipLaunchKernelGGL((attend_kernel<E, D, 1, false>), grid, th, 0, s, a);
+    else hipLaunchKernelGGL((attend_kernel<E, D, 2, false>), grid, th, 0, s, a);
+  }
   return hipGetLastError();
 }
 
 template <typename E, int D>
-hipError_t launch_d(const AttendK& a, int rt, hipStream_t s) {
-  if (a.lens) return rt == 1 ? launch_t<E, D, 1, true>(a, s) : launch_t<E, D, 2, true>(a, s);
-  return rt == 1 ? launch_t<E, D, 1, false>(a, s) : launch_t<E, D, 2, false>(a, s);
+hipError_t launch_ed(const AttendK& a, int rt, hipStream_t s) {
+  const hipError_t e = launch_d<E, D>(a, rt, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t n = (int64_t)a.entries * a.group * a.tokens * (D / 4);
+  hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((n + kAtTh - 1) / kAtTh)), dim3(kAtTh),
+                     0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-// Row tiles per block, splits and workspace of a call whose rows see at most
-// `slots` slots each.
+// Kernel, splits and workspace of a call whose rows see at most `slots` slots
+// each.
 AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots) {
   AttendPlan p;
   const int64_t R = (int64_t)group * tokens;
-  p.rt = R <= 16 ? 1 : 2;
-  p.row_groups = (int)((R + 16 * p.rt - 1) / (16 * p.rt));
-  const int tk = dtype == GRKV_BF16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
-  p.min_tiles = 8;
-  const int64_t tiles = (slots + tk - 1) / tk, most = (tiles + p.min_tiles - 1) / p.min_tiles;
-  int64_t s = 1024 / ((int64_t)entries * p.row_groups);
+  const bool bf16 = dtype == GRKV_BF16;
+  int64_t target;   // blocks
+  if (bf16 && R > 64) {
+    p.rt = 0;
+    p.rows = R <= 128 ? 128 : 256;
+    p.tile_keys = kWideKeys;
+    p.min_tiles = 8;
+    target = 512;
+  } else {
+    p.rt = R <= 16 ? 1 : 2;
+    p.rows = 16 * p.rt;
+    p.tile_keys = bf16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
+    p.min_tiles = 8;
+    target = 1024;
+  }
+  p.row_groups = (int)((R + p.rows - 1) / p.rows);
+  const int64_t tiles = (slots + p.tile_keys - 1) / p.tile_keys;
+  const int64_t most = (tiles + p.min_tiles - 1) / p.min_tiles;
+  int64_t s = target / ((int64_t)entries * p.row_groups);
   s = s < most ? s : most;
   p.splits = (int)(s < 1 ? 1 : s > 256 ? 256 : s);
-  p.blocks = ((int64_t)entries * p.splits + 7) / 8 * 8 * p.row_groups;
+  const int64_t w = (int64_t)entries * p.splits;
+  p.grouped = w % 8 == 0 || w >= 64;
+  p.blocks = (p.grouped ? (w + 7) / 8 * 8 : w) * p.row_groups;
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
-  const size_t rows = p.splits > 1 ? (size_t)entries * p.splits * R : 0;
+  const size_t rows = p.splits > 1 ? (size_t)w * R : 0;
   p.opart = 0;
   p.mpart = up(rows * d * sizeof(float));
   p.total = p.mpart + up(rows * sizeof(float4));
@@ -632,11 +496,15 @@ hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void*
   a.row_groups = p.row_groups;
   a.splits = p.splits;
   a.min_tiles = p.min_tiles;
+  a.grouped = p.grouped;
+  a.blocks = p.blocks;
+  a.rows = p.rows;
+  a.tile_keys = p.tile_keys;
   a.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
   a.opart = (float*)((char*)workspace + p.opart);
   a.mpart = (float4*)((char*)workspace + p.mpart);
-  if (dtype == GRKV_BF16) return d == 64 ? launch_d<u16, 64>(a, p.rt, s) : launch_d<u16, 128>(a, p.rt, s);
-  return d == 64 ? launch_d<float, 64>(a, p.rt, s) : launch_d<float, 128>(a, p.rt, s);
+  if (dtype == GRKV_BF16) return d == 64 ? launch_ed<u16, 64>(a, p.rt, s) : launch_ed<u16, 128>(a, p.rt, s);
+  return d == 64 ? launch_ed<float, 64>(a, p.rt, s) : launch_ed<float, 128>(a, p.rt, s);
 }
 
 }  // namespace grkv

@@ -319,6 +319,9 @@ struct AttendK {
   float4* mpart;      // [entries][splits][group * tokens] reference, sums
   int entries, group, tokens;
   int row_groups, splits, min_tiles;
+  int rows, tile_keys;   // query rows of a block, keys of a tile
+  int grouped;           // see block_work
+  int64_t blocks;
   int window, n_sink; // window 0: none
   float scale_log2;
   // pages (lens null: contiguous, query i at position n - tokens + i)
@@ -332,11 +335,14 @@ struct AttendK {
   int n;
 };
 struct AttendPlan {
-  int rt, row_groups, splits, min_tiles;
+  int rt;             // 16-row tiles of a block; 0: the wide kernel
+  int row_groups, splits, min_tiles, rows, tile_keys, grouped;
   int64_t blocks;
   size_t opart, mpart, total;
 };
 AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots);
+constexpr int kWideKeys = 64;   // keys of a tile of the wide kernel (attend_wide.hip)
+hipError_t launch_attend_wide(const AttendK& a, int d, hipStream_t s);
 hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void* workspace,
                          hipStream_t s);
 

@@ -49,6 +49,9 @@ int run(const PagesCall& c, void* stream) {
   return launch_pages(c, (hipStream_t)stream) == hipSuccess ? GRKV_OK : GRKV_ERR_HIP;
 }
 
+// A window that holds every slot (and leaves differences of positions in 32 bits).
+constexpr int kAllSlots = (1 << 30) + 64;
+
 // A call's sizes and plan.  A call without splits still asks for 256 bytes, so
 // that 0 says "invalid".
 struct TreeCall {
@@ -77,8 +80,8 @@ int make_tree(const grkv_pages* pg, const grkv_tree* tr, TreeCall* c) {
   a.entries = tr->entries;
   a.group = tr->group;
   a.tokens = tr->tokens;
-  a.window = tr->window;
-  a.n_sink = tr->n_sink;
+  a.window = tr->window < kAllSlots ? tr->window : kAllSlots;
+  a.n_sink = tr->n_sink < kAllSlots ? tr->n_sink : kAllSlots;
   a.table = pg->table;
   a.lens = pg->lens;
   a.units = tr->units;
@@ -108,8 +111,8 @@ int make_sink(const grkv_problem* prob, int64_t n, int32_t nq, int32_t window, i
   a.entries = prob->units;
   a.group = prob->group;
   a.tokens = nq;
-  a.window = window;
-  a.n_sink = n_sink;
+  a.window = window < kAllSlots ? window : kAllSlots;
+  a.n_sink = n_sink < kAllSlots ? n_sink : kAllSlots;
   a.n = (int)n;
   return GRKV_OK;
 }
