@@ -390,40 +390,58 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   }
 }
 
-// The splits of a row in order; one thread per 4 values.
-template <typename E, int D>
+// The splits of a row: one thread per 4 values and every GS-th split, whose sums
+// are added in order.  GS: threads that share a value.
+template <typename E, int D, int GS>
 __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
-  constexpr int CR = D / 4;
-  const int R = a.group * a.tokens;
-  const int64_t c = (int64_t)blockIdx.x * kAtTh + threadIdx.x;
-  const int64_t row = c / CR;
-  const int ch = (int)(c % CR);
+  constexpr int CR = D / 4, ROWS = kAtTh / (CR * GS);   // rows of a block
+  __shared__ f32x4 part[GS > 1 ? kAtTh : 1];
+  __shared__ float2 psum[GS > 1 ? kAtTh : 1];
+  const int R = a.group * a.tokens, tid = threadIdx.x;
+  const int ch = tid % CR, gs = tid / CR % GS;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + tid / (CR * GS);
   const int e = (int)(row / R), r = (int)(row % R);
-  if (e >= a.entries) return;
-  int len, t;
+  bool on = e < a.entries;
+  int len = 0, t = 0;
   const int32_t* trow;
-  entry_shape(a, e, &len, &t, &trow);
+  if (on) entry_shape(a, e, &len, &t, &trow);
   const int i = r / a.group, g = r - i * a.group;
-  if (i >= t) return;
-  const int r0 = r / a.rows * a.rows;
-  const Span sn = make_span(a, len, len - t, t, r0 / a.group, min(r0 + a.rows - 1, R - 1) / a.group,
-                            a.tile_keys);
-  if (sn.ns <= 1) return;
-  const size_t at0 = (size_t)e * a.splits * R + r;
-  float m = -kUnset;
-  for (int s = 0; s < sn.ns; ++s) m = fmaxf(m, a.mpart[at0 + (size_t)s * R].x);
-  float l = 0.f, lx = 0.f;
-  f32x4 x = zero4();
-#pragma unroll 4
-  for (int s = 0; s < sn.ns; ++s) {
-    const float4 ml = a.mpart[at0 + (size_t)s * R];
-    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-    l += ml.y * f;
-    lx += ml.z * f;
-    x += *reinterpret_cast<const f32x4*>(a.opart + (at0 + (size_t)s * R) * D + 4 * ch) * f;
+  int ns = 0;
+  if (on && i < t) {
+    const int r0 = r / a.rows * a.rows;
+    ns = make_span(a, len, len - t, t, r0 / a.group, min(r0 + a.rows - 1, R - 1) / a.group, a.tile_keys).ns;
   }
-  const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
-  write_out<E, D>(a, at, ch, x, m, l, lx);
+  on = ns > 1;   // (a single split has written its row)
+  const size_t at0 = (size_t)e * a.splits * R + r;
+  float m = -kUnset, l = 0.f, lx = 0.f;
+  f32x4 x = zero4();
+  if (on) {
+#pragma unroll 8
+    for (int s = 0; s < ns; ++s) m = fmaxf(m, a.mpart[at0 + (size_t)s * R].x);
+#pragma unroll 4
+    for (int s = gs; s < ns; s += GS) {
+      const float4 ml = a.mpart[at0 + (size_t)s * R];
+      const float f = __builtin_amdgcn_exp2f(ml.x - m);
+      l += ml.y * f;
+      lx += ml.z * f;
+      x += *reinterpret_cast<const f32x4*>(a.opart + (at0 + (size_t)s * R) * D + 4 * ch) * f;
+    }
+  }
+  if constexpr (GS > 1) {
+    part[tid] = x;
+    psum[tid] = make_float2(l, lx);
+    __syncthreads();
+    on = on && gs == 0;
+    if (on) {
+#pragma unroll
+      for (int k = 1; k < GS; ++k) {
+        x += part[tid + k * CR];
+        l += psum[tid + k * CR].x;
+        lx += psum[tid + k * CR].y;
+      }
+    }
+  }
+  if (on) write_out<E, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, x, m, l, lx);
 }
 
 template <typename E, int D>
@@ -446,9 +464,12 @@ template <typename E, int D>
 hipError_t launch_ed(const AttendK& a, int rt, hipStream_t s) {
   const hipError_t e = launch_d<E, D>(a, rt, s);
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t n = (int64_t)a.entries * a.group * a.tokens * (D / 4);
-  hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((n + kAtTh - 1) / kAtTh)), dim3(kAtTh),
-                     0, s, a);
+  const int64_t rows = (int64_t)a.entries * a.group * a.tokens;
+  constexpr int GS = kAtTh / (D / 4);
+  if (a.splits > GS)
+    hipLaunchKernelGGL((combine_kernel<E, D, GS>), dim3((unsigned)rows), dim3(kAtTh), 0, s, a);
+  else
+    hipLaunchKernelGGL((combine_kernel<E, D, 1>), dim3((unsigned)((rows + GS - 1) / GS)), dim3(kAtTh), 0, s, a);
   return hipGetLastError();
 }
 
