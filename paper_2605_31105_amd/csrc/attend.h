@@ -9,6 +9,7 @@ namespace grkv {
 
 constexpr float kUnset = 3e38f;      // minus the reference of a row without one
 constexpr float kMoveAt = 40.f;      // log2 of the largest weight before a move
+constexpr float kMoveSum = 0x1p40f;  // the largest sum of a step's weights before one
 constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
 constexpr float kLn2 = 0.6931471805599453f;
 

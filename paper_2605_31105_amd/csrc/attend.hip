@@ -484,7 +484,7 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   int64_t target;   // blocks
   if (bf16 && R > 64) {
     p.rt = 0;
-    p.rows = R <= 128 ? 128 : 256;
+    p.rows = 128;
     p.tile_keys = kWideKeys;
     p.min_tiles = 8;
     target = 512;

@@ -22,9 +22,8 @@
 namespace grkv {
 namespace {
 
-constexpr int kWWaves = 8;
+constexpr int kWWaves = 4;
 constexpr int kWTh = 64 * kWWaves;
-constexpr int kWStages = 4;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -54,28 +53,24 @@ __device__ __forceinline__ bf16x8 read_tr(const char* p, int rows8) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// KW: waves that share 32 rows and divide the keys of a tile between them.
-template <int D, int KW, bool PAGED>
+template <int D, bool PAGED>
 __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
-  constexpr int TK = kWideKeys, NS = kWStages;
+  constexpr int TK = kWideKeys;
+  constexpr int NK = TK / 32;          // 32-key parts of a step
   constexpr int RB = 2 * D;            // bytes of a row
   constexpr int CPR = RB / 16;         // chunks of a row
   constexpr int KB = TK * RB;          // bytes of a K (or V) tile
-  constexpr int SB = 2 * KB;           // of a stage
-  constexpr int WK = TK / kWWaves;     // rows of a tile that one wave brings: 8
-  constexpr int NI = WK * RB / 1024;   // load instructions per wave and tensor
+  constexpr int NI = 16 * RB / 1024;   // load instructions per wave and tensor: 16 rows
   constexpr int RPI = 64 / CPR;        // rows of one
   constexpr int KS = D / 16, DM = D / 32;
-  constexpr int RW = kWWaves / KW;     // row tiles of a block
-  static_assert(RW * 32 * D * 4 * KW <= NS * SB, "the waves' outputs fit the ring");
-  __shared__ __attribute__((aligned(1024))) char ring[NS * SB];
-  __shared__ float m_s[kWWaves][32], x_s[kWWaves][32], y_s[kWWaves][32];
+  static_assert(TK == 16 * kWWaves, "a wave brings 16 rows of a tile");
+  static_assert(kWWaves * 32 * D * 4 == 4 * KB, "the waves' outputs fit the ring");
+  __shared__ __attribute__((aligned(1024))) char ring[4 * KB];   // two K tiles, two V tiles
 
   int e, rg, sp;
   if (!block_work(a, &e, &rg, &sp)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
-  const int rw = wave / KW, kw = wave % KW;
   const int R = a.group * a.tokens, r0 = rg * a.rows;
   int len, t;
   const int32_t* trow;
@@ -88,7 +83,7 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   uint64_t family = 0;
   int depth = 0;
   if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);
-  const int w0 = r0 + 32 * rw;   // this wave's first row
+  const int w0 = r0 + 32 * wave;   // this wave's first row
   bf16x8 qf[KS];
   RowSight sight;
   {
@@ -110,21 +105,23 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
     lo = a.window > 0 ? base + min(w0 + 31, R - 1) / a.group + 1 - a.window : 0;
   }
 
-  // ---- loads: this wave brings rows WK wave .. of every tile
+  // ---- loads: this wave brings rows 16 wave .. + 15 of every tile
   auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
   auto swz_v = [](int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; };
   uint32_t ko[NI], vo[NI];
 #pragma unroll
   for (int it = 0; it < NI; ++it) {
-    const int row = (WK * wave & 15) + it * RPI + lane / CPR, ch = lane % CPR;
+    const int row = it * RPI + lane / CPR, ch = lane % CPR;
     ko[it] = (row * CPR + (ch ^ swz_k(row))) * 16;
     vo[it] = (row * CPR + (ch ^ swz_v(row))) * 16;
   }
   const int last = sn.kend - 1;
   const uint32_t ring0 = (uint32_t)(uintptr_t)(lds_void*)ring;
   auto slot_of = [&](int vt) { return (vt < sn.at ? vt : vt - sn.at + sn.bt) * TK; };
-  auto load = [&](int vt, int stage) {
-    const int s16 = slot_of(vt) + (WK * wave & ~15);   // the 16 rows that hold this wave's
+  // this wave's rows of tile vt, of K or V (the chunk offsets o, permuted by swz)
+  auto load = [&](const void* from, int vt, int to, const uint32_t (&o)[NI], auto swz)
+                  __attribute__((always_inline)) {
+    const int s16 = slot_of(vt) + 16 * wave;
     const int at = __builtin_amdgcn_readfirstlane(min(s16, last));
     size_t row;
     if (PAGED) {
@@ -134,28 +131,17 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
     } else {
       row = (size_t)e * a.n + (at & ~15);
     }
-    const char* kb = (const char*)a.k + row * RB;
-    const char* vb = (const char*)a.v + row * RB;
-    const uint32_t to = __builtin_amdgcn_readfirstlane(ring0 + stage * SB + wave * WK * RB);
-    uint32_t fk[NI], fv[NI];
+    const char* src = (const char*)from + row * RB;
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(ring0 + to + wave * 16 * RB);
+    const bool whole = s16 + 15 <= last;
 #pragma unroll
     for (int it = 0; it < NI; ++it) {
-      fk[it] = ko[it];
-      fv[it] = vo[it];
-    }
-    if (s16 + 15 > last) {   // rows past the last slot: the last one again
-#pragma unroll
-      for (int it = 0; it < NI; ++it) {
-        const int row_in = (WK * wave & 15) + it * RPI + lane / CPR, ch = lane % CPR;
-        const int from = (min(s16 + row_in, last) & 15) * CPR;
-        fk[it] = (from + (ch ^ swz_k(row_in))) * 16;
-        fv[it] = (from + (ch ^ swz_v(row_in))) * 16;
+      uint32_t f = o[it];
+      if (!whole) {   // rows past the last slot: the last one again
+        const int row_in = it * RPI + lane / CPR, ch = lane % CPR;
+        f = ((min(s16 + row_in, last) & 15) * CPR + (ch ^ swz(row_in))) * 16;
       }
-    }
-#pragma unroll
-    for (int it = 0; it < NI; ++it) {
-      ring_load(kb, fk[it], to + it * 1024);
-      ring_load(vb, fv[it], to + KB + it * 1024);
+      ring_load(src, f, dst + it * 1024);
     }
   };
 
@@ -179,42 +165,82 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
         vf[s][dm] = read_tr(tile + 16 * s * RB + (va ^ (dm << 6)), 8 * RB);
   };
 
-  f32x16 acc[DM], st;
+  f32x16 acc[DM], st[NK];
   float nref = kUnset;          // minus the reference
   float sum = 0.f, rsum = 0.f;  // weights' sums before and after their rounding (this lane's keys)
   bool odd = false;             // a value that is not finite in a step that is not seen whole
 #pragma unroll
   for (int dm = 0; dm < DM; ++dm) acc[dm] = f32x16{};
 
-  // One step: the 32 keys at slot0, whose logits are in st and whose V rows are at vt; kt:
-  // K rows of the next step.
+  auto logits = [&](const char* kt, f32x16 (&x)[NK]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+      bf16x8 kf[KS];
+      read_k(kt + n * 32 * RB, kf);
+      x[n] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) x[n] = mfma32(kf[ks], qf[ks], x[n]);
+    }
+  };
+  // One step: the 32 NK keys at slot0, whose logits are in st and whose V rows are at vt;
+  // kt: K rows of the next step.
   auto step = [&](int slot0, const char* kt, const char* vt) __attribute__((always_inline)) {
-    const bool full = slot0 + 32 <= lim && (slot0 >= lo || slot0 + 32 <= a.n_sink);
+    const bool full = slot0 + 32 * NK <= lim && (slot0 >= lo || slot0 + 32 * NK <= a.n_sink);
     if (!full) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!sees<PAGED>(sight, slot0 + 8 * (r / 4) + 4 * h + r % 4, a.n_sink, base, len))
-          st[r] = -__builtin_huge_valf();
-      bf16x8 vf[2][DM];
-      read_v(vt, vf);   // (values that are not finite?)
+      for (int n = 0; n < NK; ++n) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+        for (int r = 0; r < 16; ++r)
+          if (!sees<PAGED>(sight, slot0 + 32 * n + 8 * (r / 4) + 4 * h + r % 4, a.n_sink, base, len))
+            st[n][r] = -__builtin_huge_valf();
+        bf16x8 vf[2][DM];
+        read_v(vt + n * 32 * RB, vf);   // (values that are not finite?)
 #pragma unroll
-        for (int dm = 0; dm < DM; ++dm) {
-          const uint4 w = __builtin_bit_cast(uint4, vf[s][dm]);
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            odd |= (u[c] & 0x7f80u) == 0x7f80u || (u[c] & 0x7f800000u) == 0x7f800000u;
-        }
+          for (int dm = 0; dm < DM; ++dm) {
+            const uint4 w = __builtin_bit_cast(uint4, vf[s][dm]);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              odd |= (u[c] & 0x7f80u) == 0x7f80u || (u[c] & 0x7f800000u) == 0x7f800000u;
+          }
+      }
     }
-    float mx = st[0];
+    f32x16 nx[NK];
+    logits(kt, nx);
+    bf16x8 p[NK][2];
+    float s1, s2;   // this step's sums
+    auto weights = [&]() __attribute__((always_inline)) {
+      s1 = s2 = 0.f;
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, st[r]);
-    if (__any(!(fmaf(mx, a.scale_log2, nref) <= kMoveAt))) {
-      const float m2 = fmaxf(mx, __shfl_xor(mx, 32));
-      if (!(fmaf(m2, a.scale_log2, nref) <= kMoveAt) && m2 > -__builtin_huge_valf()) {
-        const float ref = m2 * a.scale_log2;
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int c = 0; c < 8; c += 2) {
+            const float x0 = __builtin_amdgcn_exp2f(fmaf(st[n][8 * s + c], a.scale_log2, nref));
+            const float x1 = __builtin_amdgcn_exp2f(fmaf(st[n][8 * s + c + 1], a.scale_log2, nref));
+            s1 += x0;
+            s1 += x1;
+            const bf16x2 w = __builtin_convertvector((f32x2){x0, x1}, bf16x2);
+            p[n][s][c] = w[0];
+            p[n][s][c + 1] = w[1];
+            s2 = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, kOnes), s2, false);
+          }
+    };
+    weights();
+    bool moved = !(s1 <= kMoveSum);
+    if (__any(moved)) {   // (also the first logits that a row sees)
+      moved |= __shfl_xor((int)moved, 32) != 0;
+      float mx = st[0][0];
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[n][r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      if (moved && mx > -__builtin_huge_valf()) {
+        const float ref = mx * a.scale_log2;
         const float f = __builtin_amdgcn_exp2f(-nref - ref);
         nref = -ref;
         sum *= f;
@@ -222,117 +248,70 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
 #pragma unroll
         for (int dm = 0; dm < DM; ++dm) acc[dm] *= f;
       }
+      weights();
     }
-    bf16x8 kf[KS];
-    read_k(kt, kf);
-    f32x16 nx = {};
+    sum += s1;
+    rsum += s2;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) nx = mfma32(kf[ks], qf[ks], nx);
-    bf16x8 vf[2][DM];
-    read_v(vt, vf);
-    bf16x8 p[2];
+    for (int n = 0; n < NK; ++n) {
+      bf16x8 vf[2][DM];
+      read_v(vt + n * 32 * RB, vf);
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int c = 0; c < 8; c += 2) {
-        const float x0 = __builtin_amdgcn_exp2f(fmaf(st[8 * s + c], a.scale_log2, nref));
-        const float x1 = __builtin_amdgcn_exp2f(fmaf(st[8 * s + c + 1], a.scale_log2, nref));
-        sum += x0;
-        sum += x1;
-        const bf16x2 w = __builtin_convertvector((f32x2){x0, x1}, bf16x2);
-        p[s][c] = w[0];
-        p[s][c + 1] = w[1];
-        rsum = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, kOnes), rsum, false);
-      }
+        for (int dm = 0; dm < DM; ++dm) acc[dm] = mfma32(vf[s][dm], p[n][s], acc[dm]);
+    }
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int dm = 0; dm < DM; ++dm) acc[dm] = mfma32(vf[s][dm], p[s], acc[dm]);
-    st = nx;
+    for (int n = 0; n < NK; ++n) st[n] = nx[n];
   };
 
   if (vt0 < vt1) {
-    auto tile = [&](int i) { return min(vt0 + i, vt1 - 1); };
-    load(tile(0), 0);
-    load(tile(1), 1);
-    load(tile(2), 2);
-    ring_barrier<4 * NI>();
-    {
-      bf16x8 kf[KS];
-      read_k(ring + kw * 32 * RB, kf);
-      st = f32x16{};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) st = mfma32(kf[ks], qf[ks], st);
-    }
+    // K of tile i is in half i & 1 of the first half of the ring, V in the second
+    auto load_k = [&](int i) { load(a.k, min(vt0 + i, vt1 - 1), (i & 1) * KB, ko, swz_k); };
+    auto load_v = [&](int i) { load(a.v, min(vt0 + i, vt1 - 1), (2 + (i & 1)) * KB, vo, swz_v); };
+    load_k(0);
+    load_k(1);
+    load_v(0);
+    ring_barrier<2 * NI>();
+    logits(ring, st);
     for (int i = 0; i < vt1 - vt0; ++i) {
-      const char* cur = ring + (i & (NS - 1)) * SB;
-      const char* nxt = ring + ((i + 1) & (NS - 1)) * SB;
-      const int slot0 = slot_of(vt0 + i);
-      if (KW == 1) step(slot0, cur + 32 * RB, cur + KB);
-      // tile i + 1 is here, and every wave is done with tile i - 1
-      ring_barrier<2 * NI>();
-      load(tile(i + 3), (i + 3) & (NS - 1));
-      if (KW == 1) step(slot0 + 32, nxt, cur + KB + 32 * RB);
-      else step(slot0 + 32 * kw, nxt + kw * 32 * RB, cur + KB + kw * 32 * RB);
+      // K of tile i + 1 and V of tile i are here, and every wave is done with K of
+      // tile i and V of tile i - 1
+      ring_barrier<0>();
+      load_k(i + 2);
+      load_v(i + 1);
+      step(slot_of(vt0 + i), ring + ((i + 1) & 1) * KB, ring + (2 + (i & 1)) * KB);
     }
   }
   ring_barrier<0>();   // (the ring is the output's buffer now)
   sum += __shfl_xor(sum, 32);
   rsum += __shfl_xor(rsum, 32);
-  if (h == 0) {
-    m_s[wave][l32] = -nref;
-    x_s[wave][l32] = sum;
-    y_s[wave][l32] = rsum;
-  }
-  // rows that meet such a value: 32 / KW rows per wave
-  const bool any_odd = KW == 1 ? __any(odd) : __syncthreads_or(odd);
-  if (KW == 1) __syncthreads();
-  if (any_odd) {
-    rows_by_key<u16, D, PAGED>(a, sn, e, sp, w0 + kw * (32 / KW), 32 / KW, vt0, vt1, TK, len, t, trow,
-                               family, depth);
+  if (__any(odd)) {
+    rows_by_key<u16, D, PAGED>(a, sn, e, sp, w0, 32, vt0, vt1, TK, len, t, trow, family, depth);
     return;
   }
-  // rows through LDS: lane's four columns 32 dm + 8 c + 4 h of row l32, chunks
-  // permuted by row; the waves of a row tile scaled to their largest reference
+  // a wave's rows through its part of the ring: lane's four columns 32 dm + 8 c + 4 h of
+  // row l32, chunks permuted by row
   constexpr int CR = D / 4;
-  float m = m_s[rw * KW][l32];
-#pragma unroll
-  for (int k = 1; k < KW; ++k) m = fmaxf(m, m_s[rw * KW + k][l32]);
-  const float f = KW == 1 ? 1.f : __builtin_amdgcn_exp2f(-nref - m);
   char* out = ring + wave * 32 * CR * 16;
 #pragma unroll
   for (int dm = 0; dm < DM; ++dm)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       *reinterpret_cast<f32x4*>(out + (l32 * CR + ((8 * dm + 2 * c + h) ^ (l32 & 15))) * 16) =
-          (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]} * f;
-  if (KW > 1) __syncthreads();
-  const char* in = ring + rw * KW * 32 * CR * 16;
-  for (int k = kw * 64 + lane; k < 32 * CR; k += 64 * KW) {
+          (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]};
+  for (int k = lane; k < 32 * CR; k += 64) {
     const int row = k / CR, ch = k % CR, r = w0 + row;
     const int i = r / a.group, g = r - i * a.group;
+    const float m = -__shfl(nref, row), lx = __shfl(sum, row), l = __shfl(rsum, row);
     if (r >= R || i >= t) continue;
-    float mr = m_s[rw * KW][row], lx = x_s[rw * KW][row], l = y_s[rw * KW][row];
-    f32x4 x = *reinterpret_cast<const f32x4*>(in + (row * CR + (ch ^ (row & 15))) * 16);
-    if constexpr (KW > 1) {
-      lx = l = 0.f;
-#pragma unroll
-      for (int w = 1; w < KW; ++w) mr = fmaxf(mr, m_s[rw * KW + w][row]);
-      x = zero4();
-#pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const float fw = __builtin_amdgcn_exp2f(m_s[rw * KW + w][row] - mr);
-        lx += x_s[rw * KW + w][row] * fw;
-        l += y_s[rw * KW + w][row] * fw;
-        x += *reinterpret_cast<const f32x4*>(in + w * 32 * CR * 16 + (row * CR + (ch ^ (row & 15))) * 16);
-      }
-    }
+    const f32x4 x = *reinterpret_cast<const f32x4*>(out + (row * CR + (ch ^ (row & 15))) * 16);
     if (sn.ns > 1) {
       const size_t at = ((size_t)e * a.splits + sp) * R + r;
       *reinterpret_cast<f32x4*>(a.opart + at * D + 4 * ch) = x;
-      if (ch == 0) a.mpart[at] = make_float4(mr, l, lx, 0.f);
+      if (ch == 0) a.mpart[at] = make_float4(m, l, lx, 0.f);
     } else {
-      write_out<u16, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, x, mr, l, lx);
+      write_out<u16, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, x, m, l, lx);
     }
   }
 }
@@ -340,13 +319,8 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
 template <int D>
 hipError_t launch_wide_d(const AttendK& a, hipStream_t s) {
   const dim3 grid((unsigned)a.blocks), th(kWTh);
-  if (a.lens) {
-    if (a.rows == 128) hipLaunchKernelGGL((wide_kernel<D, 2, true>), grid, th, 0, s, a);
-    else hipLaunchKernelGGL((wide_kernel<D, 1, true>), grid, th, 0, s, a);
-  } else {
-    if (a.rows == 128) hipLaunchKernelGGL((wide_kernel<D, 2, false>), grid, th, 0, s, a);
-    else hipLaunchKernelGGL((wide_kernel<D, 1, false>), grid, th, 0, s, a);
-  }
+  if (a.lens) hipLaunchKernelGGL((wide_kernel<D, true>), grid, th, 0, s, a);
+  else hipLaunchKernelGGL((wide_kernel<D, false>), grid, th, 0, s, a);
   return hipGetLastError();
 }
 
