@@ -601,7 +601,7 @@ def intermediates(res: Result) -> dict:
 
 # ------------------------------------------------------- pages of a cache ----
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class Pages:
     """The pool of pages of grkv.h (``grkv_pages``): contiguous tensors of one
     device.  ``new_pages`` makes an empty one."""
@@ -615,61 +615,78 @@ class Pages:
     def __post_init__(self):
         import torch
 
-        k, table, i32 = self.k, self.table, torch.int32
-        if not k.is_cuda:
+        k, v, table, lens, refs, free = self.k, self.v, self.table, self.lens, self.refs, self.free
+        i32, dev = torch.int32, k.get_device()
+        if dev < 0:
             raise ValueError("a pool's tensors must be device tensors")
-        if k.dtype != self.v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
+        if k.dtype != v.dtype or k.dtype not in _DTYPES:
             raise ValueError("k and v must share dtype bfloat16 or float32")
-        if k.dim() != 3 or k.shape != self.v.shape or table.dim() != 2:
+        if k.dim() != 3 or k.shape != v.shape or table.dim() != 2:
             raise ValueError("k and v must be [pages, page_size, head_dim] and table [units, max_pages]")
-        n = k.shape[0]
-        if (tuple(self.lens.shape) != (table.shape[0],) or tuple(self.refs.shape) != (n,)
-                or tuple(self.free.shape) != ((n + 31) // 32,)):
+        (n, ps, d), (units, width) = k.shape, table.shape
+        if lens.shape != (units,) or refs.shape != (n,) or free.shape != ((n + 31) // 32,):
             raise ValueError("lens, refs and free must be [units], [pages] and [ceil(pages / 32)]")
-        for t in (k, self.v, table, self.lens, self.refs, self.free):
-            if not t.is_contiguous() or t.device != k.device:
+        for t in (k, v, table, lens, refs, free):
+            if not t.is_contiguous() or t.get_device() != dev:
                 raise ValueError("a pool's tensors must be contiguous and on one device")
-        for t in (table, self.lens, self.refs, self.free):
-            if t.dtype != i32:
-                raise ValueError("table, lens, refs and free must be int32")
+        if not (table.dtype == lens.dtype == refs.dtype == free.dtype == i32):
+            raise ValueError("table, lens, refs and free must be int32")
+        object.__setattr__(self, "_c", _PagesC(
+            k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(),
+            free.data_ptr(), n, ps, units, width, d, _DTYPES[k.dtype]))
 
     @property
     def device(self):
         return self.k.device
 
-    def _c(self):
+
+class _Dtypes(dict):
+    """torch dtype -> grkv_dtype, filled when torch is first needed."""
+
+    def _fill(self):
         import torch
 
-        k = self.k
-        return _PagesC(k.data_ptr(), self.v.data_ptr(), self.table.data_ptr(),
-                       self.lens.data_ptr(), self.refs.data_ptr(), self.free.data_ptr(),
-                       k.shape[0], k.shape[1], self.table.shape[0], self.table.shape[1],
-                       k.shape[2], GRKV_BF16 if k.dtype == torch.bfloat16 else GRKV_F32)
+        if not self:
+            self.update({torch.bfloat16: GRKV_BF16, torch.float32: GRKV_F32})
+
+    def __contains__(self, key):
+        self._fill()
+        return dict.__contains__(self, key)
 
 
-def _on(device, stream):
-    """(torch stream, handle, context): the context allocates on that stream, so that a
-    workspace dropped after the call is not handed to another one while it is in use."""
-    import contextlib
+_DTYPES = _Dtypes()
 
+
+def _on(dev: int, stream):
+    """(handle, context) of a call on device ``dev``.  The context, None where nothing has to
+    change, makes that device and stream current, so that a workspace dropped after the call is
+    not handed to another stream while it is in use."""
     import torch
 
     if stream is None:
-        if torch.cuda.current_device() == device.index:
-            return torch.cuda.current_stream(device).cuda_stream, contextlib.nullcontext()
-        stream = torch.cuda.current_stream(device)
+        if torch.cuda.current_device() == dev:
+            return torch._C._cuda_getCurrentRawStream(dev), None
+        stream = torch.cuda.current_stream(dev)
     elif not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
     return stream.cuda_stream, torch.cuda.stream(stream)
 
 
-def _vector(t, name, dtype, size, device):
+def _vector(t, name, dtype, size, dev):
     """A device vector of a call, as its address; None stays."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or tuple(t.shape) != (size,):
-        raise ValueError("%s must be a contiguous %s vector of %d on %s" % (name, dtype, size, device))
+    if t.dtype != dtype or t.get_device() != dev or t.shape != (size,) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s vector of %d on cuda:%d" % (name, dtype, size, dev))
     return t.data_ptr()
+
+
+def _workspace(workspace, need, dev):
+    import torch
+
+    if workspace is None or workspace.numel() < need:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    return workspace
 
 
 def new_pages(units: int, max_pages: int, pages: int, page_size: int, head_dim: int, dtype=None,
@@ -679,11 +696,9 @@ def new_pages(units: int, max_pages: int, pages: int, page_size: int, head_dim: 
     import torch
 
     dtype = torch.bfloat16 if dtype is None else dtype
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    if device.type == "cuda" and device.index is None:
-        device = torch.device("cuda", torch.cuda.current_device())
     if min(units, max_pages, pages, page_size, head_dim) < 1:
         raise ValueError("a pool needs units, pages and rows")
+    device = torch.device("cuda" if device is None else device)
     i32 = dict(dtype=torch.int32, device=device)
     pg = Pages(k=torch.empty((pages, page_size, head_dim), dtype=dtype, device=device),
                v=torch.empty((pages, page_size, head_dim), dtype=dtype, device=device),
@@ -694,65 +709,50 @@ def new_pages(units: int, max_pages: int, pages: int, page_size: int, head_dim: 
 
 def pages_init(pages: Pages, *, stream=None) -> Pages:
     """Empties a pool: no unit holds a row, every page is free."""
-    handle, on = _on(pages.device, stream)
-    with on:
-        _check(lib().grkv_pages_init(pages._c(), handle))
+    handle, on = _on(pages.k.get_device(), stream)
+    if on is None:
+        _check(lib().grkv_pages_init(pages._c, handle))
+    else:
+        with on:
+            _check(lib().grkv_pages_init(pages._c, handle))
     return pages
 
 
 def pages_workspace_bytes(pages: Pages, entries: int) -> int:
-    return int(lib().grkv_pages_workspace_bytes(pages._c(), entries))
+    return int(lib().grkv_pages_workspace_bytes(pages._c, entries))
 
 
-def _page_call(name, pages, entries, args, *, units, rows, counts, starts, source_rows, status,
+def _page_call(name, pages, entries, args, units, rows, counts, starts, source_rows, status,
                workspace, stream):
     """One call on pages; ``args`` are those between the entries and the stream."""
     import torch
 
-    dev, i32 = pages.device, torch.int32
-    c = pages._c()
+    dev, i32 = pages.k.get_device(), torch.int32
     en = _PageEntries(entries, _vector(units, "units", i32, entries, dev), rows,
                       _vector(counts, "counts", i32, entries, dev),
                       _vector(starts, "starts", torch.int64, entries, dev), source_rows, None)
     handle, on = _on(dev, stream)
-    with on:
-        if status is None:
-            status = torch.empty(entries, dtype=i32, device=dev)
-        en.status = _vector(status, "status", i32, entries, dev)
-        fn = getattr(lib(), "grkv_pages_" + name)
-        if name == "free":
-            _check(fn(c, en, handle))
-            return status
-        need = int(lib().grkv_pages_workspace_bytes(c, entries))
-        if workspace is None or workspace.numel() < need:
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-        _check(fn(c, en, *args, handle, workspace.data_ptr(), workspace.numel()))
-    return status
+    if on is not None:
+        with on:
+            return _page_launch(name, pages, entries, args, en, dev, status, workspace, handle)
+    return _page_launch(name, pages, entries, args, en, dev, status, workspace, handle)
 
 
-def pages_append(pages: Pages, k, v, *, units=None, counts=None, starts=None, rows=None,
-                 status=None, workspace=None, stream=None):
-    """Appends rows to units (grkv_pages_append).
-
-    k, v: contiguous device tensors, bfloat16 or float32 each (rounded to the pool's type):
-    [E, rows, head_dim], ``rows`` for each of E entries, or packed [N, head_dim] with
-    ``starts`` int64 [E] (the first row of each entry) and ``rows``, a bound on the
-    counts.  ``counts`` int32 [E]: the rows of each entry (default: all ``rows``).
-    ``units`` int32 [E]: their units (default 0 .. E - 1).  Returns the status of every
-    entry, int32 [E] (PAGES_OK or why its unit is as it was)."""
+def _page_launch(name, pages, entries, args, en, dev, status, workspace, handle):
     import torch
 
-    E, rows, n = _packed(k, 3, rows, starts, "k")
-    types = {torch.bfloat16: GRKV_BF16, torch.float32: GRKV_F32}
-    for t in (k, v):
-        if t.device != pages.device or not t.is_contiguous() or t.dtype not in types:
-            raise ValueError("k and v must be contiguous bfloat16 or float32 tensors on the pool's device")
-    if k.shape != v.shape or k.shape[-1] != pages.k.shape[2]:
-        raise ValueError("shape mismatch: k %s v %s head_dim %d"
-                         % (tuple(k.shape), tuple(v.shape), pages.k.shape[2]))
-    return _page_call("append", pages, E, (k.data_ptr(), types[k.dtype], v.data_ptr(), types[v.dtype]),
-                      units=units, rows=rows, counts=counts, starts=starts, source_rows=n,
-                      status=status, workspace=workspace, stream=stream)
+    L = lib()
+    if status is None:
+        status = torch.empty(entries, dtype=torch.int32, device=pages.k.device)
+        en.status = status.data_ptr()
+    else:
+        en.status = _vector(status, "status", torch.int32, entries, dev)
+    if name == "grkv_pages_free":
+        _check(L.grkv_pages_free(pages._c, en, handle))
+        return status
+    workspace = _workspace(workspace, L.grkv_pages_workspace_bytes(pages._c, entries), pages.k.device)
+    _check(getattr(L, name)(pages._c, en, *args, handle, workspace.data_ptr(), workspace.numel()))
+    return status
 
 
 def _packed(t, dims, rows, starts, name):
@@ -766,15 +766,38 @@ def _packed(t, dims, rows, starts, name):
     raise ValueError("%s must have %d dimensions, or %d with starts and rows" % (name, dims, dims - 1))
 
 
+def pages_append(pages: Pages, k, v, *, units=None, counts=None, starts=None, rows=None,
+                 status=None, workspace=None, stream=None):
+    """Appends rows to units (grkv_pages_append).
+
+    k, v: contiguous device tensors, bfloat16 or float32 each (rounded to the pool's type):
+    [E, rows, head_dim], ``rows`` for each of E entries, or packed [N, head_dim] with
+    ``starts`` int64 [E] (the first row of each entry) and ``rows``, a bound on the
+    counts.  ``counts`` int32 [E]: the rows of each entry (default: all ``rows``).
+    ``units`` int32 [E]: their units (default 0 .. E - 1).  Returns the status of every
+    entry, int32 [E] (PAGES_OK or why its unit is as it was)."""
+    E, rows, n = _packed(k, 3, rows, starts, "k")
+    dev = pages.k.get_device()
+    for t in (k, v):
+        if t.get_device() != dev or t.dtype not in _DTYPES or not t.is_contiguous():
+            raise ValueError("k and v must be contiguous bfloat16 or float32 tensors on the pool's device")
+    if k.shape != v.shape or k.shape[-1] != pages.k.shape[2]:
+        raise ValueError("shape mismatch: k %s v %s head_dim %d"
+                         % (tuple(k.shape), tuple(v.shape), pages.k.shape[2]))
+    return _page_call("grkv_pages_append", pages, E,
+                      (k.data_ptr(), _DTYPES[k.dtype], v.data_ptr(), _DTYPES[v.dtype]),
+                      units, rows, counts, starts, n, status, workspace, stream)
+
+
 def pages_fork(pages: Pages, src, dst, *, status=None, workspace=None, stream=None):
     """Units ``dst`` (int32 [E], empty) become copies of units ``src``, full pages shared
     (grkv_pages_fork).  Returns the status of every entry."""
     import torch
 
     E = src.shape[0]
-    return _page_call("fork", pages, E, (_vector(dst, "dst", torch.int32, E, pages.device),),
-                      units=src, rows=0, counts=None, starts=None, source_rows=0, status=status,
-                      workspace=workspace, stream=stream)
+    return _page_call("grkv_pages_fork", pages, E,
+                      (_vector(dst, "dst", torch.int32, E, pages.k.get_device()),),
+                      src, 0, None, None, 0, status, workspace, stream)
 
 
 def pages_compact(pages: Pages, idx=None, *, units=None, dst=None, keep=None, counts=None,
@@ -788,59 +811,68 @@ def pages_compact(pages: Pages, idx=None, *, units=None, dst=None, keep=None, co
     (default 0).  Returns the status of every entry."""
     import torch
 
-    dev, i32 = pages.device, torch.int32
+    dev, i32 = pages.k.get_device(), torch.int32
     if idx is None:
         if counts is not None or starts is not None or rows:
             raise ValueError("counts, starts and rows belong to idx")
-        known = next((t for t in (units, keep, dst) if t is not None), None)
-        E, rows, n, at = pages.lens.shape[0] if known is None else known.shape[0], 0, 0, None
+        known = next((t for t in (units, keep, dst) if t is not None), pages.lens)
+        E, rows, n, at = known.shape[0], 0, 0, None
     else:
-        if idx.dtype != i32 or idx.device != dev or not idx.is_contiguous():
+        if idx.dtype != i32 or idx.get_device() != dev or not idx.is_contiguous():
             raise ValueError("idx must be a contiguous int32 tensor on the pool's device")
         E, rows, n = _packed(idx, 2, rows, starts, "idx")
         at = idx.data_ptr()
     args = (_vector(dst, "dst", i32, E, dev), _vector(keep, "keep", i32, E, dev), at)
-    return _page_call("compact", pages, E, args, units=units, rows=rows, counts=counts,
-                      starts=starts, source_rows=n, status=status, workspace=workspace,
-                      stream=stream)
+    return _page_call("grkv_pages_compact", pages, E, args, units, rows, counts, starts, n,
+                      status, workspace, stream)
 
 
 def pages_free(pages: Pages, units=None, *, status=None, stream=None):
     """Units (int32 [E]; default all) give up their rows and pages (grkv_pages_free)."""
-    E = pages.lens.shape[0] if units is None else units.shape[0]
-    return _page_call("free", pages, E, (), units=units, rows=0, counts=None, starts=None,
-                      source_rows=0, status=status, workspace=None, stream=stream)
+    E = (pages.lens if units is None else units).shape[0]
+    return _page_call("grkv_pages_free", pages, E, (), units, 0, None, None, 0, status, None, stream)
 
 
 # ---------------------------------------------------- attention over a cache ----
 
 def tree_attention_workspace_bytes(pages: Pages, entries, group, tokens, window=0, n_sink=0) -> int:
     tr = _Tree(entries, group, tokens, None, None, None, 0, window, n_sink)
-    return int(lib().grkv_tree_attention_workspace_bytes(pages._c(), tr))
+    return int(lib().grkv_tree_attention_workspace_bytes(pages._c, tr))
 
 
-def _attention(fn, need, q, out, lse, workspace, stream):
-    """Outputs, workspace and stream of an attention call: fn(o, lse, handle, ws, bytes)."""
+def _given(t, name, dtype, shape, dev):
+    if t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s on cuda:%d"
+                         % (name, dtype, tuple(shape), dev))
+
+
+def _attention(launch, need, q, out, lse, return_lse, workspace, stream):
+    """Outputs, workspace and stream of an attention call: launch(o, lse, handle, ws, bytes)."""
     import torch
 
-    dev = q.device
-    for t, dtype, shape, name in ((out, q.dtype, q.shape, "out"),
-                                  (lse, torch.float32, q.shape[:3], "lse")):
-        if torch.is_tensor(t) and (t.dtype != dtype or t.shape != shape or t.device != dev
-                                   or not t.is_contiguous()):
-            raise ValueError("%s must be a contiguous %s tensor %s on %s"
-                             % (name, dtype, tuple(shape), dev))
+    dev = q.get_device()
+    if out is not None:
+        _given(out, "out", q.dtype, q.shape, dev)
+    if lse is not None:
+        _given(lse, "lse", torch.float32, q.shape[:3], dev)
     handle, on = _on(dev, stream)
-    with on:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        if lse is True:
-            lse = torch.empty(q.shape[:3], dtype=torch.float32, device=dev)
-        if workspace is None or workspace.numel() < need:
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-        _check(fn(out.data_ptr(), None if lse is None else lse.data_ptr(), handle,
+    if on is not None:
+        with on:
+            return _attend(launch, need, q, out, lse, return_lse, workspace, handle)
+    return _attend(launch, need, q, out, lse, return_lse, workspace, handle)
+
+
+def _attend(launch, need, q, out, lse, return_lse, workspace, handle):
+    import torch
+
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and return_lse:
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    workspace = _workspace(workspace, need, q.device)
+    _check(launch(out.data_ptr(), None if lse is None else lse.data_ptr(), handle,
                   workspace.data_ptr(), workspace.numel()))
-    return out, lse
+    return (out, lse) if return_lse else out
 
 
 def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, window: int = 0,
@@ -857,26 +889,25 @@ def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, wi
     Returns o [E, G, t, d], with ``return_lse`` (o, lse float32 [E, G, t])."""
     import torch
 
-    dev, i32 = pages.device, torch.int32
-    if q.device != dev or q.dtype != pages.k.dtype or q.dim() != 4 or not q.is_contiguous():
+    dev, i32 = pages.k.get_device(), torch.int32
+    if q.get_device() != dev or q.dtype != pages.k.dtype or q.dim() != 4 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [E, G, t, d] tensor of the pool's type and device")
     E, G, t, d = q.shape
     if d != pages.k.shape[2]:
         raise ValueError("head_dim %d, the pool's is %d" % (d, pages.k.shape[2]))
-    trees = 0
+    trees, up = 0, None
     if parents is not None:
-        trees = parents.shape[0]
-        if (parents.dtype != i32 or parents.device != dev or not parents.is_contiguous()
-                or tuple(parents.shape) != (trees, t)):
-            raise ValueError("parents must be a contiguous int32 [trees, %d] tensor on %s" % (t, dev))
-    c = pages._c()
+        trees, up = parents.shape[0], parents.data_ptr()
+        if (parents.dtype != i32 or parents.get_device() != dev or parents.shape != (trees, t)
+                or not parents.is_contiguous()):
+            raise ValueError("parents must be a contiguous int32 [trees, %d] tensor on cuda:%d" % (t, dev))
+    c = pages._c
     tr = _Tree(E, G, t, _vector(units, "units", i32, E, dev), _vector(counts, "counts", i32, E, dev),
-               None if parents is None else parents.data_ptr(), trees, window, n_sink)
-    L = lib()
-    need = int(L.grkv_tree_attention_workspace_bytes(c, tr))
-    o, lse = _attention(lambda o, l, h, ws, n: L.grkv_tree_attention(q.data_ptr(), c, tr, o, l, h, ws, n),
-                        need, q, out, True if lse is None and return_lse else lse, workspace, stream)
-    return (o, lse) if return_lse else o
+               up, trees, window, n_sink)
+    L, qp = lib(), q.data_ptr()
+    need = L.grkv_tree_attention_workspace_bytes(c, tr)
+    return _attention(lambda o, l, h, ws, n: L.grkv_tree_attention(qp, c, tr, o, l, h, ws, n),
+                      need, q, out, lse, return_lse, workspace, stream)
 
 
 def sink_attention_workspace_bytes(units, group, head_dim, dtype, n, nq, window, n_sink) -> int:
@@ -891,11 +922,10 @@ def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = 
     q [U, G, nq, d] (the last nq positions), K and V [U, n, d]: contiguous device tensors of
     one dtype, bfloat16 or float32.  ``window`` 0: none.  Returns o [U, G, nq, d], with
     ``return_lse`` (o, lse float32 [U, G, nq])."""
-    import torch
-
-    if not (q.is_cuda and K.device == q.device and V.device == q.device):
+    dev = q.get_device()
+    if dev < 0 or K.get_device() != dev or V.get_device() != dev:
         raise ValueError("q, K and V must be tensors of one device")
-    if not (q.dtype == K.dtype == V.dtype) or K.dtype not in (torch.bfloat16, torch.float32):
+    if not (q.dtype == K.dtype == V.dtype) or K.dtype not in _DTYPES:
         raise ValueError("q, K, V must share dtype bfloat16 or float32")
     if not (q.is_contiguous() and K.is_contiguous() and V.is_contiguous()):
         raise ValueError("inputs must be contiguous")
@@ -905,10 +935,9 @@ def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = 
                          % (tuple(q.shape), tuple(K.shape), tuple(V.shape)))
     U, G, nq, d = q.shape
     n = K.shape[1]
-    prob = Problem(U, G, d, GRKV_BF16 if q.dtype == torch.bfloat16 else GRKV_F32)
-    L = lib()
-    need = int(L.grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink))
-    o, lse = _attention(lambda o, l, h, ws, b: L.grkv_sink_attention(
-        q.data_ptr(), K.data_ptr(), V.data_ptr(), n, nq, window, n_sink, h, prob, o, l, ws, b),
-        need, q, out, True if lse is None and return_lse else lse, workspace, stream)
-    return (o, lse) if return_lse else o
+    prob = Problem(U, G, d, _DTYPES[q.dtype])
+    L, qp, kp, vp = lib(), q.data_ptr(), K.data_ptr(), V.data_ptr()
+    need = L.grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink)
+    return _attention(lambda o, l, h, ws, b: L.grkv_sink_attention(
+        qp, kp, vp, n, nq, window, n_sink, h, prob, o, l, ws, b),
+        need, q, out, lse, return_lse, workspace, stream)
