@@ -24,6 +24,7 @@ namespace {
 constexpr int kPlanTh = 1024;
 constexpr int kCopyTh = 256;
 constexpr int kNoOwner = 0x7fffffff;
+constexpr int kOwnerUnits = 8192;   // units of a pool whose owners fit the plan's LDS
 
 // What an entry of a call does, written by the plan.  n1 < 0: nothing (a
 // refused entry).
@@ -58,73 +59,95 @@ __device__ __forceinline__ int load_agent(const int32_t* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Exclusive scan over the block in 64 bits (an entry may ask for 2^26 pages).
-__device__ __forceinline__ uint64_t scan64(uint64_t v, uint64_t* scratch, uint64_t* total) {
+// Exclusive scan over the block of the plan.  Calls in a row take the halves of
+// `scratch` in turn (`turn` 0, 1, 0, ..), so one barrier each is enough.
+template <typename T>
+__device__ __forceinline__ T plan_scan(T v, T (*scratch)[kPlanTh / 64], int turn, T* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t incl = v;
+  T incl = v;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
-    const uint64_t t = __shfl_up((unsigned long long)incl, off);
+    const T t = __shfl_up(incl, off);
     if (lane >= off) incl += t;
   }
-  if (lane == 63) scratch[wave] = incl;
+  if (lane == 63) scratch[turn & 1][wave] = incl;
   __syncthreads();
-  uint64_t before = 0, all = 0;
+  T before = 0, all = 0;
+#pragma unroll
   for (int k = 0; k < kPlanTh / 64; ++k) {
-    const uint64_t s = scratch[k];
+    const T s = scratch[turn & 1][k];
     if (k < wave) before += s;
     all += s;
   }
-  __syncthreads();
   *total = all;
   return before + incl - v;
 }
 
-__global__ __launch_bounds__(kPlanTh) void plan_kernel(PagesK a) {
-  __shared__ uint64_t scratch[kPlanTh / 64];
-  __shared__ uint32_t scratch32[kPlanTh / 64];
+// The plan of a call, by one block.  Most calls have at most one entry per thread;
+// then a job stays in its thread's registers until it is complete.
+__device__ __forceinline__ void make_plan_block(const PagesK& a) {
+  __shared__ int owner_s[kOwnerUnits];
+  // (an entry may ask for 2^26 pages: their sums take 64 bits)
+  __shared__ unsigned long long scratch[2][kPlanTh / 64];
+  __shared__ uint32_t scratch32[2][kPlanTh / 64];
   __shared__ int used_s;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int ps = 1 << a.shift;
   const int64_t cap = (int64_t)a.pg.max_pages << a.shift;
   auto unit_of = [&](int i) { return a.units ? a.units[i] : i; };
   auto in_pool = [&](int u) { return (unsigned)u < (unsigned)a.pg.units; };
 
-  // owner[u]: the lowest entry that writes unit u
-  for (int i = tid; i < a.entries; i += kPlanTh) {
-    const int u = unit_of(i), w = a.dst ? a.dst[i] : u;
-    if (in_pool(u)) a.owner[u] = kNoOwner;
-    if (in_pool(w)) a.owner[w] = kNoOwner;
-  }
+  // owner of a unit: the lowest entry that writes it (in LDS where the pool is
+  // small; entry i is unit i's without lists of units)
+  const bool listed = a.units || a.dst, small = a.pg.units <= kOwnerUnits;
   if (tid == 0) used_s = 0;
-  __syncthreads();
-  for (int i = tid; i < a.entries; i += kPlanTh) {
-    const int w = a.dst ? a.dst[i] : unit_of(i);
-    if (in_pool(w)) atomicMin(a.owner + w, i);
+  if (listed && small) {
+    for (int u = tid; u < a.pg.units; u += kPlanTh) owner_s[u] = kNoOwner;
+    __syncthreads();
+    for (int i = tid; i < a.entries; i += kPlanTh) {
+      const int w = a.dst ? a.dst[i] : unit_of(i);
+      if (in_pool(w)) atomicMin(owner_s + w, i);
+    }
+  } else if (listed) {
+    for (int i = tid; i < a.entries; i += kPlanTh) {
+      const int u = unit_of(i), w = a.dst ? a.dst[i] : u;
+      if (in_pool(u)) a.owner[u] = kNoOwner;
+      if (in_pool(w)) a.owner[w] = kNoOwner;
+    }
+    __syncthreads();
+    for (int i = tid; i < a.entries; i += kPlanTh) {
+      const int w = a.dst ? a.dst[i] : unit_of(i);
+      if (in_pool(w)) atomicMin(a.owner + w, i);
+    }
   }
   __syncthreads();
+  auto owner = [&](int u) { return small ? owner_s[u] : load_agent(a.owner + u); };
 
   // each entry's status and job, but for the pages it gets
-  uint64_t need_all = 0;
+  PageJob j;
+  int st = GRKV_PAGES_OK;
+  unsigned long long need_all = 0;
+  int turn = 0;
   for (int i0 = 0; i0 < a.entries; i0 += kPlanTh) {
     const int i = i0 + tid;
-    int st = GRKV_PAGES_OK;
-    PageJob j = {};
+    st = GRKV_PAGES_OK;
+    j = PageJob{};
     if (i < a.entries) {
       j.src = unit_of(i);
       j.dst = a.dst ? a.dst[i] : j.src;
       const bool moved = j.dst != j.src;
-      if (!in_pool(j.src) || !in_pool(j.dst) || load_agent(a.owner + j.dst) != i ||
-          (moved && load_agent(a.owner + j.src) != kNoOwner)) {
+      if (!in_pool(j.src) || !in_pool(j.dst) ||
+          (listed && (owner(j.dst) != i || (moved && owner(j.src) != kNoOwner)))) {
         st = GRKV_PAGES_UNIT;
       } else {
         j.n0 = a.pg.lens[j.src];
+        const int there = moved ? a.pg.lens[j.dst] : 0;
         int count = a.op == kPagesFork ? 0 : a.rows;
         if (a.counts) count = min(max(a.counts[i], 0), a.rows);
         j.start = a.starts ? a.starts[i] : (int64_t)i * a.rows;
         j.keep = a.op != kPagesCompact ? j.n0 : a.keep ? a.keep[i] : 0;
         const int64_t n1 = (int64_t)j.keep + count;
-        if (j.n0 < 0 || j.n0 > cap || (moved && a.pg.lens[j.dst] != 0)) {
+        if (j.n0 < 0 || j.n0 > cap || there != 0) {
           st = GRKV_PAGES_UNIT;
         } else if (j.keep < 0 || j.keep > j.n0 ||
                    (count > 0 && (j.start < 0 || j.start > a.source_rows - count))) {
@@ -148,77 +171,81 @@ __global__ __launch_bounds__(kPlanTh) void plan_kernel(PagesK a) {
       }
       if (st != GRKV_PAGES_OK) j.n1 = -1;
     }
-    const uint64_t need = st == GRKV_PAGES_OK ? (uint64_t)max(j.last - j.first, 0) : 0;
-    uint64_t total;
-    const uint64_t off = need_all + scan64(need, scratch, &total);
+    const unsigned long long need = st == GRKV_PAGES_OK ? max(j.last - j.first, 0) : 0;
+    unsigned long long total;
+    const unsigned long long off = need_all + plan_scan(need, scratch, turn++, &total);
     need_all += total;
-    if (i < a.entries) {
-      // (an entry whose pages end past the pool's last is refused below)
-      j.off = (int)(off < (uint64_t)a.pg.pages ? off : (uint64_t)a.pg.pages);
+    // (an entry whose pages end past the pool's last is refused below)
+    j.off = (int)(off < (unsigned)a.pg.pages ? off : (unsigned)a.pg.pages);
+    if (a.entries > kPlanTh && i < a.entries) {
       a.jobs[i] = j;
       if (a.status) a.status[i] = st;
     }
   }
 
-  // the lowest free pages, as many as are asked for: thread t of a step takes
-  // four words, so a step covers 131072 pages
+  // the lowest free pages, as many as are asked for.  A thread takes a word of 32
+  // pages; a wave writes the numbers word by word, so that neighbouring lanes
+  // write neighbouring numbers
   const int words = (a.pg.pages + 31) / 32;
-  const uint32_t want = (uint32_t)(need_all < (uint64_t)a.pg.pages ? need_all : (uint64_t)a.pg.pages);
+  const uint32_t want = (uint32_t)(need_all < (unsigned)a.pg.pages ? need_all : (unsigned)a.pg.pages);
   uint32_t found = 0;
-  for (int w0 = 0; w0 < words && found < want; w0 += 4 * kPlanTh) {
-    uint32_t bits[4], n = 0, total;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int w = w0 + 4 * tid + k;
-      bits[k] = w < words ? a.pg.free_bits[w] : 0u;
-      n += __popc(bits[k]);
+  for (int w0 = 0; w0 < words && found < want; w0 += kPlanTh) {
+    const int w = w0 + tid;
+    const uint32_t bits = w < words ? a.pg.free_bits[w] : 0u;
+    uint32_t total;
+    const uint32_t r0 = found + plan_scan((uint32_t)__popc(bits), scratch32, turn++, &total);
+    uint32_t left = 0;
+    if (r0 + __popc(bits) > want) {   // the last word taken from, and those behind it
+      left = bits;
+      for (uint32_t r = r0; r < want; ++r) left &= left - 1;
     }
-    uint32_t r = found + block_exclusive_scan(n, scratch32, &total);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      for (uint32_t b = bits[k]; b != 0 && r < want; b &= b - 1)
-        a.ids[r++] = 32 * (w0 + 4 * tid + k) + __ffs((int)b) - 1;
+    if (left != bits) a.pg.free_bits[w] = left;
+    const uint32_t taken = bits ^ left;
+    for (uint64_t live = __ballot(taken != 0); live != 0;) {
+      // two words at a time: lanes 0 .. 31 one, lanes 32 .. 63 the next
+      const int k0 = __ffsll((unsigned long long)live) - 1;
+      live &= live - 1;
+      const int k1 = live != 0 ? __ffsll((unsigned long long)live) - 1 : -1;
+      live &= live - 1;
+      const uint32_t b0 = __builtin_amdgcn_readlane(taken, k0), r_0 = __builtin_amdgcn_readlane(r0, k0);
+      const uint32_t b1 = k1 < 0 ? 0u : __builtin_amdgcn_readlane(taken, k1);
+      const uint32_t r_1 = k1 < 0 ? 0u : __builtin_amdgcn_readlane(r0, k1);
+      const uint32_t b = lane < 32 ? b0 : b1, r = lane < 32 ? r_0 : r_1;
+      const int k = lane < 32 ? k0 : k1, bit = lane & 31;
+      if (b >> bit & 1) a.ids[r + __popc(b & ((1u << bit) - 1))] = 32 * (w0 + (tid & ~63) + k) + bit;
+    }
     found += total;
   }
+  found = found < want ? found : want;
 
   // entries past the free pages are refused; lengths
   for (int i = tid; i < a.entries; i += kPlanTh) {
-    PageJob* j = a.jobs + i;
-    if (j->n1 < 0) continue;
-    const int need = j->last - j->first;
-    if (need > 0) {
-      if ((uint64_t)j->off + need > found) {
-        j->n1 = -1;
-        if (a.status) a.status[i] = GRKV_PAGES_FULL;
-        continue;
-      }
-      atomicMax(&used_s, j->off + need);
+    if (a.entries > kPlanTh) {
+      j = a.jobs[i];
+      st = GRKV_PAGES_OK;   // (a refused entry's status is written)
     }
-    a.pg.lens[j->dst] = j->n1;
+    const int need = j.n1 < 0 ? 0 : j.last - j.first;
+    if (need > 0) {
+      if ((uint64_t)j.off + need > found) {
+        j.n1 = -1;
+        st = GRKV_PAGES_FULL;
+      } else {
+        atomicMax(&used_s, j.off + need);
+      }
+    }
+    if (j.n1 >= 0) a.pg.lens[j.dst] = j.n1;
+    if (a.entries <= kPlanTh || st != GRKV_PAGES_OK) {
+      a.jobs[i] = j;
+      if (a.status) a.status[i] = st;
+    }
   }
   __syncthreads();
-
-  // the bits of the pages handed out
-  const uint32_t used = (uint32_t)used_s;
-  uint32_t before = 0;
-  for (int w0 = 0; w0 < words && before < used; w0 += 4 * kPlanTh) {
-    uint32_t bits[4], n = 0, total;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int w = w0 + 4 * tid + k;
-      bits[k] = w < words ? a.pg.free_bits[w] : 0u;
-      n += __popc(bits[k]);
-    }
-    uint32_t r = before + block_exclusive_scan(n, scratch32, &total);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      uint32_t b = bits[k];
-      for (; b != 0 && r < used; ++r) b &= b - 1;
-      if (b != bits[k]) a.pg.free_bits[w0 + 4 * tid + k] = b;
-    }
-    before += total;
-  }
+  // pages taken for refused entries go back
+  for (uint32_t r = used_s + tid; r < found; r += kPlanTh)
+    atomicOr(a.pg.free_bits + (a.ids[r] >> 5), 1u << (a.ids[r] & 31));
 }
+
+__global__ __launch_bounds__(kPlanTh) void plan_kernel(PagesK a) { make_plan_block(a); }
 
 // The rows of a launch: row g is row (g % tile + tile * ((g / tile) % per)) of
 // entry g / tile / per, so that the rows of one tile are neighbours and a
@@ -264,14 +291,13 @@ __device__ __forceinline__ void copy8(const S* src, T* dst) {
   }
 }
 
-// T, KS, VS: u16 (bf16) or float.
+// Rows g0, g0 + stride, .. of an append; T, KS, VS: u16 (bf16) or float.
 template <typename T, typename KS, typename VS>
-__global__ __launch_bounds__(kCopyTh) void append_kernel(PagesK a, RowMap m, const KS* k,
-                                                         const VS* v) {
+__device__ __forceinline__ void append_rows(const PagesK& a, const RowMap& m, const KS* k, const VS* v,
+                                            uint32_t g0, uint32_t stride) {
   const int d = a.pg.head_dim, cpr = d / 8;   // 8 or 16 steps of 8 values per row
-  const int c = (threadIdx.x & (cpr - 1)) * 8;
-  const uint32_t stride = gridDim.x * (kCopyTh / cpr);
-  for (uint32_t g = blockIdx.x * (kCopyTh / cpr) + threadIdx.x / cpr; g < m.rows; g += stride) {
+  const int c = (threadIdx.x & (cpr - 1)) * 8, mask = (1 << a.shift) - 1;
+  for (uint32_t g = g0; g < m.rows; g += stride) {
     int e, row;
     map_row(m, g, &e, &row);
     const PageJob j = a.jobs[e];
@@ -284,75 +310,117 @@ __global__ __launch_bounds__(kCopyTh) void append_kernel(PagesK a, RowMap m, con
       if ((unsigned)page >= (unsigned)a.pg.pages) continue;
     } else {
       page = a.ids[j.off + ord - j.first];
-      if (c == 0 && (slot & ((1 << a.shift) - 1)) == 0) {
+      if (c == 0 && (slot & mask) == 0) {
         *entry = page;
         a.pg.refs[page] = 1;
       }
     }
-    const size_t to = (((size_t)page << a.shift) + (slot & ((1 << a.shift) - 1))) * d + c;
+    const size_t to = (((size_t)page << a.shift) + (slot & mask)) * d + c;
     const size_t from = (size_t)(j.start + row) * d + c;
     copy8(k + from, (T*)a.pg.k + to);
     copy8(v + from, (T*)a.pg.v + to);
   }
 }
 
-// Rows of the new pages of a fork or a compaction, read through the old table.
+template <typename T, typename KS, typename VS>
+__global__ __launch_bounds__(kCopyTh) void append_kernel(PagesK a, RowMap m, const KS* k, const VS* v) {
+  const int per = kCopyTh / (a.pg.head_dim / 8);
+  append_rows<T>(a, m, k, v, blockIdx.x * per + threadIdx.x / (a.pg.head_dim / 8), gridDim.x * per);
+}
+
+// The few rows of a decoding step, by the block that plans them.
+template <typename T, typename KS, typename VS>
+__global__ __launch_bounds__(kPlanTh) void plan_append_kernel(PagesK a, RowMap m, const KS* k, const VS* v) {
+  make_plan_block(a);
+  __syncthreads();
+  const int cpr = a.pg.head_dim / 8;
+  append_rows<T>(a, m, k, v, threadIdx.x / cpr, kPlanTh / cpr);
+}
+
+// Slot `row` of the new pages of a fork or a compaction, read through the old
+// table; this thread's 16 bytes of K and V at column c.
+template <typename T>
+__device__ __forceinline__ void move_row(const PagesK& a, const PageJob& j, int e, int row, int c,
+                                         const int32_t* idx) {
+  const int d = a.pg.head_dim, mask = (1 << a.shift) - 1;
+  const int slot = (j.first << a.shift) + row;
+  if (slot >= j.n1) return;
+  int from = slot;
+  if (slot >= j.keep) from = idx[j.start + (slot - j.keep)];
+  uint4 rk = make_uint4(0, 0, 0, 0), rv = rk;
+  if ((unsigned)from < (unsigned)j.n0) {
+    const int p = a.pg.table[(size_t)j.src * a.pg.max_pages + (from >> a.shift)];
+    if ((unsigned)p < (unsigned)a.pg.pages) {
+      const size_t at = (((size_t)p << a.shift) + (from & mask)) * d + c;
+      rk = *reinterpret_cast<const uint4*>((const T*)a.pg.k + at);
+      rv = *reinterpret_cast<const uint4*>((const T*)a.pg.v + at);
+    }
+  } else if (c == 0 && a.status) {
+    a.status[e] = GRKV_PAGES_RANGE;
+  }
+  const int page = a.ids[j.off + (slot >> a.shift) - j.first];
+  const size_t to = (((size_t)page << a.shift) + (slot & mask)) * d + c;
+  *reinterpret_cast<uint4*>((T*)a.pg.k + to) = rk;
+  *reinterpret_cast<uint4*>((T*)a.pg.v + to) = rv;
+}
+
 template <typename T>
 __global__ __launch_bounds__(kCopyTh) void move_kernel(PagesK a, RowMap m, const int32_t* idx) {
   constexpr int V = 16 / sizeof(T);
-  const int d = a.pg.head_dim, cpr = d / V;   // 8, 16 or 32 chunks per row
+  const int cpr = a.pg.head_dim / V;   // 8, 16 or 32 chunks per row
   const int c = (threadIdx.x & (cpr - 1)) * V;
-  const int mask = (1 << a.shift) - 1;
   const uint32_t stride = gridDim.x * (kCopyTh / cpr);
   for (uint32_t g = blockIdx.x * (kCopyTh / cpr) + threadIdx.x / cpr; g < m.rows; g += stride) {
     int e, row;
     map_row(m, g, &e, &row);
-    const PageJob j = a.jobs[e];
-    const int slot = (j.first << a.shift) + row;
-    if (slot >= j.n1) continue;
-    int from = slot;
-    if (slot >= j.keep) from = idx[j.start + (slot - j.keep)];
-    uint4 rk = make_uint4(0, 0, 0, 0), rv = rk;
-    if ((unsigned)from < (unsigned)j.n0) {
-      const int p = a.pg.table[(size_t)j.src * a.pg.max_pages + (from >> a.shift)];
-      if ((unsigned)p < (unsigned)a.pg.pages) {
-        const size_t at = (((size_t)p << a.shift) + (from & mask)) * d + c;
-        rk = *reinterpret_cast<const uint4*>((const T*)a.pg.k + at);
-        rv = *reinterpret_cast<const uint4*>((const T*)a.pg.v + at);
-      }
-    } else if (c == 0 && a.status) {
-      a.status[e] = GRKV_PAGES_RANGE;
-    }
-    const int page = a.ids[j.off + (slot >> a.shift) - j.first];
-    const size_t to = (((size_t)page << a.shift) + (slot & mask)) * d + c;
-    *reinterpret_cast<uint4*>((T*)a.pg.k + to) = rk;
-    *reinterpret_cast<uint4*>((T*)a.pg.v + to) = rv;
+    move_row<T>(a, a.jobs[e], e, row, c, idx);
   }
 }
 
-__device__ __forceinline__ void release_page(const grkv_pages& pg, int p) {
-  if ((unsigned)p >= (unsigned)pg.pages) return;
-  if (atomicSub(pg.refs + p, 1) == 1) atomicOr(pg.free_bits + (p >> 5), 1u << (p & 31));
+// Page p of each lane (or -1) leaves one table; one that no table holds any more is
+// free.  Every lane of the wave takes part: neighbours whose pages share a word of
+// the bitmap (a unit's pages mostly follow one another) set their bits by one atomic,
+// since all words of a pool lie in few cache lines.  (2048 pages of 8 units by
+// one atomic each took 12 us.)
+__device__ __forceinline__ void release_pages(const grkv_pages& pg, int p) {
+  uint32_t bit = 0;
+  int word = -1;
+  if ((unsigned)p < (unsigned)pg.pages && atomicSub(pg.refs + p, 1) == 1) {
+    word = p >> 5;
+    bit = 1u << (p & 31);
+  }
+  const int lane = threadIdx.x & 63;
+  // bits of the run of equal words that ends at this lane
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const uint32_t b = __shfl_up(bit, k);
+    const int w = __shfl_up(word, k);
+    if (lane >= k && w == word) bit |= b;
+  }
+  const int next = __shfl_down(word, 1);
+  if (word >= 0 && (lane == 63 || next != word)) atomicOr(pg.free_bits + word, bit);
 }
 
-// One block per entry: the destination's table row, and the counts.  A page
+// The destination's table row and the counts, by the threads of a block.  A page
 // that is given up here and shared there (two entries, one page) never passes
 // zero in between: the unit it is shared from keeps it.
-__global__ __launch_bounds__(kCopyTh) void commit_kernel(PagesK a) {
-  const PageJob j = a.jobs[blockIdx.x];
+__device__ __forceinline__ void commit(const PagesK& a, const PageJob& j) {
   if (j.n1 < 0) return;
   const int32_t* from = a.pg.table + (size_t)j.src * a.pg.max_pages;
   int32_t* to = a.pg.table + (size_t)j.dst * a.pg.max_pages;
   if (j.src != j.dst) {
-    for (int o = threadIdx.x; o < j.first; o += kCopyTh) {
+    for (int o = threadIdx.x; o < j.first; o += blockDim.x) {
       const int p = from[o];
       to[o] = p;
       if ((unsigned)p < (unsigned)a.pg.pages) atomicAdd(a.pg.refs + p, 1);
     }
   }
   const int held = j.src == j.dst ? (j.n0 + (1 << a.shift) - 1) >> a.shift : 0;
-  for (int o = j.first + threadIdx.x; o < max(held, j.last); o += kCopyTh) {
-    if (o < held) release_page(a.pg, to[o]);
+  const int end = max(held, j.last);
+  for (int o0 = j.first; o0 < end; o0 += blockDim.x) {
+    const int o = o0 + threadIdx.x;
+    release_pages(a.pg, o < held ? to[o] : -1);
+    if (o >= end) continue;
     int p = -1;
     if (o < j.last) {
       p = a.ids[j.off + o - j.first];
@@ -360,6 +428,24 @@ __global__ __launch_bounds__(kCopyTh) void commit_kernel(PagesK a) {
     }
     to[o] = p;
   }
+}
+
+__global__ __launch_bounds__(kCopyTh) void commit_kernel(PagesK a) { commit(a, a.jobs[blockIdx.x]); }
+
+// Both, one block per entry: the rows that are read through the old table row are
+// copied before the row changes (no other entry reads it: a unit is not both read
+// and written by two entries).
+template <typename T>
+__global__ __launch_bounds__(kCopyTh) void move_commit_kernel(PagesK a, const int32_t* idx) {
+  constexpr int V = 16 / sizeof(T);
+  const PageJob j = a.jobs[blockIdx.x];
+  const int cpr = a.pg.head_dim / V;
+  const int c = (threadIdx.x & (cpr - 1)) * V, rows = j.n1 - (j.first << a.shift);
+#pragma unroll 4
+  for (int row = threadIdx.x / cpr; row < rows; row += kCopyTh / cpr)
+    move_row<T>(a, j, blockIdx.x, row, c, idx);
+  __syncthreads();
+  commit(a, j);
 }
 
 // One block per entry.  The first block to take a unit's length frees it.
@@ -372,11 +458,13 @@ __global__ __launch_bounds__(kCopyTh) void free_kernel(PagesK a) {
     n_s = ok ? atomicExch(a.pg.lens + u, 0) : 0;
   }
   __syncthreads();
-  const int64_t held = ((int64_t)n_s + (1 << a.shift) - 1) >> a.shift;
+  if (n_s <= 0) return;
+  const int held = min((n_s - 1 >> a.shift) + 1, a.pg.max_pages);
   int32_t* row = a.pg.table + (size_t)u * a.pg.max_pages;
-  for (int o = threadIdx.x; o < held && o < a.pg.max_pages; o += kCopyTh) {
-    release_page(a.pg, row[o]);
-    row[o] = -1;
+  for (int o0 = 0; o0 < held; o0 += kCopyTh) {
+    const int o = o0 + threadIdx.x;
+    release_pages(a.pg, o < held ? row[o] : -1);
+    if (o < held) row[o] = -1;
   }
 }
 
@@ -437,11 +525,22 @@ unsigned copy_blocks(const RowMap& m, int per_block) {
   return b < 16384 ? b : 16384;
 }
 
+// Rows of a call that the planning block stores itself (one row for each of 32
+// units: one launch of 5.7 us against two of 6.9 and 3.5).
+constexpr int64_t kInlineRows = 128;
+
 template <typename T, typename KS, typename VS>
 void launch_append(const PagesK& a, const PagesCall& c, hipStream_t s) {
   const RowMap m = make_map(a.entries, a.rows);
+  const KS* k = (const KS*)c.k;
+  const VS* v = (const VS*)c.v;
+  if ((int64_t)a.entries * a.rows <= kInlineRows) {
+    hipLaunchKernelGGL((plan_append_kernel<T, KS, VS>), dim3(1), dim3(kPlanTh), 0, s, a, m, k, v);
+    return;
+  }
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanTh), 0, s, a);
   hipLaunchKernelGGL((append_kernel<T, KS, VS>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim / 8))),
-                     dim3(kCopyTh), 0, s, a, m, (const KS*)c.k, (const VS*)c.v);
+                     dim3(kCopyTh), 0, s, a, m, k, v);
 }
 
 template <typename T>
@@ -450,6 +549,25 @@ void launch_append_t(const PagesK& a, const PagesCall& c, hipStream_t s) {
     c.v_dtype == GRKV_BF16 ? launch_append<T, u16, u16>(a, c, s) : launch_append<T, u16, float>(a, c, s);
   else
     c.v_dtype == GRKV_BF16 ? launch_append<T, float, u16>(a, c, s) : launch_append<T, float, float>(a, c, s);
+}
+
+// Fork and compact.  An entry of up to kEntryRows rows (those under keep in its page,
+// then the picked ones), or one of very many, is one block's; longer ones are
+// spread over blocks and committed by a launch of their own.
+constexpr int64_t kEntryRows = 256, kManyEntries = 512;
+
+template <typename T>
+void launch_move(const PagesK& a, const PagesCall& c, hipStream_t s) {
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanTh), 0, s, a);
+  const int64_t most = (int64_t)a.rows + (c.op == kPagesFork || c.keep ? a.pg.page_size - 1 : 0);
+  if (most <= kEntryRows || a.entries >= kManyEntries) {
+    hipLaunchKernelGGL((move_commit_kernel<T>), dim3(a.entries), dim3(kCopyTh), 0, s, a, c.idx);
+    return;
+  }
+  const RowMap m = make_map(a.entries, most);
+  hipLaunchKernelGGL((move_kernel<T>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim * (int)sizeof(T) / 16))),
+                     dim3(kCopyTh), 0, s, a, m, c.idx);
+  hipLaunchKernelGGL(commit_kernel, dim3(a.entries), dim3(kCopyTh), 0, s, a);
 }
 
 }  // namespace
@@ -475,29 +593,9 @@ hipError_t launch_pages(const PagesCall& c, hipStream_t s) {
     hipLaunchKernelGGL(free_kernel, dim3(a.entries), dim3(kCopyTh), 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanTh), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
   const bool bf16 = a.pg.dtype == GRKV_BF16;
-  if (c.op == kPagesAppend) {
-    if (a.rows == 0) return hipSuccess;
-    bf16 ? launch_append_t<u16>(a, c, s) : launch_append_t<float>(a, c, s);
-    return hipGetLastError();
-  }
-  // the rows under keep in its page (fork: keep is the length), then the picked ones
-  const int64_t most = (int64_t)a.rows + (c.op == kPagesFork || c.keep ? a.pg.page_size - 1 : 0);
-  if (most > 0) {
-    const RowMap m = make_map(a.entries, most);
-    if (bf16)
-      hipLaunchKernelGGL((move_kernel<u16>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim / 8))),
-                         dim3(kCopyTh), 0, s, a, m, c.idx);
-    else
-      hipLaunchKernelGGL((move_kernel<float>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim / 4))),
-                         dim3(kCopyTh), 0, s, a, m, c.idx);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(commit_kernel, dim3(a.entries), dim3(kCopyTh), 0, s, a);
+  if (c.op == kPagesAppend) bf16 ? launch_append_t<u16>(a, c, s) : launch_append_t<float>(a, c, s);
+  else bf16 ? launch_move<u16>(a, c, s) : launch_move<float>(a, c, s);
   return hipGetLastError();
 }
 
