@@ -46,9 +46,15 @@ __device__ __forceinline__ Span make_span(const AttendK& a, int len, int base, i
   const int end = (s.kend + tk - 1) / tk;
   s.nt = s.at + max(0, end - s.bt);
   // (a sink tile past the end: a.n_sink was cut to kend)
-  s.chunk = max(a.min_tiles, (s.nt + a.splits - 1) / a.splits);
+  s.chunk = max(a.min_tiles, (s.nt + a.splits - 1) >> a.split_shift);
   s.ns = (s.nt + s.chunk - 1) / s.chunk;
   return s;
+}
+
+// r / group for r < 2^31, by the multiplication with a rounded-up reciprocal of
+// 32 + gshift bits (its top bit is the addition).
+__device__ __forceinline__ int group_of(const AttendK& a, int r) {
+  return (int)((__umulhi((uint32_t)r, a.gmul) + (uint32_t)r) >> a.gshift);
 }
 
 // Block b's entry, row group and split.  Blocks go round the 8 XCDs in turn: with
@@ -58,7 +64,10 @@ __device__ __forceinline__ Span make_span(const AttendK& a, int len, int base, i
 __device__ __forceinline__ bool block_work(const AttendK& a, int* e, int* rg, int* sp) {
   const uint32_t b = blockIdx.x;
   uint32_t w;
-  if (a.grouped) {
+  if (a.row_groups == 1) {
+    w = b;
+    *rg = 0;
+  } else if (a.grouped) {
     const uint32_t c = b >> 3;
     w = (c / a.row_groups) * 8 + (b & 7);
     *rg = (int)(c % a.row_groups);
@@ -67,8 +76,8 @@ __device__ __forceinline__ bool block_work(const AttendK& a, int* e, int* rg, in
     w = b % all;
     *rg = (int)(b / all);
   }
-  *sp = (int)(w % a.splits);
-  const uint32_t ee = w / a.splits;
+  *sp = (int)(w & (a.splits - 1));   // (a power of two)
+  const uint32_t ee = w >> a.split_shift;
   *e = (int)ee;
   return ee < (uint32_t)a.entries;
 }
@@ -104,6 +113,89 @@ __device__ __forceinline__ void write_out(const AttendK& a, size_t at, int ch, f
     *reinterpret_cast<f32x4*>((E*)a.o + at * D + 4 * ch) = x;
   }
   if (ch == 0 && a.lse) a.lse[at] = lx == 0.f ? -__builtin_huge_valf() : (m + __log2f(lx)) * kLn2;
+}
+
+// Sums of one split.
+struct Split {
+  float m, l, lx;   // reference; weights after and before their rounding
+  f32x4 x;          // four columns
+};
+
+// Parts of splits that the blocks join themselves pass between XCDs inside one
+// launch, whose L2 caches are not coherent for plain accesses.  They are written
+// and read by atomic accesses of agent scope, which go through to where all XCDs
+// meet; a wave's own wait for its stores then orders them.  (Fences of that scope
+// write back and invalidate a whole L2: 512 units of 4250 keys, two splits, 457 us
+// against 227 with a second launch.)
+__device__ __forceinline__ void put64(void* p, uint64_t v) {
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t get64(const void* p) {
+  return __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void wait_stores() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ void put4(float* p, f32x4 v, bool shared) {
+  if (shared) {
+    const ulonglong2 w = __builtin_bit_cast(ulonglong2, v);
+    put64(p, w.x);
+    put64(p + 2, w.y);
+  } else {
+    *reinterpret_cast<f32x4*>(p) = v;
+  }
+}
+template <bool SHARED>
+__device__ __forceinline__ f32x4 get4(const float* p) {
+  if constexpr (SHARED) {
+    const ulonglong2 w = make_ulonglong2(get64(p), get64(p + 2));
+    return __builtin_bit_cast(f32x4, w);
+  } else {
+    return *reinterpret_cast<const f32x4*>(p);
+  }
+}
+
+// Columns 4 ch .. of a row from splits s0, s0 + step, .. below ns, in that order,
+// against the largest reference of all ns.  at0: the row in split 0.
+template <int D, bool SHARED>
+__device__ __forceinline__ Split add_splits(const AttendK& a, size_t at0, int ns, int s0, int step,
+                                            int ch) {
+  const int R = a.group * a.tokens;
+  Split o = {-kUnset, 0.f, 0.f, zero4()};
+#pragma unroll 8
+  for (int s = 0; s < ns; ++s) o.m = fmaxf(o.m, get4<SHARED>((const float*)(a.mpart + at0 + (size_t)s * R))[0]);
+#pragma unroll 8
+  for (int s = s0; s < ns; s += step) {
+    const size_t at = at0 + (size_t)s * R;
+    const f32x4 ml = get4<SHARED>((const float*)(a.mpart + at));
+    const float f = __builtin_amdgcn_exp2f(ml[0] - o.m);
+    o.l += ml[1] * f;
+    o.lx += ml[2] * f;
+    o.x += get4<SHARED>(a.opart + at * D + 4 * ch) * f;
+  }
+  return o;
+}
+
+// Whether this block is one that finds all `ns` splits of its row group written:
+// the last to finish, or another that finishes with it (they write the same
+// rows).  Every block marks its split with the call's nonce once its parts are
+// out, and reads all marks once its own is: of two blocks one sees the other's.  A
+// block that sees them all puts them back to zero, so that a captured call finds
+// no marks of its last replay; what else the workspace held does not equal a nonce
+// of 64 bits.
+__device__ __forceinline__ bool splits_done(const AttendK& a, size_t group, int sp, int ns) {
+  __shared__ int done_s;
+  wait_stores();   // every wave's part is out
+  __syncthreads();
+  uint64_t* f = a.flags + group * a.splits;
+  if (threadIdx.x < 64) {
+    if (threadIdx.x == 0) put64(f + sp, a.nonce);
+    wait_stores();
+    const bool all = __all((int)threadIdx.x >= ns || get64(f + threadIdx.x) == a.nonce);
+    if (all && (int)threadIdx.x < ns) put64(f + threadIdx.x, 0);
+    if (threadIdx.x == 0) done_s = all;
+  }
+  __syncthreads();
+  return done_s != 0;
 }
 
 // What this lane's row sees: slots before lim from lo on or below n_sink, and
@@ -197,7 +289,7 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
     return ((size_t)((unsigned)p < (unsigned)a.pages ? p : 0) << a.shift) + (slot & ((1 << a.shift) - 1));
   };
   for (int n = 0; n < count; ++n) {
-    const int r = first + n, i = r / a.group, g = r - i * a.group;
+    const int r = first + n, i = group_of(a, r), g = r - i * a.group;
     if (r >= R) return;
     const RowSight sight = row_sight<PAGED>(a, base, i, i < t, family, depth);
     const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
@@ -245,8 +337,9 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
     }
     if (sn.ns > 1) {
       const size_t to = ((size_t)e * a.splits + sp) * R + r;
-      for (int c = 0; c < C; ++c) a.opart[to * D + 64 * c + lane] = o[c];
-      if (lane == 0) a.mpart[to] = make_float4(m, l, lx, 0.f);
+      for (int c = 0; c < C; ++c)
+        __hip_atomic_store(a.opart + to * D + 64 * c + lane, o[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (lane == 0) put4((float*)(a.mpart + to), (f32x4){m, l, lx, 0.f}, true);
     } else {
       const float inv = l == 0.f ? 0.f : 1.f / l;
       for (int c = 0; c < C; ++c) {

@@ -32,6 +32,8 @@
 // Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
 #include "attend.h"
 
+#include <atomic>
+#include <chrono>
 #include <type_traits>
 
 namespace grkv {
@@ -79,7 +81,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   const int32_t* trow;
   entry_shape(a, e, &len, &t, &trow);
   const int base = len - t;
-  const int i0 = r0 / a.group, i1 = min(r0 + 16 * RT - 1, R - 1) / a.group;
+  const int i0 = group_of(a, r0), i1 = group_of(a, min(r0 + 16 * RT - 1, R - 1));
   const Span sn = make_span(a, len, base, t, i0, i1, TK);
   const int vt0 = sp * sn.chunk, vt1 = min(sn.nt, vt0 + sn.chunk);
   if (sp > 0 && vt0 >= sn.nt) return;
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = r0 + 16 * rt + l16;
-    const int i = r / a.group, g = r - i * a.group;
+    const int i = group_of(a, r), g = r - i * a.group;
     const bool on = r < R && i < t;
     sight[rt] = row_sight<PAGED>(a, base, i, on, family, depth);
     const E* q = (const E*)a.q + (((size_t)e * a.group + g) * a.tokens + i) * D;
@@ -329,6 +331,19 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
     }
   }
 
+  // the splits of a short call, by the block that finishes last
+  constexpr int CR = D / 4;   // 4-value chunks of a row
+  auto join = [&]() __attribute__((always_inline)) {
+    if (sn.ns < 2 || !a.flags || !splits_done(a, (size_t)e * a.row_groups + rg, sp, sn.ns)) return;
+    for (int c = tid; c < 16 * RT * CR; c += kAtTh) {
+      const int r = r0 + c / CR, ch = c % CR;
+      const int i = group_of(a, r), g = r - i * a.group;
+      if (r >= R || i >= t) continue;
+      const Split o = add_splits<D, true>(a, (size_t)e * a.splits * R + r, sn.ns, 0, 1, ch);
+      write_out<E, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, o.x, o.m, o.l, o.lx);
+    }
+  };
+
   // the waves' parts: references, then rows scaled to the largest, summed over
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
@@ -336,6 +351,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   if (__syncthreads_or(odd)) {
     rows_by_key<E, D, PAGED>(a, sn, e, sp, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
                              family, depth);
+    join();
     return;
   }
 #pragma unroll
@@ -362,10 +378,9 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
       *reinterpret_cast<f32x4*>(part + row * D * 4 + (((4 * dt + gq) ^ l16) << 4)) = acc[dt][rt] * f;
   }
   __syncthreads();
-  constexpr int CR = D / 4;   // 4-value chunks of a row
   for (int c = tid; c < 16 * RT * CR; c += kAtTh) {
     const int row = c / CR, ch = c % CR, r = r0 + row;
-    const int i = r / a.group, g = r - i * a.group;
+    const int i = group_of(a, r), g = r - i * a.group;
     if (r >= R || i >= t) continue;
     float m = m_s[0][row], l = 0.f, lx = 0.f;
 #pragma unroll
@@ -381,16 +396,17 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
     }
     if (sn.ns > 1) {
       const size_t at = ((size_t)e * a.splits + sp) * R + r;
-      *reinterpret_cast<f32x4*>(a.opart + at * D + 4 * ch) = x;
-      if (ch == 0) a.mpart[at] = make_float4(m, l, lx, 0.f);
+      put4(a.opart + at * D + 4 * ch, x, a.flags != nullptr);
+      if (ch == 0) put4((float*)(a.mpart + at), (f32x4){m, l, lx, 0.f}, a.flags != nullptr);
     } else {
       const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
       write_out<E, D>(a, at, ch, x, m, l, lx);
     }
   }
+  join();
 }
 
-// The splits of a row: one thread per 4 values and every GS-th split, whose sums
+// The splits of a row, where they are not joined by attend_kernel: one thread per 4 values and every GS-th split, whose sums
 // are added in order.  GS: threads that share a value.
 template <typename E, int D, int GS>
 __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
@@ -405,43 +421,31 @@ __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   int len = 0, t = 0;
   const int32_t* trow;
   if (on) entry_shape(a, e, &len, &t, &trow);
-  const int i = r / a.group, g = r - i * a.group;
+  const int i = group_of(a, r), g = r - i * a.group;
   int ns = 0;
   if (on && i < t) {
     const int r0 = r / a.rows * a.rows;
-    ns = make_span(a, len, len - t, t, r0 / a.group, min(r0 + a.rows - 1, R - 1) / a.group, a.tile_keys).ns;
+    ns = make_span(a, len, len - t, t, group_of(a, r0), group_of(a, min(r0 + a.rows - 1, R - 1)), a.tile_keys).ns;
   }
   on = ns > 1;   // (a single split has written its row)
   const size_t at0 = (size_t)e * a.splits * R + r;
-  float m = -kUnset, l = 0.f, lx = 0.f;
-  f32x4 x = zero4();
-  if (on) {
-#pragma unroll 8
-    for (int s = 0; s < ns; ++s) m = fmaxf(m, a.mpart[at0 + (size_t)s * R].x);
-#pragma unroll 4
-    for (int s = gs; s < ns; s += GS) {
-      const float4 ml = a.mpart[at0 + (size_t)s * R];
-      const float f = __builtin_amdgcn_exp2f(ml.x - m);
-      l += ml.y * f;
-      lx += ml.z * f;
-      x += *reinterpret_cast<const f32x4*>(a.opart + (at0 + (size_t)s * R) * D + 4 * ch) * f;
-    }
-  }
+  Split o = {-kUnset, 0.f, 0.f, zero4()};
+  if (on) o = add_splits<D, false>(a, at0, ns, gs, GS, ch);
   if constexpr (GS > 1) {
-    part[tid] = x;
-    psum[tid] = make_float2(l, lx);
+    part[tid] = o.x;
+    psum[tid] = make_float2(o.l, o.lx);
     __syncthreads();
     on = on && gs == 0;
     if (on) {
 #pragma unroll
       for (int k = 1; k < GS; ++k) {
-        x += part[tid + k * CR];
-        l += psum[tid + k * CR].x;
-        lx += psum[tid + k * CR].y;
+        o.x += part[tid + k * CR];
+        o.l += psum[tid + k * CR].x;
+        o.lx += psum[tid + k * CR].y;
       }
     }
   }
-  if (on) write_out<E, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, x, m, l, lx);
+  if (on) write_out<E, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, o.x, o.m, o.l, o.lx);
 }
 
 template <typename E, int D>
@@ -463,7 +467,7 @@ hipError_t launch_d(const AttendK& a, int rt, hipStream_t s) {
 template <typename E, int D>
 hipError_t launch_ed(const AttendK& a, int rt, hipStream_t s) {
   const hipError_t e = launch_d<E, D>(a, rt, s);
-  if (e != hipSuccess || a.splits == 1) return e;
+  if (e != hipSuccess || a.splits == 1 || a.flags) return e;
   const int64_t rows = (int64_t)a.entries * a.group * a.tokens;
   constexpr int GS = kAtTh / (D / 4);
   if (a.splits > GS)
@@ -475,9 +479,28 @@ hipError_t launch_ed(const AttendK& a, int rt, hipStream_t s) {
 
 }  // namespace
 
+// Marks of one call's splits: different for every call of a process, and unlike what
+// a workspace may hold.
+static uint64_t next_nonce() {
+  static const uint64_t seed = (uint64_t)std::chrono::system_clock::now().time_since_epoch().count();
+  static std::atomic<uint64_t> calls{0};
+  uint64_t x = seed + 0x9e3779b97f4a7c15ull * ++calls;   // (splitmix64)
+  x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;
+  x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
+  x ^= x >> 31;
+  return x != 0 ? x : 1;
+}
+
+// Splits that the blocks themselves join: a few, in calls whose blocks all run at once
+// (8 units of 2048 keys, 8 splits: one launch of 11.7 us against 9.8 and 3.9).  More
+// are combined by a launch of their own, which has more threads for them (256 units
+// of 4100 keys, 4 splits: 98 and 5 us against 110).
+constexpr int kJoinedSplits = 16, kJoinedBlocks = 512;
+
 // Kernel, splits and workspace of a call whose rows see at most `slots` slots
-// each.
-AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots) {
+// each, or (ragged) any number up to that.
+AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots,
+                       bool ragged) {
   AttendPlan p;
   const int64_t R = (int64_t)group * tokens;
   const bool bf16 = dtype == GRKV_BF16;
@@ -487,28 +510,36 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
     p.rows = 128;
     p.tile_keys = kWideKeys;
     p.min_tiles = 8;
+    // (32 units of 20k to 32k keys, 128 rows, 256 / 512 / 1024 blocks: 138 / 116 / 139 us)
     target = 512;
   } else {
     p.rt = R <= 16 ? 1 : 2;
     p.rows = 16 * p.rt;
     p.tile_keys = bf16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
     p.min_tiles = 8;
-    target = 1024;
+    // two blocks per compute unit; lengths that may differ and are many: finer, so
+    // that the longest ones end with the others (512 units of 500 to 8000 keys, 512 /
+    // 1024 / 2048 / 4096 blocks: 242 / 226 / 215 / 222 us; 8 units of 128k keys 103 / 109 /
+    // 125; 256 units with a 4k window 100 / 103 / 108)
+    target = ragged && (int64_t)entries * ((R + p.rows - 1) / p.rows) >= 256 ? 2048 : 512;
   }
   p.row_groups = (int)((R + p.rows - 1) / p.rows);
   const int64_t tiles = (slots + p.tile_keys - 1) / p.tile_keys;
   const int64_t most = (tiles + p.min_tiles - 1) / p.min_tiles;
   int64_t s = target / ((int64_t)entries * p.row_groups);
   s = s < most ? s : most;
-  p.splits = (int)(s < 1 ? 1 : s > 256 ? 256 : s);
+  p.splits = 1;   // a power of two
+  while (2 * p.splits <= s && p.splits < 256) p.splits *= 2;
   const int64_t w = (int64_t)entries * p.splits;
   p.grouped = w % 8 == 0 || w >= 64;
   p.blocks = (p.grouped ? (w + 7) / 8 * 8 : w) * p.row_groups;
+  p.joined = p.rt > 0 && p.splits > 1 && p.splits <= kJoinedSplits && p.blocks <= kJoinedBlocks;
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   const size_t rows = p.splits > 1 ? (size_t)w * R : 0;
   p.opart = 0;
   p.mpart = up(rows * d * sizeof(float));
-  p.total = p.mpart + up(rows * sizeof(float4));
+  p.flags = p.mpart + up(rows * sizeof(float4));
+  p.total = p.flags + (p.joined ? up((size_t)w * p.row_groups * sizeof(uint64_t)) : 0);
   return p;
 }
 
@@ -524,6 +555,12 @@ hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void*
   a.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
   a.opart = (float*)((char*)workspace + p.opart);
   a.mpart = (float4*)((char*)workspace + p.mpart);
+  a.flags = p.joined ? (uint64_t*)((char*)workspace + p.flags) : nullptr;
+  a.nonce = p.joined ? next_nonce() : 0;
+  a.split_shift = __builtin_ctz((unsigned)p.splits);
+  a.gshift = 0;
+  while ((1ll << a.gshift) < a.group) ++a.gshift;
+  a.gmul = (uint32_t)((((1ull << a.gshift) - (uint64_t)a.group) << 32) / (uint64_t)a.group + 1);
   if (dtype == GRKV_BF16) return d == 64 ? launch_ed<u16, 64>(a, p.rt, s) : launch_ed<u16, 128>(a, p.rt, s);
   return d == 64 ? launch_ed<float, 64>(a, p.rt, s) : launch_ed<float, 128>(a, p.rt, s);
 }

@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   const int32_t* trow;
   entry_shape(a, e, &len, &t, &trow);
   const int base = len - t;
-  const Span sn = make_span(a, len, base, t, r0 / a.group, min(r0 + a.rows - 1, R - 1) / a.group, TK);
+  const Span sn = make_span(a, len, base, t, group_of(a, r0), group_of(a, min(r0 + a.rows - 1, R - 1)), TK);
   const int vt0 = sp * sn.chunk, vt1 = min(sn.nt, vt0 + sn.chunk);
   if (sp > 0 && vt0 >= sn.nt) return;
 
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   RowSight sight;
   {
     const int r = w0 + l32;
-    const int i = r / a.group, g = r - i * a.group;
+    const int i = group_of(a, r), g = r - i * a.group;
     const bool on = r < R && i < t;
     sight = row_sight<PAGED>(a, base, i, on, family, depth);
     const u16* q = (const u16*)a.q + (((size_t)e * a.group + g) * a.tokens + i) * D;
@@ -101,8 +101,8 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   // slots that every row of the wave sees: before lim and from lo on, or sinks
   int lim = sn.lim, lo = sn.lo;
   if (!PAGED) {
-    lim = base + min(w0, R - 1) / a.group + 1;
-    lo = a.window > 0 ? base + min(w0 + 31, R - 1) / a.group + 1 - a.window : 0;
+    lim = base + group_of(a, min(w0, R - 1)) + 1;
+    lo = a.window > 0 ? base + group_of(a, min(w0 + 31, R - 1)) + 1 - a.window : 0;
   }
 
   // ---- loads: this wave brings rows 16 wave .. + 15 of every tile
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
           (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]};
   for (int k = lane; k < 32 * CR; k += 64) {
     const int row = k / CR, ch = k % CR, r = w0 + row;
-    const int i = r / a.group, g = r - i * a.group;
+    const int i = group_of(a, r), g = r - i * a.group;
     const float m = -__shfl(nref, row), lx = __shfl(sum, row), l = __shfl(rsum, row);
     if (r >= R || i >= t) continue;
     const f32x4 x = *reinterpret_cast<const f32x4*>(out + (row * CR + (ch ^ (row & 15))) * 16);

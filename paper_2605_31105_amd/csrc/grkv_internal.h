@@ -321,6 +321,10 @@ struct AttendK {
   int row_groups, splits, min_tiles;
   int rows, tile_keys;   // query rows of a block, keys of a tile
   int grouped;           // see block_work
+  uint32_t gmul;         // division by group: see group_of
+  int gshift, split_shift;
+  uint64_t* flags;       // [entries * row_groups][splits], or null: no split is joined in place
+  uint64_t nonce;
   int64_t blocks;
   int window, n_sink; // window 0: none
   float scale_log2;
@@ -336,11 +340,12 @@ struct AttendK {
 };
 struct AttendPlan {
   int rt;             // 16-row tiles of a block; 0: the wide kernel
-  int row_groups, splits, min_tiles, rows, tile_keys, grouped;
+  int row_groups, splits, min_tiles, rows, tile_keys, grouped, joined;
   int64_t blocks;
-  size_t opart, mpart, total;
+  size_t opart, mpart, flags, total;
 };
-AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots);
+AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots,
+                       bool ragged);
 constexpr int kWideKeys = 64;   // keys of a tile of the wide kernel (attend_wide.hip)
 hipError_t launch_attend_wide(const AttendK& a, int d, hipStream_t s);
 hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void* workspace,

@@ -71,7 +71,7 @@ int make_tree(const grkv_pages* pg, const grkv_tree* tr, TreeCall* c) {
   const int64_t cap = (int64_t)pg->max_pages * pg->page_size;
   const int64_t near = (int64_t)tr->n_sink + tr->window + tr->tokens;
   c->plan = attend_plan(tr->entries > 0 ? tr->entries : 1, tr->group, tr->tokens, pg->head_dim,
-                        pg->dtype, tr->window > 0 && near < cap ? near : cap);
+                        pg->dtype, tr->window > 0 && near < cap ? near : cap, tr->window == 0);
   if (c->plan.blocks >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
   AttendK& a = c->a;
   a = AttendK{};
@@ -104,7 +104,7 @@ int make_sink(const grkv_problem* prob, int64_t n, int32_t nq, int32_t window, i
   if (!sizes_ok(prob->units, prob->group, nq, prob->head_dim)) return GRKV_ERR_INVALID;
   const int64_t near = (int64_t)n_sink + window + nq;
   c->plan = attend_plan(prob->units, prob->group, nq, prob->head_dim, prob->dtype,
-                        window > 0 && near < n ? near : n);
+                        window > 0 && near < n ? near : n, false);
   if (c->plan.blocks >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
   AttendK& a = c->a;
   a = AttendK{};

@@ -261,6 +261,29 @@ def test_long_units_with_and_without_splits(units, group, tokens):
             check("unit %d" % u, o[u, h].cpu(), lse[u, h].cpu(), q[u, h].cpu(), k[u].cpu(), v[u].cpu(), seen)
 
 
+@pytest.mark.parametrize("group,tokens,n", [(4, 1, 2000), (2, 9, 1500), (4, 40, 3000), (1, 1, 40000)])
+def test_splits_do_not_depend_on_what_the_workspace_held(group, tokens, n):
+    # splits that blocks join themselves, and those combined by a second launch: with a
+    # workspace of ones, of zeros and of the last call's, the same rows bit for bit
+    import paper_2605_31105_amd as G
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    pg = G.new_pages(3, -(-n // 64), 3 * -(-n // 64), 64, 128)
+    k, v = (torch.randn((3, n, 128), device="cuda", generator=gen).to(BF) for _ in range(2))
+    assert not G.pages_append(pg, k, v).any().item()
+    q = torch.randn((3, group, tokens, 128), device="cuda", generator=gen).to(BF)
+    need = G.tree_attention_workspace_bytes(pg, 3, group, tokens)
+    assert need > 256
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    want, lse = G.tree_attention(q, pg, workspace=ws, return_lse=True)
+    for fill in (None, 0, 1, None, None):
+        if fill is not None:
+            ws.fill_(fill)
+        got, l2 = G.tree_attention(q, pg, workspace=ws, return_lse=True)
+        assert torch.equal(got, want) and torch.equal(l2, lse)
+    seen = tree_seen(n, tokens, list(range(-1, tokens - 1)), 0, 0)
+    check("unit 2", want[2, 0].cpu(), lse[2, 0].cpu(), q[2, 0].cpu(), k[2].cpu(), v[2].cpu(), seen)
+
+
 def test_captured_calls_and_another_stream():
     import paper_2605_31105_amd as G
     gen = torch.Generator().manual_seed(4)
