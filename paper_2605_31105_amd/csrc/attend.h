@@ -215,6 +215,23 @@ __device__ __forceinline__ bool sees(const RowSight& s, int j, int n_sink, int b
   return on;
 }
 
+// The same of slots slot0 .. slot0 + 31, a bit each.
+template <bool PAGED>
+__device__ __forceinline__ uint32_t sees32(const RowSight& s, int slot0, int n_sink, int base, int len) {
+  auto below = [&](int end) {   // the slots before `end`
+    const int n = end - slot0;
+    return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u;
+  };
+  uint32_t on = below(s.lim) & (~below(s.lo) | below(n_sink));
+  if (PAGED) {
+    const int n = slot0 - base;   // drafted token of the first of them
+    const uint32_t d = n >= 64 || n <= -32 ? 0u
+                       : n >= 0 ? (uint32_t)(s.bits >> n) : (uint32_t)(s.bits << -n);
+    on |= d & below(len) & ~below(0);
+  }
+  return on;
+}
+
 // Drafted token `lane` of entry e: its ancestors and itself (a bit per token) as
 // far as it sees them, and its depth, by doubling the step from a token to its
 // parent.  Every lane of the wave takes part.
@@ -267,9 +284,36 @@ __device__ __forceinline__ RowSight row_sight(const AttendK& a, int base, int i,
   return s;
 }
 
+// Whether a tile of vt0 .. vt1 - 1 that is not seen whole (by every row before lim and
+// from lo on) holds an infinity or NaN among its values.  One wave; asked only where
+// an output is NaN.
+template <typename E, int D, bool PAGED>
+__device__ __forceinline__ bool odd_values(const AttendK& a, const Span& sn, int e, int vt0, int vt1,
+                                           int tk, int lim, int lo, const int32_t* trow) {
+  const int lane = threadIdx.x & 63;
+  bool odd = false;
+  for (int vt = vt0; vt < vt1; ++vt) {
+    const int slot0 = (vt < sn.at ? vt : vt - sn.at + sn.bt) * tk;
+    if (slot0 + tk <= lim && (slot0 >= lo || slot0 + tk <= a.n_sink)) continue;
+    for (int j = slot0; j < slot0 + tk && j < sn.kend; ++j) {
+      size_t row = (size_t)e * a.n + j;
+      if (PAGED) {
+        const int p = trow[j >> a.shift];
+        row = ((size_t)((unsigned)p < (unsigned)a.pages ? p : 0) << a.shift) + (j & ((1 << a.shift) - 1));
+      }
+      for (int c = lane; c < D; c += 64) {
+        const E x = ((const E*)a.v)[row * D + c];
+        if constexpr (sizeof(E) == 2) odd |= (x & 0x7f80) == 0x7f80;
+        else odd |= (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
+      }
+    }
+  }
+  return __any(odd);
+}
+
 // Rows of a split once more, key by key: taken where a tile that some rows see
 // only part of holds an infinity or NaN among its values, since 0 x inf in a
-// product would reach the rows that do not see it.  One wave; rows first ..
+// product reaches the rows that do not see it (as NaN).  One wave; rows first ..
 // first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn.  A lane forms the
 // weight of one key of 64, then sums D / 64 columns.
 template <typename E, int D, bool PAGED>

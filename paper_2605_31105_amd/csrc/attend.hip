@@ -26,9 +26,9 @@
 //    up to one and a row of a single key is exact; the sum behind lse is of the
 //    weights before the rounding.
 //  * Tiles that every row sees whole skip the masks.  In the others an entry
-//    that a row does not see has weight zero; where such a tile holds an infinity or
-//    NaN among its values (0 x inf is NaN in a product), the block does its rows
-//    again key by key.
+//    that a row does not see has weight zero.  An infinity or NaN among the values of
+//    such a tile reaches those rows all the same, as NaN (0 x inf); where a sum is
+//    NaN and such a tile is the cause, the block does its rows again key by key.
 // Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
 #include "attend.h"
 
@@ -135,7 +135,6 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
 
   f32x4 acc[DT][RT], accl[RT];
   float nref[RT], sum[RT];   // sum: this lane's weights before their rounding
-  bool odd = false;          // a value that is not finite in a tile that is not seen whole
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     nref[rt] = kUnset;
@@ -206,13 +205,14 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
       }
     if (!full) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < RT; ++rt) {
+        const uint32_t on = sees32<PAGED>(sight[rt], slot0, a.n_sink, base, len) >> (4 * gq);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!sees<PAGED>(sight[rt], slot0 + 16 * kt + 4 * gq + i, a.n_sink, base, len))
-              s[kt][rt][i] = -__builtin_huge_valf();
+            if ((on >> (16 * kt + i) & 1) == 0) s[kt][rt][i] = -__builtin_huge_valf();
+      }
     }
     bool moved = false;
     float mx[RT];
@@ -278,25 +278,6 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
             p[rt][4 * kt + i + 1] = h[1];
           }
         accl[rt] = mfma_bf16(as_bf16x8(make_uint4(kOnes, kOnes, kOnes, kOnes)), p[rt], accl[rt]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) accl[rt] = mfma_f32(1.f, s[0][rt][i], accl[rt]);
-      }
-    }
-    if (!full) {   // values that are not finite?
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        if constexpr (BF) {
-          const uint4 w = __builtin_bit_cast(uint4, frag(dt));
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            odd |= (u[c] & 0x7f80u) == 0x7f80u || (u[c] & 0x7f800000u) == 0x7f800000u;
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            odd |= (__float_as_uint(elem(dt, i)) & 0x7f800000u) == 0x7f800000u;
-        }
       }
     }
 #pragma unroll
@@ -348,7 +329,12 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
   wait_vmcnt<0>();
-  if (__syncthreads_or(odd)) {
+  float all = 0.f;   // NaN if one of the wave's sums is
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) all += acc[dt][rt][0] + acc[dt][rt][1] + acc[dt][rt][2] + acc[dt][rt][3];
+  if (__syncthreads_or(all != all) && odd_values<E, D, PAGED>(a, sn, e, vt0, vt1, TK, sn.lim, sn.lo, trow)) {
     rows_by_key<E, D, PAGED>(a, sn, e, sp, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
                              family, depth);
     join();
@@ -360,7 +346,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
     sum[rt] += __shfl_xor(sum[rt], 32);
     if (gq == 0) {
       m_s[wave][16 * rt + l16] = -nref[rt];
-      l_s[wave][16 * rt + l16] = accl[rt][0];
+      l_s[wave][16 * rt + l16] = BF ? accl[rt][0] : sum[rt];   // (float32 weights are not rounded)
       x_s[wave][16 * rt + l16] = sum[rt];
     }
   }

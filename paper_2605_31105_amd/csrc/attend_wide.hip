@@ -168,7 +168,6 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   f32x16 acc[DM], st[NK];
   float nref = kUnset;          // minus the reference
   float sum = 0.f, rsum = 0.f;  // weights' sums before and after their rounding (this lane's keys)
-  bool odd = false;             // a value that is not finite in a step that is not seen whole
 #pragma unroll
   for (int dm = 0; dm < DM; ++dm) acc[dm] = f32x16{};
 
@@ -189,22 +188,10 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
     if (!full) {
 #pragma unroll
       for (int n = 0; n < NK; ++n) {
+        const uint32_t on = sees32<PAGED>(sight, slot0 + 32 * n, a.n_sink, base, len) >> (4 * h);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (!sees<PAGED>(sight, slot0 + 32 * n + 8 * (r / 4) + 4 * h + r % 4, a.n_sink, base, len))
-            st[n][r] = -__builtin_huge_valf();
-        bf16x8 vf[2][DM];
-        read_v(vt + n * 32 * RB, vf);   // (values that are not finite?)
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int dm = 0; dm < DM; ++dm) {
-            const uint4 w = __builtin_bit_cast(uint4, vf[s][dm]);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-              odd |= (u[c] & 0x7f80u) == 0x7f80u || (u[c] & 0x7f800000u) == 0x7f800000u;
-          }
+          if ((on >> (8 * (r / 4) + r % 4) & 1) == 0) st[n][r] = -__builtin_huge_valf();
       }
     }
     f32x16 nx[NK];
@@ -286,7 +273,12 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   ring_barrier<0>();   // (the ring is the output's buffer now)
   sum += __shfl_xor(sum, 32);
   rsum += __shfl_xor(rsum, 32);
-  if (__any(odd)) {
+  float all = 0.f;   // NaN if one of the wave's sums is
+#pragma unroll
+  for (int dm = 0; dm < DM; ++dm)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) all += acc[dm][r];
+  if (__any(all != all) && odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, lim, lo, trow)) {
     rows_by_key<u16, D, PAGED>(a, sn, e, sp, w0, 32, vt0, vt1, TK, len, t, trow, family, depth);
     return;
   }
