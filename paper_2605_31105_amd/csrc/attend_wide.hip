@@ -40,12 +40,18 @@ __device__ __forceinline__ void ring_barrier() {
 
 // 16 bytes per lane from base + voff to LDS offset lds (uniform), lane after
 // lane.  In assembly so that the compiler does not wait for these loads at every
-// LDS read; ring_barrier does where it matters.
-__device__ __forceinline__ void ring_load(const char* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(base), "s"(lds)
-               : "memory", "m0");
+// LDS read; ring_barrier does where it matters.  once: a non-temporal load.
+__device__ __forceinline__ void ring_load(const char* base, uint32_t voff, uint32_t lds, bool once) {
+  if (once)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+                 :
+                 : "v"(voff), "s"(base), "s"(lds)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(voff), "s"(base), "s"(lds)
+                 : "memory", "m0");
 }
 
 __device__ __forceinline__ bf16x8 read_tr(const char* p, int rows8) {
@@ -119,7 +125,7 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   const uint32_t ring0 = (uint32_t)(uintptr_t)(lds_void*)ring;
   auto slot_of = [&](int vt) { return (vt < sn.at ? vt : vt - sn.at + sn.bt) * TK; };
   // this wave's rows of tile vt, of K or V (the chunk offsets o, permuted by swz)
-  auto load = [&](const void* from, int vt, int to, const uint32_t (&o)[NI], auto swz)
+  auto load = [&](const void* from, int vt, int to, const uint32_t (&o)[NI], auto swz, bool once)
                   __attribute__((always_inline)) {
     const int s16 = slot_of(vt) + 16 * wave;
     const int at = __builtin_amdgcn_readfirstlane(min(s16, last));
@@ -141,7 +147,7 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
         const int row_in = it * RPI + lane / CPR, ch = lane % CPR;
         f = ((min(s16 + row_in, last) & 15) * CPR + (ch ^ swz(row_in))) * 16;
       }
-      ring_load(src, f, dst + it * 1024);
+      ring_load(src, f, dst + it * 1024, once);
     }
   };
 
@@ -253,9 +259,12 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   };
 
   if (vt0 < vt1) {
+    // values that no other row group reads are read once (32 units of 20k to 32k keys,
+    // over caches used in turn, 116 -> 114 us; keys too, 114)
+    const bool once = PAGED && a.row_groups == 1;
     // K of tile i is in half i & 1 of the first half of the ring, V in the second
-    auto load_k = [&](int i) { load(a.k, min(vt0 + i, vt1 - 1), (i & 1) * KB, ko, swz_k); };
-    auto load_v = [&](int i) { load(a.v, min(vt0 + i, vt1 - 1), (2 + (i & 1)) * KB, vo, swz_v); };
+    auto load_k = [&](int i) { load(a.k, min(vt0 + i, vt1 - 1), (i & 1) * KB, ko, swz_k, false); };
+    auto load_v = [&](int i) { load(a.v, min(vt0 + i, vt1 - 1), (2 + (i & 1)) * KB, vo, swz_v, once); };
     load_k(0);
     load_k(1);
     load_v(0);

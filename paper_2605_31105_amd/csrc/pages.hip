@@ -262,37 +262,44 @@ __device__ __forceinline__ void map_row(const RowMap& m, uint32_t g, int* entry,
   *row = (int)(((t - e * m.per) << m.tile_shift) | (g & ((1u << m.tile_shift) - 1)));
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // 8 values of a source row as 8 of the pool's type (rounded to nearest even).
-template <typename S, typename T>
+// LONG: of a long call, whose rows pass the caches on their way out (over pools used
+// in turn, a layer's 32k rows stored, thinned and released 80 -> 78 us, ragged results
+// 113 -> 110; read so too, 76 and 111).
+template <bool LONG>
+__device__ __forceinline__ void store16(void* p, u32x4 v) {
+  if constexpr (LONG) __builtin_nontemporal_store(v, (u32x4*)p);
+  else *(u32x4*)p = v;
+}
+
+template <bool LONG, typename S, typename T>
 __device__ __forceinline__ void copy8(const S* src, T* dst) {
   if constexpr (sizeof(S) == sizeof(T)) {
 #pragma unroll
     for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i)
-      reinterpret_cast<uint4*>(dst)[i] = reinterpret_cast<const uint4*>(src)[i];
+      store16<LONG>((char*)dst + 16 * i, *(const u32x4*)((const char*)src + 16 * i));
   } else if constexpr (sizeof(S) == 4) {
-    const float4 x = reinterpret_cast<const float4*>(src)[0], y = reinterpret_cast<const float4*>(src)[1];
-    const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-    bf16x8 h;
+    float f[8];
+    *(u32x4*)f = *(const u32x4*)src;
+    *(u32x4*)(f + 4) = *(const u32x4*)(src + 4);
+    u32x4 h;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const bf16x2 p = __builtin_convertvector((f32x2){f[i], f[i + 1]}, bf16x2);
-      h[i] = p[0];
-      h[i + 1] = p[1];
-    }
-    *reinterpret_cast<bf16x8*>(dst) = h;
+    for (int i = 0; i < 4; ++i)
+      h[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){f[2 * i], f[2 * i + 1]}, bf16x2));
+    store16<LONG>(dst, h);
   } else {
-    const uint4 w = *reinterpret_cast<const uint4*>(src);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    const u32x4 w = *(const u32x4*)src;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      dst[2 * i] = __uint_as_float(u[i] << 16);
-      dst[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 2; ++i)
+      store16<LONG>(dst + 4 * i, (u32x4){w[2 * i] << 16, w[2 * i] & 0xffff0000u, w[2 * i + 1] << 16,
+                                         w[2 * i + 1] & 0xffff0000u});
   }
 }
 
 // Rows g0, g0 + stride, .. of an append; T, KS, VS: u16 (bf16) or float.
-template <typename T, typename KS, typename VS>
+template <bool LONG, typename T, typename KS, typename VS>
 __device__ __forceinline__ void append_rows(const PagesK& a, const RowMap& m, const KS* k, const VS* v,
                                             uint32_t g0, uint32_t stride) {
   const int d = a.pg.head_dim, cpr = d / 8;   // 8 or 16 steps of 8 values per row
@@ -317,15 +324,15 @@ __device__ __forceinline__ void append_rows(const PagesK& a, const RowMap& m, co
     }
     const size_t to = (((size_t)page << a.shift) + (slot & mask)) * d + c;
     const size_t from = (size_t)(j.start + row) * d + c;
-    copy8(k + from, (T*)a.pg.k + to);
-    copy8(v + from, (T*)a.pg.v + to);
+    copy8<LONG>(k + from, (T*)a.pg.k + to);
+    copy8<LONG>(v + from, (T*)a.pg.v + to);
   }
 }
 
 template <typename T, typename KS, typename VS>
 __global__ __launch_bounds__(kCopyTh) void append_kernel(PagesK a, RowMap m, const KS* k, const VS* v) {
   const int per = kCopyTh / (a.pg.head_dim / 8);
-  append_rows<T>(a, m, k, v, blockIdx.x * per + threadIdx.x / (a.pg.head_dim / 8), gridDim.x * per);
+  append_rows<true, T>(a, m, k, v, blockIdx.x * per + threadIdx.x / (a.pg.head_dim / 8), gridDim.x * per);
 }
 
 // The few rows of a decoding step, by the block that plans them.
@@ -334,7 +341,7 @@ __global__ __launch_bounds__(kPlanTh) void plan_append_kernel(PagesK a, RowMap m
   make_plan_block(a);
   __syncthreads();
   const int cpr = a.pg.head_dim / 8;
-  append_rows<T>(a, m, k, v, threadIdx.x / cpr, kPlanTh / cpr);
+  append_rows<false, T>(a, m, k, v, threadIdx.x / cpr, kPlanTh / cpr);
 }
 
 // Slot `row` of the new pages of a fork or a compaction, read through the old
