@@ -49,8 +49,10 @@ int run(const PagesCall& c, void* stream) {
   return launch_pages(c, (hipStream_t)stream) == hipSuccess ? GRKV_OK : GRKV_ERR_HIP;
 }
 
-// A window that holds every slot (and leaves differences of positions in 32 bits).
-constexpr int kAllSlots = (1 << 30) + 64;
+// The window as the kernels take it: one that holds every slot is none.  (A window
+// below 2^30 also keeps differences of positions within 32 bits.)
+int window_of(int window, int64_t slots) { return window < slots ? window : 0; }
+int sinks_of(int n_sink) { return n_sink < (1 << 30) ? n_sink : 1 << 30; }
 
 // A call's sizes and plan.  A call without splits still asks for 256 bytes, so
 // that 0 says "invalid".
@@ -69,9 +71,10 @@ int make_tree(const grkv_pages* pg, const grkv_tree* tr, TreeCall* c) {
     return GRKV_ERR_INVALID;
   if (!sizes_ok(tr->entries, tr->group, tr->tokens, pg->head_dim)) return GRKV_ERR_INVALID;
   const int64_t cap = (int64_t)pg->max_pages * pg->page_size;
-  const int64_t near = (int64_t)tr->n_sink + tr->window + tr->tokens;
+  const int window = window_of(tr->window, cap);
+  const int64_t near = (int64_t)tr->n_sink + window + tr->tokens;
   c->plan = attend_plan(tr->entries > 0 ? tr->entries : 1, tr->group, tr->tokens, pg->head_dim,
-                        pg->dtype, tr->window > 0 && near < cap ? near : cap, tr->window == 0);
+                        pg->dtype, window > 0 && near < cap ? near : cap, window == 0);
   if (c->plan.blocks >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
   AttendK& a = c->a;
   a = AttendK{};
@@ -80,8 +83,8 @@ int make_tree(const grkv_pages* pg, const grkv_tree* tr, TreeCall* c) {
   a.entries = tr->entries;
   a.group = tr->group;
   a.tokens = tr->tokens;
-  a.window = tr->window < kAllSlots ? tr->window : kAllSlots;
-  a.n_sink = tr->n_sink < kAllSlots ? tr->n_sink : kAllSlots;
+  a.window = window;
+  a.n_sink = sinks_of(tr->n_sink);
   a.table = pg->table;
   a.lens = pg->lens;
   a.units = tr->units;
@@ -102,6 +105,7 @@ int make_sink(const grkv_problem* prob, int64_t n, int32_t nq, int32_t window, i
   if (nq < 1 || nq > n || n > (int64_t(1) << 30) || window < 0 || n_sink < 0) return GRKV_ERR_INVALID;
   if (prob->head_dim != 64 && prob->head_dim != 128) return GRKV_ERR_UNSUPPORTED;
   if (!sizes_ok(prob->units, prob->group, nq, prob->head_dim)) return GRKV_ERR_INVALID;
+  window = window_of(window, n);
   const int64_t near = (int64_t)n_sink + window + nq;
   c->plan = attend_plan(prob->units, prob->group, nq, prob->head_dim, prob->dtype,
                         window > 0 && near < n ? near : n, false);
@@ -111,8 +115,8 @@ int make_sink(const grkv_problem* prob, int64_t n, int32_t nq, int32_t window, i
   a.entries = prob->units;
   a.group = prob->group;
   a.tokens = nq;
-  a.window = window < kAllSlots ? window : kAllSlots;
-  a.n_sink = n_sink < kAllSlots ? n_sink : kAllSlots;
+  a.window = window;
+  a.n_sink = sinks_of(n_sink);
   a.n = (int)n;
   return GRKV_OK;
 }

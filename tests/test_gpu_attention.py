@@ -225,6 +225,29 @@ def test_later_keys_that_are_not_finite_do_not_reach_earlier_queries(dtype):
     assert torch.isinf(got[0, :, 151:153, 5]).all()
 
 
+def test_windows_and_sinks_of_every_size():
+    # up to the largest int, which is no window: the rows of the smallest that holds all
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(12)
+    q = torch.randn((1, 2, 100, 64), generator=gen).to(BF).cuda()
+    K, V = (torch.randn((1, 100, 64), generator=gen).to(BF).cuda() for _ in range(2))
+    want = G.sink_attention(q, K, V, 0)
+    big = (1 << 31) - 1
+    for window, n_sink in ((100, 0), (101, 4), (1 << 30, 0), (big, big), (1, big), (3, 100), (99, 1)):
+        if window >= 100:
+            assert torch.equal(G.sink_attention(q, K, V, window, n_sink), want)
+        check("window %d sinks %d" % (window, n_sink), *(x[0, 1].cpu() for x in G.sink_attention(
+            q, K, V, window, n_sink, return_lse=True)), q[0, 1].cpu(), K[0].cpu(), V[0].cpu(),
+            sink_seen(100, 100, window, n_sink))
+    pg, Kt, Vt = _pool([90, 2], 16, 64, BF, gen)
+    qt = torch.randn((2, 2, 5, 64), generator=gen).to(BF)
+    for window, n_sink in ((big, big), (1 << 30, 3), (1, big), (112, 0), (4, 88)):
+        o, lse = G.tree_attention(qt.cuda(), pg, units=_i32([0, 1]), window=window, n_sink=n_sink, return_lse=True)
+        for u, n in ((0, 90), (1, 2)):
+            check("unit %d window %d" % (u, window), o[u, 0].cpu(), lse[u, 0].cpu(), qt[u, 0], Kt[u], Vt[u],
+                  tree_seen(n, 5, [-1, 0, 1, 2, 3], window, n_sink))
+
+
 def test_window_calls_agree_with_each_other():
     # the last queries of a prompt, a chunk of it and single tokens give the prompt's rows
     import paper_2605_31105_amd as G
