@@ -291,29 +291,50 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
     rows_by_key<u16, D, PAGED>(a, sn, e, sp, w0, 32, vt0, vt1, TK, len, t, trow, family, depth);
     return;
   }
-  // a wave's rows through its part of the ring: lane's four columns 32 dm + 8 c + 4 h of
-  // row l32, chunks permuted by row
-  constexpr int CR = D / 4;
-  char* out = ring + wave * 32 * CR * 16;
+  // a wave's rows through its part of the ring (lane's four columns 32 dm + 8 c + 4 h of
+  // row l32, chunks permuted by row), so that they leave whole
+  const int my = w0 + l32, mi = group_of(a, my);
+  char* out = ring + wave * KB;
+  if (sn.ns > 1) {
+    constexpr int CR = D / 4;
+#pragma unroll
+    for (int dm = 0; dm < DM; ++dm)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<f32x4*>(out + (l32 * CR + ((8 * dm + 2 * c + h) ^ (l32 & 15))) * 16) =
+            (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]};
+    const size_t part = ((size_t)e * a.splits + sp) * R;
+    if (h == 0 && my < R && mi < t) a.mpart[part + my] = make_float4(-nref, rsum, sum, 0.f);
+#pragma unroll 4
+    for (int k = lane; k < 32 * CR; k += 64) {
+      const int row = k / CR, ch = k % CR, r = w0 + row;
+      if (r < R && group_of(a, r) < t)
+        *reinterpret_cast<f32x4*>(a.opart + (part + r) * D + 4 * ch) =
+            *reinterpret_cast<const f32x4*>(out + (row * CR + (ch ^ (row & 15))) * 16);
+    }
+    return;
+  }
+  const float inv = rsum == 0.f ? 0.f : 1.f / rsum;
 #pragma unroll
   for (int dm = 0; dm < DM; ++dm)
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      *reinterpret_cast<f32x4*>(out + (l32 * CR + ((8 * dm + 2 * c + h) ^ (l32 & 15))) * 16) =
-          (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]};
-  for (int k = lane; k < 32 * CR; k += 64) {
-    const int row = k / CR, ch = k % CR, r = w0 + row;
-    const int i = group_of(a, r), g = r - i * a.group;
-    const float m = -__shfl(nref, row), lx = __shfl(sum, row), l = __shfl(rsum, row);
-    if (r >= R || i >= t) continue;
-    const f32x4 x = *reinterpret_cast<const f32x4*>(out + (row * CR + (ch ^ (row & 15))) * 16);
-    if (sn.ns > 1) {
-      const size_t at = ((size_t)e * a.splits + sp) * R + r;
-      *reinterpret_cast<f32x4*>(a.opart + at * D + 4 * ch) = x;
-      if (ch == 0) a.mpart[at] = make_float4(m, l, lx, 0.f);
-    } else {
-      write_out<u16, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, x, m, l, lx);
+    for (int c = 0; c < 4; ++c) {
+      uint2 w;
+      w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+          (f32x2){acc[dm][4 * c] * inv, acc[dm][4 * c + 1] * inv}, bf16x2));
+      w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+          (f32x2){acc[dm][4 * c + 2] * inv, acc[dm][4 * c + 3] * inv}, bf16x2));
+      *reinterpret_cast<uint2*>(out + (l32 * CPR + ((4 * dm + c) ^ (l32 & (CPR - 1)))) * 16 + 8 * h) = w;
     }
+  auto place = [&](int r, int i) { return ((size_t)e * a.group + (r - i * a.group)) * a.tokens + i; };
+  if (h == 0 && a.lse && my < R && mi < t)
+    a.lse[place(my, mi)] = sum == 0.f ? -__builtin_huge_valf() : (__log2f(sum) - nref) * kLn2;
+#pragma unroll
+  for (int k = lane; k < 32 * CPR; k += 64) {
+    const int row = k / CPR, ch = k % CPR, r = w0 + row, i = group_of(a, r);
+    if (r < R && i < t)
+      *reinterpret_cast<uint4*>((u16*)a.o + place(r, i) * D + 8 * ch) =
+          *reinterpret_cast<const uint4*>(out + (row * CPR + (ch ^ (row & (CPR - 1)))) * 16);
   }
 }
 
