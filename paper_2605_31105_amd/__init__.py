@@ -619,7 +619,8 @@ class Pages:
         i32, dev = torch.int32, k.get_device()
         if dev < 0:
             raise ValueError("a pool's tensors must be device tensors")
-        if k.dtype != v.dtype or k.dtype not in _DTYPES:
+        code = _dtype_code(k)
+        if code is None or v.dtype != k.dtype:
             raise ValueError("k and v must share dtype bfloat16 or float32")
         if k.dim() != 3 or k.shape != v.shape or table.dim() != 2:
             raise ValueError("k and v must be [pages, page_size, head_dim] and table [units, max_pages]")
@@ -633,28 +634,18 @@ class Pages:
             raise ValueError("table, lens, refs and free must be int32")
         object.__setattr__(self, "_c", _PagesC(
             k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(),
-            free.data_ptr(), n, ps, units, width, d, _DTYPES[k.dtype]))
+            free.data_ptr(), n, ps, units, width, d, code))
 
     @property
     def device(self):
         return self.k.device
 
 
-class _Dtypes(dict):
-    """torch dtype -> grkv_dtype, filled when torch is first needed."""
+def _dtype_code(t):
+    """grkv_dtype of a tensor, or None."""
+    import torch
 
-    def _fill(self):
-        import torch
-
-        if not self:
-            self.update({torch.bfloat16: GRKV_BF16, torch.float32: GRKV_F32})
-
-    def __contains__(self, key):
-        self._fill()
-        return dict.__contains__(self, key)
-
-
-_DTYPES = _Dtypes()
+    return (GRKV_BF16 if t.dtype == torch.bfloat16 else GRKV_F32 if t.dtype == torch.float32 else None)
 
 
 def _on(dev: int, stream):
@@ -778,14 +769,15 @@ def pages_append(pages: Pages, k, v, *, units=None, counts=None, starts=None, ro
     entry, int32 [E] (PAGES_OK or why its unit is as it was)."""
     E, rows, n = _packed(k, 3, rows, starts, "k")
     dev = pages.k.get_device()
-    for t in (k, v):
-        if t.get_device() != dev or t.dtype not in _DTYPES or not t.is_contiguous():
+    kc, vc = _dtype_code(k), _dtype_code(v)
+    for t, code in ((k, kc), (v, vc)):
+        if t.get_device() != dev or code is None or not t.is_contiguous():
             raise ValueError("k and v must be contiguous bfloat16 or float32 tensors on the pool's device")
     if k.shape != v.shape or k.shape[-1] != pages.k.shape[2]:
         raise ValueError("shape mismatch: k %s v %s head_dim %d"
                          % (tuple(k.shape), tuple(v.shape), pages.k.shape[2]))
     return _page_call("grkv_pages_append", pages, E,
-                      (k.data_ptr(), _DTYPES[k.dtype], v.data_ptr(), _DTYPES[v.dtype]),
+                      (k.data_ptr(), kc, v.data_ptr(), vc),
                       units, rows, counts, starts, n, status, workspace, stream)
 
 
@@ -925,7 +917,8 @@ def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = 
     dev = q.get_device()
     if dev < 0 or K.get_device() != dev or V.get_device() != dev:
         raise ValueError("q, K and V must be tensors of one device")
-    if not (q.dtype == K.dtype == V.dtype) or K.dtype not in _DTYPES:
+    code = _dtype_code(q)
+    if code is None or not (q.dtype == K.dtype == V.dtype):
         raise ValueError("q, K, V must share dtype bfloat16 or float32")
     if not (q.is_contiguous() and K.is_contiguous() and V.is_contiguous()):
         raise ValueError("inputs must be contiguous")
@@ -935,7 +928,7 @@ def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = 
                          % (tuple(q.shape), tuple(K.shape), tuple(V.shape)))
     U, G, nq, d = q.shape
     n = K.shape[1]
-    prob = Problem(U, G, d, _DTYPES[q.dtype])
+    prob = Problem(U, G, d, code)
     L, qp, kp, vp = lib(), q.data_ptr(), K.data_ptr(), V.data_ptr()
     need = L.grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink)
     return _attention(lambda o, l, h, ws, b: L.grkv_sink_attention(

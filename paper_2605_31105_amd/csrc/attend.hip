@@ -41,6 +41,12 @@ namespace {
 
 constexpr int kAtWaves = 4;
 constexpr int kAtTh = 64 * kAtWaves;
+// Splits that the blocks themselves join: a few, in calls whose blocks all run at once
+// (8 units of 2048 keys, 8 splits: one launch of 11.7 us against 9.8 and 3.9).  More
+// are combined by a launch of their own, which has more threads for them (256 units
+// of 4100 keys, 4 splits: 98 and 5 us against 110).
+constexpr int kJoinedSplits = 16, kJoinedBlocks = 512;
+
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform), as
 // a non-temporal load: values are read once, and pass the caches faster so (over
 // caches used in turn: 256 units of 4100 keys 99 -> 89 us, 8 of 128k 103 -> 95, 512 of
@@ -458,12 +464,16 @@ template <typename E, int D>
 hipError_t launch_ed(const AttendK& a, int rt, hipStream_t s) {
   const hipError_t e = launch_d<E, D>(a, rt, s);
   if (e != hipSuccess || a.splits == 1 || a.flags) return e;
+  // threads that share a value: two, or with many splits a block's all (16 splits of 32
+  // units of 128 rows, call 114 -> 110 us with two; 64 splits of 8 units of 8 rows, 100
+  // with two, 95 with eight)
   const int64_t rows = (int64_t)a.entries * a.group * a.tokens;
-  constexpr int GS = kAtTh / (D / 4);
-  if (a.splits > GS)
-    hipLaunchKernelGGL((combine_kernel<E, D, GS>), dim3((unsigned)rows), dim3(kAtTh), 0, s, a);
+  constexpr int ALL = kAtTh / (D / 4), FEW = 2;
+  if (a.splits > kJoinedSplits)
+    hipLaunchKernelGGL((combine_kernel<E, D, ALL>), dim3((unsigned)rows), dim3(kAtTh), 0, s, a);
   else
-    hipLaunchKernelGGL((combine_kernel<E, D, 1>), dim3((unsigned)((rows + GS - 1) / GS)), dim3(kAtTh), 0, s, a);
+    hipLaunchKernelGGL((combine_kernel<E, D, FEW>), dim3((unsigned)((rows * FEW + ALL - 1) / ALL)),
+                       dim3(kAtTh), 0, s, a);
   return hipGetLastError();
 }
 
@@ -480,12 +490,6 @@ static uint64_t next_nonce() {
   x ^= x >> 31;
   return x != 0 ? x : 1;
 }
-
-// Splits that the blocks themselves join: a few, in calls whose blocks all run at once
-// (8 units of 2048 keys, 8 splits: one launch of 11.7 us against 9.8 and 3.9).  More
-// are combined by a launch of their own, which has more threads for them (256 units
-// of 4100 keys, 4 splits: 98 and 5 us against 110).
-constexpr int kJoinedSplits = 16, kJoinedBlocks = 512;
 
 // Kernel, splits and workspace of a call whose rows see at most `slots` slots
 // each, or (ragged) any number up to that.
