@@ -42,10 +42,12 @@ namespace {
 constexpr int kAtWaves = 4;
 constexpr int kAtTh = 64 * kAtWaves;
 // Splits that the blocks themselves join: a few, in calls whose blocks all run at once
-// (8 units of 2048 keys, 8 splits: one launch of 11.7 us against 9.8 and 3.9).  More
-// are combined by a launch of their own, which has more threads for them (256 units
-// of 4100 keys, 4 splits: 98 and 5 us against 110).
-constexpr int kJoinedSplits = 16, kJoinedBlocks = 512;
+// (8 units of 2048 keys and 8 rows, 8 splits: one launch of 11.7 us against 9.8 and 3.9).
+// More are combined by a launch of their own, which has more threads for them (256 units
+// of 4100 keys, 4 splits: 98 and 5 us against 110), and with several row groups a unit,
+// whose splits end at different times, from 16 on (8 units of 32 rows: 1000 keys, 4
+// splits, 16.3 us joined, 18.0 combined; 4000 keys, 16 splits, 20.8 and 17.6).
+constexpr int kJoinedSplits = 16, kJoinedRowSplits = 8, kJoinedBlocks = 512;
 
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform), as
 // a non-temporal load: values are read once, and pass the caches faster so (over
@@ -402,8 +404,9 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   join();
 }
 
-// The splits of a row, where they are not joined by attend_kernel: one thread per 4 values and every GS-th split, whose sums
-// are added in order.  GS: threads that share a value.
+// The splits of a row, where they are not joined by attend_kernel: one thread per 4
+// values and every GS-th split, whose sums are added in order.  GS: threads that share
+// a value.
 template <typename E, int D, int GS>
 __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   constexpr int CR = D / 4, ROWS = kAtTh / (CR * GS);   // rows of a block
@@ -444,20 +447,21 @@ __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   if (on) write_out<E, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, o.x, o.m, o.l, o.lx);
 }
 
+template <typename E, int D, int RT>
+hipError_t launch_rows(const AttendK& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.blocks), th(kAtTh);
+  if (a.lens) hipLaunchKernelGGL((attend_kernel<E, D, RT, true>), grid, th, 0, s, a);
+  else hipLaunchKernelGGL((attend_kernel<E, D, RT, false>), grid, th, 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename E, int D>
 hipError_t launch_d(const AttendK& a, int rt, hipStream_t s) {
-  const dim3 grid((unsigned)a.blocks), th(kAtTh);
   if constexpr (sizeof(E) == 2) {
     if (rt == 0) return launch_attend_wide(a, D, s);
+    if (rt == 2) return launch_rows<E, D, 2>(a, s);
   }
-  if (a.lens) {
-    if (rt == 1) hipLaunchKernelGGL((attend_kernel<E, D, 1, true>), grid, th, 0, s, a);
-    else hipLaunchKernelGGL((attend_kernel<E, D, 2, true>), grid, th, 0, s, a);
-  } else {
-    if (rt == 1) hipLaunchKernelGGL((attend_kernel<E, D, 1, false>), grid, th, 0, s, a);
-    else hipLaunchKernelGGL((attend_kernel<E, D, 2, false>), grid, th, 0, s, a);
-  }
-  return hipGetLastError();
+  return launch_rows<E, D, 1>(a, s);
 }
 
 template <typename E, int D>
@@ -507,7 +511,11 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
     // (32 units of 20k to 32k keys, 128 rows, 256 / 512 / 1024 blocks: 138 / 116 / 139 us)
     target = 512;
   } else {
-    p.rt = R <= 16 ? 1 : 2;
+    // rows of a block: 32 read the keys half as often, 16 make twice the blocks and hold
+    // twice the waves (32 rows of bf16 over 8000 keys, 16 / 32 rows a block: 24 units 36.3 /
+    // 39.0 us, 64 units 68.0 / 63.6, 512 units of 4000 keys 261 / 243).  float32 products
+    // take eight times as long: 16 always (512 units of 32 rows over 1000 keys 160 / 185 us)
+    p.rt = bf16 && R > 16 && (int64_t)entries * ((R + 31) / 32) >= 64 ? 2 : 1;
     p.rows = 16 * p.rt;
     p.tile_keys = bf16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
     p.min_tiles = 8;
@@ -527,7 +535,8 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   const int64_t w = (int64_t)entries * p.splits;
   p.grouped = w % 8 == 0 || w >= 64;
   p.blocks = (p.grouped ? (w + 7) / 8 * 8 : w) * p.row_groups;
-  p.joined = p.rt > 0 && p.splits > 1 && p.splits <= kJoinedSplits && p.blocks <= kJoinedBlocks;
+  p.joined = p.rt > 0 && p.splits > 1 && p.blocks <= kJoinedBlocks &&
+             p.splits <= (p.row_groups == 1 ? kJoinedSplits : kJoinedRowSplits);
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   const size_t rows = p.splits > 1 ? (size_t)w * R : 0;
   p.opart = 0;
