@@ -264,10 +264,13 @@ __device__ __forceinline__ void map_row(const RowMap& m, uint32_t g, int* entry,
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// 8 values of a source row as 8 of the pool's type (rounded to nearest even).
+// Source values as 16 bytes of the pool's type (rounded to nearest even), so that the
+// stores of a wave are whole lines (32 bytes per thread, in two stores of every other 16:
+// 2 units' 103k rows of float32 in 190 us).
 // LONG: of a long call, whose rows pass the caches on their way out (over pools used
 // in turn, a layer's 32k rows stored, thinned and released 80 -> 78 us, ragged results
-// 113 -> 110; read so too, 76 and 111).
+// 113 -> 110; read so too, 76 and 111); moved rows always do (8 units of 16k rows thinned
+// to 12k 72.6 -> 69.0, 500 of 300 to 500 rows to 150 68 -> 62).
 template <bool LONG>
 __device__ __forceinline__ void store16(void* p, u32x4 v) {
   if constexpr (LONG) __builtin_nontemporal_store(v, (u32x4*)p);
@@ -275,11 +278,9 @@ __device__ __forceinline__ void store16(void* p, u32x4 v) {
 }
 
 template <bool LONG, typename S, typename T>
-__device__ __forceinline__ void copy8(const S* src, T* dst) {
+__device__ __forceinline__ void copy16(const S* src, T* dst) {
   if constexpr (sizeof(S) == sizeof(T)) {
-#pragma unroll
-    for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i)
-      store16<LONG>((char*)dst + 16 * i, *(const u32x4*)((const char*)src + 16 * i));
+    store16<LONG>(dst, *(const u32x4*)src);
   } else if constexpr (sizeof(S) == 4) {
     float f[8];
     *(u32x4*)f = *(const u32x4*)src;
@@ -290,11 +291,8 @@ __device__ __forceinline__ void copy8(const S* src, T* dst) {
       h[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){f[2 * i], f[2 * i + 1]}, bf16x2));
     store16<LONG>(dst, h);
   } else {
-    const u32x4 w = *(const u32x4*)src;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      store16<LONG>(dst + 4 * i, (u32x4){w[2 * i] << 16, w[2 * i] & 0xffff0000u, w[2 * i + 1] << 16,
-                                         w[2 * i + 1] & 0xffff0000u});
+    const uint2 w = *(const uint2*)src;
+    store16<LONG>(dst, (u32x4){w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u});
   }
 }
 
@@ -302,8 +300,9 @@ __device__ __forceinline__ void copy8(const S* src, T* dst) {
 template <bool LONG, typename T, typename KS, typename VS>
 __device__ __forceinline__ void append_rows(const PagesK& a, const RowMap& m, const KS* k, const VS* v,
                                             uint32_t g0, uint32_t stride) {
-  const int d = a.pg.head_dim, cpr = d / 8;   // 8 or 16 steps of 8 values per row
-  const int c = (threadIdx.x & (cpr - 1)) * 8, mask = (1 << a.shift) - 1;
+  constexpr int V = 16 / sizeof(T);
+  const int d = a.pg.head_dim, cpr = d / V;   // 8, 16 or 32 chunks per row
+  const int c = (threadIdx.x & (cpr - 1)) * V, mask = (1 << a.shift) - 1;
   for (uint32_t g = g0; g < m.rows; g += stride) {
     int e, row;
     map_row(m, g, &e, &row);
@@ -324,15 +323,15 @@ __device__ __forceinline__ void append_rows(const PagesK& a, const RowMap& m, co
     }
     const size_t to = (((size_t)page << a.shift) + (slot & mask)) * d + c;
     const size_t from = (size_t)(j.start + row) * d + c;
-    copy8<LONG>(k + from, (T*)a.pg.k + to);
-    copy8<LONG>(v + from, (T*)a.pg.v + to);
+    copy16<LONG>(k + from, (T*)a.pg.k + to);
+    copy16<LONG>(v + from, (T*)a.pg.v + to);
   }
 }
 
 template <typename T, typename KS, typename VS>
 __global__ __launch_bounds__(kCopyTh) void append_kernel(PagesK a, RowMap m, const KS* k, const VS* v) {
-  const int per = kCopyTh / (a.pg.head_dim / 8);
-  append_rows<true, T>(a, m, k, v, blockIdx.x * per + threadIdx.x / (a.pg.head_dim / 8), gridDim.x * per);
+  const int cpr = a.pg.head_dim * (int)sizeof(T) / 16, per = kCopyTh / cpr;
+  append_rows<true, T>(a, m, k, v, blockIdx.x * per + threadIdx.x / cpr, gridDim.x * per);
 }
 
 // The few rows of a decoding step, by the block that plans them.
@@ -340,7 +339,7 @@ template <typename T, typename KS, typename VS>
 __global__ __launch_bounds__(kPlanTh) void plan_append_kernel(PagesK a, RowMap m, const KS* k, const VS* v) {
   make_plan_block(a);
   __syncthreads();
-  const int cpr = a.pg.head_dim / 8;
+  const int cpr = a.pg.head_dim * (int)sizeof(T) / 16;
   append_rows<false, T>(a, m, k, v, threadIdx.x / cpr, kPlanTh / cpr);
 }
 
@@ -354,21 +353,21 @@ __device__ __forceinline__ void move_row(const PagesK& a, const PageJob& j, int 
   if (slot >= j.n1) return;
   int from = slot;
   if (slot >= j.keep) from = idx[j.start + (slot - j.keep)];
-  uint4 rk = make_uint4(0, 0, 0, 0), rv = rk;
+  u32x4 rk = {0, 0, 0, 0}, rv = rk;
   if ((unsigned)from < (unsigned)j.n0) {
     const int p = a.pg.table[(size_t)j.src * a.pg.max_pages + (from >> a.shift)];
     if ((unsigned)p < (unsigned)a.pg.pages) {
       const size_t at = (((size_t)p << a.shift) + (from & mask)) * d + c;
-      rk = *reinterpret_cast<const uint4*>((const T*)a.pg.k + at);
-      rv = *reinterpret_cast<const uint4*>((const T*)a.pg.v + at);
+      rk = *(const u32x4*)((const T*)a.pg.k + at);
+      rv = *(const u32x4*)((const T*)a.pg.v + at);
     }
   } else if (c == 0 && a.status) {
     a.status[e] = GRKV_PAGES_RANGE;
   }
   const int page = a.ids[j.off + (slot >> a.shift) - j.first];
   const size_t to = (((size_t)page << a.shift) + (slot & mask)) * d + c;
-  *reinterpret_cast<uint4*>((T*)a.pg.k + to) = rk;
-  *reinterpret_cast<uint4*>((T*)a.pg.v + to) = rv;
+  store16<true>((T*)a.pg.k + to, rk);
+  store16<true>((T*)a.pg.v + to, rv);
 }
 
 template <typename T>
@@ -546,7 +545,7 @@ void launch_append(const PagesK& a, const PagesCall& c, hipStream_t s) {
     return;
   }
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanTh), 0, s, a);
-  hipLaunchKernelGGL((append_kernel<T, KS, VS>), dim3(copy_blocks(m, kCopyTh / (a.pg.head_dim / 8))),
+  hipLaunchKernelGGL((append_kernel<T, KS, VS>), dim3(copy_blocks(m, kCopyTh * 16 / (a.pg.head_dim * (int)sizeof(T)))),
                      dim3(kCopyTh), 0, s, a, m, k, v);
 }
 
