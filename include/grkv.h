@@ -492,8 +492,8 @@ typedef struct {
 } grkv_tree;
 
 /* q, o: pages' dtype [entries][group][tokens][head_dim], 16-byte aligned; lse float
- * [entries][group][tokens] or NULL.  A logit's weight is rounded to bf16 over bf16
- * values; sums are float32.  The length of a unit is read on the device.  Errors:
+ * [entries][group][tokens] or NULL; neither may overlap q, the pool or another array of the
+ * call.  A logit's weight is rounded to bf16 over bf16 values; sums are float32.  The length of a unit is read on the device.  Errors:
  * those of the calls on pages; GRKV_ERR_INVALID for bad counts in `tree` (also
  * entries * group * tokens * head_dim >= 2^40); GRKV_ERR_UNSUPPORTED for
  * tokens > 64. */

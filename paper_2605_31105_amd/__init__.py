@@ -675,9 +675,18 @@ def _vector(t, name, dtype, size, dev):
 def _workspace(workspace, need, dev):
     import torch
 
-    if workspace is None or workspace.numel() < need:
-        return torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-    return workspace
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on cuda:%d" % dev)
+        if workspace.numel() >= need:
+            return workspace
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=torch.device("cuda", dev))
+
+
+def _int32(bits):
+    """The bits of a call's sizes, which ctypes would cut to 32 without a word."""
+    if bits >> 31 not in (0, -1):
+        raise ValueError("sizes must fit 32 bits")
 
 
 def new_pages(units: int, max_pages: int, pages: int, page_size: int, head_dim: int, dtype=None,
@@ -719,6 +728,7 @@ def _page_call(name, pages, entries, args, units, rows, counts, starts, source_r
     import torch
 
     dev, i32 = pages.k.get_device(), torch.int32
+    _int32(entries | rows)
     en = _PageEntries(entries, _vector(units, "units", i32, entries, dev), rows,
                       _vector(counts, "counts", i32, entries, dev),
                       _vector(starts, "starts", torch.int64, entries, dev), source_rows, None)
@@ -741,7 +751,7 @@ def _page_launch(name, pages, entries, args, en, dev, status, workspace, handle)
     if name == "grkv_pages_free":
         _check(L.grkv_pages_free(pages._c, en, handle))
         return status
-    workspace = _workspace(workspace, L.grkv_pages_workspace_bytes(pages._c, entries), pages.k.device)
+    workspace = _workspace(workspace, L.grkv_pages_workspace_bytes(pages._c, entries), dev)
     _check(getattr(L, name)(pages._c, en, *args, handle, workspace.data_ptr(), workspace.numel()))
     return status
 
@@ -861,7 +871,7 @@ def _attend(launch, need, q, out, lse, return_lse, workspace, handle):
         out = torch.empty_like(q)
     if lse is None and return_lse:
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-    workspace = _workspace(workspace, need, q.device)
+    workspace = _workspace(workspace, need, q.get_device())
     _check(launch(out.data_ptr(), None if lse is None else lse.data_ptr(), handle,
                   workspace.data_ptr(), workspace.numel()))
     return (out, lse) if return_lse else out
@@ -885,6 +895,7 @@ def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, wi
     if q.get_device() != dev or q.dtype != pages.k.dtype or q.dim() != 4 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [E, G, t, d] tensor of the pool's type and device")
     E, G, t, d = q.shape
+    _int32(window | n_sink)
     if d != pages.k.shape[2]:
         raise ValueError("head_dim %d, the pool's is %d" % (d, pages.k.shape[2]))
     trees, up = 0, None
@@ -928,6 +939,7 @@ def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = 
                          % (tuple(q.shape), tuple(K.shape), tuple(V.shape)))
     U, G, nq, d = q.shape
     n = K.shape[1]
+    _int32(window | n_sink)
     prob = Problem(U, G, d, code)
     L, qp, kp, vp = lib(), q.data_ptr(), K.data_ptr(), V.data_ptr()
     need = L.grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink)

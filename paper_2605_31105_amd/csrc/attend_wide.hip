@@ -2,21 +2,22 @@
 // of them with a window and sinks, trees of drafted tokens with more than 64 rows.
 //
 // The sums are those of attend.hip; here the products and the exponentials bound
-// them, so the eight waves of a block (two per SIMD) share tiles of 64 keys in LDS:
-//  * A wave holds 32 rows and forms, in one step, the weights of 32 keys beside the
-//    logits of the next 32, then P.V; the other wave of its SIMD fills the
-//    gaps.  (One wave of 64 rows per SIMD, which reads half as much LDS, waited
-//    for its own chain of logit, maximum, exponential and product: a 16k prompt with
-//    a 4k window, 8 units of 4 heads, 1374 us against 969.)
-//  * 256 rows a block (KW = 1), or 128 with the tile's keys divided between two
-//    waves (KW = 2), whose sums meet in LDS at the end.
-//  * K and V go from memory to a ring of four LDS stages (global_load_lds), two
-//    tiles ahead, one barrier per tile.  16-byte chunks are permuted by row so
-//    that neither the K operand reads nor the V transpose reads conflict.
+// them, so the four waves of a block share tiles of 64 keys in LDS:
+//  * A wave holds 32 rows and forms, in one step, the weights of 64 keys beside the
+//    logits of the next 64, then P.V.  Two blocks share a compute unit, and the wave of
+//    the other one on its SIMD fills the gaps.  (8 units of 4 heads, a 16k prompt with a
+//    4k window: 1004 us beside 1374 of one wave of 64 rows per SIMD, which
+//    reads half as much LDS but waits for its own chain of logit, exponential and
+//    product.  One block of eight waves and 256 rows: 969, and with head_dim 64 476
+//    beside 402, since its waves meet at one barrier.)
+//  * K and V go from memory to LDS (global_load_lds): two K tiles and two V tiles, K one
+//    step ahead of V, one barrier per tile.  16-byte chunks are permuted by row so that
+//    neither the K operand reads nor the V transpose reads conflict.
 //  * 32x32x16 MFMAs: S^T = K Q^T leaves a query row in each lane column, where
 //    P^T already is the B operand of O^T = V^T P^T.
-//  * References, rounding and values that are not finite: as in attend.hip.  The
-//    sum of the rounded weights comes from the dot product with ones.
+//  * References, rounding and values that are not finite: as in attend.hip, but that
+//    a step looks for a row's largest logit only where its sum of weights passes 2^40.
+//    The sum of the rounded weights comes from the dot product with ones.
 #include "attend.h"
 
 namespace grkv {

@@ -414,3 +414,122 @@ def test_binding_checks():
                  lambda: G.sink_attention(q, K, K, -1)):
         with pytest.raises(G.GrkvError):
             call()
+
+
+# calls whose blocks hold 32 rows (many units of 17 to 64 rows), and splits of several row
+# groups, joined (few) or combined (many): dtype, d, page, group, tokens, lens, units, window, sinks
+ROW_CASES = [
+    (BF, 128, 64, 5, 6, [6, 7, 40, 64, 65, 150, 333], 70, 0, 0),
+    (BF, 64, 16, 8, 8, [8, 31, 100, 260], 36, 0, 0),
+    (BF, 128, 32, 3, 7, [7, 90, 600], 66, 50, 6),
+    (BF, 128, 64, 4, 8, [900, 1000, 8], 3, 0, 0),
+    (BF, 64, 64, 4, 8, [4000, 5000, 700], 3, 0, 0),
+    (F32, 128, 64, 4, 12, [1000, 300], 2, 0, 0),
+    (F32, 64, 64, 2, 20, [3000, 30], 2, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", ROW_CASES, ids=lambda c: "%s-d%d-p%d-g%d-t%d-u%d-w%d" % (
+    "bf16" if c[0] == BF else "f32", c[1], c[2], c[3], c[4], c[6], c[7]))
+def test_row_groups_of_many_units_and_of_few(case):
+    import paper_2605_31105_amd as G
+    dtype, d, ps, group, t, lens, units, window, n_sink = case
+    gen = torch.Generator().manual_seed(units + d)
+    pg, K, V = _pool(lens, ps, d, dtype, gen)
+    at = [e % len(lens) for e in range(units)]
+    parents, plist = _parents("tree", 1, t, gen)
+    q = torch.randn((units, group, t, d), generator=gen).to(dtype)
+    o, lse = G.tree_attention(q.cuda(), pg, parents, units=_i32(at), window=window, n_sink=n_sink,
+                              return_lse=True)
+    again = G.tree_attention(q.cuda(), pg, parents, units=_i32(at), window=window, n_sink=n_sink)
+    assert torch.equal(o, again)
+    o, lse = o.cpu(), lse.cpu()
+    for e in sorted({*range(len(lens)), *range(0, units, 11), units - 1}):
+        u = at[e]
+        for g in range(0, group, 2):
+            check("entry %d" % e, o[e, g], lse[e, g], q[e, g], K[u], V[u],
+                  tree_seen(lens[u], t, plist[0], window, n_sink))
+
+
+def test_siblings_that_are_not_finite_in_calls_of_many_units():
+    # a NaN and an infinity among the values of drafted token 2: only its own rows hold them
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(5)
+    plist = [-1, 0, 0, 1, 2, 4, 3, 3]
+    pg, K, V = _pool([70, 45], 16, 64, BF, gen)
+    at = [e % 2 for e in range(64)]
+    q = torch.randn((64, 3, 8, 64), generator=gen).to(BF)
+    for unit, slot, value in ((0, 64, math.nan), (1, 39, math.inf)):
+        pg.v[int(pg.table[unit, slot // 16]), slot % 16] = value
+    o, lse = (x.cpu() for x in G.tree_attention(q.cuda(), pg, _i32([plist]), units=_i32(at), return_lse=True))
+    for e in (0, 1, 30, 63):
+        u = at[e]
+        n = (70, 45)[u]
+        seen = tree_seen(n, 8, plist, 0, 0)
+        see = seen[:, (64, 39)[u]]
+        assert see.any() and not see.all()
+        for g in range(3):
+            check("entry %d head %d" % (e, g), o[e, g, ~see], lse[e, g, ~see], q[e, g, ~see], K[u], V[u], seen[~see])
+            assert not torch.isfinite(o[e, g, see]).any()
+
+
+def test_prompts_of_few_rows_and_many_units():
+    import paper_2605_31105_amd as G
+    for dtype, U, group, nq, n, d, window in ((BF, 64, 4, 5, 77, 128, 0), (BF, 32, 4, 16, 300, 64, 40),
+                                              (F32, 6, 4, 9, 500, 128, 0), (F32, 70, 3, 11, 64, 64, 9)):
+        gen = torch.Generator().manual_seed(n)
+        q = torch.randn((U, group, nq, d), generator=gen).to(dtype)
+        K, V = (torch.randn((U, n, d), generator=gen).to(dtype) for _ in range(2))
+        o, lse = (x.cpu() for x in G.sink_attention(q.cuda(), K.cuda(), V.cuda(), window, 3, return_lse=True))
+        for u in (0, U // 2, U - 1):
+            for g in range(group):
+                check("unit %d head %d" % (u, g), o[u, g], lse[u, g], q[u, g], K[u], V[u],
+                      sink_seen(n, nq, window, 3))
+
+
+def test_two_captured_calls_share_a_workspace():
+    # a call whose blocks join their splits, and one with a second launch: replayed in turn,
+    # with an eager call of the same workspace and one that refills it between them
+    import paper_2605_31105_amd as G
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    K, V = (torch.randn((3, 6000, 128), device="cuda", generator=gen).to(BF) for _ in range(2))
+    qs = [torch.randn((3, 4, nq, 128), device="cuda", generator=gen).to(BF) for nq in (2, 12)]
+    ws = torch.full((64 << 20,), 77, dtype=torch.uint8, device="cuda")
+    want = [G.sink_attention(q, K, V, 0, return_lse=True) for q in qs]
+    outs = [(torch.empty_like(o), torch.empty_like(l)) for o, l in want]
+    graphs = []
+    for q, (o, l) in zip(qs, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            G.sink_attention(q, K, V, 0, out=o, lse=l, workspace=ws)
+    for k in range(6):
+        for graph, (o, l), (wo, wl) in zip(graphs, outs, want):
+            o.zero_()
+            l.zero_()
+            graph.replay()
+            assert torch.equal(o, wo) and torch.equal(l, wl)
+        eager = G.sink_attention(qs[k % 2], K, V, 0, workspace=ws)
+        assert torch.equal(eager, want[k % 2][0])
+        if k == 3:
+            ws.fill_(3)
+
+
+def test_workspaces_and_sizes_that_the_binding_refuses():
+    import paper_2605_31105_amd as G
+    pg = G.new_pages(4, 4, 8, 16, 64)
+    q = torch.zeros(4, 2, 3, 64, dtype=BF, device="cuda")
+    K = torch.zeros(4, 5, 64, dtype=BF, device="cuda")
+    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    starts = torch.zeros(1, dtype=torch.int64, device="cuda")
+    for call in (lambda: G.tree_attention(q, pg, workspace=ws),
+                 lambda: G.sink_attention(q, K, K, 4, workspace=ws),
+                 lambda: G.sink_attention(q, K, K, 4, workspace=ws.cuda()[::2]),
+                 lambda: G.sink_attention(q, K, K, 4, workspace=ws.cuda()[:1].expand(1 << 16)),
+                 lambda: G.pages_append(pg, K, K, workspace=ws),
+                 lambda: G.sink_attention(q, K, K, 1 << 32), lambda: G.sink_attention(q, K, K, 4, 1 << 31),
+                 lambda: G.tree_attention(q, pg, window=(1 << 32) + 5),
+                 lambda: G.pages_append(pg, K[0], K[0], starts=starts, rows=1 << 32),
+                 lambda: G.pages_compact(pg, _i32([0]), starts=starts, rows=(1 << 32) + 1)):
+        with pytest.raises(ValueError):
+            call()
+    assert not pg.lens.any()
