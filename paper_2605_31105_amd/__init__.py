@@ -601,7 +601,7 @@ def intermediates(res: Result) -> dict:
 
 # ------------------------------------------------------- pages of a cache ----
 
-@dataclass(frozen=True, eq=False)
+@dataclass(frozen=True, eq=False, init=False)
 class Pages:
     """The pool of pages of grkv.h (``grkv_pages``): contiguous tensors of one
     device.  ``new_pages`` makes an empty one."""
@@ -612,10 +612,9 @@ class Pages:
     refs: "object"    # int32 [pages]
     free: "object"    # int32 [ceil(pages / 32)], bit p % 32 of word p // 32: page p is free
 
-    def __post_init__(self):
+    def __init__(self, k, v, table, lens, refs, free):
         import torch
 
-        k, v, table, lens, refs, free = self.k, self.v, self.table, self.lens, self.refs, self.free
         i32, dev = torch.int32, k.get_device()
         if dev < 0:
             raise ValueError("a pool's tensors must be device tensors")
@@ -632,7 +631,9 @@ class Pages:
                 raise ValueError("a pool's tensors must be contiguous and on one device")
         if not (table.dtype == lens.dtype == refs.dtype == free.dtype == i32):
             raise ValueError("table, lens, refs and free must be int32")
-        object.__setattr__(self, "_c", _PagesC(
+        # (a pool is often wrapped anew for a call: one update instead of a guarded assignment
+        # per field)
+        self.__dict__.update(k=k, v=v, table=table, lens=lens, refs=refs, free=free, _c=_PagesC(
             k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(),
             free.data_ptr(), n, ps, units, width, d, code))
 
@@ -680,7 +681,7 @@ def _workspace(workspace, need, dev):
             raise ValueError("workspace must be a contiguous tensor on cuda:%d" % dev)
         if workspace.numel() >= need:
             return workspace
-    return torch.empty(max(need, 256), dtype=torch.uint8, device=torch.device("cuda", dev))
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
 
 
 def _int32(bits):
@@ -870,7 +871,8 @@ def _attend(launch, need, q, out, lse, return_lse, workspace, handle):
     if out is None:
         out = torch.empty_like(q)
     if lse is None and return_lse:
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+        U, G, t, _ = q.shape
+        lse = torch.empty(U, G, t, dtype=torch.float32, device=q.device)
     workspace = _workspace(workspace, need, q.get_device())
     _check(launch(out.data_ptr(), None if lse is None else lse.data_ptr(), handle,
                   workspace.data_ptr(), workspace.numel()))
