@@ -642,11 +642,16 @@ class Pages:
         return self.k.device
 
 
+_CODES = {}
+
+
 def _dtype_code(t):
     """grkv_dtype of a tensor, or None."""
-    import torch
+    if not _CODES:
+        import torch
 
-    return (GRKV_BF16 if t.dtype == torch.bfloat16 else GRKV_F32 if t.dtype == torch.float32 else None)
+        _CODES.update({torch.bfloat16: GRKV_BF16, torch.float32: GRKV_F32})
+    return _CODES.get(t.dtype)
 
 
 def _on(dev: int, stream):
@@ -656,12 +661,12 @@ def _on(dev: int, stream):
     import torch
 
     if stream is None:
-        if torch.cuda.current_device() == dev:
+        if torch._C._cuda_getDevice() == dev:   # (a tensor of the call is there, so it is set up)
             return torch._C._cuda_getCurrentRawStream(dev), None
         stream = torch.cuda.current_stream(dev)
     elif not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=dev)
-    return stream.cuda_stream, torch.cuda.stream(stream)
+    return None, torch.cuda.stream(stream)
 
 
 def _vector(t, name, dtype, size, dev):
@@ -711,11 +716,10 @@ def new_pages(units: int, max_pages: int, pages: int, page_size: int, head_dim: 
 def pages_init(pages: Pages, *, stream=None) -> Pages:
     """Empties a pool: no unit holds a row, every page is free."""
     handle, on = _on(pages.k.get_device(), stream)
-    if on is None:
-        _check(lib().grkv_pages_init(pages._c, handle))
-    else:
+    if on is not None:
         with on:
-            _check(lib().grkv_pages_init(pages._c, handle))
+            return pages_init(pages)
+    _check(lib().grkv_pages_init(pages._c, handle))
     return pages
 
 
@@ -729,26 +733,21 @@ def _page_call(name, pages, entries, args, units, rows, counts, starts, source_r
     import torch
 
     dev, i32 = pages.k.get_device(), torch.int32
-    _int32(entries | rows)
-    en = _PageEntries(entries, _vector(units, "units", i32, entries, dev), rows,
-                      _vector(counts, "counts", i32, entries, dev),
-                      _vector(starts, "starts", torch.int64, entries, dev), source_rows, None)
     handle, on = _on(dev, stream)
     if on is not None:
         with on:
-            return _page_launch(name, pages, entries, args, en, dev, status, workspace, handle)
-    return _page_launch(name, pages, entries, args, en, dev, status, workspace, handle)
-
-
-def _page_launch(name, pages, entries, args, en, dev, status, workspace, handle):
-    import torch
-
+            return _page_call(name, pages, entries, args, units, rows, counts, starts, source_rows,
+                              status, workspace, None)
+    _int32(entries | rows)
     L = lib()
     if status is None:
-        status = torch.empty(entries, dtype=torch.int32, device=pages.k.device)
-        en.status = status.data_ptr()
+        status = torch.empty(entries, dtype=i32, device=dev)
+        at = status.data_ptr()
     else:
-        en.status = _vector(status, "status", torch.int32, entries, dev)
+        at = _vector(status, "status", i32, entries, dev)
+    en = _PageEntries(entries, _vector(units, "units", i32, entries, dev), rows,
+                      _vector(counts, "counts", i32, entries, dev),
+                      _vector(starts, "starts", torch.int64, entries, dev), source_rows, at)
     if name == "grkv_pages_free":
         _check(L.grkv_pages_free(pages._c, en, handle))
         return status
@@ -849,34 +848,19 @@ def _given(t, name, dtype, shape, dev):
                          % (name, dtype, tuple(shape), dev))
 
 
-def _attention(launch, need, q, out, lse, return_lse, workspace, stream):
-    """Outputs, workspace and stream of an attention call: launch(o, lse, handle, ws, bytes)."""
-    import torch
-
-    dev = q.get_device()
-    if out is not None:
-        _given(out, "out", q.dtype, q.shape, dev)
-    if lse is not None:
-        _given(lse, "lse", torch.float32, q.shape[:3], dev)
-    handle, on = _on(dev, stream)
-    if on is not None:
-        with on:
-            return _attend(launch, need, q, out, lse, return_lse, workspace, handle)
-    return _attend(launch, need, q, out, lse, return_lse, workspace, handle)
-
-
-def _attend(launch, need, q, out, lse, return_lse, workspace, handle):
+def _outputs(q, shape, dev, out, lse, return_lse):
+    """o, lse and lse's address."""
     import torch
 
     if out is None:
         out = torch.empty_like(q)
-    if lse is None and return_lse:
-        U, G, t, _ = q.shape
-        lse = torch.empty(U, G, t, dtype=torch.float32, device=q.device)
-    workspace = _workspace(workspace, need, q.get_device())
-    _check(launch(out.data_ptr(), None if lse is None else lse.data_ptr(), handle,
-                  workspace.data_ptr(), workspace.numel()))
-    return (out, lse) if return_lse else out
+    else:
+        _given(out, "out", q.dtype, q.shape, dev)
+    if lse is not None:
+        _given(lse, "lse", torch.float32, shape, dev)
+    elif return_lse:
+        lse = torch.empty(*shape, dtype=torch.float32, device=dev)
+    return out, lse, None if lse is None else lse.data_ptr()
 
 
 def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, window: int = 0,
@@ -894,25 +878,33 @@ def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, wi
     import torch
 
     dev, i32 = pages.k.get_device(), torch.int32
+    handle, on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return tree_attention(q, pages, parents, units=units, counts=counts, window=window,
+                                  n_sink=n_sink, return_lse=return_lse, out=out, lse=lse,
+                                  workspace=workspace)
     if q.get_device() != dev or q.dtype != pages.k.dtype or q.dim() != 4 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [E, G, t, d] tensor of the pool's type and device")
     E, G, t, d = q.shape
+    c = pages._c
     _int32(window | n_sink)
-    if d != pages.k.shape[2]:
-        raise ValueError("head_dim %d, the pool's is %d" % (d, pages.k.shape[2]))
+    if d != c.head_dim:
+        raise ValueError("head_dim %d, the pool's is %d" % (d, c.head_dim))
     trees, up = 0, None
     if parents is not None:
         trees, up = parents.shape[0], parents.data_ptr()
         if (parents.dtype != i32 or parents.get_device() != dev or parents.shape != (trees, t)
                 or not parents.is_contiguous()):
             raise ValueError("parents must be a contiguous int32 [trees, %d] tensor on cuda:%d" % (t, dev))
-    c = pages._c
     tr = _Tree(E, G, t, _vector(units, "units", i32, E, dev), _vector(counts, "counts", i32, E, dev),
                up, trees, window, n_sink)
-    L, qp = lib(), q.data_ptr()
-    need = L.grkv_tree_attention_workspace_bytes(c, tr)
-    return _attention(lambda o, l, h, ws, n: L.grkv_tree_attention(qp, c, tr, o, l, h, ws, n),
-                      need, q, out, lse, return_lse, workspace, stream)
+    out, lse, lp = _outputs(q, (E, G, t), dev, out, lse, return_lse)
+    L = lib()
+    workspace = _workspace(workspace, L.grkv_tree_attention_workspace_bytes(c, tr), dev)
+    _check(L.grkv_tree_attention(q.data_ptr(), c, tr, out.data_ptr(), lp, handle,
+                                 workspace.data_ptr(), workspace.numel()))
+    return (out, lse) if return_lse else out
 
 
 def sink_attention_workspace_bytes(units, group, head_dim, dtype, n, nq, window, n_sink) -> int:
@@ -930,21 +922,29 @@ def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = 
     dev = q.get_device()
     if dev < 0 or K.get_device() != dev or V.get_device() != dev:
         raise ValueError("q, K and V must be tensors of one device")
+    handle, on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return sink_attention(q, K, V, window, n_sink, return_lse=return_lse, out=out, lse=lse,
+                                  workspace=workspace)
     code = _dtype_code(q)
     if code is None or not (q.dtype == K.dtype == V.dtype):
         raise ValueError("q, K, V must share dtype bfloat16 or float32")
     if not (q.is_contiguous() and K.is_contiguous() and V.is_contiguous()):
         raise ValueError("inputs must be contiguous")
-    if (q.dim() != 4 or K.dim() != 3 or K.shape != V.shape or q.shape[0] != K.shape[0]
-            or q.shape[3] != K.shape[2]):
+    kv = K.shape
+    if q.dim() != 4 or len(kv) != 3 or kv != V.shape or q.shape[::3] != kv[::2]:
         raise ValueError("shape mismatch: q %s K %s V %s"
                          % (tuple(q.shape), tuple(K.shape), tuple(V.shape)))
     U, G, nq, d = q.shape
-    n = K.shape[1]
+    n = kv[1]
     _int32(window | n_sink)
     prob = Problem(U, G, d, code)
-    L, qp, kp, vp = lib(), q.data_ptr(), K.data_ptr(), V.data_ptr()
-    need = L.grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink)
-    return _attention(lambda o, l, h, ws, b: L.grkv_sink_attention(
-        qp, kp, vp, n, nq, window, n_sink, h, prob, o, l, ws, b),
-        need, q, out, lse, return_lse, workspace, stream)
+    out, lse, lp = _outputs(q, (U, G, nq), dev, out, lse, return_lse)
+    L = lib()
+    workspace = _workspace(workspace, L.grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink),
+                           dev)
+    _check(L.grkv_sink_attention(q.data_ptr(), K.data_ptr(), V.data_ptr(), n, nq, window, n_sink,
+                                 handle, prob, out.data_ptr(), lp, workspace.data_ptr(),
+                                 workspace.numel()))
+    return (out, lse) if return_lse else out
