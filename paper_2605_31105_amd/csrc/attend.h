@@ -154,23 +154,48 @@ __device__ __forceinline__ f32x4 get4(const float* p) {
   }
 }
 
-// Columns 4 ch .. of a row from splits s0, s0 + step, .. below ns, in that order,
-// against the largest reference of all ns.  at0: the row in split 0.
+// Adds split `y` to `o`, both against the larger of their references.
+__device__ __forceinline__ void add_split(Split& o, const Split& y) {
+  const float m = fmaxf(o.m, y.m), f = __builtin_amdgcn_exp2f(o.m - m), fy = __builtin_amdgcn_exp2f(y.m - m);
+  o.m = m;
+  o.l = o.l * f + y.l * fy;
+  o.lx = o.lx * f + y.lx * fy;
+  o.x = o.x * f + y.x * fy;
+}
+
+// Columns 4 ch .. of a row from splits s0, s0 + step, .. below ns, in that order.  The
+// reads of eight splits go out together.  at0: the row in split 0.
 template <int D, bool SHARED>
 __device__ __forceinline__ Split add_splits(const AttendK& a, size_t at0, int ns, int s0, int step,
                                             int ch) {
+  constexpr int B = 8;
   const int R = a.group * a.tokens;
   Split o = {-kUnset, 0.f, 0.f, zero4()};
-#pragma unroll 8
-  for (int s = 0; s < ns; ++s) o.m = fmaxf(o.m, get4<SHARED>((const float*)(a.mpart + at0 + (size_t)s * R))[0]);
-#pragma unroll 8
-  for (int s = s0; s < ns; s += step) {
-    const size_t at = at0 + (size_t)s * R;
-    const f32x4 ml = get4<SHARED>((const float*)(a.mpart + at));
-    const float f = __builtin_amdgcn_exp2f(ml[0] - o.m);
-    o.l += ml[1] * f;
-    o.lx += ml[2] * f;
-    o.x += get4<SHARED>(a.opart + at * D + 4 * ch) * f;
+  for (; s0 < ns; s0 += B * step) {
+    f32x4 ml[B], x[B];
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const int s = s0 + k * step;
+      ml[k] = (f32x4){-kUnset, 0.f, 0.f, 0.f};
+      x[k] = zero4();
+      if (s < ns) {
+        const size_t at = at0 + (size_t)s * R;
+        ml[k] = get4<SHARED>((const float*)(a.mpart + at));
+        x[k] = get4<SHARED>(a.opart + at * D + 4 * ch);
+      }
+    }
+    float m = o.m;
+#pragma unroll
+    for (int k = 0; k < B; ++k) m = fmaxf(m, ml[k][0]);
+    const float f0 = __builtin_amdgcn_exp2f(o.m - m);
+    o = {m, o.l * f0, o.lx * f0, o.x * f0};
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const float f = __builtin_amdgcn_exp2f(ml[k][0] - m);
+      o.l += ml[k][1] * f;
+      o.lx += ml[k][2] * f;
+      o.x += x[k] * f;
+    }
   }
   return o;
 }

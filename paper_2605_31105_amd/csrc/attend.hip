@@ -45,8 +45,8 @@ constexpr int kAtTh = 64 * kAtWaves;
 // (8 units of 2048 keys and 8 rows, 8 splits: one launch of 11.7 us against 9.8 and 3.9).
 // More are combined by a launch of their own, which has more threads for them (256 units
 // of 4100 keys, 4 splits: 98 and 5 us against 110), and with several row groups a unit,
-// whose splits end at different times, from 16 on (8 units of 32 rows: 1000 keys, 4
-// splits, 16.3 us joined, 18.0 combined; 4000 keys, 16 splits, 20.8 and 17.6).
+// whose splits end at different times, from 16 on (calls of 8 units of 32 rows: 1000 keys,
+// 4 splits, 13.7 us joined, 16.6 combined; 4000 keys, 16 splits, 18.4 and 16.5).
 constexpr int kJoinedSplits = 16, kJoinedRowSplits = 8, kJoinedBlocks = 512;
 
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform), as
@@ -411,7 +411,7 @@ template <typename E, int D, int GS>
 __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   constexpr int CR = D / 4, ROWS = kAtTh / (CR * GS);   // rows of a block
   __shared__ f32x4 part[GS > 1 ? kAtTh : 1];
-  __shared__ float2 psum[GS > 1 ? kAtTh : 1];
+  __shared__ float psum[3][GS > 1 ? kAtTh : 1];
   const int R = a.group * a.tokens, tid = threadIdx.x;
   const int ch = tid % CR, gs = tid / CR % GS;
   const int64_t row = (int64_t)blockIdx.x * ROWS + tid / (CR * GS);
@@ -432,15 +432,16 @@ __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   if (on) o = add_splits<D, false>(a, at0, ns, gs, GS, ch);
   if constexpr (GS > 1) {
     part[tid] = o.x;
-    psum[tid] = make_float2(o.l, o.lx);
+    psum[0][tid] = o.m;
+    psum[1][tid] = o.l;
+    psum[2][tid] = o.lx;
     __syncthreads();
     on = on && gs == 0;
     if (on) {
 #pragma unroll
       for (int k = 1; k < GS; ++k) {
-        o.x += part[tid + k * CR];
-        o.l += psum[tid + k * CR].x;
-        o.lx += psum[tid + k * CR].y;
+        const int t = tid + k * CR;
+        add_split(o, {psum[0][t], psum[1][t], psum[2][t], part[t]});
       }
     }
   }
