@@ -164,12 +164,12 @@ __device__ __forceinline__ void add_split(Split& o, const Split& y) {
 }
 
 // Columns 4 ch .. of a row from splits s0, s0 + step, .. below ns, in that order.  The
-// reads of eight splits go out together.  at0: the row in split 0.
+// reads of eight splits go out together.  The row is at0 + first in split 0 and at0 + s *
+// stride in split s > 0.
 template <int D, bool SHARED>
-__device__ __forceinline__ Split add_splits(const AttendK& a, size_t at0, int ns, int s0, int step,
-                                            int ch) {
+__device__ __forceinline__ Split add_splits(const AttendK& a, size_t at0, int first, int stride, int ns,
+                                            int s0, int step, int ch) {
   constexpr int B = 8;
-  const int R = a.group * a.tokens;
   Split o = {-kUnset, 0.f, 0.f, zero4()};
   for (; s0 < ns; s0 += B * step) {
     f32x4 ml[B], x[B];
@@ -179,7 +179,7 @@ __device__ __forceinline__ Split add_splits(const AttendK& a, size_t at0, int ns
       ml[k] = (f32x4){-kUnset, 0.f, 0.f, 0.f};
       x[k] = zero4();
       if (s < ns) {
-        const size_t at = at0 + (size_t)s * R;
+        const size_t at = at0 + (s == 0 ? (size_t)first : (size_t)s * stride);
         ml[k] = get4<SHARED>((const float*)(a.mpart + at));
         x[k] = get4<SHARED>(a.opart + at * D + 4 * ch);
       }
@@ -339,10 +339,11 @@ __device__ __forceinline__ bool odd_values(const AttendK& a, const Span& sn, int
 // Rows of a split once more, key by key: taken where a tile that some rows see
 // only part of holds an infinity or NaN among its values, since 0 x inf in a
 // product reaches the rows that do not see it (as NaN).  One wave; rows first ..
-// first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn.  A lane forms the
-// weight of one key of 64, then sums D / 64 columns.
+// first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn, left as partial rows
+// from `part` on or (part < 0) as outputs.  A lane forms the weight of one key of 64, then
+// sums D / 64 columns.
 template <typename E, int D, bool PAGED>
-__device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, int e, int sp, int first,
+__device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, int e, int64_t part, int first,
                                             int count, int vt0, int vt1, int tk, int len, int t,
                                             const int32_t* trow, uint64_t family, int depth) {
   constexpr bool BF = sizeof(E) == 2;
@@ -404,8 +405,8 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
         }
       }
     }
-    if (sn.ns > 1) {
-      const size_t to = ((size_t)e * a.splits + sp) * R + r;
+    if (part >= 0) {
+      const size_t to = part + r;
       for (int c = 0; c < C; ++c)
         __hip_atomic_store(a.opart + to * D + 64 * c + lane, o[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (lane == 0) put4((float*)(a.mpart + to), (f32x4){m, l, lx, 0.f}, true);

@@ -47,6 +47,7 @@ constexpr int kAtTh = 64 * kAtWaves;
 // of 4100 keys, 4 splits: 98 and 5 us against 110), and with several row groups a unit,
 // whose splits end at different times, from 16 on (calls of 8 units of 32 rows: 1000 keys,
 // 4 splits, 13.7 us joined, 16.6 combined; 4000 keys, 16 splits, 18.4 and 16.5).
+constexpr int kEvenEntries = 4096, kEvenTiles = 32, kEvenBlocks = 512;
 constexpr int kJoinedSplits = 16, kJoinedRowSplits = 8, kJoinedBlocks = 512;
 
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform), as
@@ -66,8 +67,13 @@ struct Tile {
   static constexpr int KT = KEYS / 16;
 };
 
+// Rows r0 .. r0 + 16 RT - 1 of entry e over the tiles vt0 .. vt1 - 1 of its span, by a block:
+// partial rows from `part` on (passed to other blocks of the launch with `shared`) or,
+// with part < 0, the outputs.
 template <typename E, int D, int RT, bool PAGED>
-__global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_kernel(AttendK a) {
+__device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, int e, int r0, int vt0,
+                                            int vt1, int64_t part, bool shared, int len, int t,
+                                            const int32_t* trow) {
   constexpr bool BF = sizeof(E) == 2;
   constexpr int TK = Tile<E>::KEYS, KT = Tile<E>::KT;
   constexpr int RB = D * (int)sizeof(E);          // bytes of a row
@@ -77,6 +83,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   constexpr int RPI = 64 / CPR;                   // rows of one of them
   constexpr int DS = BF ? D / 32 : D / 16;        // 16-byte K fragments of a key
   constexpr int DT = D / 16;
+  constexpr int CR = D / 4;                       // 4-value chunks of a row
   static_assert(2 * VB == 16 * 2 * D * 4, "two stages hold the partial rows of a wave");
   typedef typename std::conditional<BF, bf16x8, float4>::type Frag;
 
@@ -84,19 +91,9 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
   __shared__ __attribute__((aligned(16))) char v1_s[kAtWaves * VB];
   __shared__ float m_s[kAtWaves][16 * RT], l_s[kAtWaves][16 * RT], x_s[kAtWaves][16 * RT];
 
-  int e, rg, sp;
-  if (!block_work(a, &e, &rg, &sp)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, gq = lane >> 4;
-  const int R = a.group * a.tokens, r0 = rg * 16 * RT;
-  int len, t;
-  const int32_t* trow;
-  entry_shape(a, e, &len, &t, &trow);
-  const int base = len - t;
-  const int i0 = group_of(a, r0), i1 = group_of(a, min(r0 + 16 * RT - 1, R - 1));
-  const Span sn = make_span(a, len, base, t, i0, i1, TK);
-  const int vt0 = sp * sn.chunk, vt1 = min(sn.nt, vt0 + sn.chunk);
-  if (sp > 0 && vt0 >= sn.nt) return;
+  const int R = a.group * a.tokens, base = len - t;
 
   uint64_t family = 0;
   int depth = 0;
@@ -324,19 +321,6 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
     }
   }
 
-  // the splits of a short call, by the block that finishes last
-  constexpr int CR = D / 4;   // 4-value chunks of a row
-  auto join = [&]() __attribute__((always_inline)) {
-    if (sn.ns < 2 || !a.flags || !splits_done(a, (size_t)e * a.row_groups + rg, sp, sn.ns)) return;
-    for (int c = tid; c < 16 * RT * CR; c += kAtTh) {
-      const int r = r0 + c / CR, ch = c % CR;
-      const int i = group_of(a, r), g = r - i * a.group;
-      if (r >= R || i >= t) continue;
-      const Split o = add_splits<D, true>(a, (size_t)e * a.splits * R + r, sn.ns, 0, 1, ch);
-      write_out<E, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, o.x, o.m, o.l, o.lx);
-    }
-  };
-
   // the waves' parts: references, then rows scaled to the largest, summed over
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
@@ -347,9 +331,8 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) all += acc[dt][rt][0] + acc[dt][rt][1] + acc[dt][rt][2] + acc[dt][rt][3];
   if (__syncthreads_or(all != all) && odd_values<E, D, PAGED>(a, sn, e, vt0, vt1, TK, sn.lim, sn.lo, trow)) {
-    rows_by_key<E, D, PAGED>(a, sn, e, sp, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
+    rows_by_key<E, D, PAGED>(a, sn, e, part, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
                              family, depth);
-    join();
     return;
   }
 #pragma unroll
@@ -363,7 +346,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
     }
   }
   __syncthreads();
-  char* part = (wave < 2 ? v0_s : v1_s) + (wave & 1) * 2 * VB;
+  char* mine = (wave < 2 ? v0_s : v1_s) + (wave & 1) * 2 * VB;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int row = 16 * rt + l16;
@@ -373,7 +356,7 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
     const float f = __builtin_amdgcn_exp2f(-nref[rt] - m);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
-      *reinterpret_cast<f32x4*>(part + row * D * 4 + (((4 * dt + gq) ^ l16) << 4)) = acc[dt][rt] * f;
+      *reinterpret_cast<f32x4*>(mine + row * D * 4 + (((4 * dt + gq) ^ l16) << 4)) = acc[dt][rt] * f;
   }
   __syncthreads();
   for (int c = tid; c < 16 * RT * CR; c += kAtTh) {
@@ -392,16 +375,122 @@ __global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_ker
       x += *reinterpret_cast<const f32x4*>((w < 2 ? v0_s : v1_s) + (w & 1) * 2 * VB + row * D * 4 +
                                            ((ch ^ (row & 15)) << 4));
     }
-    if (sn.ns > 1) {
-      const size_t at = ((size_t)e * a.splits + sp) * R + r;
-      put4(a.opart + at * D + 4 * ch, x, a.flags != nullptr);
-      if (ch == 0) put4((float*)(a.mpart + at), (f32x4){m, l, lx, 0.f}, a.flags != nullptr);
+    if (part >= 0) {
+      put4(a.opart + (part + r) * D + 4 * ch, x, shared);
+      if (ch == 0) put4((float*)(a.mpart + part + r), (f32x4){m, l, lx, 0.f}, shared);
     } else {
       const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
       write_out<E, D>(a, at, ch, x, m, l, lx);
     }
   }
-  join();
+}
+
+template <typename E, int D, int RT, bool PAGED>
+__global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_kernel(AttendK a) {
+  int e, rg, sp;
+  if (!block_work(a, &e, &rg, &sp)) return;
+  const int R = a.group * a.tokens, r0 = rg * 16 * RT;
+  int len, t;
+  const int32_t* trow;
+  entry_shape(a, e, &len, &t, &trow);
+  const Span sn = make_span(a, len, len - t, t, group_of(a, r0), group_of(a, min(r0 + 16 * RT - 1, R - 1)),
+                            Tile<E>::KEYS);
+  const int vt0 = sp * sn.chunk, vt1 = min(sn.nt, vt0 + sn.chunk);
+  if (sp > 0 && vt0 >= sn.nt) return;
+  attend_rows<E, D, RT, PAGED>(a, sn, e, r0, vt0, vt1, sn.ns > 1 ? ((int64_t)e * a.splits + sp) * R : -1,
+                               a.flags != nullptr, len, t, trow);
+
+  // the splits of a short call, by the block that finishes last
+  if (sn.ns < 2 || !a.flags || !splits_done(a, (size_t)e * a.row_groups + rg, sp, sn.ns)) return;
+  constexpr int CR = D / 4;
+  for (int c = threadIdx.x; c < 16 * RT * CR; c += kAtTh) {
+    const int r = r0 + c / CR, ch = c % CR;
+    const int i = group_of(a, r), g = r - i * a.group;
+    if (r >= R || i >= t) continue;
+    const Split o = add_splits<D, true>(a, (size_t)e * a.splits * R + r, 0, R, sn.ns, 0, 1, ch);
+    write_out<E, D>(a, ((size_t)e * a.group + g) * a.tokens + i, ch, o.x, o.m, o.l, o.lx);
+  }
+}
+
+// The tiles of an entry, as attend_even_kernel counts them: one at least, so that an
+// entry without keys is some block's too.
+template <typename E, int RT>
+__device__ __forceinline__ Span even_span(const AttendK& a, int len, int t, int* tiles) {
+  const int R = a.group * a.tokens;
+  const Span sn = make_span(a, len, len - t, t, 0, group_of(a, min(16 * RT - 1, R - 1)), Tile<E>::KEYS);
+  *tiles = max(sn.nt, 1);
+  return sn;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | lo);
+}
+
+// Units of any lengths, one row group each: the tiles of all of them in a row, cut into
+// as many equal parts as there are blocks, so that no block waits for a longer one.  A
+// part goes over the ends of units; of the rows of a part only the first and the last
+// unit's may be partial.  Every block adds up the lengths for itself.
+template <typename E, int D, int RT>
+__global__ __launch_bounds__(kAtTh, RT == 2 && D == 128 ? 1 : 2) void attend_even_kernel(AttendK a) {
+  __shared__ int64_t sum_s[kAtWaves];
+  __shared__ int64_t at_s;
+  __shared__ int first_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, R = a.group * a.tokens;
+  // tiles before this thread's entries, and of all
+  const int per = (a.entries + kAtTh - 1) / kAtTh, e0 = tid * per, e1 = min(a.entries, e0 + per);
+  int len, t, tiles;
+  const int32_t* trow;
+  int64_t own = 0;
+  for (int e = e0; e < e1; ++e) {
+    entry_shape(a, e, &len, &t, &trow);
+    even_span<E, RT>(a, len, t, &tiles);
+    own += tiles;
+  }
+  int64_t incl = own;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const int64_t b = __shfl_up((long long)incl, k);
+    if (lane >= k) incl += b;
+  }
+  if (lane == 63) sum_s[wave] = incl;
+  __syncthreads();
+  int64_t all = 0, at = incl - own;
+#pragma unroll
+  for (int w = 0; w < kAtWaves; ++w) {
+    if (w < wave) at += sum_s[w];
+    all += sum_s[w];
+  }
+  all = uniform64(all);
+  const int64_t blocks = gridDim.x, b = blockIdx.x;
+  const int64_t part = max((int64_t)a.min_tiles, (all + blocks - 1) / blocks);
+  const int64_t lo = b * part, hi = min(all, lo + part);
+  if (lo >= all) return;
+  if (at <= lo && lo < at + own) {   // this thread's: the entry of the part's first tile
+    int e = e0;
+    for (;; ++e) {
+      entry_shape(a, e, &len, &t, &trow);
+      even_span<E, RT>(a, len, t, &tiles);
+      if (lo < at + tiles) break;
+      at += tiles;
+    }
+    first_s = e;
+    at_s = at;
+  }
+  __syncthreads();
+  int64_t from = uniform64(at_s);
+  for (int e = __builtin_amdgcn_readfirstlane(first_s); from < hi; ++e) {
+    entry_shape(a, e, &len, &t, &trow);
+    const Span sn = even_span<E, RT>(a, len, t, &tiles);
+    const int64_t to = from + __builtin_amdgcn_readfirstlane(tiles);
+    const int vt0 = (int)(max(lo, from) - from), vt1 = (int)(min(hi, to) - from);
+    const bool whole = from >= lo && to <= hi;
+    const int64_t slot = 2 * b + (from > lo ? 1 : 0);
+    if (from >= lo && tid == 0) a.even[e] = make_int2((int)slot, whole ? 1 : (int)((to - 1) / part - b) + 1);
+    attend_rows<E, D, RT, true>(a, sn, e, 0, vt0, min(vt1, sn.nt), whole ? -1 : slot * R, false, len, t, trow);
+    __syncthreads();   // (the next rows take the same stages)
+    from = to;
+  }
 }
 
 // The splits of a row, where they are not joined by attend_kernel: one thread per 4
@@ -421,15 +510,21 @@ __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
   const int32_t* trow;
   if (on) entry_shape(a, e, &len, &t, &trow);
   const int i = group_of(a, r), g = r - i * a.group;
-  int ns = 0;
-  if (on && i < t) {
+  int ns = 0, first = 0, stride = R;
+  size_t at0 = (size_t)e * a.splits * R + r;
+  if (on && i < t && a.even) {
+    const int2 p = a.even[e];   // the first part, which may be its block's second
+    ns = p.y;
+    first = (p.x & 1) * R;
+    at0 = (size_t)(p.x & ~1) * R + r;
+    stride = 2 * R;
+  } else if (on && i < t) {
     const int r0 = r / a.rows * a.rows;
     ns = make_span(a, len, len - t, t, group_of(a, r0), group_of(a, min(r0 + a.rows - 1, R - 1)), a.tile_keys).ns;
   }
   on = ns > 1;   // (a single split has written its row)
-  const size_t at0 = (size_t)e * a.splits * R + r;
   Split o = {-kUnset, 0.f, 0.f, zero4()};
-  if (on) o = add_splits<D, false>(a, at0, ns, gs, GS, ch);
+  if (on) o = add_splits<D, false>(a, at0, first, stride, ns, gs, GS, ch);
   if constexpr (GS > 1) {
     part[tid] = o.x;
     psum[0][tid] = o.m;
@@ -451,7 +546,8 @@ __global__ __launch_bounds__(kAtTh) void combine_kernel(AttendK a) {
 template <typename E, int D, int RT>
 hipError_t launch_rows(const AttendK& a, hipStream_t s) {
   const dim3 grid((unsigned)a.blocks), th(kAtTh);
-  if (a.lens) hipLaunchKernelGGL((attend_kernel<E, D, RT, true>), grid, th, 0, s, a);
+  if (a.even) hipLaunchKernelGGL((attend_even_kernel<E, D, RT>), grid, th, 0, s, a);
+  else if (a.lens) hipLaunchKernelGGL((attend_kernel<E, D, RT, true>), grid, th, 0, s, a);
   else hipLaunchKernelGGL((attend_kernel<E, D, RT, false>), grid, th, 0, s, a);
   return hipGetLastError();
 }
@@ -468,7 +564,7 @@ hipError_t launch_d(const AttendK& a, int rt, hipStream_t s) {
 template <typename E, int D>
 hipError_t launch_ed(const AttendK& a, int rt, hipStream_t s) {
   const hipError_t e = launch_d<E, D>(a, rt, s);
-  if (e != hipSuccess || a.splits == 1 || a.flags) return e;
+  if (e != hipSuccess || (a.splits == 1 && !a.even) || a.flags) return e;
   // threads that share a value: two, or with many splits a block's all (16 splits of 32
   // units of 128 rows, call 114 -> 110 us with two; 64 splits of 8 units of 8 rows, 100
   // with two, 95 with eight)
@@ -538,12 +634,19 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   p.blocks = (p.grouped ? (w + 7) / 8 * 8 : w) * p.row_groups;
   p.joined = p.rt > 0 && p.splits > 1 && p.blocks <= kJoinedBlocks &&
              p.splits <= (p.row_groups == 1 ? kJoinedSplits : kJoinedRowSplits);
+  p.even = ragged && p.rt > 0 && p.row_groups == 1 && entries <= kEvenEntries &&
+           entries * tiles >= kEvenTiles * (int64_t)kEvenBlocks;
+  if (p.even) {
+    p.joined = 0;
+    p.blocks = kEvenBlocks;
+  }
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
-  const size_t rows = p.splits > 1 ? (size_t)w * R : 0;
+  const size_t rows = p.even ? 2 * (size_t)p.blocks * R : p.splits > 1 ? (size_t)w * R : 0;
   p.opart = 0;
   p.mpart = up(rows * d * sizeof(float));
   p.flags = p.mpart + up(rows * sizeof(float4));
-  p.total = p.flags + (p.joined ? up((size_t)w * p.row_groups * sizeof(uint64_t)) : 0);
+  p.total = p.flags + (p.joined ? up((size_t)w * p.row_groups * sizeof(uint64_t))
+                       : p.even ? up((size_t)entries * sizeof(int2)) : 0);
   return p;
 }
 
@@ -560,6 +663,7 @@ hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void*
   a.opart = (float*)((char*)workspace + p.opart);
   a.mpart = (float4*)((char*)workspace + p.mpart);
   a.flags = p.joined ? (uint64_t*)((char*)workspace + p.flags) : nullptr;
+  a.even = p.even ? (int2*)((char*)workspace + p.flags) : nullptr;
   a.nonce = p.joined ? next_nonce() : 0;
   a.split_shift = __builtin_ctz((unsigned)p.splits);
   a.gshift = 0;

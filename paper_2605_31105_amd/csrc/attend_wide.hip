@@ -288,8 +288,9 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   for (int dm = 0; dm < DM; ++dm)
 #pragma unroll
     for (int r = 0; r < 16; ++r) all += acc[dm][r];
+  const int64_t part = ((int64_t)e * a.splits + sp) * R;
   if (__any(all != all) && odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, lim, lo, trow)) {
-    rows_by_key<u16, D, PAGED>(a, sn, e, sp, w0, 32, vt0, vt1, TK, len, t, trow, family, depth);
+    rows_by_key<u16, D, PAGED>(a, sn, e, sn.ns > 1 ? part : -1, w0, 32, vt0, vt1, TK, len, t, trow, family, depth);
     return;
   }
   // a wave's rows through its part of the ring (lane's four columns 32 dm + 8 c + 4 h of
@@ -304,7 +305,6 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
       for (int c = 0; c < 4; ++c)
         *reinterpret_cast<f32x4*>(out + (l32 * CR + ((8 * dm + 2 * c + h) ^ (l32 & 15))) * 16) =
             (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]};
-    const size_t part = ((size_t)e * a.splits + sp) * R;
     if (h == 0 && my < R && mi < t) a.mpart[part + my] = make_float4(-nref, rsum, sum, 0.f);
 #pragma unroll 4
     for (int k = lane; k < 32 * CR; k += 64) {

@@ -325,6 +325,7 @@ struct AttendK {
   int gshift, split_shift;
   uint64_t* flags;       // [entries * row_groups][splits], or null: no split is joined in place
   uint64_t nonce;
+  int2* even;            // [entries] first partial rows (in R) and splits, or null: attend_even_kernel
   int64_t blocks;
   int window, n_sink; // window 0: none
   float scale_log2;
@@ -341,8 +342,9 @@ struct AttendK {
 struct AttendPlan {
   int rt;             // 16-row tiles of a block; 0: the wide kernel
   int row_groups, splits, min_tiles, rows, tile_keys, grouped, joined;
+  int even;           // the keys of all entries in equal parts
   int64_t blocks;
-  size_t opart, mpart, flags, total;
+  size_t opart, mpart, flags, total;   // flags: also the table of an even call
 };
 AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int64_t slots,
                        bool ragged);

@@ -533,3 +533,82 @@ def test_workspaces_and_sizes_that_the_binding_refuses():
         with pytest.raises(ValueError):
             call()
     assert not pg.lens.any()
+
+
+# calls of enough keys that they are cut into equal parts over the units: dtype, d, page, group,
+# tokens, lens, entries, longest table row, window, sinks
+EVEN_CASES = [
+    (BF, 128, 64, 4, 1, [0, 1, 33, 2000, 640, 31, 900], 300, 32, 0, 0),
+    (BF, 64, 16, 3, 5, [5, 0, 777, 1500, 6, 4], 420, 94, 0, 0),
+    (BF, 128, 32, 8, 4, [4, 1100, 90, 2100], 280, 66, 0, 0),
+    (BF, 128, 256, 1, 1, [0, 0, 1, 0], 4096, 2, 0, 0),
+    (BF, 64, 64, 2, 7, [50, 3000, 200], 9, 1024, 40, 9),
+    (BF, 128, 64, 4, 2, [60000, 70, 2], 5, 2048, 0, 0),
+    (F32, 128, 16, 2, 3, [3, 400, 1000, 0], 270, 63, 0, 0),
+    (F32, 64, 64, 5, 2, [2, 1234, 65], 250, 20, 300, 5),
+]
+
+
+@pytest.mark.parametrize("case", EVEN_CASES, ids=lambda c: "%s-d%d-p%d-g%d-t%d-e%d-w%d" % (
+    "bf16" if c[0] == BF else "f32", c[1], c[2], c[3], c[4], c[6], c[8]))
+def test_units_of_any_lengths_in_equal_parts(case):
+    import paper_2605_31105_amd as G
+    dtype, d, ps, group, t, lens, entries, width, window, n_sink = case
+    gen = torch.Generator().manual_seed(entries)
+    pg, K, V = _pool(lens, ps, d, dtype, gen)
+    table = torch.full((len(lens) + 1, width), -1, dtype=torch.int32, device="cuda")
+    table[:, :pg.table.shape[1]] = pg.table[:, :width]
+    pg = G.Pages(pg.k, pg.v, table, pg.lens, pg.refs, pg.free)
+    at = torch.randint(len(lens), (entries,), generator=gen).tolist()
+    counts = [t if k % 5 else k % (t + 1) for k in range(entries)]
+    parents, plist = _parents("tree", 1, t, gen)
+    q = torch.randn((entries, group, t, d), generator=gen).to(dtype)
+    o = torch.full(q.shape, 5.0, dtype=dtype, device="cuda")
+    lse = torch.full(q.shape[:3], 6.0, device="cuda")
+    G.tree_attention(q.cuda(), pg, parents, units=_i32(at), counts=_i32(counts), window=window,
+                     n_sink=n_sink, out=o, lse=lse)
+    again = torch.full_like(o, 5.0)
+    G.tree_attention(q.cuda(), pg, parents, units=_i32(at), counts=_i32(counts), window=window,
+                     n_sink=n_sink, out=again)
+    assert torch.equal(o, again)
+    o, lse = o.cpu(), lse.cpu()
+    for e in sorted({*range(0, entries, max(1, entries // 40)), entries - 1, entries - 2}):
+        u, c = at[e], counts[e]
+        assert (o[e, :, c:] == 5).all() and (lse[e, :, c:] == 6).all()
+        for g in range(0, group, 2):
+            check("entry %d" % e, o[e, g, :c], lse[e, g, :c], q[e, g, :c], K[u], V[u],
+                  tree_seen(lens[u], c, plist[0], window, n_sink))
+
+
+def test_equal_parts_captured_and_values_that_are_not_finite():
+    # drafted token 2 of one unit holds a NaN; replays with other lengths than at the capture
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(8)
+    lens, entries, plist = [1500, 300, 20], 360, [-1, 0, 0, 1]
+    pg, K, V = _pool(lens, 64, 64, BF, gen)
+    slot = 300 - 4 + 2
+    pg.v[int(pg.table[1, slot // 64]), slot % 64, 7] = math.nan
+    at = [e % 3 for e in range(entries)]
+    q = torch.randn((entries, 2, 4, 64), generator=gen).to(BF)
+    qd, units, parents = q.cuda(), _i32(at), _i32([plist])
+    out, lse = torch.empty_like(qd), torch.empty(q.shape[:3], device="cuda")
+    G.tree_attention(qd, pg, parents, units=units, out=out, lse=lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G.tree_attention(qd, pg, parents, units=units, out=out, lse=lse)
+    for held in (lens, [700, 300, 4], lens):
+        pg.lens[:3] = _i32(held)
+        out.zero_()
+        graph.replay()
+        eager, le = G.tree_attention(qd, pg, parents, units=units, return_lse=True)
+        assert torch.equal(torch.nan_to_num(out, 9.0), torch.nan_to_num(eager, 9.0)) and torch.equal(lse, le)
+        for e in (0, 1, 2, 178, 358, 359):
+            u = at[e]
+            n = held[u]
+            seen = tree_seen(n, 4, plist, 0, 0)
+            clean = ~seen[:, slot] if u == 1 else torch.ones(4, dtype=torch.bool)
+            for g in range(2):
+                check("entry %d" % e, eager[e, g].cpu()[clean], le[e, g].cpu()[clean], q[e, g, clean],
+                      K[u][:n], V[u][:n], seen[clean])
+                assert u != 1 or torch.isnan(eager[e, g, 2, 7]).item()
