@@ -6,8 +6,11 @@
 //   o_r = sum_j 2^(t_rj - m_r) v_j / sum_j 2^(t_rj - m_r),  t = q . k log2(e) / sqrt(d),
 // in one pass over the keys with a running reference m_r.  Rows are the
 // (query, head of the group) pairs, query-major, 16 RT per block; a unit's keys
-// are split over blocks when there are few units, and over the four waves of a
-// block always.
+// are split over blocks when there are few units, or all units' keys cut into equal
+// parts when their lengths may differ (attend_even_kernel), and over the four waves of
+// a block always.  Long calls are bound by HBM: 512 units of 500 to 8000 keys, 1.1 GB in
+// 187 us, 6.0 TB/s (6.3 is what a read-only stream reaches); short ones by the chain of
+// dependent reads and the launch (8 units of 2048 keys, 11.7 us).
 //
 //  * A wave walks its own key tiles (32 keys of bf16, 16 of float32) with no
 //    barrier: K fragments go from memory to registers in the MFMA A layout and
@@ -47,8 +50,13 @@ constexpr int kAtTh = 64 * kAtWaves;
 // of 4100 keys, 4 splits: 98 and 5 us against 110), and with several row groups a unit,
 // whose splits end at different times, from 16 on (calls of 8 units of 32 rows: 1000 keys,
 // 4 splits, 13.7 us joined, 16.6 combined; 4000 keys, 16 splits, 18.4 and 16.5).
-constexpr int kEvenEntries = 4096, kEvenTiles = 32, kEvenBlocks = 512;
 constexpr int kJoinedSplits = 16, kJoinedRowSplits = 8, kJoinedBlocks = 512;
+// Units of any lengths are cut into equal parts (attend_even_kernel) where a part of the
+// longest would have 32 tiles or more (calls of 128 units of 500 to 8000 keys, bf16: 59 us,
+// with splits joined 64; 512 units 188, in four splits each 203, in one 228; 64 units of
+// 8000 keys, 31 tiles: 55, joined 49), for two blocks per compute unit (512 units: 768 blocks
+// 212 us, 1024 194), and up to 4096 units, whose lengths every block reads.
+constexpr int kEvenTiles = 32, kEvenBlocks = 512, kEvenEntries = 4096;
 
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform), as
 // a non-temporal load: values are read once, and pass the caches faster so (over
@@ -599,14 +607,14 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   AttendPlan p;
   const int64_t R = (int64_t)group * tokens;
   const bool bf16 = dtype == GRKV_BF16;
-  int64_t target;   // blocks
+  // two blocks per compute unit (32 units of 20k to 32k keys, 128 rows, 256 / 512 / 1024
+  // blocks: 138 / 116 / 139 us; 300 units of 500 to 4000 keys, 64 rows, 512 / 2048: 168 / 180)
+  constexpr int64_t target = 512;
   if (bf16 && R > 64) {
     p.rt = 0;
     p.rows = 128;
     p.tile_keys = kWideKeys;
     p.min_tiles = 8;
-    // (32 units of 20k to 32k keys, 128 rows, 256 / 512 / 1024 blocks: 138 / 116 / 139 us)
-    target = 512;
   } else {
     // rows of a block: 32 read the keys half as often, 16 make twice the blocks and hold
     // twice the waves (32 rows of bf16 over 8000 keys, 16 / 32 rows a block: 24 units 36.3 /
@@ -616,11 +624,6 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
     p.rows = 16 * p.rt;
     p.tile_keys = bf16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
     p.min_tiles = 8;
-    // two blocks per compute unit; lengths that may differ and are many: finer, so
-    // that the longest ones end with the others (512 units of 500 to 8000 keys, 512 /
-    // 1024 / 2048 / 4096 blocks: 242 / 226 / 215 / 222 us; 8 units of 128k keys 103 / 109 /
-    // 125; 256 units with a 4k window 100 / 103 / 108)
-    target = ragged && (int64_t)entries * ((R + p.rows - 1) / p.rows) >= 256 ? 2048 : 512;
   }
   p.row_groups = (int)((R + p.rows - 1) / p.rows);
   const int64_t tiles = (slots + p.tile_keys - 1) / p.tile_keys;
