@@ -315,8 +315,8 @@ struct AttendK {
   const void* v;
   void* o;            // as q
   float* lse;         // [entries][group][tokens] or null
-  float* opart;       // [entries][splits][group * tokens][d]
-  float4* mpart;      // [entries][splits][group * tokens] reference, sums
+  float* opart;       // [entries][splits][group * tokens][d], or with `even` [blocks][2][..
+  float4* mpart;      // the same rows: reference, sums
   int entries, group, tokens;
   int row_groups, splits, min_tiles;
   int rows, tile_keys;   // query rows of a block, keys of a tile
