@@ -90,12 +90,17 @@ __device__ __forceinline__ void make_plan_block(const PagesK& a) {
   // (an entry may ask for 2^26 pages: their sums take 64 bits)
   __shared__ unsigned long long scratch[2][kPlanTh / 64];
   __shared__ uint32_t scratch32[2][kPlanTh / 64];
+  __shared__ uint32_t taken_s[kPlanTh], rank_s[kPlanTh];   // pages taken of a word, the first one's rank
   __shared__ int used_s;
   const int tid = threadIdx.x, lane = tid & 63;
   const int ps = 1 << a.shift;
   const int64_t cap = (int64_t)a.pg.max_pages << a.shift;
   auto unit_of = [&](int i) { return a.units ? a.units[i] : i; };
   auto in_pool = [&](int u) { return (unsigned)u < (unsigned)a.pg.units; };
+
+  // (read here, while the entries are)
+  const int words = (a.pg.pages + 31) / 32;
+  const uint32_t bits0 = tid < words ? a.pg.free_bits[tid] : 0u;
 
   // owner of a unit: the lowest entry that writes it (in LDS where the pool is
   // small; entry i is unit i's without lists of units)
@@ -184,14 +189,14 @@ __device__ __forceinline__ void make_plan_block(const PagesK& a) {
   }
 
   // the lowest free pages, as many as are asked for.  A thread takes a word of 32
-  // pages; a wave writes the numbers word by word, so that neighbouring lanes
-  // write neighbouring numbers
-  const int words = (a.pg.pages + 31) / 32;
+  // pages; the numbers are written two words at a time by a wave, neighbouring lanes
+  // neighbouring numbers, the waves in turn (plans of 2048 and 34k pages 6.3 and 12.4 us;
+  // each wave the words that its lanes hold, 10.1 and 19.2)
   const uint32_t want = (uint32_t)(need_all < (unsigned)a.pg.pages ? need_all : (unsigned)a.pg.pages);
   uint32_t found = 0;
   for (int w0 = 0; w0 < words && found < want; w0 += kPlanTh) {
     const int w = w0 + tid;
-    const uint32_t bits = w < words ? a.pg.free_bits[w] : 0u;
+    const uint32_t bits = w0 == 0 ? bits0 : w < words ? a.pg.free_bits[w] : 0u;
     uint32_t total;
     const uint32_t r0 = found + plan_scan((uint32_t)__popc(bits), scratch32, turn++, &total);
     uint32_t left = 0;
@@ -200,25 +205,20 @@ __device__ __forceinline__ void make_plan_block(const PagesK& a) {
       for (uint32_t r = r0; r < want; ++r) left &= left - 1;
     }
     if (left != bits) a.pg.free_bits[w] = left;
-    const uint32_t taken = bits ^ left;
-    for (uint64_t live = __ballot(taken != 0); live != 0;) {
-      // two words at a time: lanes 0 .. 31 one, lanes 32 .. 63 the next
-      const int k0 = __ffsll((unsigned long long)live) - 1;
-      live &= live - 1;
-      const int k1 = live != 0 ? __ffsll((unsigned long long)live) - 1 : -1;
-      live &= live - 1;
-      const uint32_t b0 = __builtin_amdgcn_readlane(taken, k0), r_0 = __builtin_amdgcn_readlane(r0, k0);
-      const uint32_t b1 = k1 < 0 ? 0u : __builtin_amdgcn_readlane(taken, k1);
-      const uint32_t r_1 = k1 < 0 ? 0u : __builtin_amdgcn_readlane(r0, k1);
-      const uint32_t b = lane < 32 ? b0 : b1, r = lane < 32 ? r_0 : r_1;
-      const int k = lane < 32 ? k0 : k1, bit = lane & 31;
-      if (b >> bit & 1) a.ids[r + __popc(b & ((1u << bit) - 1))] = 32 * (w0 + (tid & ~63) + k) + bit;
+    taken_s[tid] = bits ^ left;
+    rank_s[tid] = r0;
+    __syncthreads();   // (read before the next scan's barrier)
+    const int here = min(words - w0, kPlanTh), bit = lane & 31;
+    for (int k = (tid >> 6) * 2 + (lane >> 5); k < here; k += kPlanTh / 32) {
+      const uint32_t t = taken_s[k];
+      if (t >> bit & 1) a.ids[rank_s[k] + __popc(t & ((1u << bit) - 1))] = 32 * (w0 + k) + bit;
     }
     found += total;
   }
   found = found < want ? found : want;
 
   // entries past the free pages are refused; lengths
+  int used = 0;
   for (int i = tid; i < a.entries; i += kPlanTh) {
     if (a.entries > kPlanTh) {
       j = a.jobs[i];
@@ -230,7 +230,7 @@ __device__ __forceinline__ void make_plan_block(const PagesK& a) {
         j.n1 = -1;
         st = GRKV_PAGES_FULL;
       } else {
-        atomicMax(&used_s, j.off + need);
+        used = max(used, j.off + need);
       }
     }
     if (j.n1 >= 0) a.pg.lens[j.dst] = j.n1;
@@ -239,6 +239,9 @@ __device__ __forceinline__ void make_plan_block(const PagesK& a) {
       if (a.status) a.status[i] = st;
     }
   }
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) used = max(used, __shfl_xor(used, k));
+  if (lane == 0 && used > 0) atomicMax(&used_s, used);
   __syncthreads();
   // pages taken for refused entries go back
   for (uint32_t r = used_s + tid; r < found; r += kPlanTh)
