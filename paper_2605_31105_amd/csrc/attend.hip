@@ -339,6 +339,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) all += acc[dt][rt][0] + acc[dt][rt][1] + acc[dt][rt][2] + acc[dt][rt][3];
   if (__syncthreads_or(all != all) && odd_values<E, D, PAGED>(a, sn, e, vt0, vt1, TK, sn.lim, sn.lo, trow)) {
+    if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);   // (not held until here)
     rows_by_key<E, D, PAGED>(a, sn, e, part, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
                              family, depth);
     return;
