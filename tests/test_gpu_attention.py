@@ -546,6 +546,9 @@ EVEN_CASES = [
     (BF, 128, 64, 4, 2, [60000, 70, 2], 5, 2048, 0, 0),
     (F32, 128, 16, 2, 3, [3, 400, 1000, 0], 270, 63, 0, 0),
     (F32, 64, 64, 5, 2, [2, 1234, 65], 250, 20, 300, 5),
+    (BF, 128, 64, 4, 32, [32, 2000, 0, 700, 31], 240, 140, 0, 0),
+    (BF, 64, 16, 2, 40, [41, 1500, 64, 90], 430, 94, 0, 0),
+    (BF, 128, 128, 9, 14, [14, 33000, 400], 7, 2400, 0, 0),
 ]
 
 
