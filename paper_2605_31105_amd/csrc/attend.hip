@@ -51,6 +51,8 @@ constexpr int kAtTh = 64 * kAtWaves;
 // whose splits end at different times, from 16 on (calls of 8 units of 32 rows: 1000 keys,
 // 4 splits, 13.7 us joined, 16.6 combined; 4000 keys, 16 splits, 18.4 and 16.5).
 constexpr int kJoinedSplits = 16, kJoinedRowSplits = 8, kJoinedBlocks = 512;
+// Logits of a call (rows by slots) from which the wide kernel is worth its blocks.
+constexpr int64_t kWideLogits = 1 << 20;
 // Units of any lengths are cut into equal parts (attend_even_kernel) where a part of the
 // longest would have 32 tiles or more (calls of 128 units of 500 to 8000 keys, bf16: 59 us,
 // with splits joined 64; 512 units 188, in four splits each 203, in one 228; 64 units of
@@ -616,11 +618,14 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   // two blocks per compute unit (32 units of 20k to 32k keys, 128 rows, 256 / 512 / 1024
   // blocks: 138 / 116 / 139 us; 300 units of 500 to 4000 keys, 64 rows, 512 / 2048: 168 / 180)
   constexpr int64_t target = 512;
-  if (bf16 && R > 64) {
+  // the wide kernel from 65 rows on, but for calls of few logits, which one launch of small
+  // blocks ends first (2 prompts of 564, 11.2 us beside 14.1; 2 units of 120 rows and 1000
+  // keys 13.9 and 16.7, 8 units of 128 rows and 2000 keys 20.9 and 19.1)
+  if (bf16 && R > 64 && entries * R * slots > kWideLogits) {
     p.rt = 0;
     p.rows = 128;
     p.tile_keys = kWideKeys;
-    p.min_tiles = 8;
+    p.min_tiles = 2;
   } else {
     // rows of a block: 32 read the keys half as often, 16 make twice the blocks and hold
     // twice the waves (32 rows of bf16 over 8000 keys, 16 / 32 rows a block: 24 units 36.3 /
@@ -637,7 +642,19 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   int64_t s = target / ((int64_t)entries * p.row_groups);
   s = s < most ? s : most;
   p.splits = 1;   // a power of two
-  while (2 * p.splits <= s && p.splits < 256) p.splits *= 2;
+  if (p.rt == 0) {
+    // a tile takes its block 1.35 us, a row's part 0.26 ns to write and read back, the launch
+    // that adds them 6 us.  (8 units of 128 rows and 2000 keys, 1 / 2 / 4 / 8 splits: 52 / 34 /
+    // 24 / 19 us; 8 prompts of 4 heads and 1000 positions, 1 / 2: 25 / 44; 100 units of 120
+    // rows and 300 keys 16 / 28)
+    auto cost = [&](int64_t n) {
+      return 1.35 * (double)((tiles + n - 1) / n) + (n > 1 ? 6 + 0.26e-3 * (double)(entries * R * n) : 0);
+    };
+    for (int n = 2; n <= s && n <= 256; n *= 2)
+      if (cost(n) < cost(p.splits)) p.splits = n;
+  } else {
+    while (2 * p.splits <= s && p.splits < 256) p.splits *= 2;
+  }
   const int64_t w = (int64_t)entries * p.splits;
   p.grouped = w % 8 == 0 || w >= 64;
   p.blocks = (p.grouped ? (w + 7) / 8 * 8 : w) * p.row_groups;

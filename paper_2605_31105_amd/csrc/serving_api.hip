@@ -106,7 +106,8 @@ int make_sink(const grkv_problem* prob, int64_t n, int32_t nq, int32_t window, i
   if (prob->head_dim != 64 && prob->head_dim != 128) return GRKV_ERR_UNSUPPORTED;
   if (!sizes_ok(prob->units, prob->group, nq, prob->head_dim)) return GRKV_ERR_INVALID;
   window = window_of(window, n);
-  const int64_t near = (int64_t)n_sink + window + nq;
+  // (a block's rows, 128 at most, lie at 128 / group + 2 positions or fewer)
+  const int64_t near = (int64_t)n_sink + window + (nq < 128 / prob->group + 2 ? nq : 128 / prob->group + 2);
   c->plan = attend_plan(prob->units, prob->group, nq, prob->head_dim, prob->dtype,
                         window > 0 && near < n ? near : n, false);
   if (c->plan.blocks >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
