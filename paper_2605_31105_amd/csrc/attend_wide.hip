@@ -1,12 +1,13 @@
 // Attention of many query rows over the keys of a unit (bf16): prompts and chunks
-// of them with a window and sinks, trees of drafted tokens with more than 64 rows.
+// of them with a window and sinks, trees of drafted tokens with more than 64 rows
+// (attend_plan in attend.hip says from where on).
 //
 // The sums are those of attend.hip; here the products and the exponentials bound
 // them, so the four waves of a block share tiles of 64 keys in LDS:
 //  * A wave holds 32 rows and forms, in one step, the weights of 64 keys beside the
 //    logits of the next 64, then P.V.  Two blocks share a compute unit, and the wave of
 //    the other one on its SIMD fills the gaps.  (8 units of 4 heads, a 16k prompt with a
-//    4k window: 1004 us beside 1374 of one wave of 64 rows per SIMD, which
+//    4k window: 955 to 1015 us beside 1374 of one wave of 64 rows per SIMD, which
 //    reads half as much LDS but waits for its own chain of logit, exponential and
 //    product.  One block of eight waves and 256 rows: 969, and with head_dim 64 476
 //    beside 402, since its waves meet at one barrier.)

@@ -549,6 +549,8 @@ EVEN_CASES = [
     (BF, 128, 64, 4, 32, [32, 2000, 0, 700, 31], 240, 140, 0, 0),
     (BF, 64, 16, 2, 40, [41, 1500, 64, 90], 430, 94, 0, 0),
     (BF, 128, 128, 9, 14, [14, 33000, 400], 7, 2400, 0, 0),
+    (BF, 128, 64, 4, 32, [32, 2000, 0, 700, 31], 240, 40, 300, 5),
+    (BF, 64, 32, 5, 30, [1500, 0, 64], 5, 1000, 900, 40),
 ]
 
 
@@ -615,3 +617,60 @@ def test_equal_parts_captured_and_values_that_are_not_finite():
                 check("entry %d" % e, eager[e, g].cpu()[clean], le[e, g].cpu()[clean], q[e, g, clean],
                       K[u][:n], V[u][:n], seen[clean])
                 assert u != 1 or torch.isnan(eager[e, g, 2, 7]).item()
+
+
+def _wide_table(pg, units, width):
+    table = torch.full((units + 1, width), -1, dtype=torch.int32, device="cuda")
+    table[:, :pg.table.shape[1]] = pg.table
+    return __import__("paper_2605_31105_amd").Pages(pg.k, pg.v, table, pg.lens, pg.refs, pg.free)
+
+
+@pytest.mark.parametrize("d,group,tokens,lens", [(64, 48, 6, [70, 6, 5]), (128, 16, 6, [90, 4000]),
+                                                 (128, 5, 40, [41, 300, 39, 1200])])
+def test_many_rows_and_siblings_that_are_not_finite(d, group, tokens, lens):
+    # tables long enough that calls of these rows are the wide kernel's
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + tokens)
+    pg, K, V = _pool(lens, 16, d, BF, gen)
+    pg = _wide_table(pg, len(lens), 1200)
+    assert len(lens) * group * tokens * 1200 * 16 > 1 << 20
+    parents, plist = _parents("tree", 1, tokens, gen)
+    q = torch.randn((len(lens), group, tokens, d), generator=gen).to(BF)
+    for value in (None, math.nan, math.inf):
+        where = [max(0, n - tokens) + 2 for n in lens]   # a drafted token of each unit
+        for u, slot in enumerate(where):
+            if value is not None:
+                pg.v[int(pg.table[u, slot // 16]), slot % 16, 3:9] = value
+        o, lse = (x.cpu() for x in G.tree_attention(q.cuda(), pg, parents, units=_i32(list(range(len(lens)))),
+                                                    return_lse=True))
+        for u, n in enumerate(lens):
+            seen = tree_seen(n, tokens, plist[0], 0, 0)
+            see = seen[:, where[u]] if value is not None else torch.zeros(tokens, dtype=torch.bool)
+            for g in range(0, group, 5):
+                check("unit %d head %d" % (u, g), o[u, g, ~see], lse[u, g, ~see], q[u, g, ~see], K[u], V[u], seen[~see])
+                assert not torch.isfinite(o[u, g, see, 3:9]).any()
+
+
+@pytest.mark.parametrize("d,window", [(64, 0), (128, 0), (128, 230)])
+def test_prompts_of_many_rows_with_values_that_are_not_finite(d, window):
+    # a NaN and an infinity among the values of keys 300 and 301: queries before them, and those
+    # whose window has passed them, are the finite prompt's
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + window)
+    n, group = 700, 3
+    q = torch.randn((2, group, n, d), generator=gen).to(BF)
+    K, V = (torch.randn((2, n, d), generator=gen).to(BF) for _ in range(2))
+    bad = V.clone()
+    bad[:, 300, 5], bad[:, 301, 6] = math.nan, -math.inf
+    assert 2 * group * n * (window + 48 if window else n) > 1 << 20   # (the wide kernel's)
+    seen = sink_seen(n, n, window, 4)
+    see = seen[:, 300] | seen[:, 301]
+    for values in (V, bad):
+        o, lse = (x.cpu() for x in G.sink_attention(q.cuda(), K.cuda(), values.cuda(), window, 4, return_lse=True))
+        ok = ~see if values is bad else torch.ones(n, dtype=torch.bool)
+        for u in range(2):
+            for g in range(group):
+                check("unit %d head %d" % (u, g), o[u, g, ok], lse[u, g, ok], q[u, g, ok], K[u], V[u], seen[ok])
+        if values is bad:
+            assert torch.isnan(o[:, :, seen[:, 300], 5]).all()
+            assert not torch.isfinite(o[:, :, seen[:, 301], 6]).any()
