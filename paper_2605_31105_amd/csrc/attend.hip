@@ -52,7 +52,7 @@ constexpr int kAtTh = 64 * kAtWaves;
 // 4 splits, 13.7 us joined, 16.6 combined; 4000 keys, 16 splits, 18.4 and 16.5).
 constexpr int kJoinedSplits = 16, kJoinedRowSplits = 8, kJoinedBlocks = 512;
 // Logits of a call (rows by slots) from which the wide kernel is worth its blocks.
-constexpr int64_t kWideLogits = 1 << 20;
+constexpr double kWideLogits = 1 << 20;
 // Units of any lengths are cut into equal parts (attend_even_kernel) where a part of the
 // longest would have 32 tiles or more (calls of 128 units of 500 to 8000 keys, bf16: 59 us,
 // with splits joined 64; 512 units 188, in four splits each 203, in one 228; 64 units of
@@ -621,7 +621,7 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   // the wide kernel from 65 rows on, but for calls of few logits, which one launch of small
   // blocks ends first (2 prompts of 564, 11.2 us beside 14.1; 2 units of 120 rows and 1000
   // keys 13.9 and 16.7, 8 units of 128 rows and 2000 keys 20.9 and 19.1)
-  if (bf16 && R > 64 && entries * R * slots > kWideLogits) {
+  if (bf16 && R > 64 && (double)entries * (double)R * (double)slots > kWideLogits) {
     p.rt = 0;
     p.rows = 128;
     p.tile_keys = kWideKeys;
