@@ -493,7 +493,9 @@ typedef struct {
 
 /* q, o: pages' dtype [entries][group][tokens][head_dim], 16-byte aligned; lse float
  * [entries][group][tokens] or NULL; neither may overlap q, the pool or another array of the
- * call.  A logit's weight is rounded to bf16 over bf16 values; sums are float32.  The length of a unit is read on the device.  Errors:
+ * call.  Over bf16 values a weight is held to 2^-16 of it where memory bounds a call (up to 64
+ * rows, group * tokens, a unit, and small calls of more) and rounded to bf16 (2^-8) in the others;
+ * sums are float32.  The length of a unit is read on the device.  Errors:
  * those of the calls on pages; GRKV_ERR_INVALID for bad counts in `tree` (also
  * entries * group * tokens * head_dim >= 2^40); GRKV_ERR_UNSUPPORTED for
  * tokens > 64. */

@@ -310,8 +310,8 @@ __device__ __forceinline__ RowSight row_sight(const AttendK& a, int base, int i,
 }
 
 // Whether a tile of vt0 .. vt1 - 1 that is not seen whole (by every row before lim and
-// from lo on) holds an infinity or NaN among its values.  One wave; asked only where
-// an output is NaN.
+// from lo on; lim 0: any tile) holds an infinity or NaN among its values.  One wave; asked
+// only where an output is NaN.
 template <typename E, int D, bool PAGED>
 __device__ __forceinline__ bool odd_values(const AttendK& a, const Span& sn, int e, int vt0, int vt1,
                                            int tk, int lim, int lo, const int32_t* trow) {
@@ -336,9 +336,9 @@ __device__ __forceinline__ bool odd_values(const AttendK& a, const Span& sn, int
   return __any(odd);
 }
 
-// Rows of a split once more, key by key: taken where a tile that some rows see
-// only part of holds an infinity or NaN among its values, since 0 x inf in a
-// product reaches the rows that do not see it (as NaN).  One wave; rows first ..
+// Rows of a split once more, key by key and with float32 weights: taken where an infinity
+// or NaN among the values of a tile may have reached rows that do not see it, since 0 x inf
+// in a product is NaN (see odd_values).  One wave; rows first ..
 // first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn, left as partial rows
 // from `part` on or (part < 0) as outputs.  A lane forms the weight of one key of 64, then
 // sums D / 64 columns.
@@ -365,7 +365,7 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
     const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
     if (i >= t) continue;
     const E* q = (const E*)a.q + at * D;
-    float m = -kUnset, l = 0.f, lx = 0.f, o[C] = {};
+    float m = -kUnset, l = 0.f, o[C] = {};
     for (int vt = vt0; vt < vt1; ++vt) {
       const int slot0 = (vt < sn.at ? vt : vt - sn.at + sn.bt) * tk;
       for (int j0 = slot0; j0 < slot0 + tk; j0 += 64) {
@@ -384,21 +384,14 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
           const float f = __builtin_amdgcn_exp2f(m - mx);
           m = mx;
           l *= f;
-          lx *= f;
           for (int c = 0; c < C; ++c) o[c] *= f;
         }
         const float w = on ? __builtin_amdgcn_exp2f(x - m) : 0.f;
-        float wr = w;
-        if constexpr (BF) wr = (float)(__bf16)w;
-        float s = w, sr = wr;
-        for (int k = 1; k < 64; k <<= 1) {
-          s += __shfl_xor(s, k);
-          sr += __shfl_xor(sr, k);
-        }
-        lx += s;
-        l += sr;
+        float s = w;
+        for (int k = 1; k < 64; k <<= 1) s += __shfl_xor(s, k);
+        l += s;
         for (int k = 0; k < 64; ++k) {
-          const float wk = __shfl(wr, k);
+          const float wk = __shfl(w, k);
           if (!__shfl((int)on, k)) continue;
           const E* v = (const E*)a.v + slot_row(j0 + k) * D;
           for (int c = 0; c < C; ++c) o[c] = fmaf(wk, value(v[64 * c + lane]), o[c]);
@@ -409,7 +402,7 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
       const size_t to = part + r;
       for (int c = 0; c < C; ++c)
         __hip_atomic_store(a.opart + to * D + 64 * c + lane, o[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (lane == 0) put4((float*)(a.mpart + to), (f32x4){m, l, lx, 0.f}, true);
+      if (lane == 0) put4((float*)(a.mpart + to), (f32x4){m, l, l, 0.f}, true);
     } else {
       const float inv = l == 0.f ? 0.f : 1.f / l;
       for (int c = 0; c < C; ++c) {
@@ -417,7 +410,7 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
         if constexpr (BF) *reinterpret_cast<__bf16*>(to) = (__bf16)(o[c] * inv);
         else *to = o[c] * inv;
       }
-      if (lane == 0 && a.lse) a.lse[at] = lx == 0.f ? -__builtin_huge_valf() : (m + __log2f(lx)) * kLn2;
+      if (lane == 0 && a.lse) a.lse[at] = l == 0.f ? -__builtin_huge_valf() : (m + __log2f(l)) * kLn2;
     }
   }
 }

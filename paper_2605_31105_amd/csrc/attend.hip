@@ -24,14 +24,16 @@
 //  * The reference of a row moves only when a logit exceeds it by 2^40: float32
 //    sums (and bf16 P) lose nothing by a reference that is too low, so most
 //    tiles need no exchange between lanes.
-//  * P is rounded to bf16 for the product with bf16 values, and o divided by the
-//    sum of the rounded weights (an MFMA with ones), so the weights of a row add
-//    up to one and a row of a single key is exact; the sum behind lse is of the
-//    weights before the rounding.
+//  * Over bf16 values P enters the product in two bf16 parts, itself rounded and what the
+//    rounding left, so that a weight is off by 2^-16 of it instead of 2^-8: memory bounds
+//    these calls, and the second product costs them 0 to 5% (one token over 512 ragged
+//    units 188.0 -> 189.0 us, over 8 of 128k 93.4 -> 94.8, 64 units of 32 rows 74.3 -> 76.6,
+//    300 of 64 rows 162 -> 170).
 //  * Tiles that every row sees whole skip the masks.  In the others an entry
 //    that a row does not see has weight zero.  An infinity or NaN among the values of
-//    such a tile reaches those rows all the same, as NaN (0 x inf); where a sum is
-//    NaN and such a tile is the cause, the block does its rows again key by key.
+//    such a tile reaches those rows all the same, as NaN (0 x inf), and over bf16 values
+//    an infinity makes a NaN of any row, whose second parts have both signs; where a sum is
+//    NaN and such a value is the cause, the block does its rows again key by key.
 // Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
 #include "attend.h"
 
@@ -99,7 +101,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
 
   __shared__ __attribute__((aligned(16))) char v0_s[kAtWaves * VB];
   __shared__ __attribute__((aligned(16))) char v1_s[kAtWaves * VB];
-  __shared__ float m_s[kAtWaves][16 * RT], l_s[kAtWaves][16 * RT], x_s[kAtWaves][16 * RT];
+  __shared__ float m_s[kAtWaves][16 * RT], l_s[kAtWaves][16 * RT];
 
   // (what follows from it is formed anew for each unit of a block's part, not held over that
   // loop: float32 of 128 columns in 213 registers instead of 254 and spills, 300 units of
@@ -157,13 +159,12 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     return ((size_t)e * a.n + (slot & ~15)) * RB;
   };
 
-  f32x4 acc[DT][RT], accl[RT];
-  float nref[RT], sum[RT];   // sum: this lane's weights before their rounding
+  f32x4 acc[DT][RT];
+  float nref[RT], sum[RT];   // sum: this lane's weights
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     nref[rt] = kUnset;
     sum[rt] = 0.f;
-    accl[rt] = zero4();
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt][rt] = zero4();
   }
@@ -256,7 +257,6 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
         if (!(fmaf(m4, a.scale_log2, nref[rt]) <= kMoveAt) && m4 > -__builtin_huge_valf()) {
           const float f = __builtin_amdgcn_exp2f(-nref[rt] - m4 * a.scale_log2);
           nref[rt] = -(m4 * a.scale_log2);
-          accl[rt] *= f;
           sum[rt] *= f;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) acc[dt][rt] *= f;
@@ -289,7 +289,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
       const int row = 4 * gq + i, ch = 4 * dt + (l16 >> 2);
       return *reinterpret_cast<const float*>(vs + (row * CPR + (ch ^ swz(row))) * 16 + 4 * (l16 & 3));
     };
-    bf16x8 p[RT];
+    bf16x8 p[RT], pl[RT];   // a weight in two parts, so that its rounding is 2^-16 of it
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       if constexpr (BF) {
@@ -297,11 +297,15 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
-            const bf16x2 h = __builtin_convertvector((f32x2){s[kt][rt][i], s[kt][rt][i + 1]}, bf16x2);
+            const f32x2 w = {s[kt][rt][i], s[kt][rt][i + 1]};
+            const bf16x2 h = __builtin_convertvector(w, bf16x2);
+            const f32x2 r = {w[0] - (float)h[0], w[1] - (float)h[1]};
+            const bf16x2 l = __builtin_convertvector(r, bf16x2);
             p[rt][4 * kt + i] = h[0];
             p[rt][4 * kt + i + 1] = h[1];
+            pl[rt][4 * kt + i] = l[0];
+            pl[rt][4 * kt + i + 1] = l[1];
           }
-        accl[rt] = mfma_bf16(as_bf16x8(make_uint4(kOnes, kOnes, kOnes, kOnes)), p[rt], accl[rt]);
       }
     }
 #pragma unroll
@@ -310,6 +314,8 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
         const bf16x8 vf = frag(dt);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) acc[dt][rt] = mfma_bf16(vf, p[rt], acc[dt][rt]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[dt][rt] = mfma_bf16(vf, pl[rt], acc[dt][rt]);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -345,7 +351,10 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) all += acc[dt][rt][0] + acc[dt][rt][1] + acc[dt][rt][2] + acc[dt][rt][3];
-  if (__syncthreads_or(all != all) && odd_values<E, D, PAGED>(a, sn, e, vt0, vt1, TK, sn.lim, sn.lo, trow)) {
+  // (over bf16 values in tiles that every row sees whole too, since a second part may be zero
+  // or negative)
+  if (__syncthreads_or(all != all) &&
+      odd_values<E, D, PAGED>(a, sn, e, vt0, vt1, TK, BF ? 0 : sn.lim, sn.lo, trow)) {
     if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);   // (not held until here)
     rows_by_key<E, D, PAGED>(a, sn, e, part, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
                              family, depth);
@@ -357,8 +366,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     sum[rt] += __shfl_xor(sum[rt], 32);
     if (gq == 0) {
       m_s[wave][16 * rt + l16] = -nref[rt];
-      l_s[wave][16 * rt + l16] = BF ? accl[rt][0] : sum[rt];   // (float32 weights are not rounded)
-      x_s[wave][16 * rt + l16] = sum[rt];
+      l_s[wave][16 * rt + l16] = sum[rt];
     }
   }
   __syncthreads();
@@ -379,7 +387,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     const int row = c / CR, ch = c % CR, r = r0 + row;
     const int i = group_of(a, r), g = r - i * a.group;
     if (r >= R || i >= t) continue;
-    float m = m_s[0][row], l = 0.f, lx = 0.f;
+    float m = m_s[0][row], l = 0.f;
 #pragma unroll
     for (int w = 1; w < kAtWaves; ++w) m = fmaxf(m, m_s[w][row]);
     f32x4 x = zero4();
@@ -387,16 +395,15 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     for (int w = 0; w < kAtWaves; ++w) {
       const float f = __builtin_amdgcn_exp2f(m_s[w][row] - m);
       l += l_s[w][row] * f;
-      lx += x_s[w][row] * f;
       x += *reinterpret_cast<const f32x4*>((w < 2 ? v0_s : v1_s) + (w & 1) * 2 * VB + row * D * 4 +
                                            ((ch ^ (row & 15)) << 4));
     }
     if (part >= 0) {
       put4(a.opart + (part + r) * D + 4 * ch, x, shared);
-      if (ch == 0) put4((float*)(a.mpart + part + r), (f32x4){m, l, lx, 0.f}, shared);
+      if (ch == 0) put4((float*)(a.mpart + part + r), (f32x4){m, l, l, 0.f}, shared);
     } else {
       const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
-      write_out<E, D>(a, at, ch, x, m, l, lx);
+      write_out<E, D>(a, at, ch, x, m, l, l);
     }
   }
 }

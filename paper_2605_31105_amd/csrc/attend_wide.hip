@@ -18,7 +18,13 @@
 //    P^T already is the B operand of O^T = V^T P^T.
 //  * References, rounding and values that are not finite: as in attend.hip, but that
 //    a step looks for a row's largest logit only where its sum of weights passes 2^40.
-//    The sum of the rounded weights comes from the dot product with ones.
+//  * P is rounded to bf16 (2^-8 of a weight), and o divided by the sum of the rounded weights
+//    (dot products with ones), so that the weights of a row add up to one; lse comes from
+//    the sum before the rounding.  A second product with what the rounding leaves, as in
+//    attend.hip, would cost what bounds these calls: a 16k prompt with a 4k window 995 -> 1300
+//    us (head_dim 64 595 -> 790), trees of 32 over 32k keys 109 -> 123, 8 prompts of 1000 25.3
+//    -> 29.6.  (The error of o against 64 bits, rounded to bf16 as it is, falls from 0.0022
+//    to 0.0017 of its norm.)
 #include "attend.h"
 
 namespace grkv {
