@@ -346,14 +346,21 @@ __global__ __launch_bounds__(kPlanTh) void plan_append_kernel(PagesK a, RowMap m
   append_rows<false, T>(a, m, k, v, threadIdx.x / cpr, kPlanTh / cpr);
 }
 
+// The slot of row `row` behind the first `first` rows of a unit that has n1 after the call
+// (-1 where it is refused), or -1.  `row` may come near 2^31, as a call's rows are only a bound
+// on its counts, so it is compared before it is added.
+__device__ __forceinline__ int new_slot(int first, int row, int n1) {
+  return row < n1 - first ? first + row : -1;
+}
+
 // Slot `row` of the new pages of a fork or a compaction, read through the old
 // table; this thread's 16 bytes of K and V at column c.
 template <typename T>
 __device__ __forceinline__ void move_row(const PagesK& a, const PageJob& j, int e, int row, int c,
                                          const int32_t* idx) {
   const int d = a.pg.head_dim, mask = (1 << a.shift) - 1;
-  const int slot = (j.first << a.shift) + row;
-  if (slot >= j.n1) return;
+  const int slot = new_slot(j.first << a.shift, row, j.n1);
+  if (slot < 0) return;
   int from = slot;
   if (slot >= j.keep) from = idx[j.start + (slot - j.keep)];
   u32x4 rk = {0, 0, 0, 0}, rv = rk;
