@@ -458,7 +458,8 @@ size_t grkv_pages_workspace_bytes(const grkv_pages* pages, int32_t entries);
 /* All of these are asynchronous on stream, allocate nothing and may be captured.
  * Errors: GRKV_ERR_INVALID for null pointers, misaligned k, v or workspace, sizes out of
  * range (pages, units, max_pages < 1, pages > 2^30, max_pages * page_size > 2^30, entries or
- * rows < 0, entries * (rows + page_size) >= 2^31), an unknown dtype;
+ * rows < 0, entries * (rows + page_size) >= 2^31, 2^24 entries or more of a fork, a compaction
+ * or a free), an unknown dtype;
  * GRKV_ERR_UNSUPPORTED for another head_dim or page_size;
  * GRKV_ERR_WORKSPACE; GRKV_ERR_HIP. */
 
@@ -497,8 +498,8 @@ typedef struct {
  * rows, group * tokens, a unit, and small calls of more) and rounded to bf16 (2^-8) in the others;
  * sums are float32.  The length of a unit is read on the device.  Errors:
  * those of the calls on pages; GRKV_ERR_INVALID for bad counts in `tree` (also
- * entries * group * tokens * head_dim >= 2^40); GRKV_ERR_UNSUPPORTED for
- * tokens > 64. */
+ * entries * group * tokens * head_dim >= 2^40, and 2^24 blocks or more: entries times the row
+ * groups of a unit, of 16 rows at least); GRKV_ERR_UNSUPPORTED for tokens > 64. */
 int grkv_tree_attention(const void* q, const grkv_pages* pages, const grkv_tree* tree, void* o,
                         float* lse, void* stream, void* workspace, size_t workspace_bytes);
 
@@ -513,8 +514,8 @@ size_t grkv_tree_attention_workspace_bytes(const grkv_pages* pages, const grkv_t
  *   lse      float [U][G][nq], or NULL
  * all 16-byte aligned; o and lse as in grkv_tree_attention.  Errors:
  * GRKV_ERR_INVALID (null pointers, nq outside 1 .. n, n > 2^30, window or n_sink
- * < 0, units or group < 1, an unknown dtype, U * G * nq * d >= 2^40),
- * GRKV_ERR_UNSUPPORTED (head_dim), GRKV_ERR_WORKSPACE, GRKV_ERR_HIP. */
+ * < 0, units or group < 1, an unknown dtype, U * G * nq * d >= 2^40, 2^24 blocks or
+ * more as above), GRKV_ERR_UNSUPPORTED (head_dim), GRKV_ERR_WORKSPACE, GRKV_ERR_HIP. */
 int grkv_sink_attention(const void* q, const void* K, const void* V, int64_t n, int32_t nq,
                         int32_t window, int32_t n_sink, void* stream, const grkv_problem* prob,
                         void* o, float* lse, void* workspace, size_t workspace_bytes);

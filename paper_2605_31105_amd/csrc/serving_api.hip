@@ -8,6 +8,9 @@ namespace {
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+// Blocks of 256 threads in a launch, which has fewer than 2^32 threads.
+constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
+
 // Rows and elements of q within the kernels' indices.
 bool sizes_ok(int64_t entries, int64_t group, int64_t tokens, int64_t d) {
   return group * tokens < (int64_t(1) << 30) &&
@@ -75,7 +78,7 @@ int make_tree(const grkv_pages* pg, const grkv_tree* tr, TreeCall* c) {
   const int64_t near = (int64_t)tr->n_sink + window + tr->tokens;
   c->plan = attend_plan(tr->entries > 0 ? tr->entries : 1, tr->group, tr->tokens, pg->head_dim,
                         pg->dtype, window > 0 && near < cap ? near : cap, window == 0);
-  if (c->plan.blocks >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
+  if (c->plan.blocks > kMostBlocks) return GRKV_ERR_INVALID;
   AttendK& a = c->a;
   a = AttendK{};
   a.k = pg->k;
@@ -110,7 +113,7 @@ int make_sink(const grkv_problem* prob, int64_t n, int32_t nq, int32_t window, i
   const int64_t near = (int64_t)n_sink + window + (nq < 128 / prob->group + 2 ? nq : 128 / prob->group + 2);
   c->plan = attend_plan(prob->units, prob->group, nq, prob->head_dim, prob->dtype,
                         window > 0 && near < n ? near : n, false);
-  if (c->plan.blocks >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
+  if (c->plan.blocks > kMostBlocks) return GRKV_ERR_INVALID;
   AttendK& a = c->a;
   a = AttendK{};
   a.entries = prob->units;
@@ -178,6 +181,7 @@ int grkv_pages_fork(const grkv_pages* pages, const grkv_page_entries* entries, c
   int st = check_entries(pages, entries, false);
   if (st != GRKV_OK) return st;
   if ((int64_t)entries->entries * pages->page_size >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
+  if (entries->entries > kMostBlocks) return GRKV_ERR_INVALID;
   if (entries->entries > 0 && !dst) return GRKV_ERR_INVALID;
   st = check_workspace(pages, entries, workspace, workspace_bytes);
   if (st != GRKV_OK) return st;
@@ -195,6 +199,7 @@ int grkv_pages_compact(const grkv_pages* pages, const grkv_page_entries* entries
                        void* workspace, size_t workspace_bytes) {
   int st = check_entries(pages, entries, true);
   if (st != GRKV_OK) return st;
+  if (entries->entries > kMostBlocks) return GRKV_ERR_INVALID;
   if (entries->entries > 0 && entries->rows > 0 && entries->source_rows > 0 && !idx)
     return GRKV_ERR_INVALID;
   st = check_workspace(pages, entries, workspace, workspace_bytes);
@@ -213,6 +218,7 @@ int grkv_pages_compact(const grkv_pages* pages, const grkv_page_entries* entries
 int grkv_pages_free(const grkv_pages* pages, const grkv_page_entries* entries, void* stream) {
   const int st = check_entries(pages, entries, false);
   if (st != GRKV_OK) return st;
+  if (entries->entries > kMostBlocks) return GRKV_ERR_INVALID;
   PagesCall c = {};
   c.op = kPagesFree;
   c.pages = pages;

@@ -111,3 +111,18 @@ def test_the_reference_masks_by_hand():
     q, K = torch.eye(2, 64) * 8, torch.eye(2, 64)
     o, lse, _, _ = rows(q, K, K * 3, torch.tensor([[T, F], [F, F]]), False)
     assert o[0, 0] == 3 and not o[1].any() and abs(lse[0] - 1) < 1e-12 and lse[1] == float("-inf")
+
+
+def test_calls_of_more_blocks_than_a_launch_has(L):
+    # a launch has fewer than 2^32 threads, and a block 256: known from the sizes alone
+    most = (1 << 24) - 8
+    assert G.sink_attention_workspace_bytes(most, 1, 64, 0, 1, 1, 0, 0) == 256
+    assert G.sink_attention_workspace_bytes(1 << 24, 1, 64, 0, 1, 1, 0, 0) == 0
+    assert G.sink_attention_workspace_bytes(1 << 21, 1, 64, 1, 128, 128, 0, 0) == 0   # 8 row groups each
+    pg = _pool()
+    assert L.grkv_tree_attention_workspace_bytes(pg, _tree(entries=most, group=1)) == 256
+    for kw in (dict(entries=1 << 24, group=1), dict(entries=1 << 22, group=64, tokens=8)):
+        assert L.grkv_tree_attention_workspace_bytes(pg, _tree(**kw)) == 0
+        assert L.grkv_tree_attention(4096, pg, _tree(**kw), 4096, None, None, 4096, 1 << 40) == INV
+    prob = G.Problem(1 << 24, 1, 64, 0)
+    assert L.grkv_sink_attention(4096, 4096, 4096, 1, 1, 0, 0, None, prob, 4096, None, 4096, 1 << 40) == INV

@@ -96,3 +96,18 @@ def test_binding_refuses_host_tensors():
         G.new_pages(1, 1, 1, 16, 64, device="cpu")
     with pytest.raises(ValueError):
         G.new_pages(0, 1, 1, 16, 64, device="cpu")
+
+
+def test_calls_of_more_entries_than_a_launch_has_blocks(L):
+    # fork, compact and free are a block per entry, of 256 threads of a launch's 2^32: refused
+    # on the host, before the plan changes the pool
+    pg, ws = _pool(page_size=16), 1 << 40
+    for n, code in (((1 << 24) - 1, WS), (1 << 24, INV), (3 << 24, INV)):
+        en = _entries(entries=n, rows=1, source_rows=n)
+        size = 256 if code == WS else ws   # (below the limit the workspace is what is refused)
+        assert L.grkv_pages_fork(pg, en, 4096, None, 4096, size) == code
+        assert L.grkv_pages_compact(pg, en, None, 4096, 4096, None, 4096, size) == code
+        if code == INV:
+            assert L.grkv_pages_free(pg, en, None) == code
+    assert L.grkv_pages_append(pg, _entries(entries=1 << 25, rows=1, source_rows=1 << 25), 4096, 0, 4096, 0, None, 4096,
+                               256) == WS
