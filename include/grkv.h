@@ -496,7 +496,7 @@ typedef struct {
  * [entries][group][tokens] or NULL; neither may overlap q, the pool or another array of the
  * call.  Over bf16 values a weight is held to 2^-16 of it where memory bounds a call (up to 64
  * rows, group * tokens, a unit, and small calls of more) and rounded to bf16 (2^-8) in the others;
- * sums are float32.  The length of a unit is read on the device.  Errors:
+ * sums are float32, of weights of 1 at most.  The length of a unit is read on the device.  Errors:
  * those of the calls on pages; GRKV_ERR_INVALID for bad counts in `tree` (also
  * entries * group * tokens * head_dim >= 2^40, and 2^24 blocks or more: entries times the row
  * groups of a unit, of 16 rows at least); GRKV_ERR_UNSUPPORTED for tokens > 64. */

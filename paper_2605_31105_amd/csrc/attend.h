@@ -8,8 +8,17 @@
 namespace grkv {
 
 constexpr float kUnset = 3e38f;      // minus the reference of a row without one
-constexpr float kMoveAt = 40.f;      // log2 of the largest weight before a move
-constexpr float kMoveSum = 0x1p40f;  // the largest sum of a step's weights before one
+// The reference of a row, by kernel.  Few rows (attend.hip): it is set this much (log2) above
+// the largest logit so far and moves when a logit passes it, so that no weight is above 1 and
+// sums hold whatever those against the largest logit would, values near a float's largest
+// included.
+constexpr float kRefAbove = 8.f;
+// Many rows (attend_wide.hip): it is the largest logit and moves where a step's weights of a
+// lane sum to more than this.  Values past 2^128 / 2^16 / keys may then overflow, and are summed
+// again (rows_by_key).  (A reference set above the logits there takes two registers more, 170
+// of head_dim 64, where 168 leave room for a third wave: a 16k prompt with a 4k window 577 ->
+// 630 us.)
+constexpr float kMoveSum = 0x1p16f;
 constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -309,36 +318,10 @@ __device__ __forceinline__ RowSight row_sight(const AttendK& a, int base, int i,
   return s;
 }
 
-// Whether a tile of vt0 .. vt1 - 1 that is not seen whole (by every row before lim and
-// from lo on; lim 0: any tile) holds an infinity or NaN among its values.  One wave; asked
-// only where an output is NaN.
-template <typename E, int D, bool PAGED>
-__device__ __forceinline__ bool odd_values(const AttendK& a, const Span& sn, int e, int vt0, int vt1,
-                                           int tk, int lim, int lo, const int32_t* trow) {
-  const int lane = threadIdx.x & 63;
-  bool odd = false;
-  for (int vt = vt0; vt < vt1; ++vt) {
-    const int slot0 = (vt < sn.at ? vt : vt - sn.at + sn.bt) * tk;
-    if (slot0 + tk <= lim && (slot0 >= lo || slot0 + tk <= a.n_sink)) continue;
-    for (int j = slot0; j < slot0 + tk && j < sn.kend; ++j) {
-      size_t row = (size_t)e * a.n + j;
-      if (PAGED) {
-        const int p = trow[j >> a.shift];
-        row = ((size_t)((unsigned)p < (unsigned)a.pages ? p : 0) << a.shift) + (j & ((1 << a.shift) - 1));
-      }
-      for (int c = lane; c < D; c += 64) {
-        const E x = ((const E*)a.v)[row * D + c];
-        if constexpr (sizeof(E) == 2) odd |= (x & 0x7f80) == 0x7f80;
-        else odd |= (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
-      }
-    }
-  }
-  return __any(odd);
-}
-
-// Rows of a split once more, key by key and with float32 weights: taken where an infinity
-// or NaN among the values of a tile may have reached rows that do not see it, since 0 x inf
-// in a product is NaN (see odd_values).  One wave; rows first ..
+// Rows of a split once more, key by key, with float32 weights against the largest logit:
+// taken where a sum of values is not finite, though its weights' is.  An infinity or NaN
+// among the values may be one that the row does not see (0 x inf in a product is NaN), or
+// large values may have overflowed under a reference that was too low.  One wave; rows first ..
 // first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn, left as partial rows
 // from `part` on or (part < 0) as outputs.  A lane forms the weight of one key of 64, then
 // sums D / 64 columns.

@@ -21,19 +21,19 @@
 //    order of the keys inside a tile is free as long as V^T uses the same), so P
 //    never leaves the registers.  V^T comes from the row-major tile by the LDS
 //    transpose read.
-//  * The reference of a row moves only when a logit exceeds it by 2^40: float32
-//    sums (and bf16 P) lose nothing by a reference that is too low, so most
-//    tiles need no exchange between lanes.
+//  * The reference of a row is set 2^8 above its largest logit and moves only when a
+//    logit passes it, so most tiles need no exchange between lanes.  No weight is above 1,
+//    so large values (finite ones up to the type's largest) do not overflow the sums.
 //  * Over bf16 values P enters the product in two bf16 parts, itself rounded and what the
 //    rounding left, so that a weight is off by 2^-16 of it instead of 2^-8: memory bounds
 //    these calls, and the second product costs them 0 to 5% (one token over 512 ragged
 //    units 188.0 -> 189.0 us, over 8 of 128k 93.4 -> 94.8, 64 units of 32 rows 74.3 -> 76.6,
 //    300 of 64 rows 162 -> 170).
 //  * Tiles that every row sees whole skip the masks.  In the others an entry
-//    that a row does not see has weight zero.  An infinity or NaN among the values of
-//    such a tile reaches those rows all the same, as NaN (0 x inf), and over bf16 values
-//    an infinity makes a NaN of any row, whose second parts have both signs; where a sum is
-//    NaN and such a value is the cause, the block does its rows again key by key.
+//    that a row does not see has weight zero.  An infinity or NaN among the values
+//    reaches rows all the same, as NaN (0 x inf; over bf16 values also where it is seen,
+//    beside second parts of both signs); where a sum of values is not finite
+//    and that of its weights is, the block does its rows again key by key.
 // Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
 #include "attend.h"
 
@@ -248,15 +248,16 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx[rt] = fmaxf(mx[rt], s[kt][rt][i]);
-      moved |= !(fmaf(mx[rt], a.scale_log2, nref[rt]) <= kMoveAt);
+      moved |= !(fmaf(mx[rt], a.scale_log2, nref[rt]) <= 0.f);
     }
     if (__any(moved)) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const float m4 = max_over_groups(mx[rt]);
-        if (!(fmaf(m4, a.scale_log2, nref[rt]) <= kMoveAt) && m4 > -__builtin_huge_valf()) {
-          const float f = __builtin_amdgcn_exp2f(-nref[rt] - m4 * a.scale_log2);
-          nref[rt] = -(m4 * a.scale_log2);
+        if (!(fmaf(m4, a.scale_log2, nref[rt]) <= 0.f) && m4 > -__builtin_huge_valf()) {
+          const float ref = fmaf(m4, a.scale_log2, kRefAbove);
+          const float f = __builtin_amdgcn_exp2f(-nref[rt] - ref);
+          nref[rt] = -ref;
           sum[rt] *= f;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) acc[dt][rt] *= f;
@@ -346,15 +347,19 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
   wait_vmcnt<0>();
-  float all = 0.f;   // NaN if one of the wave's sums is
+  bool odd = false;   // a sum of values is not finite, though its weights' is
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+  for (int rt = 0; rt < RT; ++rt) {
+    sum[rt] += __shfl_xor(sum[rt], 16);
+    sum[rt] += __shfl_xor(sum[rt], 32);
+    float z = 0.f;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) all += acc[dt][rt][0] + acc[dt][rt][1] + acc[dt][rt][2] + acc[dt][rt][3];
-  // (over bf16 values in tiles that every row sees whole too, since a second part may be zero
-  // or negative)
-  if (__syncthreads_or(all != all) &&
-      odd_values<E, D, PAGED>(a, sn, e, vt0, vt1, TK, BF ? 0 : sn.lim, sn.lo, trow)) {
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z = fmaf(acc[dt][rt][i], 0.f, z);
+    odd |= z != z && sum[rt] == sum[rt];
+  }
+  if (__syncthreads_or(odd)) {
     if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);   // (not held until here)
     rows_by_key<E, D, PAGED>(a, sn, e, part, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
                              family, depth);
@@ -362,8 +367,6 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    sum[rt] += __shfl_xor(sum[rt], 16);
-    sum[rt] += __shfl_xor(sum[rt], 32);
     if (gq == 0) {
       m_s[wave][16 * rt + l16] = -nref[rt];
       l_s[wave][16 * rt + l16] = sum[rt];

@@ -17,7 +17,7 @@
 //  * 32x32x16 MFMAs: S^T = K Q^T leaves a query row in each lane column, where
 //    P^T already is the B operand of O^T = V^T P^T.
 //  * References, rounding and values that are not finite: as in attend.hip, but that
-//    a step looks for a row's largest logit only where its sum of weights passes 2^40.
+//    a step looks for a row's largest logit only where its sum of weights passes 2^16.
 //  * P is rounded to bf16 (2^-8 of a weight), and o divided by the sum of the rounded weights
 //    (dot products with ones), so that the weights of a row add up to one; lse comes from
 //    the sum before the rounding.  A second product with what the rounding leaves, as in
@@ -290,13 +290,13 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   ring_barrier<0>();   // (the ring is the output's buffer now)
   sum += __shfl_xor(sum, 32);
   rsum += __shfl_xor(rsum, 32);
-  float all = 0.f;   // NaN if one of the wave's sums is
+  float odd = 0.f;   // NaN if a sum of values is not finite
 #pragma unroll
   for (int dm = 0; dm < DM; ++dm)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) all += acc[dm][r];
+    for (int r = 0; r < 16; ++r) odd = fmaf(acc[dm][r], 0.f, odd);
   const int64_t part = ((int64_t)e * a.splits + sp) * R;
-  if (__any(all != all) && odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, lim, lo, trow)) {
+  if (__any(odd != odd && sum == sum)) {
     if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);   // (not held until here)
     rows_by_key<u16, D, PAGED>(a, sn, e, sn.ns > 1 ? part : -1, w0, 32, vt0, vt1, TK, len, t, trow, family, depth);
     return;

@@ -1,8 +1,8 @@
 """Attention where its number format shows: weights held to 2^-16 of them, values whose outputs
-cancel."""
+cancel, values near a float's largest."""
 import pytest
 
-from tests.attention_ref import rows, sink_seen, tree_seen
+from tests.attention_ref import check, rows, sink_seen, tree_seen
 from tests.test_gpu_attention import BF, F32, _i32, _parents, _pool, _wide_table
 
 pytestmark = pytest.mark.gpu
@@ -87,3 +87,74 @@ def test_infinities_that_every_row_sees_stay_infinities():
             for g in range(4):
                 want, wl, tol, _ = rows(q[u, g], K[u], torch.nan_to_num(V[u].float(), 0, 0, 0), seen, dtype == BF)
                 assert ((o[u, g].double() - want).abs() <= tol)[:, rest].all()
+
+
+def _ramp(q, K, V, lo, hi):
+    """Logits that rise along the keys from lo to hi (log2), values of 1e36 and random signs."""
+    d, n = K.shape[-1], K.shape[-2]
+    q[..., :2] = torch.tensor([8.0, 0.0])
+    K[..., 0] = torch.linspace(lo, hi, n) * d ** 0.5 / 1.4426950408889634 / 8
+    K[..., 2:] *= 0.1
+    V *= 1e36
+
+
+@pytest.mark.parametrize("dtype,d,group,t,lens,entries,width", [
+    (BF, 128, 4, 1, [300, 40], 2, 5), (BF, 64, 2, 3, [900, 33], 2, 20), (F32, 128, 4, 2, [500], 1, 9),
+    (F32, 64, 1, 1, [100, 17], 2, 9), (BF, 128, 2, 9, [300, 1500], 2, 900), (BF, 64, 4, 2, [900, 5], 300, 60),
+    (BF, 128, 4, 8, [300, 900], 70, 20), (BF, 128, 5, 16, [900, 70], 300, 20), (BF, 64, 40, 4, [600, 5], 300, 20),
+])
+def test_large_values_under_growing_logits(dtype, d, group, t, lens, entries, width):
+    # weights against an early, low reference must not carry finite values past a float's range:
+    # logits that rise by 39 (log2) under values of 1e36, whose outputs are of that size
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(t)
+    pg, K, V = _pool(lens, 64, d, dtype, gen)
+    q = torch.randn((entries, group, t, d), generator=gen)
+    for u, n in enumerate(lens):
+        K[u], V[u] = K[u].float(), V[u].float()
+        _ramp(q, K[u], V[u], -19.5, 19.5)
+        K[u], V[u] = K[u].to(dtype), V[u].to(dtype)
+        slot = torch.arange(n, device="cuda")
+        pg.k[pg.table[u, slot // 64].long(), slot % 64] = K[u].cuda()
+        pg.v[pg.table[u, slot // 64].long(), slot % 64] = V[u].cuda()
+    q = q.to(dtype)
+    if width > pg.table.shape[1]:
+        pg = _wide_table(pg, len(lens), width)
+    at = [e % len(lens) for e in range(entries)]
+    if group * t > 64:   # (the wide kernel's)
+        assert dtype == BF and entries * group * t * width * 64 > 1 << 20
+    o, lse = (x.cpu() for x in G.tree_attention(q.cuda(), pg, units=_i32(at), return_lse=True))
+    for e in (*range(len(lens)), entries - 1):
+        u = at[e]
+        seen = tree_seen(lens[u], t, list(range(-1, t - 1)), 0, 0)
+        for g in range(0, group, 3):
+            check("entry %d head %d" % (e, g), o[e, g], lse[e, g], q[e, g], K[u], V[u], seen)
+
+
+@pytest.mark.parametrize("dtype,d,group,n,nq", [(BF, 128, 2, 1100, 1100), (BF, 64, 4, 800, 800), (F32, 64, 2, 300, 100),
+                                                (BF, 128, 3, 200, 9)])
+def test_large_values_of_a_prompt_under_growing_logits(dtype, d, group, n, nq):
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(n)
+    q = torch.randn((1, group, nq, d), generator=gen)
+    K, V = (torch.randn((1, n, d), generator=gen) for _ in range(2))
+    _ramp(q, K, V, -19.5, 19.5)
+    q, K, V = q.to(dtype), K.to(dtype), V.to(dtype)
+    assert nq < 800 or group * nq * n > 1 << 20   # (the long ones are the wide kernel's)
+    o, lse = (x.cpu() for x in G.sink_attention(q.cuda(), K.cuda(), V.cuda(), 0, return_lse=True))
+    for g in range(group):
+        check("head %d" % g, o[0, g], lse[0, g], q[0, g], K[0], V[0], sink_seen(n, nq, 0, 0))
+
+
+def test_values_at_the_types_largest():
+    # one key far above the others, whose value is the largest finite one
+    import paper_2605_31105_amd as G
+    for dtype in (BF, F32):
+        K, V = torch.zeros(1, 300, 64, dtype=dtype), torch.full((1, 300, 64), -1.0, dtype=dtype)
+        K[0, 200, 0] = 1000.0
+        V[0, 200] = torch.finfo(dtype).max
+        V[0, 5] = torch.finfo(dtype).min
+        q = torch.zeros(1, 2, 1, 64, dtype=dtype)
+        q[..., 0] = 8.0
+        o = G.sink_attention(q.cuda(), K.cuda(), V.cuda(), 0).cpu()
+        assert (o == torch.finfo(dtype).max).all(), o
