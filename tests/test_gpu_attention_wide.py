@@ -1,0 +1,159 @@
+"""The attention kernel of many rows (bf16, more than 64 rows a unit and more than 2^20 logits):
+windows, sinks, keys that are not finite and growing logits, each call asserted to be that
+kernel's by its sizes."""
+import math
+
+import pytest
+
+from tests.attention_ref import check, sink_seen, tree_seen
+from tests.test_gpu_attention import BF, _i32, _parents, _pool, _wide_table
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _assert_wide(entries, group, tokens, slots, window, n_sink, tree):
+    """The rule of attend_plan: rows a unit, and rows by the slots that a row may see."""
+    reach = tokens if tree else min(tokens, 128 // group + 2)
+    if 0 < window < slots:
+        slots = min(slots, n_sink + window + reach)
+    assert group * tokens > 64 and entries * group * tokens * slots > 1 << 20
+
+
+SINK_CASES = [
+    # d, U, G, n, nq, window, sinks
+    (64, 4, 3, 900, 900, 200, 4), (64, 2, 8, 1300, 700, 333, 130), (64, 1, 5, 2000, 2000, 64, 65),
+    (64, 3, 7, 1025, 1025, 1000, 0), (64, 2, 4, 1100, 900, 0, 0), (128, 2, 4, 1500, 1500, 256, 300),
+    (128, 1, 16, 1000, 999, 1, 64), (128, 3, 6, 777, 400, 100, 63), (128, 2, 33, 450, 300, 37, 128),
+]
+
+
+@pytest.mark.parametrize("case", SINK_CASES, ids=lambda c: "d%d-u%d-g%d-n%d-q%d-w%d-s%d" % c)
+def test_windows_and_sinks_of_prompts(case):
+    import paper_2605_31105_amd as G
+    d, U, group, n, nq, window, n_sink = case
+    _assert_wide(U, group, nq, n, window, n_sink, False)
+    gen = torch.Generator().manual_seed(n + nq + d)
+    q = torch.randn((U, group, nq, d), generator=gen).to(BF)
+    K, V = (torch.randn((U, n, d), generator=gen).to(BF) for _ in range(2))
+    o, lse = (x.cpu() for x in G.sink_attention(q.cuda(), K.cuda(), V.cuda(), window, n_sink, return_lse=True))
+    seen = sink_seen(n, nq, window, n_sink)
+    for u in {0, U - 1}:
+        for g in {0, group - 1}:
+            check("unit %d head %d" % (u, g), o[u, g], lse[u, g], q[u, g], K[u], V[u], seen)
+
+
+TREE_CASES = [
+    # d, page, group, tokens, lens, entries, window, sinks
+    (64, 16, 8, 12, [12, 300, 1000, 2000], 128, 100, 4), (64, 64, 16, 16, [16, 700, 1500], 24, 300, 100),
+    (64, 128, 9, 33, [33, 400, 20], 120, 1, 0), (64, 32, 5, 30, [1500, 0, 64], 60, 900, 40),
+    (128, 32, 4, 40, [40, 333, 900], 60, 50, 70), (128, 64, 5, 64, [64, 65, 2000], 40, 20, 10),
+    (128, 16, 3, 22, [22, 500, 130, 4], 70, 200, 130),
+]
+
+
+@pytest.mark.parametrize("case", TREE_CASES, ids=lambda c: "d%d-p%d-g%d-t%d-e%d-w%d-s%d" % (c[:4] + c[5:]))
+def test_windows_and_sinks_of_trees(case):
+    import paper_2605_31105_amd as G
+    d, ps, group, t, lens, entries, window, n_sink = case
+    gen = torch.Generator().manual_seed(d + t)
+    pg, K, V = _pool(lens, ps, d, BF, gen)
+    _assert_wide(entries, group, t, pg.table.shape[1] * ps, window, n_sink, True)
+    at = [e % len(lens) for e in range(entries)]
+    counts = [t if e % 5 else e % (t + 1) for e in range(entries)]
+    parents, plist = _parents("tree", 1, t, gen)
+    q = torch.randn((entries, group, t, d), generator=gen).to(BF)
+    o = torch.full(q.shape, 5.0, dtype=BF, device="cuda")
+    lse = torch.full(q.shape[:3], 6.0, device="cuda")
+    G.tree_attention(q.cuda(), pg, parents, units=_i32(at), counts=_i32(counts), window=window, n_sink=n_sink, out=o,
+                     lse=lse)
+    o, lse = o.cpu(), lse.cpu()
+    for e in sorted({*range(len(lens)), *range(5, 5 + len(lens)), entries // 2, entries - 1}):
+        u, c = at[e], counts[e]
+        assert (o[e, :, c:] == 5).all() and (lse[e, :, c:] == 6).all()
+        for g in {0, group - 1}:
+            check("entry %d" % e, o[e, g, :c], lse[e, g, :c], q[e, g, :c], K[u], V[u],
+                  tree_seen(lens[u], c, plist[0], window, n_sink))
+
+
+@pytest.mark.parametrize("d,group,t,window", [(64, 16, 6, 0), (64, 20, 6, 25), (128, 16, 6, 0), (128, 12, 9, 40)])
+def test_keys_and_values_of_trees_that_are_not_finite(d, group, t, window):
+    # NaN and infinities in the keys or the values of a drafted token, and of a slot that the
+    # window has passed: the rows that do not see them are within their bounds
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + group)
+    lens, entries, n_sink = [90, 300], 300, 3
+    pg, K, V = _pool(lens, 16, d, BF, gen)
+    pg = _wide_table(pg, 2, 40)
+    _assert_wide(entries, group, t, 640, window, n_sink, True)
+    parents, plist = _parents("tree", 1, t, gen)
+    q = torch.randn((entries, group, t, d), generator=gen).to(BF)
+    units = _i32([e % 2 for e in range(entries)])
+    for u, slot, value in ((0, 90 - t + 2, math.nan), (1, 300 - t + 1, math.inf), (1, 40, math.nan), (0, 20, -math.inf)):
+        seen = tree_seen(lens[u], t, plist[0], window, n_sink)
+        see = seen[:, slot]
+        page, row = int(pg.table[u, slot // 16]), slot % 16
+        for x in (pg.k, pg.v):
+            keep = x[page, row].clone()
+            x[page, row] = value
+            o, lse = (y.cpu() for y in G.tree_attention(q.cuda(), pg, parents, units=units, window=window,
+                                                        n_sink=n_sink, return_lse=True))
+            x[page, row] = keep
+            for e in (u, entries - 2 + u):
+                for g in {0, group - 1}:
+                    check("unit %d slot %d %s" % (u, slot, value), o[e, g, ~see], lse[e, g, ~see], q[e, g, ~see],
+                          K[u], V[u], seen[~see])
+                    if x is pg.v or math.isnan(value):
+                        assert not torch.isfinite(o[e, g, see]).any()
+
+
+@pytest.mark.parametrize("d,window", [(64, 0), (64, 150), (128, 150)])
+def test_keys_of_prompts_that_are_not_finite(d, window):
+    # NaN and an infinity in the keys: queries before them and those whose window has passed
+    # them are the finite prompt's
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + window)
+    n, group = 900, 6
+    _assert_wide(2, group, n, n, window, 4, False)
+    q = torch.randn((2, group, n, d), generator=gen).to(BF)
+    K, V = (torch.randn((2, n, d), generator=gen).to(BF) for _ in range(2))
+    bad = K.clone()
+    bad[:, 300], bad[:, 310, 3] = math.nan, math.inf
+    seen = sink_seen(n, n, window, 4)
+    see = seen[:, 300] | seen[:, 310]
+    o, lse = (x.cpu() for x in G.sink_attention(q.cuda(), bad.cuda(), V.cuda(), window, 4, return_lse=True))
+    for u in range(2):
+        for g in (0, group - 1):
+            check("unit %d head %d" % (u, g), o[u, g, ~see], lse[u, g, ~see], q[u, g, ~see], K[u], V[u], seen[~see])
+    assert torch.isnan(o[:, :, seen[:, 300]]).all()
+
+
+@pytest.mark.parametrize("d,entries", [(128, 1), (128, 40), (64, 300)])
+def test_growing_logits_move_the_reference(d, entries):
+    # logits that grow along the cache by thousands, and a key far above all others
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(5)
+    group, t, n = 35, 2, 2000
+    pg, K, V = _pool([n], 64, d, BF, gen)
+    pg = _wide_table(pg, 1, 300)
+    _assert_wide(entries, group, t, 300 * 64, 0, 0, True)
+    q = torch.randn((entries, group, t, d), generator=gen)
+    q[:, 0, 0] = 0
+    q[:, 0, 0, 0] = 64.0
+    K[0][:, 0] = torch.linspace(-400, 400, n).to(BF)
+    K[0][777] = (K[0][777].float() * 300).to(BF)
+    q = q.to(BF)
+    slot = torch.arange(n, device="cuda")
+    pg.k[pg.table[0, slot // 64].long(), slot % 64] = K[0].cuda()
+    o, lse = (x.cpu() for x in G.tree_attention(q.cuda(), pg, units=_i32([0] * entries), return_lse=True))
+    seen = tree_seen(n, t, [-1, 0], 0, 0)
+    for e in {0, entries - 1}:
+        for g in (0, 1, 17, group - 1):
+            check("entry %d head %d" % (e, g), o[e, g], lse[e, g], q[e, g], K[0], V[0], seen)
