@@ -397,7 +397,7 @@ typedef struct {
 #define GRKV_PAGES_LENGTH 2 /* more rows than the unit's table row holds */
 #define GRKV_PAGES_UNIT 3   /* no such unit; the unit is written by an earlier entry of
                                the call, or read here and written by another entry; or
-                               the destination of a copy is not empty */
+                               the destination of a copy is another unit and not empty */
 #define GRKV_PAGES_RANGE 4  /* rows outside their source */
 
 /* The units a call works on, one per entry: device arrays of `entries`
@@ -428,7 +428,8 @@ int grkv_pages_append(const grkv_pages* pages, const grkv_page_entries* entries,
 
 /* Unit dst[i] (int32 [entries], device memory; empty before) becomes a copy of
  * unit units[i]: the full pages are shared, the rows of a last page that is not
- * full are copied to one of its own.  A unit may be the source of many entries.
+ * full are copied to one of its own.  A unit may be the source of many entries; one
+ * that is its own destination (dst[i] equal to units[i]) stays as it is, GRKV_PAGES_OK.
  * rows, counts, starts and source_rows are not read. */
 int grkv_pages_fork(const grkv_pages* pages, const grkv_page_entries* entries, const int32_t* dst,
                     void* stream, void* workspace, size_t workspace_bytes);

@@ -792,8 +792,9 @@ def pages_append(pages: Pages, k, v, *, units=None, counts=None, starts=None, ro
 
 
 def pages_fork(pages: Pages, src, dst, *, status=None, workspace=None, stream=None):
-    """Units ``dst`` (int32 [E], empty) become copies of units ``src``, full pages shared
-    (grkv_pages_fork).  Returns the status of every entry."""
+    """Units ``dst`` (int32 [E], empty) become copies of units ``src``, full pages shared; a
+    unit that is its own destination stays as it is (grkv_pages_fork).  Returns the status of
+    every entry."""
     import torch
 
     E = src.shape[0]

@@ -97,3 +97,13 @@ def test_long_rows_of_many_entries():
     idx = [[rng.randrange(320) for _ in range(257 + k % 50)] for k in range(520)]
     p.compact(units, keep, idx)
     p.compact(units[:100], [0] * 100, [[rng.randrange(257) for _ in range(300)] for _ in range(100)])   # fewer: spread
+
+
+def test_a_unit_forked_to_itself_stays():
+    p = Pair(4, 4, 12, 16, 64, torch.bfloat16)
+    p.append([0, 1, 2], [20, 32, 0])
+    p.fork([1], [3])                            # unit 1's pages are shared
+    p.fork([0, 1, 2], [0, 1, 2])
+    assert p.m.lens == [20, 32, 0, 32]
+    p.fork([0, 0], [0, 2])                      # read by the second entry, the first's own
+    assert p.m.lens == [20, 32, 0, 32]

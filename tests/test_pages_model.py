@@ -71,3 +71,12 @@ def test_every_page_is_counted(seed):
             assert len(m.table[u]) == -(-m.lens[u] // 16)
             if m.lens[u] % 16:
                 assert m.refs[m.table[u][-1]] == 1   # a page that is not full is one unit's own
+
+
+def test_a_unit_forked_to_itself_stays():
+    m = PagesModel(3, 4, 8, 16)
+    m.append([0, 1], [_rows(20), _rows(16)])
+    before = [list(t) for t in m.table], list(m.refs)
+    assert m.fork([0, 1, 2], [0, 1, 2]) == [OK, OK, OK]
+    assert ([list(t) for t in m.table], m.refs) == before and m.lens == [20, 16, 0]
+    assert m.fork([0, 0], [0, 2]) == [OK, UNIT]
