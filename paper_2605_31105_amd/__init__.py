@@ -666,6 +666,8 @@ def _on(dev: int, stream):
         stream = torch.cuda.current_stream(dev)
     elif not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    elif stream.device.index != dev:
+        raise ValueError("stream is one of %s, the call's tensors are on cuda:%d" % (stream.device, dev))
     return None, torch.cuda.stream(stream)
 
 

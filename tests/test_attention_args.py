@@ -126,3 +126,15 @@ def test_calls_of_more_blocks_than_a_launch_has(L):
         assert L.grkv_tree_attention(4096, pg, _tree(**kw), 4096, None, None, 4096, 1 << 40) == INV
     prob = G.Problem(1 << 24, 1, 64, 0)
     assert L.grkv_sink_attention(4096, 4096, 4096, 1, 1, 0, 0, None, prob, 4096, None, 4096, 1 << 40) == INV
+
+
+def test_binding_refuses_streams_of_another_device():
+    # a call's stream is one of its tensors' device: any other would be left for that
+    # device's current one
+    torch = pytest.importorskip("torch")
+
+    class Stream:
+        cuda_stream, device = 4096, torch.device("cuda", 1)
+
+    with pytest.raises(ValueError, match="stream"):
+        G._on(0, Stream())
