@@ -700,19 +700,23 @@ def _int32(bits):
 def new_pages(units: int, max_pages: int, pages: int, page_size: int, head_dim: int, dtype=None,
               device=None, *, stream=None) -> Pages:
     """An empty pool of ``pages`` pages of ``page_size`` rows for ``units`` units of at most
-    ``max_pages`` pages each."""
+    ``max_pages`` pages each.  With ``stream`` its memory is that stream's, which writes it."""
     import torch
 
     dtype = torch.bfloat16 if dtype is None else dtype
     if min(units, max_pages, pages, page_size, head_dim) < 1:
         raise ValueError("a pool needs units, pages and rows")
     device = torch.device("cuda" if device is None else device)
+    if stream is not None and device.type == "cuda":
+        dev = torch.cuda.current_device() if device.index is None else device.index
+        with _on(dev, stream)[1]:
+            return new_pages(units, max_pages, pages, page_size, head_dim, dtype, torch.device("cuda", dev))
     i32 = dict(dtype=torch.int32, device=device)
     pg = Pages(k=torch.empty((pages, page_size, head_dim), dtype=dtype, device=device),
                v=torch.empty((pages, page_size, head_dim), dtype=dtype, device=device),
                table=torch.empty((units, max_pages), **i32), lens=torch.empty(units, **i32),
                refs=torch.empty(pages, **i32), free=torch.empty((pages + 31) // 32, **i32))
-    return pages_init(pg, stream=stream)
+    return pages_init(pg)
 
 
 def pages_init(pages: Pages, *, stream=None) -> Pages:

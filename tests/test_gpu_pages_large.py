@@ -107,3 +107,21 @@ def test_a_unit_forked_to_itself_stays():
     assert p.m.lens == [20, 32, 0, 32]
     p.fork([0, 0], [0, 2])                      # read by the second entry, the first's own
     assert p.m.lens == [20, 32, 0, 32]
+
+
+def test_a_pool_made_on_another_stream_owns_its_memory_there():
+    # memory that the current stream has let go of but still writes is not the new pool's
+    import paper_2605_31105_amd as G
+    x = torch.empty((1024, 4096), dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)
+    x.fill_(7)
+    del x
+    pg = G.new_pages(1024, 4096, 64, 16, 64, stream=side)
+    torch.cuda.synchronize()
+    assert (pg.table == -1).all() and not pg.lens.any() and (pg.free == -1).all()
+    with torch.cuda.stream(side):
+        assert not G.pages_append(pg, *(torch.ones(3, 5, 64, device="cuda") for _ in range(2))).any()
+    side.synchronize()
+    assert pg.lens[:4].tolist() == [5, 5, 5, 0]
