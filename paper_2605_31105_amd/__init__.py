@@ -902,8 +902,9 @@ def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, wi
     if parents is not None:
         trees, up = parents.shape[0], parents.data_ptr()
         if (parents.dtype != i32 or parents.get_device() != dev or parents.shape != (trees, t)
-                or not parents.is_contiguous()):
-            raise ValueError("parents must be a contiguous int32 [trees, %d] tensor on cuda:%d" % (t, dev))
+                or trees < 1 or not parents.is_contiguous()):
+            raise ValueError("parents must be a contiguous int32 [trees, %d] tensor on cuda:%d, "
+                             "trees >= 1" % (t, dev))
     tr = _Tree(E, G, t, _vector(units, "units", i32, E, dev), _vector(counts, "counts", i32, E, dev),
                up, trees, window, n_sink)
     out, lse, lp = _outputs(q, (E, G, t), dev, out, lse, return_lse)

@@ -674,3 +674,12 @@ def test_prompts_of_many_rows_with_values_that_are_not_finite(d, window):
         if values is bad:
             assert torch.isnan(o[:, :, seen[:, 300], 5]).all()
             assert not torch.isfinite(o[:, :, seen[:, 301], 6]).any()
+
+
+def test_parents_without_a_tree_are_refused():
+    # (an empty tensor has no address, which would say "a chain")
+    import paper_2605_31105_amd as G
+    pg = G.new_pages(4, 4, 8, 16, 64)
+    q = torch.zeros(4, 2, 3, 64, dtype=BF, device="cuda")
+    with pytest.raises(ValueError):
+        G.tree_attention(q, pg, torch.zeros((0, 3), dtype=torch.int32, device="cuda"))
