@@ -624,6 +624,7 @@ class Pages:
         if k.dim() != 3 or k.shape != v.shape or table.dim() != 2:
             raise ValueError("k and v must be [pages, page_size, head_dim] and table [units, max_pages]")
         (n, ps, d), (units, width) = k.shape, table.shape
+        _int32(n | units | width)
         if lens.shape != (units,) or refs.shape != (n,) or free.shape != ((n + 31) // 32,):
             raise ValueError("lens, refs and free must be [units], [pages] and [ceil(pages / 32)]")
         for t in (k, v, table, lens, refs, free):
@@ -730,6 +731,7 @@ def pages_init(pages: Pages, *, stream=None) -> Pages:
 
 
 def pages_workspace_bytes(pages: Pages, entries: int) -> int:
+    _int32(entries)
     return int(lib().grkv_pages_workspace_bytes(pages._c, entries))
 
 
@@ -845,6 +847,7 @@ def pages_free(pages: Pages, units=None, *, status=None, stream=None):
 # ---------------------------------------------------- attention over a cache ----
 
 def tree_attention_workspace_bytes(pages: Pages, entries, group, tokens, window=0, n_sink=0) -> int:
+    _int32(entries | group | tokens | window | n_sink)
     tr = _Tree(entries, group, tokens, None, None, None, 0, window, n_sink)
     return int(lib().grkv_tree_attention_workspace_bytes(pages._c, tr))
 
@@ -916,6 +919,7 @@ def tree_attention(q, pages: Pages, parents=None, *, units=None, counts=None, wi
 
 
 def sink_attention_workspace_bytes(units, group, head_dim, dtype, n, nq, window, n_sink) -> int:
+    _int32(units | group | head_dim | nq | window | n_sink)
     prob = Problem(units, group, head_dim, dtype)
     return int(lib().grkv_sink_attention_workspace_bytes(prob, n, nq, window, n_sink))
 

@@ -111,3 +111,44 @@ def test_calls_of_more_entries_than_a_launch_has_blocks(L):
             assert L.grkv_pages_free(pg, en, None) == code
     assert L.grkv_pages_append(pg, _entries(entries=1 << 25, rows=1, source_rows=1 << 25), 4096, 0, 4096, 0, None, 4096,
                                256) == WS
+
+
+def test_sizes_past_32_bits_are_refused():
+    # (ctypes would cut them, and ask for or work on another size)
+    torch = pytest.importorskip("torch")
+
+    class Pool:
+        _c = _pool()
+
+    class Tensor:
+        def __init__(self, dtype, *shape):
+            self.dtype, self.shape = dtype, torch.Size(shape)
+
+        def dim(self):
+            return len(self.shape)
+
+        def get_device(self):
+            return 0
+
+        def is_contiguous(self):
+            return True
+
+        def data_ptr(self):
+            return 4096
+
+    def pool(units, width, pages):
+        rows, i32 = (Tensor(torch.bfloat16, pages, 16, 64) for _ in range(2)), torch.int32
+        return G.Pages(*rows, Tensor(i32, units, width), Tensor(i32, units), Tensor(i32, pages),
+                       Tensor(i32, (pages + 31) // 32))
+
+    big = 1 << 32
+    assert pool(4, 3, 40)._c.units == 4
+    for call in (lambda: pool(big + 4, 3, 40), lambda: pool(4, big + 3, 40), lambda: pool(4, 3, big + 40),
+                 lambda: G.pages_workspace_bytes(Pool, big + 4),
+                 lambda: G.tree_attention_workspace_bytes(Pool, big + 4, 1, 1),
+                 lambda: G.tree_attention_workspace_bytes(Pool, 4, 1, 1, big),
+                 lambda: G.sink_attention_workspace_bytes(big + 8, 4, 128, 0, 4096, 1, 0, 0),
+                 lambda: G.sink_attention_workspace_bytes(8, 4, 128, 0, big + 4096, big + 1, 0, 0),
+                 lambda: G.sink_attention_workspace_bytes(8, 4, 128, 0, 4096, 1, 0, big)):
+        with pytest.raises(ValueError):
+            call()
