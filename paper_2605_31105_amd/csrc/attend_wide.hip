@@ -46,22 +46,6 @@ __device__ __forceinline__ void ring_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// 16 bytes per lane from base + voff to LDS offset lds (uniform), lane after
-// lane.  In assembly so that the compiler does not wait for these loads at every
-// LDS read; ring_barrier does where it matters.  once: a non-temporal load.
-__device__ __forceinline__ void ring_load(const char* base, uint32_t voff, uint32_t lds, bool once) {
-  if (once)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
-                 :
-                 : "v"(voff), "s"(base), "s"(lds)
-                 : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(voff), "s"(base), "s"(lds)
-                 : "memory", "m0");
-}
-
 __device__ __forceinline__ bf16x8 read_tr(const char* p, int rows8) {
   const v4i16 x = ds_read_tr16(p), y = ds_read_tr16(p + rows8);
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -155,7 +139,8 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
         const int row_in = it * RPI + lane / CPR, ch = lane % CPR;
         f = ((min(s16 + row_in, last) & 15) * CPR + (ch ^ swz(row_in))) * 16;
       }
-      ring_load(src, f, dst + it * 1024, once);
+      if (once) ring_load<true>(src, f, dst + it * 1024);
+      else ring_load(src, f, dst + it * 1024);
     }
   };
 

@@ -97,6 +97,32 @@ typedef short v8i16 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
+// 16 bytes per lane from memory straight into LDS, for rings whose waits (vmcnt, then a
+// barrier) are the kernel's own: lane source base + voff (base wave-uniform, voff a
+// per-lane byte offset), the wave's 1 KB landing lane after lane at the wave-uniform
+// LDS byte offset lds.  ONCE: a non-temporal load.  Written as inline assembly so that
+// the compiler does not track these loads: tracked, they make it wait for every
+// outstanding LDS access before each use of one (it no longer counts LDS
+// accesses in order) and order accesses to other LDS buffers after them.  m0, which
+// names the destination, is the compiler's and is put back; a wait state lies between
+// its write and the load that reads it.
+template <bool ONCE = false>
+__device__ __forceinline__ void ring_load(const void* base, uint32_t voff, uint32_t lds) {
+  uint32_t m0;
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0)
+                 : "v"(voff), "s"(base), "s"(lds)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0)
+                 : "v"(voff), "s"(base), "s"(lds)
+                 : "memory");
+}
+
 // LDS transpose read of 4 x 16-bit values: within a 16-lane group, lane
 // 4e + q supplies the address of row e, elements 4q..4q+3 (8 bytes), and
 // lane i receives element i of the four rows (rows 0..3 in order).

@@ -91,20 +91,6 @@ __device__ __forceinline__ uint32_t lds_off(const void* p) {
   return (uint32_t)(uintptr_t)(lds_void*)p;
 }
 
-// 16 bytes per lane from HBM straight into LDS: lane source base + voff
-// (base wave-uniform, voff a per-lane byte offset), the wave's 1 KB landing
-// at the wave-uniform LDS byte offset lds.  Written as inline assembly so that the
-// compiler does not track these loads: tracked, they make it wait for every
-// outstanding LDS access before each use of one (it no longer counts LDS
-// accesses in order) and order accesses to other LDS buffers after them.  The
-// ring's own waits (vmcnt, then a barrier) establish completion.
-__device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds))
-               : "memory", "m0");
-}
-
 template <bool FINAL>
 __global__ __launch_bounds__(kRTh) void key_ring_kernel(RingArgs a) {
   __shared__ __attribute__((aligned(16))) char stg0[kRStage];
@@ -161,14 +147,15 @@ __global__ __launch_bounds__(kRTh) void key_ring_kernel(RingArgs a) {
       const int instr = wave * kRLoads + it;      // 0..31
       if (instr < kRXB / 1024) {
         const float* base = a.xs + ((size_t)u * a.ntc + tg0 + t) * (kRXB / 4);
-        dma16(base, (uint32_t)(instr * 1024 + lane * 16), lds_off(stage) + instr * 1024);
+        ring_load(base, (uint32_t)(instr * 1024 + lane * 16),
+                  __builtin_amdgcn_readfirstlane(lds_off(stage) + instr * 1024));
       } else {
         const int vi = instr - kRXB / 1024, tensor = vi >> 3, part = vi & 7;
         const int r = part * 4 + (lane >> 4), pos = lane & 15;
         const u16* base = (tensor == 0 ? a.vh : a.vl) + ((size_t)u * c + tile0) * kRD;
         const int rr = min(tile0 + r, j1 - 1) - tile0;
         const uint32_t vo = (uint32_t)((rr * kRD + (pos ^ vswz(r)) * 8) * 2);
-        dma16(base, vo, lds_off(stage) + kRXB + tensor * kRTB + part * 1024);
+        ring_load(base, vo, __builtin_amdgcn_readfirstlane(lds_off(stage) + kRXB + tensor * kRTB + part * 1024));
       }
     }
   };
