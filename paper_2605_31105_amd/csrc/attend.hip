@@ -15,7 +15,8 @@
 //  * A wave walks its own key tiles (32 keys of bf16, 16 of float32) with no
 //    barrier: K fragments go from memory to registers in the MFMA A layout and
 //    V tiles to LDS (global_load_lds), both one tile ahead of the products, so a
-//    compute unit keeps 8 waves x 16 KB in flight.
+//    compute unit keeps 8 waves x 16 KB in flight (4 with blocks of 32 rows of 128 columns,
+//    whose 300 registers and more leave room for one block).
 //  * S^T = K Q^T puts a query row in each lane column: the four lanes of a row
 //    hold its logits as P^T already lies in the B operand of O^T = V^T P^T (the
 //    order of the keys inside a tile is free as long as V^T uses the same), so P
@@ -625,8 +626,9 @@ AttendPlan attend_plan(int entries, int group, int tokens, int d, int dtype, int
   AttendPlan p;
   const int64_t R = (int64_t)group * tokens;
   const bool bf16 = dtype == GRKV_BF16;
-  // two blocks per compute unit (32 units of 20k to 32k keys, 128 rows, 256 / 512 / 1024
-  // blocks: 138 / 116 / 139 us; 300 units of 500 to 4000 keys, 64 rows, 512 / 2048: 168 / 180)
+  // two blocks for each compute unit, which hold them at once but for blocks of 32 rows of 128
+  // columns (32 units of 20k to 32k keys, 128 rows, 256 / 512 / 1024 blocks: 138 / 116 / 139
+  // us; 300 units of 500 to 4000 keys, 64 rows, 512 / 2048: 168 / 180)
   constexpr int64_t target = 512;
   // the wide kernel from 65 rows on, but for calls of few logits, which one launch of small
   // blocks ends first (2 prompts of 564, 11.2 us beside 14.1; 2 units of 120 rows and 1000
