@@ -18,7 +18,7 @@ constexpr float kRefAbove = 8.f;
 // again (rows_by_key).  (A reference set above the logits there takes two registers more, 170
 // of head_dim 64, where 168 leave room for a third wave: a 16k prompt with a 4k window 577 ->
 // 630 us.)
-constexpr float kMoveSum = 0x1p16f;
+constexpr float kMoveLog = 16.f, kMoveSum = 0x1p16f;   // log2 of it, and it
 constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
 constexpr float kLn2 = 0.6931471805599453f;
 

@@ -292,13 +292,15 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
   char* out = ring + wave * KB;
   if (sn.ns > 1) {
     constexpr int CR = D / 4;
+    const float fit = 1.f / kMoveSum;   // (weights of 1 at most, so that parts may be added)
 #pragma unroll
     for (int dm = 0; dm < DM; ++dm)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         *reinterpret_cast<f32x4*>(out + (l32 * CR + ((8 * dm + 2 * c + h) ^ (l32 & 15))) * 16) =
-            (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]};
-    if (h == 0 && my < R && mi < t) a.mpart[part + my] = make_float4(-nref, rsum, sum, 0.f);
+            (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]} * fit;
+    if (h == 0 && my < R && mi < t)
+      a.mpart[part + my] = make_float4(kMoveLog - nref, rsum * fit, sum * fit, 0.f);
 #pragma unroll 4
     for (int k = lane; k < 32 * CR; k += 64) {
       const int row = k / CR, ch = k % CR, r = w0 + row;

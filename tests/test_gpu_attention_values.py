@@ -158,3 +158,25 @@ def test_values_at_the_types_largest():
         q[..., 0] = 8.0
         o = G.sink_attention(q.cuda(), K.cuda(), V.cuda(), 0).cpu()
         assert (o == torch.finfo(dtype).max).all(), o
+
+
+def test_large_values_summed_over_splits():
+    # the kernel of many rows, 4 tiles and more a split: a peak of 2^15 over the first tiles'
+    # logits in every fourth tile, whose parts are finite while their sum against those logits
+    # is not; o is the peaks' value
+    import paper_2605_31105_amd as G
+    n, d, group = 65536, 64, 40
+    K, V = torch.zeros((n, d)), torch.zeros((n, d))
+    peak = torch.arange(n // 256) * 256 + 3 * 64 + 17
+    K[peak, 0] = 15 * d ** 0.5 / 1.4426950408889634 / 8
+    V[peak] = 2.0 ** 110
+    V[peak, 1] = -(2.0 ** 110)
+    pg = G.new_pages(1, n // 64, n // 64, 64, d)
+    K, V = K.to(BF), V.to(BF)
+    assert not G.pages_append(pg, K[None].cuda(), V[None].cuda()).any().item()
+    q = torch.zeros((1, group, 2, d), dtype=BF)
+    q[..., 0] = 8.0
+    o, lse = (x.cpu() for x in G.tree_attention(q.cuda(), pg, return_lse=True))
+    seen = tree_seen(n, 2, [-1, 0], 0, 0)
+    for g in (0, group - 1):
+        check("head %d" % g, o[0, g], lse[0, g], q[0, g], K, V, seen)
