@@ -475,7 +475,7 @@ size_t grkv_pages_workspace_bytes(const grkv_pages* pages, int32_t entries);
  *   o = sum_j softmax_j(q . k_j / sqrt(d)) v_j,  lse = ln sum_j exp(q . k_j / sqrt(d)).
  * A query that sees nothing (or whose weights are all zero) gets o = 0, lse =
  * -infinity.  What a query does not see never reaches it, infinities and NaN
- * included. */
+ * included (its last bits may differ beside those, as its rows are summed in another way). */
 typedef struct {
   int32_t entries;        /* >= 0; with 0 the call does nothing */
   int32_t group;          /* query heads per KV head, >= 1 */

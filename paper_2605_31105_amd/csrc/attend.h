@@ -318,10 +318,18 @@ __device__ __forceinline__ RowSight row_sight(const AttendK& a, int base, int i,
   return s;
 }
 
+// Whether a row is to be summed again: its sum of values is not finite (zero times it, z, is
+// NaN) though its weights' is no NaN, or its weights are all next to nothing though it has a
+// reference (of logits past 2^30, whose step is many powers of two, the largest may lie far from
+// its own reference, on either side).
+__device__ __forceinline__ bool again(float z, float sum, float nref) {
+  return (z != z && sum == sum) || (sum < 0x1p-60f && nref != kUnset);
+}
+
 // Rows of a split once more, key by key, with float32 weights against the largest logit:
-// taken where a sum of values is not finite, though its weights' is.  An infinity or NaN
-// among the values may be one that the row does not see (0 x inf in a product is NaN), or
-// large values may have overflowed under a reference that was too low.  One wave; rows first ..
+// taken by `again`.  An infinity or NaN among the values may be one that the row does not
+// see (0 x inf in a product is NaN), or large values may have overflowed under a reference
+// that was too low.  One wave; rows first ..
 // first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn, left as partial rows
 // from `part` on or (part < 0) as outputs.  A lane forms the weight of one key of 64, then
 // sums D / 64 columns.

@@ -9,7 +9,7 @@
 // are split over blocks when there are few units, or all units' keys cut into equal
 // parts when their lengths may differ (attend_even_kernel), and over the four waves of
 // a block always.  Long calls are bound by HBM: 512 units of 500 to 8000 keys, 1.1 GB in
-// 187 us, 6.0 TB/s (6.3 is what a read-only stream reaches); short ones by the chain of
+// 189 us, 6.0 TB/s (6.3 is what a read-only stream reaches); short ones by the chain of
 // dependent reads and the launch (8 units of 2048 keys, 11.7 us).
 //
 //  * A wave walks its own key tiles (32 keys of bf16, 16 of float32) with no
@@ -34,7 +34,7 @@
 //    that a row does not see has weight zero.  An infinity or NaN among the values
 //    reaches rows all the same, as NaN (0 x inf; over bf16 values also where it is seen,
 //    beside second parts of both signs); where a sum of values is not finite
-//    and that of its weights is, the block does its rows again key by key.
+//    and that of its weights is no NaN, the block does its rows again key by key (`again`).
 // Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
 #include "attend.h"
 
@@ -348,7 +348,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
   wait_vmcnt<0>();
-  bool odd = false;   // a sum of values is not finite, though its weights' is
+  bool odd = false;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16);
@@ -358,7 +358,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) z = fmaf(acc[dt][rt][i], 0.f, z);
-    odd |= z != z && sum[rt] == sum[rt];
+    odd |= again(z, sum[rt], nref[rt]);
   }
   if (__syncthreads_or(odd)) {
     if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);   // (not held until here)

@@ -180,3 +180,30 @@ def test_large_values_summed_over_splits():
     seen = tree_seen(n, 2, [-1, 0], 0, 0)
     for g in (0, group - 1):
         check("head %d" % g, o[0, g], lse[0, g], q[0, g], K, V, seen)
+
+
+@pytest.mark.parametrize("dtype,d,group,t", [(BF, 128, 1, 1), (F32, 64, 1, 1), (BF, 64, 5, 6), (BF, 128, 40, 2), (BF, 64, 40, 2)])
+def test_logits_past_a_floats_step(dtype, d, group, t):
+    # logits of 10^10, a step of which is many powers of two: a row's largest still has a weight
+    # (o is that key's value), whichever way the reference was rounded.  A unit's rows are alike.
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + group)
+    n, top, E = 500, 211, 40
+    pg, K, V = _pool([n], 64, d, dtype, gen)
+    pg = _wide_table(pg, 1, 12)
+    assert group * t <= 64 or E * group * t * 12 * 64 > 1 << 20
+    sign = torch.randint(0, 2, (d,), generator=gen) * 2.0 - 1
+    q = (sign * (20000 + 20000 * torch.rand((E, 1, 1, d), generator=gen))).expand(E, group, t, d).to(dtype).contiguous()
+    K[0] = (K[0].float() * 1000).to(dtype)
+    K[0][top] = (sign * 30000).to(dtype)
+    slot = torch.arange(n, device="cuda")
+    pg.k[pg.table[0, slot // 64].long(), slot % 64] = K[0].cuda()
+    o, lse = (x.cpu() for x in G.tree_attention(q.cuda(), pg, units=_i32([0] * E), return_lse=True))
+    logit = (q.double() @ K[0][top].double()) / d ** 0.5
+    assert ((lse.double() - logit).abs() <= 2.0 ** -18 * logit).all()
+    # o = (w v) (1 / l) with l = w, which need not be a power of two: the product, the reciprocal (one
+    # step, 2^-23) and their product are off by at most 2^-24 + 2^-23 + 2^-24 = 2^-22 together; the
+    # rounding to bf16 takes that, and the weights' 2^-16, back to v
+    v = V[0][top].expand(E, group, t, d)
+    off = (o.double() - v.double()).abs()
+    assert (off <= (0.0 if dtype == BF else 2.0 ** -22) * v.double().abs()).all()
