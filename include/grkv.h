@@ -495,7 +495,7 @@ typedef struct {
 
 /* q, o: pages' dtype [entries][group][tokens][head_dim], 16-byte aligned; lse float
  * [entries][group][tokens] or NULL; neither may overlap q, the pool or another array of the
- * call.  Over bf16 values a weight is held to 2^-16 of it where memory bounds a call (up to 64
+ * call.  Over bf16 values a weight is held to 2^-15 of it where memory bounds a call (up to 64
  * rows, group * tokens, a unit, and small calls of more) and rounded to bf16 (2^-8) in the others;
  * sums are float32, of weights of 1 at most.  The length of a unit is read on the device.  Errors:
  * those of the calls on pages; GRKV_ERR_INVALID for bad counts in `tree` (also

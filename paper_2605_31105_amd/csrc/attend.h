@@ -14,10 +14,10 @@ constexpr float kUnset = 3e38f;      // minus the reference of a row without one
 // included.
 constexpr float kRefAbove = 8.f;
 // Many rows (attend_wide.hip): it is the largest logit and moves where a step's weights of a
-// lane sum to more than this.  Values past 2^128 / 2^16 / keys may then overflow, and are summed
-// again (rows_by_key).  (A reference set above the logits there takes two registers more, 170
-// of head_dim 64, where 168 leave room for a third wave: a 16k prompt with a 4k window 577 ->
-// 630 us.)
+// lane sum to more than this.  Values past 2^128 / 2^16 / keys may then overflow: where a sum
+// is not finite and no value is the cause, rows are summed again (rows_by_key).  (A reference
+// set above the logits there takes two registers more, 170 of head_dim 64, where 168 leave
+// room for a third wave: a 16k prompt with a 4k window 577 -> 630 us.)
 constexpr float kMoveLog = 16.f, kMoveSum = 0x1p16f;   // log2 of it, and it
 constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
 constexpr float kLn2 = 0.6931471805599453f;
@@ -318,18 +318,48 @@ __device__ __forceinline__ RowSight row_sight(const AttendK& a, int base, int i,
   return s;
 }
 
-// Whether a row is to be summed again: its sum of values is not finite (zero times it, z, is
-// NaN) though its weights' is no NaN, or its weights are all next to nothing though it has a
-// reference (of logits past 2^30, whose step is many powers of two, the largest may lie far from
-// its own reference, on either side).
-__device__ __forceinline__ bool again(float z, float sum, float nref) {
-  return (z != z && sum == sum) || (sum < 0x1p-60f && nref != kUnset);
+// Whether a tile of vt0 .. vt1 - 1 that is not seen whole (by every row before lim and
+// from lo on; lim 0: any tile) holds an infinity or NaN among its values.  One wave; asked
+// only where a sum of values is not finite.
+template <typename E, int D, bool PAGED>
+__device__ __forceinline__ bool odd_values(const AttendK& a, const Span& sn, int e, int vt0, int vt1,
+                                           int tk, int lim, int lo, const int32_t* trow) {
+  constexpr int CPR = D * (int)sizeof(E) / 16;   // 16-byte chunks of a row
+  const int lane = threadIdx.x & 63;
+  for (int vt = vt0; vt < vt1; ++vt) {
+    const int slot0 = (vt < sn.at ? vt : vt - sn.at + sn.bt) * tk;
+    if (slot0 + tk <= lim && (slot0 >= lo || slot0 + tk <= a.n_sink)) continue;
+    bool odd = false;
+#pragma unroll 4
+    for (int k = lane; k < tk * CPR; k += 64) {
+      const int j = slot0 + k / CPR;
+      if (j >= sn.kend) continue;
+      size_t row = (size_t)e * a.n + j;
+      if (PAGED) {
+        const int p = trow[j >> a.shift];
+        row = ((size_t)((unsigned)p < (unsigned)a.pages ? p : 0) << a.shift) + (j & ((1 << a.shift) - 1));
+      }
+      const uint4 x = *reinterpret_cast<const uint4*>((const E*)a.v + row * D + k % CPR * (16 / sizeof(E)));
+      for (const uint32_t w : {x.x, x.y, x.z, x.w}) {
+        odd |= (w & 0x7f800000u) == 0x7f800000u;
+        if constexpr (sizeof(E) == 2) odd |= (w & 0x7f80u) == 0x7f80u;
+      }
+    }
+    if (__any(odd)) return true;
+  }
+  return false;
+}
+
+// Whether a row's weights left float32's reach: of logits past 2^30, whose step is many powers
+// of two, the largest may lie far from its own reference, on either side.
+__device__ __forceinline__ bool far_off(float sum, float nref) {
+  return sum > 0x1p40f || (sum < 0x1p-60f && nref != kUnset);
 }
 
 // Rows of a split once more, key by key, with float32 weights against the largest logit:
-// taken by `again`.  An infinity or NaN among the values may be one that the row does not
-// see (0 x inf in a product is NaN), or large values may have overflowed under a reference
-// that was too low.  One wave; rows first ..
+// taken where an infinity or NaN among the values of a tile that is not seen whole may have
+// reached rows that do not see it (0 x inf in a product is NaN), where large values overflowed
+// under a reference that was too low, and where weights are far off.  One wave; rows first ..
 // first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn, left as partial rows
 // from `part` on or (part < 0) as outputs.  A lane forms the weight of one key of 64, then
 // sums D / 64 columns.

@@ -25,16 +25,17 @@
 //  * The reference of a row is set 2^8 above its largest logit and moves only when a
 //    logit passes it, so most tiles need no exchange between lanes.  No weight is above 1,
 //    so large values (finite ones up to the type's largest) do not overflow the sums.
-//  * Over bf16 values P enters the product in two bf16 parts, itself rounded and what the
-//    rounding left, so that a weight is off by 2^-16 of it instead of 2^-8: memory bounds
-//    these calls, and the second product costs them 0 to 5% (one token over 512 ragged
-//    units 188.0 -> 189.0 us, over 8 of 128k 93.4 -> 94.8, 64 units of 32 rows 74.3 -> 76.6,
-//    300 of 64 rows 162 -> 170).
+//  * Over bf16 values P enters the product in two bf16 parts, its upper bits and a rounded
+//    rest, so that a weight is off by 2^-15 of it instead of 2^-8: memory bounds these
+//    calls, and the second product costs them 0 to 2% (one token over 512 ragged
+//    units 187.7 -> 188.8 us, over 8 of 128k 93.2 -> 95.0, 64 units of 32 rows 74.2 -> 74.3,
+//    300 of 64 rows 161 -> 161; a rounded upper part takes those two to 76.6 and 170).  Both parts are above zero (the rest with 2^-18 of the weight
+//    added), so an infinity that a row sees stays one.
 //  * Tiles that every row sees whole skip the masks.  In the others an entry
-//    that a row does not see has weight zero.  An infinity or NaN among the values
-//    reaches rows all the same, as NaN (0 x inf; over bf16 values also where it is seen,
-//    beside second parts of both signs); where a sum of values is not finite
-//    and that of its weights is no NaN, the block does its rows again key by key (`again`).
+//    that a row does not see has weight zero.  An infinity or NaN among the values of
+//    such a tile reaches those rows all the same, as NaN (0 x inf); where a sum is
+//    NaN and such a tile is the cause, the block does its rows again key by key.  So it does
+//    where a row's weights left float32's reach (`far_off`).
 // Splits leave (m, sum, O) in float32; combine_kernel adds them in order.
 #include "attend.h"
 
@@ -47,6 +48,7 @@ namespace {
 
 constexpr int kAtWaves = 4;
 constexpr int kAtTh = 64 * kAtWaves;
+constexpr float kPartUp = 1.f + 0x1p-18f;   // of a weight, before its upper bits are taken away
 // Splits that the blocks themselves join: a few, in calls whose blocks all run at once
 // (8 units of 2048 keys and 8 rows, 8 splits: one launch of 11.7 us against 9.8 and 3.9).
 // More are combined by a launch of their own, which has more threads for them (256 units
@@ -291,7 +293,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
       const int row = 4 * gq + i, ch = 4 * dt + (l16 >> 2);
       return *reinterpret_cast<const float*>(vs + (row * CPR + (ch ^ swz(row))) * 16 + 4 * (l16 & 3));
     };
-    bf16x8 p[RT], pl[RT];   // a weight in two parts, so that its rounding is 2^-16 of it
+    bf16x8 p[RT], pl[RT];   // the two parts of the weights
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       if constexpr (BF) {
@@ -299,9 +301,10 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
-            const f32x2 w = {s[kt][rt][i], s[kt][rt][i + 1]};
-            const bf16x2 h = __builtin_convertvector(w, bf16x2);
-            const f32x2 r = {w[0] - (float)h[0], w[1] - (float)h[1]};
+            const uint32_t w0 = __float_as_uint(s[kt][rt][i]), w1 = __float_as_uint(s[kt][rt][i + 1]);
+            const bf16x2 h = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(w1, w0, 0x07060302u));
+            const f32x2 r = {fmaf(s[kt][rt][i], kPartUp, -__uint_as_float(w0 & 0xffff0000u)),
+                             fmaf(s[kt][rt][i + 1], kPartUp, -__uint_as_float(w1 & 0xffff0000u))};
             const bf16x2 l = __builtin_convertvector(r, bf16x2);
             p[rt][4 * kt + i] = h[0];
             p[rt][4 * kt + i + 1] = h[1];
@@ -348,19 +351,21 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
   wait_vmcnt<0>();
-  bool odd = false;
+  bool odd = false, far = false;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16);
     sum[rt] += __shfl_xor(sum[rt], 32);
-    float z = 0.f;
+    float z = 0.f;   // NaN if a sum of values is not finite
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) z = fmaf(acc[dt][rt][i], 0.f, z);
-    odd |= again(z, sum[rt], nref[rt]);
+    odd |= z != z && sum[rt] == sum[rt];
+    far |= far_off(sum[rt], nref[rt]);
   }
-  if (__syncthreads_or(odd)) {
+  if (__syncthreads_or(odd || far) &&
+      (__syncthreads_or(far) || odd_values<E, D, PAGED>(a, sn, e, vt0, vt1, TK, sn.lim, sn.lo, trow))) {
     if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);   // (not held until here)
     rows_by_key<E, D, PAGED>(a, sn, e, part, r0 + wave * (4 * RT), 4 * RT, vt0, vt1, TK, len, t, trow,
                              family, depth);

@@ -281,7 +281,10 @@ __global__ __launch_bounds__(kWTh, 2) void wide_kernel(AttendK a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) odd = fmaf(acc[dm][r], 0.f, odd);
   const int64_t part = ((int64_t)e * a.splits + sp) * R;
-  if (__any(again(odd, sum, nref))) {
+  const bool far = far_off(sum, nref);
+  if (__any(far || (odd != odd && sum == sum)) &&
+      (__any(far) || odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, lim, lo, trow) ||
+       !odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, 0, lo, trow))) {
     if (PAGED) draft_family(a, e, t, base, lane, &family, &depth);   // (not held until here)
     rows_by_key<u16, D, PAGED>(a, sn, e, sn.ns > 1 ? part : -1, w0, 32, vt0, vt1, TK, len, t, trow, family, depth);
     return;

@@ -157,3 +157,23 @@ def test_growing_logits_move_the_reference(d, entries):
     for e in {0, entries - 1}:
         for g in (0, 1, 17, group - 1):
             check("entry %d head %d" % (e, g), o[e, g], lse[e, g], q[e, g], K[0], V[0], seen)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_every_row_sees_and_are_not_finite(d):
+    # in tiles that are seen whole: infinities stay infinities, a NaN stays in its column, and the
+    # other columns are the finite call's
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d)
+    n, nq, group = 900, 300, 6
+    _assert_wide(2, group, nq, n, 0, 0, False)
+    q = torch.randn((2, group, nq, d), generator=gen).to(BF)
+    K, V = (torch.randn((2, n, d), generator=gen).to(BF) for _ in range(2))
+    bad = V.clone()
+    bad[:, 200, 7], bad[:, 300, 9], bad[0, 130, 11] = math.inf, -math.inf, math.nan
+    want = G.sink_attention(q.cuda(), K.cuda(), V.cuda(), 0, return_lse=True)
+    o, lse = G.sink_attention(q.cuda(), K.cuda(), bad.cuda(), 0, return_lse=True)
+    rest = [c for c in range(d) if c not in (7, 9, 11)]
+    assert torch.equal(o[..., rest], want[0][..., rest]) and torch.equal(lse, want[1])
+    assert (o[..., 7] == math.inf).all() and (o[..., 9] == -math.inf).all()
+    assert torch.isnan(o[0, ..., 11]).all() and torch.equal(o[1, ..., 11], want[0][1, ..., 11])
