@@ -29,8 +29,9 @@
 //    rest, so that a weight is off by 2^-15 of it instead of 2^-8: memory bounds these
 //    calls, and the second product costs them 0 to 2% (one token over 512 ragged
 //    units 187.7 -> 188.8 us, over 8 of 128k 93.2 -> 95.0, 64 units of 32 rows 74.2 -> 74.3,
-//    300 of 64 rows 161 -> 161; a rounded upper part takes those two to 76.6 and 170).  Both parts are above zero (the rest with 2^-18 of the weight
-//    added), so an infinity that a row sees stays one.
+//    300 of 64 rows 161 -> 161; a rounded upper part takes those two to 76.6 and 170).
+//    Both parts are above zero (the rest with 2^-18 of the weight added, which o is divided
+//    by too), so an infinity that a row sees stays one.
 //  * Tiles that every row sees whole skip the masks.  In the others an entry
 //    that a row does not see has weight zero.  An infinity or NaN among the values of
 //    such a tile reaches those rows all the same, as NaN (0 x inf); where a sum is
@@ -392,6 +393,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
       *reinterpret_cast<f32x4*>(mine + row * D * 4 + (((4 * dt + gq) ^ l16) << 4)) = acc[dt][rt] * f;
   }
   __syncthreads();
+  const float up = BF ? kPartUp : 1.f;   // (what the parts add up to, of a weight)
   for (int c = tid; c < 16 * RT * CR; c += kAtTh) {
     const int row = c / CR, ch = c % CR, r = r0 + row;
     const int i = group_of(a, r), g = r - i * a.group;
@@ -409,10 +411,10 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     }
     if (part >= 0) {
       put4(a.opart + (part + r) * D + 4 * ch, x, shared);
-      if (ch == 0) put4((float*)(a.mpart + part + r), (f32x4){m, l, l, 0.f}, shared);
+      if (ch == 0) put4((float*)(a.mpart + part + r), (f32x4){m, l * up, l, 0.f}, shared);
     } else {
       const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
-      write_out<E, D>(a, at, ch, x, m, l, l);
+      write_out<E, D>(a, at, ch, x, m, l * up, l);
     }
   }
 }
