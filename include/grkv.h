@@ -524,6 +524,136 @@ int grkv_sink_attention(const void* q, const void* K, const void* V, int64_t n, 
 size_t grkv_sink_attention_workspace_bytes(const grkv_problem* prob, int64_t n, int32_t nq,
                                            int32_t window, int32_t n_sink);
 
+/* ------------------------------------------------------------------------
+ * A step of a served model over pages.  A step takes new tokens of a batch of
+ * sequences, any number of each (a token where a sequence decodes, a chunk of its
+ * prompt, or none), packed one behind the other into `tokens` rows; sequence b's
+ * rows are starts[b] .. starts[b + 1] - 1.  Each sequence has `heads` units of a
+ * pool, of lengths of their own: those of a layer's KV heads, or of all layers'
+ * (then one grkv_pages_extend serves the whole step).  A layer of the step is
+ *   grkv_pages_extend    the units grow; every token's position and slots,
+ *   grkv_pages_store     queries and keys rotated, keys and values stored there,
+ *   grkv_chunk_attention attention of the new tokens over their units. */
+typedef struct {
+  int32_t sequences;    /* >= 0; with 0 a call does nothing */
+  int32_t heads;        /* units of a sequence, >= 1 */
+  const int32_t* units; /* int32 [sequences][unit_stride]: the unit of head h of sequence b at
+                           b * unit_stride + h; NULL: unit b * heads + h */
+  int64_t unit_stride;  /* >= heads (not read without units) */
+  int32_t tokens;       /* rows of the packed tokens, >= 0 */
+} grkv_step;
+
+/* Of rows that are no sequence's, or a refused one's: they have no position. */
+#define GRKV_NO_POSITION INT32_MIN
+
+/* Grows the units of every sequence by counts[b] (int32 [sequences], below 0 taken as 0)
+ * rows, whose content is whatever the pages held, and gives
+ *   starts     int32 [sequences + 1]    sums of the counts before each sequence, `tokens` at most
+ *   positions  int32 [tokens]           seen[b] + i of the i-th new token of sequence b
+ *   slots      int64 [tokens][heads]    where row lens[u] + i of its units is to be stored:
+ *                                       row page * page_size + s % page_size of k and v
+ *   status     int32 [sequences]        or NULL
+ * seen (int32 [sequences]): how many tokens a sequence had, which its units' lengths do not say
+ * once they are compressed; NULL: the length of its first unit.  All units of a sequence
+ * grow, or none: a sequence is refused for the largest of its units' GRKV_PAGES_ codes (_UNIT
+ * also for a unit that an earlier head or sequence of the call names; _RANGE: its rows pass
+ * `tokens`, or its positions leave 0 .. 2^31 - 1), and its rows, like those behind the
+ * last sequence, have position GRKV_NO_POSITION and slots -1.  New pages are handed
+ * out in the order of the sequences and their heads. */
+int grkv_pages_extend(const grkv_pages* pages, const grkv_step* step, const int32_t* counts,
+                      const int32_t* seen, int32_t* starts, int32_t* positions, int64_t* slots,
+                      int32_t* status, void* stream, void* workspace, size_t workspace_bytes);
+
+/* 256-byte aligned; 0 if invalid. */
+size_t grkv_pages_extend_workspace_bytes(const grkv_pages* pages, const grkv_step* step);
+
+/* Rotary positions: the first `dims` columns of a row are dims / 2 pairs (a, b), columns
+ * (2 i, 2 i + 1) where interleaved, else (i, i + dims / 2); at position p pair i becomes
+ *   scale * (a cos x - b sin x, a sin x + b cos x),  x = p freqs[i],
+ * or with `inverse` the same with -x, which carries a gradient back through the call.  Angles
+ * are formed in 64 bits; the other columns stay as they are. */
+typedef struct {
+  const double* freqs;  /* [dims / 2], device memory: radians per position */
+  int32_t dims;         /* even, 2 .. head_dim */
+  int32_t interleaved;
+  int32_t inverse;
+  float scale;
+} grkv_rotation;
+
+/* Rows of heads: column c of head h of token t at data[t * token_stride + h * head_stride + c]
+ * (strides in elements, any layout with whole rows). */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride;
+} grkv_rows;
+
+/* y = x rotated: `heads` rows of head_dim columns for each of `tokens` tokens at positions
+ * int32 [tokens] (any sign; rows of a token at GRKV_NO_POSITION are left as they were).  y is x
+ * itself (data and strides) or does not overlap it.  Float32 inside, rounded once.  Rows
+ * whose addresses and parts are multiples of 16 bytes take the fast path. */
+int grkv_rotary(const grkv_rows* x, const grkv_rows* y, int32_t tokens, int32_t heads,
+                int32_t head_dim, int32_t dtype, const int32_t* positions,
+                const grkv_rotation* rotation, void* stream);
+
+/* Host only: the frequencies of base^(-2 i / dims) radians, scaled for contexts `factor` (>= 1)
+ * times as long as the `length` that a model was trained at, into freqs [dims / 2] (host memory):
+ *   GRKV_ROTARY_PLAIN   as they are
+ *   GRKV_ROTARY_LINEAR  divided by factor
+ *   GRKV_ROTARY_BASE    of base * factor^(dims / (dims - 2)): the lowest divided by factor (2 dims:
+ *                       as they are)
+ *   GRKV_ROTARY_PARTS   f (1 - y + y factor) / factor with y = (length f / (2 pi) - low) / (high - low)
+ *                       taken to 0 .. 1: pairs that make `high` turns or more over the length
+ *                       stay, those of `low` or fewer are divided (arXiv 2309.00071, Sec. 3.2) */
+#define GRKV_ROTARY_PLAIN 0
+#define GRKV_ROTARY_LINEAR 1
+#define GRKV_ROTARY_BASE 2
+#define GRKV_ROTARY_PARTS 3
+int grkv_rotary_freqs(int32_t dims, double base, int32_t method, double factor, double length,
+                      double low, double high, double* freqs);
+
+/* Stores the step's keys and values: row (t, h) of k and v goes to row slots[t * slot_stride + h]
+ * of the pool's k and v, rounded to the pool's type; a negative slot, or one past the pool's
+ * rows, stores nothing.  With a rotation (whose `inverse` is not read as a special case) keys
+ * are rotated by positions, and so are q's `q_heads` rows into q_out (as in grkv_rotary);
+ * rows of tokens at GRKV_NO_POSITION are left as they were.  rotation NULL: positions and q are
+ * not read.  q_heads 0: no queries.  k, v and q have head_dim columns of one type, dtype.  Slots of
+ * a call are different from one another (grkv_pages_extend's are). */
+int grkv_pages_store(const grkv_pages* pages, int32_t tokens, int32_t heads, const int64_t* slots,
+                     int64_t slot_stride, const grkv_rows* k, const grkv_rows* v, int32_t dtype,
+                     const grkv_rows* q, const grkv_rows* q_out, int32_t q_heads,
+                     const int32_t* positions, const grkv_rotation* rotation, void* stream);
+
+/* Attention of the new tokens: the c = starts[b + 1] - starts[b] (`longest` at most) tokens of
+ * sequence b are the last c slots of each of its units, query head h * group + g reads
+ * the unit of head h, and query i sees the slots j <= p = L - c + i, with window > 0 only
+ * j > p - window or j < n_sink:
+ *   q, o  pages' dtype [tokens][heads * group][head_dim], 16-byte aligned
+ *   lse   float [tokens][heads * group], or NULL
+ * as in grkv_tree_attention, also for queries that see nothing, values that are not seen, and
+ * roundings.  Rows of no sequence, and those from a sequence's `longest` on, stay as they
+ * were.  `longest` bounds the workspace.  Of a refused sequence (grkv_pages_extend) the rows
+ * mean nothing. */
+typedef struct {
+  int32_t group;    /* query heads per unit, >= 1 */
+  int32_t longest;  /* most new tokens of a sequence, >= 1 */
+  int32_t window;   /* >= 0; 0: none */
+  int32_t n_sink;   /* >= 0 (not read without a window) */
+} grkv_chunk;
+
+int grkv_chunk_attention(const void* q, const grkv_pages* pages, const grkv_step* step,
+                         const int32_t* starts, const grkv_chunk* chunk, void* o, float* lse,
+                         void* stream, void* workspace, size_t workspace_bytes);
+
+size_t grkv_chunk_attention_workspace_bytes(const grkv_pages* pages, const grkv_step* step,
+                                            const grkv_chunk* chunk);
+
+/* These are asynchronous on stream, allocate nothing and may be captured.  Errors: those of the
+ * calls on pages; GRKV_ERR_INVALID for null pointers and sizes out of range (sequences *
+ * heads >= 2^24, tokens * heads or tokens * head_dim >= 2^31, heads or q_heads of a
+ * store or a rotation > 65535, tokens * heads * group >= 2^30, a chunk call of 2^24
+ * row tiles or more), a factor below 1 or other constants that are not finite and
+ * positive; GRKV_ERR_UNSUPPORTED for head_dim > 32768 of grkv_rotary. */
+
 /* Workspace bytes grkv_compress needs for this shape; 0 if the shape is
  * invalid or unsupported. */
 size_t grkv_workspace_bytes(const grkv_problem* prob, int64_t n,

@@ -23,7 +23,9 @@ __all__ = [
     "compress_scored", "h2o_workspace_bytes", "Pages", "new_pages", "pages_init", "pages_append",
     "pages_fork", "pages_compact", "pages_free", "pages_workspace_bytes", "PAGES_OK", "PAGES_FULL",
     "PAGES_LENGTH", "PAGES_UNIT", "PAGES_RANGE", "tree_attention", "sink_attention",
-    "tree_attention_workspace_bytes", "sink_attention_workspace_bytes",
+    "tree_attention_workspace_bytes", "sink_attention_workspace_bytes", "Step", "pages_extend",
+    "pages_extend_workspace_bytes", "rotary", "rotary_freqs", "NO_POSITION", "pages_store",
+    "chunk_attention", "chunk_attention_workspace_bytes",
 ]
 
 GRKV_OK, GRKV_ERR_INVALID, GRKV_ERR_WORKSPACE, GRKV_ERR_UNSUPPORTED, GRKV_ERR_HIP = 0, -1, -2, -3, -4
@@ -40,10 +42,15 @@ EXPORTED_SYMBOLS = ("grkv_compress", "grkv_workspace_bytes", "grkv_workspace_lay
                     "grkv_pages_append", "grkv_pages_fork", "grkv_pages_compact",
                     "grkv_pages_free", "grkv_pages_workspace_bytes", "grkv_tree_attention",
                     "grkv_tree_attention_workspace_bytes", "grkv_sink_attention",
-                    "grkv_sink_attention_workspace_bytes")
+                    "grkv_sink_attention_workspace_bytes", "grkv_pages_extend",
+                    "grkv_pages_extend_workspace_bytes", "grkv_rotary", "grkv_rotary_freqs",
+                    "grkv_pages_store", "grkv_chunk_attention",
+                    "grkv_chunk_attention_workspace_bytes")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 KEY_CONVERGED, KEY_MAX_ITER, KEY_SKIPPED, KEY_BREAKDOWN = 1, 2, 3, 4
 PAGES_OK, PAGES_FULL, PAGES_LENGTH, PAGES_UNIT, PAGES_RANGE = 0, 1, 2, 3, 4
+NO_POSITION = -(1 << 31)
+ROTARY_METHODS = ("plain", "linear", "base", "parts")
 CARRIER_METRICS = ("b", "b_eff", "a_max", "gini", "boundary_fraction", "boundary_share",
                    "enrichment", "boundary_interior_load")
 
@@ -102,6 +109,26 @@ class _Tree(ctypes.Structure):
     _fields_ = [("entries", ctypes.c_int32), ("group", ctypes.c_int32), ("tokens", ctypes.c_int32),
                 ("units", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("parents", ctypes.c_void_p),
                 ("trees", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32)]
+
+
+class _StepC(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int32), ("heads", ctypes.c_int32), ("units", ctypes.c_void_p),
+                ("unit_stride", ctypes.c_int64), ("tokens", ctypes.c_int32)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("freqs", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("inverse", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class _Chunk(ctypes.Structure):
+    _fields_ = [("group", ctypes.c_int32), ("longest", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("n_sink", ctypes.c_int32)]
 
 
 _LIB = None
@@ -194,6 +221,19 @@ def lib() -> ctypes.CDLL:
                                           P(Problem), vp, vp, vp, sz]
         L.grkv_sink_attention_workspace_bytes.restype = sz
         L.grkv_sink_attention_workspace_bytes.argtypes = [P(Problem), ctypes.c_int64, i32, i32, i32]
+        st, rw, i64, f64 = P(_StepC), P(_Rows), ctypes.c_int64, ctypes.c_double
+        for name, res, args in (
+                ("pages_extend", ctypes.c_int, [pg, st, vp, vp, vp, vp, vp, vp, vp, vp, sz]),
+                ("pages_extend_workspace_bytes", sz, [pg, st]),
+                ("rotary", ctypes.c_int, [rw, rw, i32, i32, i32, i32, vp, P(_Rotation), vp]),
+                ("rotary_freqs", ctypes.c_int, [i32, f64, i32, f64, f64, f64, f64, vp]),
+                ("pages_store", ctypes.c_int, [pg, i32, i32, vp, i64, rw, rw, i32, rw, rw, i32, vp,
+                                               P(_Rotation), vp]),
+                ("chunk_attention", ctypes.c_int, [vp, pg, st, vp, P(_Chunk), vp, vp, vp, vp, sz]),
+                ("chunk_attention_workspace_bytes", sz, [pg, st, P(_Chunk)])):
+            fn = getattr(L, "grkv_" + name)
+            fn.restype = res
+            fn.argtypes = args
         L.grkv_status_string.restype = ctypes.c_char_p
         L.grkv_status_string.argtypes = [ctypes.c_int]
         _LIB = L
@@ -959,4 +999,258 @@ def sink_attention(q, K, V, window: int, n_sink: int = 4, *, return_lse: bool = 
     _check(L.grkv_sink_attention(q.data_ptr(), K.data_ptr(), V.data_ptr(), n, nq, window, n_sink,
                                  handle, prob, out.data_ptr(), lp, workspace.data_ptr(),
                                  workspace.numel()))
+    return (out, lse) if return_lse else out
+
+
+# ------------------------------------------------- a served model's step ----
+
+def rotary_freqs(dims: int, base: float = 1e4, *, method: str = "plain", factor: float = 1.0,
+                 length: float = 0.0, low: float = 1.0, high: float = 32.0, device=None):
+    """Radians per position of the ``dims`` / 2 pairs, float64 [dims / 2] on ``device``
+    (grkv_rotary_freqs): "plain", or for contexts ``factor`` times as long as ``length`` "linear",
+    "base" or "parts" (pairs of ``high`` turns over the length stay, those of ``low`` are
+    divided)."""
+    import torch
+
+    if method not in ROTARY_METHODS:
+        raise ValueError("method must be one of %s" % (ROTARY_METHODS,))
+    _int32(dims)
+    out = torch.empty(max(dims // 2, 1), dtype=torch.float64)
+    _check(lib().grkv_rotary_freqs(dims, float(base), ROTARY_METHODS.index(method), float(factor),
+                                   float(length), float(low), float(high), out.data_ptr()))
+    return out if device is None else out.to(device)
+
+
+def _rotation(freqs, scale, interleaved, inverse, dev):
+    import torch
+
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or freqs.get_device() != dev or not freqs.is_contiguous():
+        raise ValueError("freqs must be a contiguous float64 vector on cuda:%d" % dev)
+    return _Rotation(freqs.data_ptr(), 2 * freqs.shape[0], bool(interleaved), bool(inverse), scale)
+
+
+def _rows(t, name, dev, tokens=None, distinct=False):
+    """A [tokens, heads, columns] tensor of whole rows."""
+    if t.get_device() != dev or _dtype_code(t) is None or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError("%s must be a bfloat16 or float32 [tokens, heads, columns] tensor on cuda:%d whose "
+                         "last dimension is contiguous" % (name, dev))
+    if tokens is not None and t.shape[0] != tokens:
+        raise ValueError("%s has %d tokens, expected %d" % (name, t.shape[0], tokens))
+    if distinct:   # rows that are written do not overlap
+        ends = t.shape[2]
+        for step, n in sorted((t.stride(i), t.shape[i]) for i in (0, 1) if t.shape[i] > 1):
+            if step < ends:
+                raise ValueError("%s has rows that overlap" % name)
+            ends = step * (n - 1) + ends
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _out_rows(x, out, name, dev):
+    """The output of rotated rows: ``out``, or a tensor like x."""
+    import torch
+
+    if out is None:
+        out = torch.empty_like(x)
+    if out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("%s must have %s and dtype %s" % (name, tuple(x.shape), x.dtype))
+    if out.data_ptr() == x.data_ptr() and out.stride() != x.stride() and x.numel() > 0:
+        raise ValueError("%s overlaps its input" % name)
+    return out, _rows(out, name, dev, distinct=True)
+
+
+def rotary(x, positions, freqs, *, scale: float = 1.0, interleaved: bool = False,
+           inverse: bool = False, out=None, stream=None):
+    """Rows rotated by their positions (grkv_rotary): x [tokens, heads, columns], bfloat16 or
+    float32, of any strides with whole rows (queries as ``compress`` takes them, [G, w, d], as
+    ``x.transpose(0, 1)``); positions int32 [tokens]; freqs float64 [dims / 2] (``rotary_freqs``).
+    Pairs are columns (i, i + dims / 2), or (2 i, 2 i + 1) with ``interleaved``; columns from
+    dims on stay.  ``inverse`` rotates back, which is the gradient of the call.  ``out`` may be x.
+    Rows at NO_POSITION are left as they were.  Returns out."""
+    import torch
+
+    dev = x.get_device()
+    if dev < 0:
+        raise ValueError("x must be a device tensor")
+    handle, on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return rotary(x, positions, freqs, scale=scale, interleaved=interleaved, inverse=inverse,
+                          out=out)
+    xr = _rows(x, "x", dev)
+    out, yr = _out_rows(x, out, "out", dev)
+    T, H, d = x.shape
+    _int32(T | H | d)
+    _check(lib().grkv_rotary(xr, yr, T, H, d, _dtype_code(x), _vector(positions, "positions", torch.int32, T, dev),
+                             _rotation(freqs, scale, interleaved, inverse, dev), handle))
+    return out
+
+
+def _step(pages, B, T, heads, units):
+    """The sequences of a step and their units."""
+    import torch
+
+    at, stride = None, 0
+    if units is not None:
+        if (units.dtype != torch.int32 or units.get_device() != pages.k.get_device() or units.dim() != 2
+                or units.shape[0] != B or (units.shape[1] > 1 and units.stride(1) != 1)):
+            raise ValueError("units must be an int32 [%d, heads] tensor on the pool's device whose last "
+                             "dimension is contiguous" % B)
+        if heads is not None and heads != units.shape[1]:
+            raise ValueError("units has %d heads, not %d" % (units.shape[1], heads))
+        heads, at = units.shape[1], units.data_ptr()
+        stride = units.stride(0) if B > 1 else max(units.stride(0), heads)
+    elif heads is None:
+        raise ValueError("a step needs units or heads")
+    _int32(B | T | heads)
+    return _StepC(B, heads, at, stride, T)
+
+
+@dataclass
+class Step:
+    """What ``pages_extend`` gives for the new tokens of a step."""
+    starts: "object"      # int32 [sequences + 1]: a sequence's rows are starts[b] .. starts[b + 1] - 1
+    positions: "object"   # int32 [tokens], NO_POSITION where there is none
+    slots: "object"       # int64 [tokens, heads]: rows of the pool, -1 where there is none
+    status: "object"      # int32 [sequences]: PAGES_OK, or why a sequence is as it was
+
+
+def pages_extend_workspace_bytes(pages: Pages, sequences: int, heads: int, tokens: int) -> int:
+    _int32(sequences | heads | tokens)
+    return int(lib().grkv_pages_extend_workspace_bytes(pages._c, _StepC(sequences, heads, None, 0, tokens)))
+
+
+def pages_extend(pages: Pages, counts, tokens: int, *, heads=None, units=None, seen=None, out=None,
+                 workspace=None, stream=None) -> Step:
+    """Grows the units of sequences by their new tokens, and gives every token's position and
+    slots (grkv_pages_extend).
+
+    counts: int32 [B], the new tokens of each sequence, packed into ``tokens`` rows.  ``units``:
+    int32 [B, heads] (default: unit b * heads + h).  ``seen``: int32 [B], the tokens that a
+    sequence had (default: the length of its first unit).  ``out``: the Step of a previous call
+    of these sizes, written again."""
+    import torch
+
+    dev, i32 = pages.k.get_device(), torch.int32
+    handle, on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return pages_extend(pages, counts, tokens, heads=heads, units=units, seen=seen, out=out,
+                                workspace=workspace)
+    B = counts.shape[0] if counts.dim() else 0
+    st = _step(pages, B, tokens, heads, units)
+    if out is None:
+        if min(tokens, st.heads) < 0:
+            raise ValueError("a step needs heads, and tokens of 0 or more")
+        out = Step(torch.empty(B + 1, dtype=i32, device=dev), torch.empty(tokens, dtype=i32, device=dev),
+                   torch.empty((tokens, st.heads), dtype=torch.int64, device=dev),
+                   torch.empty(B, dtype=i32, device=dev))
+    else:
+        _given(out.slots, "out.slots", torch.int64, (tokens, st.heads), dev)
+    L = lib()
+    args = (_vector(counts, "counts", i32, B, dev), _vector(seen, "seen", i32, B, dev),
+            _vector(out.starts, "out.starts", i32, B + 1, dev),
+            _vector(out.positions, "out.positions", i32, tokens, dev), out.slots.data_ptr(),
+            _vector(out.status, "out.status", i32, B, dev))
+    workspace = _workspace(workspace, L.grkv_pages_extend_workspace_bytes(pages._c, st), dev)
+    _check(L.grkv_pages_extend(pages._c, st, *args, handle, workspace.data_ptr(), workspace.numel()))
+    if B == 0:   # (the call does nothing)
+        out.starts.zero_()
+        out.positions.fill_(NO_POSITION)
+        out.slots.fill_(-1)
+    return out
+
+
+def pages_store(pages: Pages, slots, k, v, *, q=None, positions=None, freqs=None, scale: float = 1.0,
+                interleaved: bool = False, out=None, stream=None):
+    """Stores a step's keys and values at their slots, keys rotated (grkv_pages_store).
+
+    slots: int64 [tokens, heads] (``pages_extend``; a layer's columns of a model's); k, v:
+    [tokens, heads, d], bfloat16 or float32, of any strides with whole rows, rounded to the
+    pool's type.  With ``freqs`` (float64 [dims / 2]) and ``positions`` (int32 [tokens]) keys are
+    rotated as by ``rotary``, and so are queries q [tokens, query heads, d] of k's type into ``out``
+    (which may be q).  Returns out, None without q."""
+    import torch
+
+    dev = pages.k.get_device()
+    handle, on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return pages_store(pages, slots, k, v, q=q, positions=positions, freqs=freqs, scale=scale,
+                               interleaved=interleaved, out=out)
+    kr = _rows(k, "k", dev)
+    T, H, d = k.shape
+    vr = _rows(v, "v", dev, T)
+    _int32(T | H)
+    if v.shape != k.shape or v.dtype != k.dtype or d != pages._c.head_dim:
+        raise ValueError("shape mismatch: k %s %s v %s %s head_dim %d"
+                         % (tuple(k.shape), k.dtype, tuple(v.shape), v.dtype, pages._c.head_dim))
+    if (slots.dtype != torch.int64 or slots.get_device() != dev or slots.shape != (T, H)
+            or (H > 1 and slots.stride(1) != 1)):
+        raise ValueError("slots must be an int64 [%d, %d] tensor on cuda:%d whose last dimension is "
+                         "contiguous" % (T, H, dev))
+    if (freqs is None) != (positions is None) or (q is not None and freqs is None):
+        raise ValueError("positions and freqs belong together, and q needs them")
+    if out is not None and q is None:
+        raise ValueError("out belongs to q")
+    rot = qr = yr = at = None
+    Q = 0
+    if freqs is not None:
+        rot, at = _rotation(freqs, scale, interleaved, False, dev), _vector(positions, "positions", torch.int32, T, dev)
+    if q is not None:
+        qr = _rows(q, "q", dev, T)
+        out, yr = _out_rows(q, out, "out", dev)
+        Q = q.shape[1]
+        _int32(Q)
+        if q.shape[2] != d or q.dtype != k.dtype:
+            raise ValueError("q must have k's columns and dtype")
+    _check(lib().grkv_pages_store(pages._c, T, H, slots.data_ptr(), max(slots.stride(0), H) if T < 2 else
+                                  slots.stride(0), kr, vr, _dtype_code(k), qr, yr, Q, at, rot, handle))
+    return out
+
+
+def chunk_attention_workspace_bytes(pages: Pages, sequences, heads, tokens, group, longest=None, window=0,
+                                    n_sink=0) -> int:
+    longest = max(tokens, 1) if longest is None else longest
+    _int32(sequences | heads | tokens | group | longest | window | n_sink)
+    return int(lib().grkv_chunk_attention_workspace_bytes(
+        pages._c, _StepC(sequences, heads, None, 0, tokens), _Chunk(group, longest, window, n_sink)))
+
+
+def chunk_attention(q, pages: Pages, starts, *, heads=None, units=None, longest=None, window: int = 0,
+                    n_sink: int = 0, return_lse: bool = False, out=None, lse=None, workspace=None,
+                    stream=None):
+    """Attention of a step's new tokens over their units (grkv_chunk_attention).
+
+    q: [tokens, heads * G, d] of the pool's type, the tokens of all sequences one behind the other;
+    starts: int32 [B + 1] (``pages_extend``), sequence b's rows; its keys and values are the
+    last slots of the sequence's units.  ``units``: int32 [B, heads] (default: unit b * heads +
+    h).  ``longest``: the most new tokens of a sequence (default: all rows), which bounds the
+    workspace.  ``window`` > 0: only the last ``window`` slots and the first ``n_sink``.  Rows of no
+    sequence stay as they were.  Returns o, with ``return_lse`` (o, lse float32 [tokens, heads *
+    G])."""
+    import torch
+
+    dev = pages.k.get_device()
+    handle, on = _on(dev, stream)
+    if on is not None:
+        with on:
+            return chunk_attention(q, pages, starts, heads=heads, units=units, longest=longest, window=window,
+                                   n_sink=n_sink, return_lse=return_lse, out=out, lse=lse, workspace=workspace)
+    if q.get_device() != dev or q.dtype != pages.k.dtype or q.dim() != 3 or not q.is_contiguous():
+        raise ValueError("q must be a contiguous [tokens, query heads, d] tensor of the pool's type and device")
+    T, Q, d = q.shape
+    B = starts.shape[0] - 1 if starts.dim() else -1
+    if B < 0:
+        raise ValueError("starts must hold a number for each sequence and one more")
+    st = _step(pages, B, T, heads, units)
+    if d != pages._c.head_dim or st.heads < 1 or Q < 1 or Q % st.heads:
+        raise ValueError("q %s does not fit %d heads of %d columns" % (tuple(q.shape), st.heads, pages._c.head_dim))
+    longest = max(T, 1) if longest is None else int(longest)
+    _int32(longest | window | n_sink)
+    ch = _Chunk(Q // st.heads, longest, window, n_sink)
+    out, lse, lp = _outputs(q, (T, Q), dev, out, lse, return_lse)
+    L = lib()
+    workspace = _workspace(workspace, L.grkv_chunk_attention_workspace_bytes(pages._c, st, ch), dev)
+    _check(L.grkv_chunk_attention(q.data_ptr(), pages._c, st, _vector(starts, "starts", torch.int32, B + 1, dev), ch,
+                                  out.data_ptr(), lp, handle, workspace.data_ptr(), workspace.numel()))
     return (out, lse) if return_lse else out

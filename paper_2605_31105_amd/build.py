@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libgrkv.so")
 SOURCES = ["attention.hip", "stream.hip", "selection.hip", "merge.hip", "solve_big.hip", "merge_generic.hip", "key.hip", "key_ring.hip", "carrier.hip", "frontend.hip",
-           "h2o.hip", "noalloc.hip", "api.hip", "pages.hip", "attend.hip", "attend_wide.hip", "serving_api.hip"]
+           "h2o.hip", "noalloc.hip", "api.hip", "pages.hip", "attend.hip", "attend_wide.hip", "serving_api.hip",
+           "extend.hip", "rotary.hip", "chunk.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -22,6 +22,12 @@ constexpr float kMoveLog = 16.f, kMoveSum = 0x1p16f;   // log2 of it, and it
 constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
 constexpr float kLn2 = 0.6931471805599453f;
 
+// What the rows of a call are: queries over contiguous keys, drafted tokens over pages, or
+// the new tokens of a step over pages (packed, each seeing the slots up to its own).
+enum Rows { kContiguous, kTree, kChunk };
+
+constexpr int64_t kWhole = INT64_MIN;   // in place of a partial row: rows that are no part, but outputs
+
 // The slots a block's rows may see, in tiles of TK: tiles 0 .. at - 1 (sinks)
 // and bt .. (the window), `nt` in all; `full` slots before `lim` and from `lo` on
 // (or among the sinks) are seen by every row.
@@ -32,21 +38,21 @@ struct Span {
   int chunk, ns;   // tiles per split, splits in use
 };
 
-__device__ __forceinline__ Span make_span(const AttendK& a, int len, int base, int t, int i0, int i1,
-                                          int tk) {
+__device__ __forceinline__ Span make_span(const AttendK& a, bool tree, int len, int base, int t, int i0,
+                                          int i1, int tk) {
   Span s;
-  if (a.lens) {   // drafted tokens i0 .. i1 lie at positions base .. base + t - 1
+  if (tree) {     // drafted tokens i0 .. i1 lie at positions base .. base + t - 1
     s.kend = t > 0 ? len : 0;
     s.lim = base;
     s.lo = base + t - a.window;
   } else {        // query i is position base + i
-    s.kend = base + i1 + 1;
+    s.kend = max(base + i1 + 1, 0);   // (base below zero: a step's unit shorter than its new tokens)
     s.lim = base + i0 + 1;
     s.lo = base + i1 + 1 - a.window;
   }
   s.at = s.bt = 0;
   if (a.window > 0) {
-    const int first = (a.lens ? base : base + i0) + 1 - a.window;
+    const int first = (tree ? base : base + i0) + 1 - a.window;
     s.at = (min(a.n_sink, s.kend) + tk - 1) / tk;
     s.bt = max(first > 0 ? first / tk : 0, s.at);
   } else {
@@ -105,6 +111,18 @@ __device__ __forceinline__ void entry_shape(const AttendK& a, int e, int* len, i
     *t = a.tokens;
     *row = nullptr;
   }
+}
+
+// Where query i of head g of entry e lies among the rows of q and o.
+template <Rows KIND>
+__device__ __forceinline__ size_t row_at(const AttendK& a, int e, int g, int i) {
+  if (KIND == kChunk) return (size_t)i * a.q_heads + g;   // (q is the entry's first row)
+  return ((size_t)e * a.group + g) * a.tokens + i;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | lo);
 }
 
 // Four values of output row `at`: x / l; lse from the reference m and the sum
@@ -239,10 +257,10 @@ struct RowSight {
   uint64_t bits;
 };
 
-template <bool PAGED>
+template <bool TREE>
 __device__ __forceinline__ bool sees(const RowSight& s, int j, int n_sink, int base, int len) {
   bool on = j < s.lim && (j >= s.lo || j < n_sink);
-  if (PAGED) {
+  if (TREE) {
     const int n = j - base;
     on |= n >= 0 && n < 64 && j < len && (s.bits >> (n & 63) & 1) != 0;
   }
@@ -250,14 +268,14 @@ __device__ __forceinline__ bool sees(const RowSight& s, int j, int n_sink, int b
 }
 
 // The same of slots slot0 .. slot0 + 31, a bit each.
-template <bool PAGED>
+template <bool TREE>
 __device__ __forceinline__ uint32_t sees32(const RowSight& s, int slot0, int n_sink, int base, int len) {
   auto below = [&](int end) {   // the slots before `end`
     const int n = end - slot0;
     return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u;
   };
   uint32_t on = below(s.lim) & (~below(s.lo) | below(n_sink));
-  if (PAGED) {
+  if (TREE) {
     const int n = slot0 - base;   // drafted token of the first of them
     const uint32_t d = n >= 64 || n <= -32 ? 0u
                        : n >= 0 ? (uint32_t)(s.bits >> n) : (uint32_t)(s.bits << -n);
@@ -302,18 +320,18 @@ __device__ __forceinline__ void draft_family(const AttendK& a, int e, int t, int
 
 // The row of (query i, head) with drafted token i's family and depth held by
 // lane i.
-template <bool PAGED>
+template <bool TREE>
 __device__ __forceinline__ RowSight row_sight(const AttendK& a, int base, int i, bool on,
                                               uint64_t family, int depth) {
   RowSight s;
   int pos = base + i;
   s.bits = 0;
-  if (PAGED) {
+  if (TREE) {
     const uint64_t f = __shfl((unsigned long long)family, i & 63);
     pos = base + __shfl(depth, i & 63);
     if (on) s.bits = f;
   }
-  s.lim = on ? (PAGED ? base : pos + 1) : 0;
+  s.lim = on ? (TREE ? base : pos + 1) : 0;
   s.lo = a.window > 0 ? pos + 1 - a.window : 0;
   return s;
 }
@@ -361,13 +379,14 @@ __device__ __forceinline__ bool far_off(float sum, float nref) {
 // reached rows that do not see it (0 x inf in a product is NaN), where large values overflowed
 // under a reference that was too low, and where weights are far off.  One wave; rows first ..
 // first + count - 1 of entry e over tiles vt0 .. vt1 - 1 of sn, left as partial rows
-// from `part` on or (part < 0) as outputs.  A lane forms the weight of one key of 64, then
+// from `part` on or (kWhole) as outputs.  A lane forms the weight of one key of 64, then
 // sums D / 64 columns.
-template <typename E, int D, bool PAGED>
+template <typename E, int D, Rows KIND>
 __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, int e, int64_t part, int first,
                                             int count, int vt0, int vt1, int tk, int len, int t,
                                             const int32_t* trow, uint64_t family, int depth) {
   constexpr bool BF = sizeof(E) == 2;
+  constexpr bool PAGED = KIND != kContiguous, TREE = KIND == kTree;
   constexpr int C = D / 64;
   const int lane = threadIdx.x & 63, R = a.group * a.tokens, base = len - t;
   auto value = [](E x) -> float {
@@ -382,8 +401,8 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
   for (int n = 0; n < count; ++n) {
     const int r = first + n, i = group_of(a, r), g = r - i * a.group;
     if (r >= R) return;
-    const RowSight sight = row_sight<PAGED>(a, base, i, i < t, family, depth);
-    const size_t at = ((size_t)e * a.group + g) * a.tokens + i;
+    const RowSight sight = row_sight<TREE>(a, base, i, i < t, family, depth);
+    const size_t at = row_at<KIND>(a, e, g, i);
     if (i >= t) continue;
     const E* q = (const E*)a.q + at * D;
     float m = -kUnset, l = 0.f, o[C] = {};
@@ -391,7 +410,7 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
       const int slot0 = (vt < sn.at ? vt : vt - sn.at + sn.bt) * tk;
       for (int j0 = slot0; j0 < slot0 + tk; j0 += 64) {
         const int j = j0 + lane;
-        const bool on = j < slot0 + tk && j < sn.kend && sees<PAGED>(sight, j, a.n_sink, base, len);
+        const bool on = j < slot0 + tk && j < sn.kend && sees<TREE>(sight, j, a.n_sink, base, len);
         float x = -__builtin_huge_valf();
         if (on) {
           const E* k = (const E*)a.k + slot_row(j) * D;
@@ -419,7 +438,7 @@ __device__ __forceinline__ void rows_by_key(const AttendK& a, const Span& sn, in
         }
       }
     }
-    if (part >= 0) {
+    if (part != kWhole) {
       const size_t to = part + r;
       for (int c = 0; c < C; ++c)
         __hip_atomic_store(a.opart + to * D + 64 * c + lane, o[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

@@ -338,6 +338,13 @@ struct AttendK {
   int per_tree;       // entries of a tree
   int max_pages, shift, pages, pool_units;
   int n;
+  // a step (chunk.hip); q, o, lse, tokens and row_groups are an entry's own
+  const int32_t* starts;
+  int64_t unit_stride;
+  int sequences, heads, q_heads, longest, step_tokens;
+  int part_rows;      // rows of a partial result
+  int64_t jobs;
+  int4* ends;         // [blocks] the entry rows that a block began and others went on with
 };
 struct AttendPlan {
   int rt;             // 16-row tiles of a block; 0: the wide kernel
@@ -352,5 +359,51 @@ constexpr int kWideKeys = 64;   // keys of a tile of the wide kernel (attend_wid
 hipError_t launch_attend_wide(const AttendK& a, int d, hipStream_t s);
 hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void* workspace,
                          hipStream_t s);
+
+void set_group(AttendK& a);
+
+// Attention of a step's new tokens (chunk.hip): blocks and workspace.
+struct ChunkPlan {
+  int64_t jobs;       // row tiles of all units
+  int blocks, min_part, part_rows;
+  size_t opart, mpart, ends, total;
+};
+ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dtype, int64_t slots);
+hipError_t launch_chunk(AttendK a, const ChunkPlan& p, int d, int dtype, void* workspace, hipStream_t s);
+
+// The units of a step grown (extend.hip).
+struct ExtendLayout {
+  size_t owner, code, first, jobs, ids, total;
+};
+ExtendLayout extend_layout(const grkv_pages* pg, int sequences, int heads);
+hipError_t launch_extend(const grkv_pages* pg, const grkv_step* step, const int32_t* counts,
+                         const int32_t* seen, int32_t* starts, int32_t* positions, int64_t* slots,
+                         int32_t* status, void* workspace, hipStream_t s);
+
+// Rotary positions (rotary.hip).
+struct RotaryK {
+  grkv_rows x, y;
+  uint32_t tokens;
+  int heads, d, dims;
+  bool interleaved, inverse;
+  float scale;
+  const double* freqs;
+  const int32_t* positions;
+  int turned, pieces; // pieces of a head, those that are turned first
+  int per;            // heads of a thread
+};
+struct StoreK {
+  RotaryK r;          // of q
+  grkv_rows k, v;
+  void* pool_k;
+  void* pool_v;
+  int heads;
+  const int64_t* slots;
+  int64_t slot_stride;
+  int64_t rows;       // of the pool
+  int q_groups, k_groups;
+};
+hipError_t launch_rotary(const RotaryK& r, int dtype, hipStream_t s);
+hipError_t launch_store(const StoreK& a, int dtype, int pool_dtype, hipStream_t s);
 
 }  // namespace grkv

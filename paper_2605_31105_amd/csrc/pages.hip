@@ -15,16 +15,12 @@
 //    written once) or, for the few rows of a decoding step, the launches.
 //  * commit_kernel (fork, compact): the table rows and reference counts, after
 //    the rows that move_kernel reads through the old table are copied.
-#include "grkv_device.h"
-#include "grkv_internal.h"
+#include "pages.h"
 
 namespace grkv {
 namespace {
 
-constexpr int kPlanTh = 1024;
 constexpr int kCopyTh = 256;
-constexpr int kNoOwner = 0x7fffffff;
-constexpr int kOwnerUnits = 8192;   // units of a pool whose owners fit the plan's LDS
 
 // What an entry of a call does, written by the plan.  n1 < 0: nothing (a
 // refused entry).
@@ -55,42 +51,12 @@ struct PagesK {
   int32_t* ids;         // [pages] pages handed out, in order
 };
 
-__device__ __forceinline__ int load_agent(const int32_t* p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// Exclusive scan over the block of the plan.  Calls in a row take the halves of
-// `scratch` in turn (`turn` 0, 1, 0, ..), so one barrier each is enough.
-template <typename T>
-__device__ __forceinline__ T plan_scan(T v, T (*scratch)[kPlanTh / 64], int turn, T* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  T incl = v;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const T t = __shfl_up(incl, off);
-    if (lane >= off) incl += t;
-  }
-  if (lane == 63) scratch[turn & 1][wave] = incl;
-  __syncthreads();
-  T before = 0, all = 0;
-#pragma unroll
-  for (int k = 0; k < kPlanTh / 64; ++k) {
-    const T s = scratch[turn & 1][k];
-    if (k < wave) before += s;
-    all += s;
-  }
-  *total = all;
-  return before + incl - v;
-}
-
 // The plan of a call, by one block.  Most calls have at most one entry per thread;
 // then a job stays in its thread's registers until it is complete.
 __device__ __forceinline__ void make_plan_block(const PagesK& a) {
   __shared__ int owner_s[kOwnerUnits];
   // (an entry may ask for 2^26 pages: their sums take 64 bits)
   __shared__ unsigned long long scratch[2][kPlanTh / 64];
-  __shared__ uint32_t scratch32[2][kPlanTh / 64];
-  __shared__ uint32_t taken_s[kPlanTh], rank_s[kPlanTh];   // pages taken of a word, the first one's rank
   __shared__ int used_s;
   const int tid = threadIdx.x, lane = tid & 63;
   const int ps = 1 << a.shift;
@@ -188,34 +154,9 @@ __device__ __forceinline__ void make_plan_block(const PagesK& a) {
     }
   }
 
-  // the lowest free pages, as many as are asked for.  A thread takes a word of 32
-  // pages; the numbers are written two words at a time by a wave, neighbouring lanes
-  // neighbouring numbers, the waves in turn (plans of 2048 and 34k pages 6.3 and 12.4 us;
-  // each wave the words that its lanes hold, 10.1 and 19.2)
+  // the lowest free pages, as many as are asked for
   const uint32_t want = (uint32_t)(need_all < (unsigned)a.pg.pages ? need_all : (unsigned)a.pg.pages);
-  uint32_t found = 0;
-  for (int w0 = 0; w0 < words && found < want; w0 += kPlanTh) {
-    const int w = w0 + tid;
-    const uint32_t bits = w0 == 0 ? bits0 : w < words ? a.pg.free_bits[w] : 0u;
-    uint32_t total;
-    const uint32_t r0 = found + plan_scan((uint32_t)__popc(bits), scratch32, turn++, &total);
-    uint32_t left = 0;
-    if (r0 + __popc(bits) > want) {   // the last word taken from, and those behind it
-      left = bits;
-      for (uint32_t r = r0; r < want; ++r) left &= left - 1;
-    }
-    if (left != bits) a.pg.free_bits[w] = left;
-    taken_s[tid] = bits ^ left;
-    rank_s[tid] = r0;
-    __syncthreads();   // (read before the next scan's barrier)
-    const int here = min(words - w0, kPlanTh), bit = lane & 31;
-    for (int k = (tid >> 6) * 2 + (lane >> 5); k < here; k += kPlanTh / 32) {
-      const uint32_t t = taken_s[k];
-      if (t >> bit & 1) a.ids[rank_s[k] + __popc(t & ((1u << bit) - 1))] = 32 * (w0 + k) + bit;
-    }
-    found += total;
-  }
-  found = found < want ? found : want;
+  const uint32_t found = take_pages(a.pg, want, bits0, a.ids, &turn);
 
   // entries past the free pages are refused; lengths
   int used = 0;

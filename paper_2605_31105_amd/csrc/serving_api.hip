@@ -1,5 +1,7 @@
 // C entry points of the pages of a cache and of the attention that reads them:
 // argument checks on the host, then the launches.
+#include <math.h>
+
 #include "grkv_internal.h"
 
 using namespace grkv;
@@ -123,6 +125,85 @@ int make_sink(const grkv_problem* prob, int64_t n, int32_t nq, int32_t window, i
   a.n_sink = sinks_of(n_sink);
   a.n = (int)n;
   return GRKV_OK;
+}
+
+int check_step(const grkv_pages* pg, const grkv_step* st) {
+  const int ok = check_pages(pg);
+  if (ok != GRKV_OK) return ok;
+  if (!st || st->sequences < 0 || st->heads < 1 || st->tokens < 0) return GRKV_ERR_INVALID;
+  if (st->units && st->unit_stride < st->heads) return GRKV_ERR_INVALID;
+  if ((int64_t)st->sequences * st->heads > kMostBlocks) return GRKV_ERR_INVALID;
+  return (int64_t)st->tokens * st->heads >= (int64_t(1) << 31) ? GRKV_ERR_INVALID : GRKV_OK;
+}
+
+struct ChunkCall {
+  AttendK a;
+  ChunkPlan plan;
+};
+
+int make_chunk(const grkv_pages* pg, const grkv_step* st, const grkv_chunk* ch, ChunkCall* c) {
+  const int ok = check_step(pg, st);
+  if (ok != GRKV_OK) return ok;
+  if (!ch || ch->group < 1 || ch->longest < 1 || ch->window < 0 || ch->n_sink < 0) return GRKV_ERR_INVALID;
+  const int64_t per = (int64_t)st->heads * ch->group;
+  if (per >= (int64_t(1) << 30) || per * st->tokens >= (int64_t(1) << 30)) return GRKV_ERR_INVALID;
+  const int64_t cap = (int64_t)pg->max_pages * pg->page_size;
+  const int window = window_of(ch->window, cap);
+  // (a job's rows, 128 at most, lie at 128 / group + 2 positions or fewer)
+  const int64_t near = (int64_t)ch->n_sink + window + 128 / ch->group + 2;
+  c->plan = chunk_plan(st, ch, pg->head_dim, pg->dtype, window > 0 && near < cap ? near : cap);
+  if (c->plan.jobs > kMostBlocks) return GRKV_ERR_INVALID;
+  AttendK& a = c->a;
+  a = AttendK{};
+  a.k = pg->k;
+  a.v = pg->v;
+  a.group = ch->group;
+  a.window = window;
+  a.n_sink = sinks_of(ch->n_sink);
+  a.table = pg->table;
+  a.lens = pg->lens;
+  a.units = st->units;
+  a.max_pages = pg->max_pages;
+  a.shift = __builtin_ctz((unsigned)pg->page_size);
+  a.pages = pg->pages;
+  a.pool_units = pg->units;
+  a.unit_stride = st->unit_stride;
+  a.sequences = st->sequences;
+  a.heads = st->heads;
+  a.q_heads = st->heads * ch->group;
+  a.longest = ch->longest;
+  a.step_tokens = st->tokens;
+  return GRKV_OK;
+}
+
+// A rotation of rows of d columns; with rows to rotate, their pieces fit a launch.
+int check_rotation(const grkv_rotation* rot, const int32_t* positions, int32_t d) {
+  if (!rot || !rot->freqs || !positions || !aligned(rot->freqs, 8)) return GRKV_ERR_INVALID;
+  if (rot->dims < 2 || rot->dims > d || rot->dims % 2 != 0) return GRKV_ERR_INVALID;
+  return GRKV_OK;
+}
+
+bool rows_ok(const grkv_rows* r, int dtype) {
+  return r && r->data && aligned(r->data, dtype == GRKV_BF16 ? 2 : 4);
+}
+
+RotaryK rotary_of(const grkv_rows* x, const grkv_rows* y, int32_t tokens, int32_t heads, int32_t d,
+                  const int32_t* positions, const grkv_rotation* rot) {
+  RotaryK r = {};
+  if (x) r.x = *x;
+  if (y) r.y = *y;
+  r.tokens = (uint32_t)tokens;
+  r.heads = heads;
+  r.d = d;
+  if (rot) {
+    r.dims = rot->dims;
+    r.interleaved = rot->interleaved != 0;
+    r.inverse = rot->inverse != 0;
+    r.scale = rot->scale;
+    r.freqs = rot->freqs;
+    r.positions = positions;
+  }
+  return r;
 }
 
 size_t workspace_of(const AttendPlan& p) { return p.total > 256 ? p.total : 256; }
@@ -267,6 +348,118 @@ int grkv_sink_attention(const void* q, const void* K, const void* V, int64_t n, 
   c.a.o = o;
   c.a.lse = lse;
   return run_attend(c, prob->head_dim, prob->dtype, stream, workspace, workspace_bytes);
+}
+
+size_t grkv_pages_extend_workspace_bytes(const grkv_pages* pages, const grkv_step* step) {
+  if (check_step(pages, step) != GRKV_OK) return 0;
+  return extend_layout(pages, step->sequences, step->heads).total;
+}
+
+int grkv_pages_extend(const grkv_pages* pages, const grkv_step* step, const int32_t* counts,
+                      const int32_t* seen, int32_t* starts, int32_t* positions, int64_t* slots,
+                      int32_t* status, void* stream, void* workspace, size_t workspace_bytes) {
+  const int st = check_step(pages, step);
+  if (st != GRKV_OK) return st;
+  if (step->sequences == 0) return GRKV_OK;
+  if (!counts || !starts || (step->tokens > 0 && (!positions || !slots))) return GRKV_ERR_INVALID;
+  if (!workspace || !aligned(workspace, 256)) return GRKV_ERR_INVALID;
+  if (workspace_bytes < grkv_pages_extend_workspace_bytes(pages, step)) return GRKV_ERR_WORKSPACE;
+  return launch_extend(pages, step, counts, seen, starts, positions, slots, status, workspace,
+                       (hipStream_t)stream) == hipSuccess ? GRKV_OK : GRKV_ERR_HIP;
+}
+
+int grkv_rotary(const grkv_rows* x, const grkv_rows* y, int32_t tokens, int32_t heads,
+                int32_t head_dim, int32_t dtype, const int32_t* positions,
+                const grkv_rotation* rotation, void* stream) {
+  if (tokens < 0 || heads < 0 || heads > 65535 || head_dim < 2) return GRKV_ERR_INVALID;
+  if (dtype != GRKV_BF16 && dtype != GRKV_F32) return GRKV_ERR_INVALID;
+  if (head_dim > 32768) return GRKV_ERR_UNSUPPORTED;
+  if ((int64_t)tokens * head_dim >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
+  if (tokens == 0 || heads == 0) return GRKV_OK;
+  const int st = check_rotation(rotation, positions, head_dim);
+  if (st != GRKV_OK) return st;
+  if (!rows_ok(x, dtype) || !rows_ok(y, dtype)) return GRKV_ERR_INVALID;
+  return launch_rotary(rotary_of(x, y, tokens, heads, head_dim, positions, rotation), dtype,
+                       (hipStream_t)stream) == hipSuccess ? GRKV_OK : GRKV_ERR_HIP;
+}
+
+int grkv_rotary_freqs(int32_t dims, double base, int32_t method, double factor, double length,
+                      double low, double high, double* freqs) {
+  if (dims < 2 || dims % 2 != 0 || dims > 32768 || !freqs || !(base > 0.0) || !isfinite(base)) return GRKV_ERR_INVALID;
+  if (method < GRKV_ROTARY_PLAIN || method > GRKV_ROTARY_PARTS) return GRKV_ERR_INVALID;
+  if (method != GRKV_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return GRKV_ERR_INVALID;
+  if (method == GRKV_ROTARY_PARTS &&
+      (!(length > 0.0) || !isfinite(length) || !(low >= 0.0) || !(high > low) || !isfinite(high)))
+    return GRKV_ERR_INVALID;
+  if (method == GRKV_ROTARY_BASE && dims > 2) base *= pow(factor, (double)dims / (dims - 2));
+  for (int i = 0; i < dims / 2; ++i) {
+    double f = pow(base, -2.0 * i / dims);
+    if (method == GRKV_ROTARY_LINEAR) f /= factor;
+    if (method == GRKV_ROTARY_PARTS) {
+      const double turns = length * f / 6.283185307179586477;
+      double stay = (turns - low) / (high - low);
+      stay = stay < 0.0 ? 0.0 : stay > 1.0 ? 1.0 : stay;
+      f = f * stay + f / factor * (1.0 - stay);
+    }
+    freqs[i] = f;
+  }
+  return GRKV_OK;
+}
+
+int grkv_pages_store(const grkv_pages* pages, int32_t tokens, int32_t heads, const int64_t* slots,
+                     int64_t slot_stride, const grkv_rows* k, const grkv_rows* v, int32_t dtype,
+                     const grkv_rows* q, const grkv_rows* q_out, int32_t q_heads,
+                     const int32_t* positions, const grkv_rotation* rotation, void* stream) {
+  int st = check_pages(pages);
+  if (st != GRKV_OK) return st;
+  if (tokens < 0 || heads < 0 || heads > 65535 || q_heads < 0 || q_heads > 65535 || slot_stride < heads)
+    return GRKV_ERR_INVALID;
+  if (dtype != GRKV_BF16 && dtype != GRKV_F32) return GRKV_ERR_INVALID;
+  if ((int64_t)tokens * pages->head_dim >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
+  if (!rotation) q_heads = 0;
+  if (tokens == 0 || heads + q_heads == 0) return GRKV_OK;
+  if (rotation && (st = check_rotation(rotation, positions, pages->head_dim)) != GRKV_OK) return st;
+  if (heads > 0 && (!slots || !rows_ok(k, dtype) || !rows_ok(v, dtype))) return GRKV_ERR_INVALID;
+  if (q_heads > 0 && (!rows_ok(q, dtype) || !rows_ok(q_out, dtype))) return GRKV_ERR_INVALID;
+  StoreK a = {};
+  a.r = rotary_of(q_heads > 0 ? q : nullptr, q_heads > 0 ? q_out : nullptr, tokens, q_heads, pages->head_dim,
+                  positions, rotation);
+  if (heads > 0) {
+    a.k = *k;
+    a.v = *v;
+  }
+  a.pool_k = pages->k;
+  a.pool_v = pages->v;
+  a.heads = heads;
+  a.slots = slots;
+  a.slot_stride = slot_stride;
+  a.rows = (int64_t)pages->pages * pages->page_size;
+  return launch_store(a, dtype, pages->dtype, (hipStream_t)stream) == hipSuccess ? GRKV_OK : GRKV_ERR_HIP;
+}
+
+size_t grkv_chunk_attention_workspace_bytes(const grkv_pages* pages, const grkv_step* step,
+                                            const grkv_chunk* chunk) {
+  ChunkCall c;
+  if (make_chunk(pages, step, chunk, &c) != GRKV_OK) return 0;
+  return c.plan.total;
+}
+
+int grkv_chunk_attention(const void* q, const grkv_pages* pages, const grkv_step* step,
+                         const int32_t* starts, const grkv_chunk* chunk, void* o, float* lse,
+                         void* stream, void* workspace, size_t workspace_bytes) {
+  ChunkCall c;
+  const int st = make_chunk(pages, step, chunk, &c);
+  if (st != GRKV_OK) return st;
+  if (step->sequences == 0 || step->tokens == 0) return GRKV_OK;
+  if (!q || !o || !starts || !aligned(q, 16) || !aligned(o, 16) || !aligned(lse, 4)) return GRKV_ERR_INVALID;
+  if (!workspace || !aligned(workspace, 256)) return GRKV_ERR_INVALID;
+  if (workspace_bytes < c.plan.total) return GRKV_ERR_WORKSPACE;
+  c.a.q = q;
+  c.a.o = o;
+  c.a.lse = lse;
+  c.a.starts = starts;
+  return launch_chunk(c.a, c.plan, pages->head_dim, pages->dtype, workspace, (hipStream_t)stream) == hipSuccess
+             ? GRKV_OK : GRKV_ERR_HIP;
 }
 
 }  // extern "C"

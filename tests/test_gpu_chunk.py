@@ -1,0 +1,266 @@
+"""Attention of a step's new tokens (chunk_attention) against float64 rows, within the bounds of
+tests/attention_ref.py."""
+import math
+
+import pytest
+
+from tests.attention_ref import check, sink_seen
+from tests.test_gpu_attention import BF, F32, _i32, _pool
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _run(name, lens, counts, H, group, ps, d, dtype, window=0, n_sink=0, pad=0, longest=None, heads=None):
+    """A call on units of these lengths (new tokens included), checked row by row; lens [B][H]."""
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + ps)
+    flat = [n for row in lens for n in row]
+    pg, K, V = _pool(flat, ps, d, dtype, gen)
+    B, T = len(counts), sum(counts) + pad
+    q = torch.randn((T, H * group, d), generator=gen).to(dtype)
+    starts = [sum(counts[:b]) for b in range(B + 1)]
+    o = torch.full(q.shape, 5.0, dtype=dtype, device="cuda")
+    lse = torch.full(q.shape[:2], 6.0, device="cuda")
+    G.chunk_attention(q.cuda(), pg, _i32(starts), heads=H, longest=longest, window=window, n_sink=n_sink,
+                      out=o, lse=lse)
+    torch.cuda.synchronize()
+    o, lse = o.cpu(), lse.cpu()
+    assert (o[starts[-1]:] == 5).all() and (lse[starts[-1]:] == 6).all()
+    for b, c in enumerate(counts):
+        m = min(c, longest) if longest else c
+        at = slice(starts[b], starts[b] + m)
+        assert (o[starts[b] + m:starts[b + 1]] == 5).all() and (lse[starts[b] + m:starts[b + 1]] == 6).all()
+        for h in range(H) if heads is None else heads:
+            n, u = lens[b][h], b * H + h
+            seen = sink_seen(n, m, window, n_sink)
+            for g in {0, group - 1}:
+                x = h * group + g
+                check("%s seq %d (%d of %d) head %d" % (name, b, m, n, x), o[at, x], lse[at, x], q[at, x], K[u], V[u],
+                      seen)
+    return o, lse
+
+
+CASES = [
+    # dtype, d, page, group, new tokens, lengths before them (per sequence; units differ by 3), window, sinks
+    (BF, 128, 64, 4, [1, 1, 1], [0, 63, 2000], 0, 0), (BF, 64, 16, 1, [5, 1, 40], [0, 300, 17], 0, 0),
+    (BF, 128, 64, 4, [300, 1, 0, 33, 5], [500, 900, 10, 0, 64], 0, 0), (BF, 128, 16, 5, [129, 2], [77, 1000], 0, 0),
+    (BF, 64, 256, 8, [16, 17, 2, 3], [1000, 0, 5, 64], 0, 0), (BF, 128, 1024, 3, [600], [700], 0, 0),
+    (BF, 64, 32, 7, [100, 1, 9], [900, 900, 900], 100, 4), (BF, 128, 64, 4, [200, 1], [300, 2500], 64, 70),
+    (BF, 128, 64, 16, [1, 2, 40], [100, 100, 100], 1, 0), (BF, 64, 64, 33, [4, 1], [60, 700], 37, 300),
+    (F32, 128, 32, 3, [5, 100, 0, 1], [100, 40, 7, 900], 0, 0), (F32, 64, 16, 4, [33, 1, 1], [0, 16, 500], 0, 0),
+    (F32, 64, 64, 5, [50, 3], [300, 1000], 60, 5), (F32, 128, 16, 17, [3, 1], [100, 31], 0, 0),
+    (BF, 128, 64, 1, [129, 127, 128, 1], [0, 1, 0, 0], 0, 0), (BF, 64, 16, 2, [0, 0, 64, 0, 65, 0], [5] * 6, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "%s-d%d-p%d-g%d-c%s-w%d" % (
+    "bf16" if c[0] == BF else "f32", c[1], c[2], c[3], "_".join(map(str, c[4])), c[6]))
+def test_chunk_attention(case):
+    dtype, d, ps, group, counts, before, window, n_sink = case
+    H = 2
+    lens = [[max(b + 3 * h, 0) + c for h in range(H)] for b, c in zip(before, counts)]
+    _run("case", lens, counts, H, group, ps, d, dtype, window, n_sink, pad=5)
+
+
+@pytest.mark.parametrize("d,dtype", [(128, BF), (64, BF), (64, F32)])
+def test_units_shorter_than_their_new_tokens_and_bad_units(d, dtype):
+    # the first queries see nothing; units outside the pool see nothing; longest cuts
+    import paper_2605_31105_amd as G
+    _run("short", [[3, 0], [40, 100], [0, 200]], [10, 90, 150], 2, 2, 16, d, dtype)
+    _run("window", [[3, 0], [40, 100], [0, 200]], [10, 90, 150], 2, 2, 16, d, dtype, window=20, n_sink=3)
+    _run("cut", [[30, 30], [300, 100]], [30, 90], 2, 3, 16, d, dtype, longest=7, pad=1)
+    gen = torch.Generator().manual_seed(1)
+    pg, K, V = _pool([50, 60], 16, d, dtype, gen)
+    q = torch.randn((6, 4, d), generator=gen).to(dtype).cuda()
+    o, lse = G.chunk_attention(q, pg, _i32([0, 4, 6]), units=_i32([[-1, 1], [0, 99]]), return_lse=True)
+    for rows, heads in ((slice(0, 4), slice(0, 2)), (slice(4, 6), slice(2, 4))):
+        assert (o[rows, heads] == 0).all() and torch.isneginf(lse[rows, heads]).all()
+    check("unit 1", o[:4, 2].cpu(), lse[:4, 2].cpu(), q[:4, 2].cpu(), K[1], V[1], sink_seen(60, 4, 0, 0))
+    check("unit 0", o[4:, 1].cpu(), lse[4:, 1].cpu(), q[4:, 1].cpu(), K[0], V[0], sink_seen(50, 2, 0, 0))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_units_cut_into_many_parts(d):
+    # single tokens over long keys, beside chunks: parts that begin and end inside units
+    _run("long", [[20001, 5], [300, 9000], [1, 1], [4000, 7777]], [1, 3, 1, 1], 2, 4, 64, d, BF)
+    _run("beside", [[20500, 800], [300, 9000]], [500, 1], 2, 4, 64, d, BF, heads=[0, 1])
+    _run("one", [[30000]], [1], 1, 8, 128, d, BF)
+    _run("wide", [[6000]], [40], 1, 4, 128, d, BF)
+
+
+def test_many_sequences_of_one_token():
+    lens = [[1 + (37 * b + 11 * h) % 700 for h in range(3)] for b in range(300)]
+    _run("many", lens, [1] * 300, 3, 4, 16, 64, BF, heads=[1])
+
+
+def test_many_short_jobs_and_idle_sequences():
+    counts = [(b * 7) % 23 if b % 3 else 0 for b in range(150)]
+    lens = [[c + (13 * b) % 90 for _ in range(2)] for b, c in enumerate(counts)]
+    _run("short", lens, counts, 2, 3, 16, 64, BF, pad=9)
+
+
+@pytest.mark.parametrize("dtype,group,counts", [(BF, 2, [6]), (BF, 16, [12, 1]), (F32, 2, [6]), (BF, 4, [100])])
+def test_what_a_query_does_not_see_never_reaches_it(dtype, group, counts):
+    # NaN and infinities among later keys and values, and in the slots behind a unit
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(3)
+    n, d = 70 + counts[0], 64
+    pg, K, V = _pool([n] + [40] * (len(counts) - 1), 16, d, dtype, gen)
+    bad = n - 3
+    q = torch.randn((sum(counts), group, d), generator=gen).to(dtype)
+    starts = _i32([0] + [sum(counts[:b + 1]) for b in range(len(counts))])
+    for value in (math.nan, math.inf, -math.inf):
+        for x in (pg.k, pg.v):
+            x[pg.table[0, bad // 16].long(), bad % 16] = value
+        o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, starts, heads=1, return_lse=True))
+        c = counts[0]
+        before = c - 3                     # queries that lie before the bad slot
+        seen = sink_seen(n, c, 0, 0)[:before, :bad]
+        for g in {0, group - 1}:
+            check("%s head %d" % (value, g), o[:before, g], lse[:before, g], q[:before, g], K[0][:bad], V[0][:bad], seen)
+        assert not torch.isfinite(o[before:c]).all()
+        assert torch.isfinite(o[c:]).all()
+
+
+def test_large_logits_and_values():
+    # growing logits move the reference; weights of zero beside logits past 2^30; values near the largest float
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(5)
+    d, n, c = 64, 400, 40
+    for group in (1, 8):
+        pg, K, V = _pool([n], 16, d, BF, gen)
+        for j in range(n):
+            K[0][j] = 0
+            K[0][j, 0] = j / 4
+        pg.k.view(-1, d)[(pg.table[0].long()[torch.arange(n) // 16] * 16).cpu() + torch.arange(n) % 16] = K[0].cuda()
+        q = torch.zeros((c, group, d), dtype=BF)
+        q[..., 0] = torch.linspace(-20, 20, c)[:, None].to(BF)
+        o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32([0, c]), heads=1, return_lse=True))
+        for g in {0, group - 1}:
+            check("growing", o[:, g], lse[:, g], q[:, g], K[0], V[0], sink_seen(n, c, 0, 0))
+
+
+def test_results_do_not_depend_on_the_workspace_or_the_run():
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(7)
+    lens, counts = [5000, 40, 900, 3000], [1, 30, 200, 2]
+    pg, _, _ = _pool(lens, 64, 128, BF, gen)
+    q = torch.randn((sum(counts), 4, 128), generator=gen).to(BF).cuda()
+    starts = _i32([0, 1, 31, 231, 233])
+    ws = torch.empty(G.chunk_attention_workspace_bytes(pg, 4, 1, 233, 4), dtype=torch.uint8, device="cuda")
+    first = None
+    for fill in (0, 255, 127):
+        ws.fill_(fill)
+        o, lse = G.chunk_attention(q, pg, starts, heads=1, return_lse=True, workspace=ws)
+        if first is None:
+            first = o, lse
+        assert torch.equal(o, first[0]) and torch.equal(lse, first[1])
+
+
+def test_captured_calls_and_another_stream():
+    # lengths and starts change between the replays; two graphs over one workspace
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(11)
+    B, H, group, d, T = 4, 2, 4, 64, 80
+    pg, _, _ = _pool([700] * (B * H), 16, d, BF, gen)
+    pg.k.nan_to_num_(0.0)
+    pg.v.nan_to_num_(0.0)
+    q = torch.randn((T, H * group, d), generator=gen).to(BF).cuda()
+    starts = _i32([0, 1, 2, 60, 61])
+    ws = torch.empty(G.chunk_attention_workspace_bytes(pg, B, H, T, group), dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros_like(q), torch.zeros_like(q)]
+    graphs = []
+    for out in outs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            G.chunk_attention(q, pg, starts, heads=H, out=out, workspace=ws)
+        graphs.append(g)
+    for turn in range(4):
+        starts.copy_(_i32([0, 5 * turn, 5 * turn, 50 + turn, T]))
+        pg.lens[:B * H] = 700 - 130 * turn
+        want = G.chunk_attention(q, pg, starts, heads=H)
+        for g, out in zip(graphs, outs):
+            out.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        for out in outs:
+            assert torch.equal(out, want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o = G.chunk_attention(q, pg, starts, heads=H, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(o, want)
+
+
+def test_agrees_with_the_calls_beside_it():
+    # a chain of drafted tokens, and a prompt over contiguous keys: the same rows, other kernels or
+    # other cuts; each within its bounds of the formula, so within twice those of each other
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(13)
+    d, n, c, group = 128, 500, 12, 4
+    pg, K, V = _pool([n, n], 64, d, BF, gen)
+    q = torch.randn((2, c, group, d), generator=gen).to(BF).cuda()
+    o, lse = G.chunk_attention(q.view(2 * c, group, d), pg, _i32([0, c, 2 * c]), heads=1, return_lse=True)
+    qt = q.transpose(1, 2).contiguous()
+    to, tl = G.tree_attention(qt, pg, units=_i32([0, 1]), return_lse=True)
+    so, sl = G.sink_attention(qt, torch.stack(K).cuda(), torch.stack(V).cuda(), 0, return_lse=True)
+    for x, l in ((to, tl), (so, sl)):
+        for e in range(2):
+            for g in range(group):
+                check("beside", x[e, g].cpu(), l[e, g].cpu(), qt[e, g].cpu(), K[e], V[e], sink_seen(n, c, 0, 0))
+    for e in range(2):
+        for g in range(group):
+            at = slice(e * c, e * c + c)
+            check("chunk", o[at, g].cpu(), lse[at, g].cpu(), qt[e, g].cpu(), K[e], V[e], sink_seen(n, c, 0, 0))
+
+
+def test_units_of_a_layer():
+    # a layer's columns of a model's units
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(17)
+    B, L, H, group, d = 3, 2, 2, 2, 64
+    lens = [20 + 9 * u for u in range(B * L * H)]
+    pg, K, V = _pool(lens, 16, d, BF, gen)
+    every = torch.arange(B * L * H, dtype=torch.int32, device="cuda").view(B, L, H)
+    counts = [1, 12, 3]
+    q = torch.randn((16, H * group, d), generator=gen).to(BF)
+    for layer in range(L):
+        o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32([0, 1, 13, 16]), units=every[:, layer],
+                                                     return_lse=True))
+        at = 0
+        for b, c in enumerate(counts):
+            for h in range(H):
+                u = (b * L + layer) * H + h
+                for x in range(h * group, (h + 1) * group):
+                    check("layer %d" % layer, o[at:at + c, x], lse[at:at + c, x], q[at:at + c, x], K[u], V[u],
+                          sink_seen(lens[u], c, 0, 0))
+            at += c
+
+
+def test_binding_checks():
+    import paper_2605_31105_amd as G
+    pg = G.new_pages(4, 4, 16, 16, 64)
+    q, starts = torch.zeros((3, 4, 64), dtype=BF, device="cuda"), _i32([0, 1, 3])
+    for call in (lambda: G.chunk_attention(q, pg, starts), lambda: G.chunk_attention(q.float(), pg, starts, heads=2),
+                 lambda: G.chunk_attention(q, pg, starts, heads=3), lambda: G.chunk_attention(q[0], pg, starts, heads=2),
+                 lambda: G.chunk_attention(q, pg, starts.long(), heads=2), lambda: G.chunk_attention(q.cpu(), pg, starts, heads=2),
+                 lambda: G.chunk_attention(q[..., :32].contiguous(), pg, starts, heads=2),
+                 lambda: G.chunk_attention(q.transpose(0, 1), pg, starts, heads=1), lambda: G.chunk_attention(q, pg, starts[:0], heads=2),
+                 lambda: G.chunk_attention(q, pg, starts, heads=2, out=q[:2]), lambda: G.chunk_attention(q, pg, starts, units=_i32([[0, 1]])),
+                 lambda: G.chunk_attention(q, pg, starts, heads=2, window=1 << 31)):
+        with pytest.raises(ValueError):
+            call()
+    for kw in (dict(window=-1), dict(n_sink=-1), dict(longest=0)):
+        with pytest.raises(G.GrkvError) as e:
+            G.chunk_attention(q, pg, starts, heads=2, **kw)
+        assert e.value.status == G.GRKV_ERR_INVALID
+    assert G.chunk_attention(q[:0], pg, _i32([0, 0]), heads=2).shape == (0, 4, 64)
+    assert G.chunk_attention_workspace_bytes(pg, 2, 2, 3, 2, longest=0) == 0
