@@ -113,6 +113,21 @@ __device__ __forceinline__ void entry_shape(const AttendK& a, int e, int* len, i
   }
 }
 
+// Of the two blocks of a step's kernel on a compute unit, the waves of the one that started
+// first are served first: with equal work it ended 20% before the other (a 4 x 2048 chunk 1340
+// and 1650 us), which then ran alone.  So the other takes the higher priority every other tile
+// (1345 to 1390 and 1620).  A matter of speed alone.
+__device__ __forceinline__ bool younger_block() { return blockIdx.x >= 256; }
+
+// Page `ord` of a unit's table row, both the same in all lanes.  In a step's kernel, which also
+// writes between the units, the compiler takes such a read through the vector cache, where its
+// wait is one for all tiles in flight, unless told that the table is constant.
+template <Rows KIND>
+__device__ __forceinline__ int page_of(const int32_t* trow, int ord) {
+  if (KIND == kChunk) return ((const __attribute__((address_space(4))) int32_t*)trow)[ord];
+  return trow[ord];
+}
+
 // Where query i of head g of entry e lies among the rows of q and o.
 template <Rows KIND>
 __device__ __forceinline__ size_t row_at(const AttendK& a, int e, int g, int i) {

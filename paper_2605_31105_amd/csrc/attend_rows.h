@@ -102,10 +102,14 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   const char* vb = (const char*)a.v;
   const int last = sn.kend - 1;
   auto slot_of = [&](int vt) { return (vt < sn.at ? vt : vt - sn.at + sn.bt) * TK; };
-  // byte offset of the 16 rows around `slot` (uniform)
-  auto rows16 = [&](int slot) -> size_t {
+  // the page of 16-row part h of tile vt, and the byte offset of its rows (uniform)
+  auto slot16 = [&](int vt, int h) { return __builtin_amdgcn_readfirstlane(min(slot_of(vt) + 16 * h, last)); };
+  auto page16 = [&](int vt, int h) -> int {
+    if (PAGED) return page_of<KIND>(trow, slot16(vt, h) >> a.shift);
+    return 0;
+  };
+  auto rows16 = [&](int slot, int p) -> size_t {
     if (PAGED) {
-      int p = trow[slot >> a.shift];
       p = (unsigned)p < (unsigned)a.pages ? p : 0;
       return (((size_t)p << a.shift) + ((slot & ((1 << a.shift) - 1)) & ~15)) * RB;
     }
@@ -125,12 +129,16 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   // loads of tile vt: V into the stage `vs`, then K into registers (in that
   // order: the K fragments' arrival says that V has arrived too).  Rows past the
   // last slot read the last one again.
+  int ahead[KT];   // pages of the tile to be loaded next (a step's kernel: see wide_rows.h)
+  auto next_tile = [&](int vt) { return min(vt + kAtWaves, vt1 - 1); };   // (past the end: the last tile again)
   auto load = [&](int vt, char* vs, Frag (&kf)[KT][DS]) __attribute__((always_inline)) {
     const int slot0 = slot_of(vt);
     size_t rb[KT];
 #pragma unroll
-    for (int h = 0; h < KT; ++h)
-      rb[h] = rows16(__builtin_amdgcn_readfirstlane(min(slot0 + 16 * h, last)));
+    for (int h = 0; h < KT; ++h) {
+      rb[h] = rows16(slot16(vt, h), KIND == kChunk ? ahead[h] : page16(vt, h));
+      if (KIND == kChunk) ahead[h] = page16(next_tile(vt), h);
+    }
     const bool whole = slot0 + TK - 1 <= last;
     auto lane_row = [&](int row) { return min(slot0 + row, last) & 15; };
     // the stage's last reads are done before its refill is asked for
@@ -159,7 +167,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
 
   auto step = [&](int vt, char* vs, char* nxt, const Frag (&kf)[KT][DS], Frag (&kn)[KT][DS])
                   __attribute__((always_inline)) {
-    load(min(vt + kAtWaves, vt1 - 1), nxt, kn);   // (past the end: the last tile again)
+    load(next_tile(vt), nxt, kn);
     const int slot0 = slot_of(vt);
     const bool full = slot0 + TK <= sn.lim && (slot0 >= sn.lo || slot0 + TK <= a.n_sink);
     // s[kt][rt][i]: slot slot0 + 16 kt + 4 gq + i of row l16
@@ -286,11 +294,17 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   int vt = vt0 + wave;
   if (vt < vt1) {
     Frag ka[KT][DS], kc[KT][DS];
+#pragma unroll
+    for (int h = 0; h < KT; ++h)
+      if (KIND == kChunk) ahead[h] = page16(vt, h);
     load(vt, va, ka);
+    const bool turns = KIND == kChunk && younger_block();
     for (;;) {
+      if (turns) __builtin_amdgcn_s_setprio(1);
       step(vt, va, vc, ka, kc);
       vt += kAtWaves;
       if (vt >= vt1) break;
+      if (turns) __builtin_amdgcn_s_setprio(0);
       step(vt, vc, va, kc, ka);
       vt += kAtWaves;
       if (vt >= vt1) break;
@@ -300,6 +314,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   // the waves' parts: references, then rows scaled to the largest, summed over
   // the waves in order.  Every load in flight has to land before its stage is
   // written here.
+  if (KIND == kChunk) __builtin_amdgcn_s_setprio(0);
   wait_vmcnt<0>();
   bool odd = false, far = false;
 #pragma unroll

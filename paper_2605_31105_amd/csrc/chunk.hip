@@ -27,28 +27,26 @@ static_assert(kAtTh == kWTh, "one kernel holds both");
 template <typename E>
 constexpr int kJobShift = sizeof(E) == 2 ? 7 : 4;
 constexpr int kFewRows = 16;
+// Costs, in half tiles of 32 keys read for few rows: MEASURED
+constexpr int kFewFixed = 6, kFewTile = 2, kWideFixed = 15, kWideTile = 5;
+// Starts that a block keeps in LDS, where the searches of its threads read them.
+constexpr int kStartsHeld = 1024;
 
 // First row tile of sequence b in the row of all sequences' tiles: one tile more than
 // its rows fill for each sequence before it, so that no sum over sequences is needed.
 template <typename E>
-__device__ __forceinline__ int tile_of(const AttendK& a, int b) {
-  const int s = min(max(a.starts[b], 0), a.step_tokens);
+__device__ __forceinline__ int tile_of(const AttendK& a, const int32_t* starts, int b) {
+  const int s = min(max(starts[b], 0), a.step_tokens);
   return (int)((int64_t)s * a.group >> kJobShift<E>) + b;
 }
 
-// Where a job lies: a sequence, a unit of it and rows r0 ...
-struct Job {
-  int b;         // sequence, -1: none
-  int tile, next;   // its first tile, and the next sequence's
-};
-
 // The last sequence whose tiles start at tile w or before (-1: none).
 template <typename E>
-__device__ __forceinline__ int find_sequence(const AttendK& a, int w) {
+__device__ __forceinline__ int find_sequence(const AttendK& a, const int32_t* starts, int w) {
   int lo = 0, hi = a.sequences;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
-    if (tile_of<E>(a, mid) <= w) lo = mid + 1;
+    if (tile_of<E>(a, starts, mid) <= w) lo = mid + 1;
     else hi = mid;
   }
   return lo - 1;
@@ -56,20 +54,24 @@ __device__ __forceinline__ int find_sequence(const AttendK& a, int w) {
 
 // A job's shape.
 struct Shape {
-  int b, h, start, t, r0, rows, len;
+  int h, start, t, r0, rows, len;
   const int32_t* trow;
+  __device__ __forceinline__ void hold() {   // (see Walk)
+    for (int* x : {&h, &start, &t, &r0, &rows, &len}) *x = __builtin_amdgcn_readfirstlane(*x);
+    trow = (const int32_t*)uniform64((int64_t)trow);
+  }
 };
 
 // Job j of sequence b, whose tiles are tile .. next - 1; false where there are no rows.
 template <typename E>
-__device__ __forceinline__ bool shape_of(const AttendK& a, int64_t j, int b, int tile, int next, Shape* s) {
+__device__ __forceinline__ bool shape_of(const AttendK& a, const int32_t* starts, int64_t j, int b, int tile, int next,
+                                         Shape* s) {
   const int n = next - tile;
   const int64_t local = j - (int64_t)tile * a.heads;
   if (b < 0 || n < 1 || local < 0 || local >= (int64_t)n * a.heads) return false;   // (starts that fall)
-  s->b = b;
   s->h = (int)((uint32_t)local / (uint32_t)n);
-  s->start = min(max(a.starts[b], 0), a.step_tokens);
-  s->t = min(min(max(a.starts[b + 1], 0), a.step_tokens) - s->start, a.longest);
+  s->start = min(max(starts[b], 0), a.step_tokens);
+  s->t = min(min(max(starts[b + 1], 0), a.step_tokens) - s->start, a.longest);
   s->r0 = ((int)local - s->h * n) << kJobShift<E>;
   const int64_t R = (int64_t)s->t * a.group;
   if (s->r0 >= R) return false;
@@ -92,31 +94,53 @@ __device__ __forceinline__ Span span_of(const AttendK& a, const Shape& s) {
                    few<E>(s) ? Tile<E>::KEYS : kWideKeys);
 }
 
-// The tiles of a job as parts count them: one at least, so that a job without keys is some
-// block's too; 0 without rows.
+// What jobs cost: `fixed` for the rows themselves, then `tile` for each of `n` tiles (one at least, so that a job without keys is some block's too).
+struct Cost {
+  int fixed, tile, n;
+  __device__ __forceinline__ int all() const { return fixed + tile * n; }
+  // Tiles before a cut `at` this far into the job.  A cut among the fixed costs lies before the job.
+  __device__ __forceinline__ int tiles(int64_t at) const {
+    if (at <= fixed) return 0;
+    const int64_t t = (at - fixed + tile - 1) / tile;
+    return t < n ? (int)t : n;
+  }
+};
 template <typename E>
-__device__ __forceinline__ int job_tiles(const AttendK& a, int64_t j, int b, int tile, int next) {
+__device__ __forceinline__ Cost cost_of(const Shape& s, const Span& sn) {
+  const int n = max(sn.nt, 1);
+  return few<E>(s) ? Cost{kFewFixed, kFewTile, n} : Cost{kWideFixed, kWideTile, n};
+}
+template <typename E>
+__device__ __forceinline__ int job_cost(const AttendK& a, const int32_t* starts, int64_t j, int b, int tile, int next) {
   Shape s;
-  if (!shape_of<E>(a, j, b, tile, next, &s)) return 0;
-  return max(span_of<E>(a, s).nt, 1);
+  if (!shape_of<E>(a, starts, j, b, tile, next, &s)) return 0;
+  return cost_of<E>(s, span_of<E>(a, s)).all();
 }
 
 // A walk over jobs in order, which keeps the sequence it is in.
 template <typename E>
 struct Walk {
+  const int32_t* starts;
   int b, tile, next;
   int64_t end;    // first job behind the sequence
   __device__ __forceinline__ void enter(const AttendK& a, int to) {
     b = to;
-    tile = b >= 0 ? tile_of<E>(a, b) : 0;
-    next = b + 1 <= a.sequences ? tile_of<E>(a, b + 1) : tile;
+    tile = b >= 0 ? tile_of<E>(a, starts, b) : 0;
+    next = b + 1 <= a.sequences ? tile_of<E>(a, starts, b + 1) : tile;
     end = (int64_t)next * a.heads;
   }
   __device__ __forceinline__ void start(const AttendK& a, int64_t j) {
-    enter(a, min(find_sequence<E>(a, (int)(j / a.heads)), a.sequences - 1));
+    enter(a, min(find_sequence<E>(a, starts, (int)((uint32_t)j / (uint32_t)a.heads)), a.sequences - 1));
   }
   __device__ __forceinline__ void to(const AttendK& a, int64_t j) {
     while (j >= end && b + 1 < a.sequences) enter(a, b + 1);
+  }
+  // (the same in all lanes: kept in scalar registers)
+  __device__ __forceinline__ void hold() {
+    b = __builtin_amdgcn_readfirstlane(b);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    next = __builtin_amdgcn_readfirstlane(next);
+    end = uniform64(end);
   }
 };
 
@@ -128,85 +152,107 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
   __shared__ __attribute__((aligned(1024))) char v1_s[BYTES];
   __shared__ int64_t sum_s[kChunkTh / 64];
   __shared__ int64_t at_s, first_s;
+  __shared__ int32_t starts_s[kStartsHeld];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t blocks = gridDim.x, b = (blockIdx.x % kXcds) * (blocks / kXcds) + blockIdx.x / kXcds;
 
-  // tiles before this thread's jobs, and of all
-  const int64_t per = (a.jobs + kChunkTh - 1) / kChunkTh;
-  const int64_t j0 = tid * per, j1 = j0 + per < a.jobs ? j0 + per : a.jobs;
-  int64_t own = 0;
-  Walk<E> w;
-  if (j0 < j1) {
-    w.start(a, j0);
-    for (int64_t j = j0; j < j1; ++j) {
-      w.to(a, j);
-      own += job_tiles<E>(a, j, w.b, w.tile, w.next);
+  // This block's part: costs lo .. hi - 1 of all jobs' costs in a row.  Each thread adds up the
+  // costs of a run of jobs; the one that has lo's job says where it begins.
+  int64_t part = 0, lo = 0, hi = 0;
+  auto plan = [&](const int32_t* starts) __attribute__((always_inline)) {
+    const int64_t per = (a.jobs + kChunkTh - 1) / kChunkTh;
+    const int64_t j0 = tid * per, j1 = min(j0 + per, a.jobs);
+    int64_t own = 0;
+    Walk<E> w{starts};
+    if (j0 < j1) {
+      w.start(a, j0);
+      for (int64_t j = j0; j < j1; ++j) {
+        w.to(a, j);
+        own += job_cost<E>(a, starts, j, w.b, w.tile, w.next);
+      }
     }
-  }
-  int64_t incl = own;
+    int64_t incl = own;
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const int64_t x = __shfl_up((long long)incl, k);
-    if (lane >= k) incl += x;
-  }
-  if (lane == 63) sum_s[wave] = incl;
-  __syncthreads();
-  int64_t all = 0, at = incl - own;
+    for (int k = 1; k < 64; k <<= 1) {
+      const int64_t x = __shfl_up((long long)incl, k);
+      if (lane >= k) incl += x;
+    }
+    if (lane == 63) sum_s[wave] = incl;
+    __syncthreads();
+    int64_t all = 0, at = incl - own;
 #pragma unroll
-  for (int k = 0; k < kChunkTh / 64; ++k) {
-    if (k < wave) at += sum_s[k];
-    all += sum_s[k];
-  }
-  all = uniform64(all);
-  const int64_t part = max((int64_t)a.min_tiles, (all + blocks - 1) / blocks);
-  const int64_t lo = b * part, hi = min(all, lo + part);
-  if (tid == 0) a.ends[b] = make_int4(-1, 0, 0, 0);
-  if (lo >= all) return;
-  if (at <= lo && lo < at + own) {   // this thread's: the job of the part's first tile
-    int64_t j = j0;
-    w.start(a, j);
-    for (; j < j1; ++j) {
-      w.to(a, j);
-      const int n = job_tiles<E>(a, j, w.b, w.tile, w.next);
-      if (lo < at + n) break;
-      at += n;
+    for (int k = 0; k < kChunkTh / 64; ++k) {
+      if (k < wave) at += sum_s[k];
+      all += sum_s[k];
     }
-    first_s = j;
-    at_s = at;
+    all = uniform64(all);
+    part = max((int64_t)a.min_tiles, (all + blocks - 1) / blocks);
+    lo = b * part;
+    hi = min(all, lo + part);
+    if (at <= lo && lo < at + own) {
+      int64_t j = j0;
+      w.start(a, j);
+      for (; j < j1; ++j) {
+        w.to(a, j);
+        const int cost = job_cost<E>(a, starts, j, w.b, w.tile, w.next);
+        if (lo < at + cost) break;
+        at += cost;
+      }
+      first_s = j;
+      at_s = at;
+    }
+  };
+  if (a.sequences < kStartsHeld) {
+    for (int k = tid; k <= a.sequences; k += kChunkTh) starts_s[k] = a.starts[k];
+    __syncthreads();
+    plan(starts_s);
+  } else {
+    plan(a.starts);
   }
+  if (tid == 0) a.ends[b].parts = 0;
+  if (lo >= hi) return;
   __syncthreads();
-  int64_t from = uniform64(at_s), j = uniform64(first_s);
-  w.start(a, j);
-  for (; from < hi && j < a.jobs; ++j) {
-    w.to(a, j);
-    Shape s;
-    if (!shape_of<E>(a, j, __builtin_amdgcn_readfirstlane(w.b), __builtin_amdgcn_readfirstlane(w.tile),
-                     __builtin_amdgcn_readfirstlane(w.next), &s))
-      continue;
-    AttendK x = a;   // the unit's own rows
-    const size_t row0 = (size_t)s.start * a.q_heads + (size_t)s.h * a.group;
-    x.q = (const E*)a.q + row0 * D;
-    x.o = (E*)a.o + row0 * D;
-    x.lse = a.lse ? a.lse + row0 : nullptr;
-    x.tokens = s.t;
-    x.row_groups = (int64_t)s.t * a.group <= 1 << kJobShift<E> ? 1 : 2;   // (one or more)
-    const Span sn = span_of<E>(a, s);
-    const int64_t to = from + max(sn.nt, 1);
-    const int vt0 = (int)(max(lo, from) - from), vt1 = min((int)(min(hi, to) - from), sn.nt);
-    const bool whole = from >= lo && to <= hi;
-    const int64_t slot = 2 * b + (from > lo ? 1 : 0);
-    const int64_t rows_at = slot * a.part_rows - s.r0;   // partial row of row r: this + r
-    if (from >= lo && !whole && tid == 0)
-      a.ends[b] = make_int4((int)j, (int)(min((to - 1) / part, blocks - 1) - b) + 1, (int)(slot & 1), 0);
-    if (few<E>(s)) {
-      attend_rows<E, D, 1, kChunk>(x, sn, 0, s.r0, vt0, vt1, whole ? kWhole : rows_at, false, s.len, s.t, s.trow,
-                                   v0_s, v1_s);
-    } else if constexpr (sizeof(E) == 2) {
-      wide_rows<D, kChunk>(x, sn, 0, s.r0, vt0, vt1, [&] { return Part{!whole, rows_at}; }, s.len, s.t, s.trow,
-                           v0_s, v1_s);
+  // whole jobs first: those of a unit, in blocks of one XCD, begin with the same keys at the
+  // same time
+  for (int pass = 0; pass < 2; ++pass) {
+    int64_t from = uniform64(at_s), j = uniform64(first_s);
+    Walk<E> u{a.starts};
+    u.start(a, j);
+    for (; from < hi && j < a.jobs; ++j) {
+      u.to(a, j);
+      u.hold();
+      Shape s;
+      if (!shape_of<E>(a, a.starts, j, u.b, u.tile, u.next, &s)) continue;
+      s.hold();
+      const Span sn = span_of<E>(a, s);
+      const Cost cost = cost_of<E>(s, sn);
+      const int64_t at = from;
+      from = at + cost.all();
+      const int vt0 = cost.tiles(lo - at), vt1 = cost.tiles(hi - at);
+      const bool whole = vt0 == 0 && vt1 == cost.n;
+      if (vt1 <= vt0 || whole != (pass == 0)) continue;
+      AttendK x = a;   // the unit's own rows
+      const size_t row0 = (size_t)s.start * a.q_heads + (size_t)s.h * a.group;
+      x.q = (const E*)a.q + row0 * D;
+      x.o = (E*)a.o + row0 * D;
+      x.lse = a.lse ? a.lse + row0 : nullptr;
+      x.tokens = s.t;
+      // a part's two places: what it goes on with, and what it begins and leaves to others
+      const int64_t rows_at = (2 * b + (vt0 == 0)) * a.part_rows - s.r0;   // partial row of row r: this + r
+      if (vt0 == 0 && !whole && tid == 0) {
+        const int64_t last = (at + cost.all() - cost.tile) / part;   // the part that ends the job
+        a.ends[b] = {row0, s.r0, s.rows, (int)(min(last, blocks - 1) - b) + 1};
+      }
+      const int end = min(vt1, sn.nt);
+      if (few<E>(s)) {
+        attend_rows<E, D, 1, kChunk>(x, sn, 0, s.r0, vt0, end, whole ? kWhole : rows_at, false, s.len, s.t, s.trow,
+                                     v0_s, v1_s);
+      } else if constexpr (sizeof(E) == 2) {
+        wide_rows<D, kChunk>(x, sn, 0, s.r0, vt0, end, [&] { return Part{!whole, rows_at}; }, s.len, s.t, s.trow,
+                             v0_s, v1_s);
+      }
+      __syncthreads();   // (the next rows take the same stages)
     }
-    __syncthreads();   // (the next rows take the same stages)
-    from = to;
   }
 }
 
@@ -214,23 +260,18 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
 template <typename E, int D>
 __global__ __launch_bounds__(kChunkTh) void chunk_combine_kernel(AttendK a) {
   constexpr int CR = D / 4;
-  const int4 p = a.ends[blockIdx.x];
-  if (p.x < 0 || p.y < 2) return;
-  Walk<E> w;
-  w.start(a, p.x);
-  Shape s;
-  if (!shape_of<E>(a, p.x, w.b, w.tile, w.next, &s)) return;
+  const CutJob p = a.ends[blockIdx.x];
+  if (p.parts < 2) return;
   const int first = 16 * blockIdx.y;
-  const size_t row0 = (size_t)s.start * a.q_heads + (size_t)s.h * a.group;
   AttendK x = a;
-  x.o = (E*)a.o + row0 * D;
-  x.lse = a.lse ? a.lse + row0 : nullptr;
+  x.o = (E*)a.o + p.row0 * D;
+  x.lse = a.lse ? a.lse + p.row0 : nullptr;
   for (int c = threadIdx.x; c < 16 * CR; c += kChunkTh) {
     const int row = first + c / CR, ch = c % CR;
-    if (row >= s.rows) continue;
-    const int r = s.r0 + row, i = group_of(a, r), g = r - i * a.group;
-    const Split o = add_splits<D, false>(a, (size_t)2 * blockIdx.x * a.part_rows + row, p.z * a.part_rows,
-                                         2 * a.part_rows, p.y, 0, 1, ch);
+    if (row >= p.rows) continue;
+    const int r = p.r0 + row, i = group_of(a, r), g = r - i * a.group;
+    const Split o = add_splits<D, false>(a, (size_t)2 * blockIdx.x * a.part_rows + row, a.part_rows, 2 * a.part_rows,
+                                         p.parts, 0, 1, ch);
     write_out<E, D>(x, row_at<kChunk>(x, 0, g, i), ch, o.x, o.m, o.l, o.lx);
   }
 }
@@ -249,12 +290,12 @@ ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dty
   ChunkPlan p;
   const int shift = dtype == GRKV_BF16 ? kJobShift<u16> : kJobShift<float>;
   p.jobs = (((int64_t)step->tokens * ch->group >> shift) + step->sequences) * step->heads;
-  p.min_part = 8;   // (two tiles for each wave of a block of few rows)
+  p.min_part = 8 * kFewTile;   // (two tiles for each wave of a block of few rows)
   const int64_t rows = (int64_t)(ch->longest < step->tokens ? ch->longest : step->tokens) * ch->group;
   p.part_rows = rows >= 1 << shift ? 1 << shift : rows > 16 ? (int)((rows + 15) / 16 * 16) : 16;
   // parts of the longest units, if all are
   const int64_t keys = dtype == GRKV_BF16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
-  const int64_t parts = ((slots + keys - 1) / keys + p.min_part - 1) / p.min_part;
+  const int64_t parts = (((slots + keys - 1) / keys) * kFewTile + kFewFixed + p.min_part - 1) / p.min_part;
   int64_t blocks = p.jobs < kChunkBlocks ? p.jobs * (parts < kChunkBlocks ? parts : kChunkBlocks) : kChunkBlocks;
   blocks = blocks < kChunkBlocks ? (blocks + kXcds - 1) / kXcds * kXcds : kChunkBlocks;
   p.blocks = (int)(blocks > kXcds ? blocks : kXcds);
@@ -263,7 +304,7 @@ ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dty
   p.opart = 0;
   p.mpart = up(part * d * sizeof(float));
   p.ends = p.mpart + up(part * sizeof(float4));
-  p.total = p.ends + up((size_t)p.blocks * sizeof(int4));
+  p.total = p.ends + up((size_t)p.blocks * sizeof(CutJob));
   return p;
 }
 
@@ -277,7 +318,7 @@ hipError_t launch_chunk(AttendK a, const ChunkPlan& p, int d, int dtype, void* w
   a.scale_log2 = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
   a.opart = (float*)((char*)workspace + p.opart);
   a.mpart = (float4*)((char*)workspace + p.mpart);
-  a.ends = (int4*)((char*)workspace + p.ends);
+  a.ends = (CutJob*)((char*)workspace + p.ends);
   set_group(a);
   if (dtype == GRKV_BF16) return d == 64 ? launch_ed<u16, 64>(a, s) : launch_ed<u16, 128>(a, s);
   return d == 64 ? launch_ed<float, 64>(a, s) : launch_ed<float, 128>(a, s);

@@ -308,6 +308,13 @@ struct PagesLayout {
 PagesLayout pages_layout(const grkv_pages* pg, int entries);
 hipError_t launch_pages(const PagesCall& c, hipStream_t s);
 
+// Rows of a step that a block began and others went on with (chunk.hip).
+struct CutJob {
+  uint64_t row0;      // of q and o: the unit's first
+  int r0, rows;       // which of its rows
+  int parts;          // blocks; below 2: no such rows
+};
+
 // Attention over pages or over contiguous keys (attend.hip).
 struct AttendK {
   const void* q;      // [entries][group][tokens][d]
@@ -344,7 +351,7 @@ struct AttendK {
   int sequences, heads, q_heads, longest, step_tokens;
   int part_rows;      // rows of a partial result
   int64_t jobs;
-  int4* ends;         // [blocks] the entry rows that a block began and others went on with
+  struct CutJob* ends;   // [blocks]
 };
 struct AttendPlan {
   int rt;             // 16-row tiles of a block; 0: the wide kernel

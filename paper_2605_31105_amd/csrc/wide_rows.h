@@ -90,42 +90,47 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
   // ---- loads: this wave brings rows 16 wave .. + 15 of every tile
   auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
   auto swz_v = [](int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; };
-  uint32_t ko[NI], vo[NI];
-#pragma unroll
-  for (int it = 0; it < NI; ++it) {
-    const int row = it * RPI + lane / CPR, ch = lane % CPR;
-    ko[it] = (row * CPR + (ch ^ swz_k(row))) * 16;
-    vo[it] = (row * CPR + (ch ^ swz_v(row))) * 16;
-  }
+  // (lane's byte in the first kilobyte; the rows of the next ones are 1 KB on, where K's chunks
+  // are also permuted by 4)
+  const int row0 = lane / CPR, ch0 = lane % CPR;
+  const uint32_t ko = (row0 * CPR + (ch0 ^ swz_k(row0))) * 16, vo = (row0 * CPR + (ch0 ^ swz_v(row0))) * 16;
+  static_assert(RPI == 4 || RPI == 8, "rows of a kilobyte");
   const int last = sn.kend - 1;
   const uint32_t kr0 = (uint32_t)(uintptr_t)(lds_void*)kring;
   const uint32_t vr0 = KIND == kChunk ? (uint32_t)(uintptr_t)(lds_void*)vring : kr0 + 2 * KB;
   auto slot_of = [&](int vt) { return (vt < sn.at ? vt : vt - sn.at + sn.bt) * TK; };
-  // this wave's rows of tile vt, of K or V (the chunk offsets o, permuted by swz)
-  auto load = [&](const void* from, int vt, uint32_t to, const uint32_t (&o)[NI], auto swz, bool once)
+  // this wave's first slot of tile vt, its page, and its row
+  auto wave_slot = [&](int vt) { return __builtin_amdgcn_readfirstlane(min(slot_of(vt) + 16 * wave, last)); };
+  auto page_at = [&](int vt) -> int {
+    if (PAGED) return page_of<KIND>(trow, wave_slot(vt) >> a.shift);
+    return 0;
+  };
+  auto row_in = [&](int vt, int p) -> size_t {
+    const int at = wave_slot(vt);
+    if (!PAGED) return (size_t)e * a.n + (at & ~15);
+    p = (unsigned)p < (unsigned)a.pages ? p : 0;
+    return ((size_t)p << a.shift) + ((at & ((1 << a.shift) - 1)) & ~15);
+  };
+  // this wave's rows of tile vt in page p, of K or V (o: its lane offset; step: how the next
+  // kilobyte's differs)
+  auto load = [&](const void* from, int vt, int p, uint32_t to, uint32_t o, int step, bool once)
                   __attribute__((always_inline)) {
     const int s16 = slot_of(vt) + 16 * wave;
-    const int at = __builtin_amdgcn_readfirstlane(min(s16, last));
-    size_t row;
-    if (PAGED) {
-      int p = trow[at >> a.shift];
-      p = (unsigned)p < (unsigned)a.pages ? p : 0;
-      row = ((size_t)p << a.shift) + ((at & ((1 << a.shift) - 1)) & ~15);
-    } else {
-      row = (size_t)e * a.n + (at & ~15);
-    }
-    const char* src = (const char*)from + row * RB;
+    const char* src = (const char*)from + row_in(vt, p) * RB;
     const uint32_t dst = __builtin_amdgcn_readfirstlane(to + wave * 16 * RB);
-    const bool whole = s16 + 15 <= last;
+    auto bring = [&](const char* at, uint32_t f, int it) __attribute__((always_inline)) {
+      if (once) ring_load<true>(at, f, dst + it * 1024);
+      else ring_load(at, f, dst + it * 1024);
+    };
+    if (s16 + 15 <= last) {
 #pragma unroll
-    for (int it = 0; it < NI; ++it) {
-      uint32_t f = o[it];
-      if (!whole) {   // rows past the last slot: the last one again
-        const int row_in = it * RPI + lane / CPR, ch = lane % CPR;
-        f = ((min(s16 + row_in, last) & 15) * CPR + (ch ^ swz(row_in))) * 16;
-      }
-      if (once) ring_load<true>(src, f, dst + it * 1024);
-      else ring_load(src, f, dst + it * 1024);
+      for (int it = 0; it < NI; ++it) bring(src + it * 1024, o ^ (it * step), it);
+    } else {   // rows past the last slot: the last one again
+      int l = lane;
+      asm volatile("" : "+v"(l));   // (formed here, not held over the loop)
+#pragma unroll
+      for (int it = 0; it < NI; ++it)
+        bring(src, (min(s16 + it * RPI + l / CPR, last) & 15) * RB + ((o ^ (it * step)) & (RB - 1)), it);
     }
   };
 
@@ -232,6 +237,16 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
 #pragma unroll
         for (int dm = 0; dm < DM; ++dm) acc[dm] = mfma32(vf[s][dm], p[n][s], acc[dm]);
     }
+    if (KIND == kChunk) {
+      constexpr int ALL = NK * 2 * DM, AHEAD = 4;   // products of the step, operands read ahead
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
+#pragma unroll
+      for (int k = 0; k < ALL - AHEAD; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+    }
 #pragma unroll
     for (int n = 0; n < NK; ++n) st[n] = nx[n];
   };
@@ -239,24 +254,43 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
   if (vt0 < vt1) {
     // values that no other row group reads are read once (32 units of 20k to 32k keys,
     // over caches used in turn, 116 -> 114 us; keys too, 114)
-    const bool once = PAGED && a.row_groups == 1;
+    const bool once = TREE && a.row_groups == 1;
     // tile i is in half i & 1 of either ring
-    auto load_k = [&](int i) { load(a.k, min(vt0 + i, vt1 - 1), kr0 + (i & 1) * KB, ko, swz_k, false); };
-    auto load_v = [&](int i) { load(a.v, min(vt0 + i, vt1 - 1), vr0 + (i & 1) * KB, vo, swz_v, once); };
-    load_k(0);
-    load_k(1);
-    load_v(0);
+    auto tile = [&](int i) { return min(vt0 + i, vt1 - 1); };
+    auto load_k = [&](int i, int p) { load(a.k, tile(i), p, kr0 + (i & 1) * KB, ko, 64, false); };
+    auto load_v = [&](int i, int p) { load(a.v, tile(i), p, vr0 + (i & 1) * KB, vo, 0, once); };
+    const int p0 = page_at(tile(0));
+    // Pages are looked up a step before their keys are asked for (and values take those of
+    // the keys), so that no step waits for the table (MEASURED)
+    int pv = page_at(tile(1)), pk = 0;
+    const bool turns = KIND == kChunk && younger_block();
+    load_k(0, p0);
+    load_k(1, pv);
+    load_v(0, p0);
+    if (KIND == kChunk) pk = page_at(tile(2));
     ring_barrier<2 * NI>();
     logits(kring, st);
     for (int i = 0; i < vt1 - vt0; ++i) {
       // K of tile i + 1 and V of tile i are here, and every wave is done with K of
       // tile i and V of tile i - 1
       ring_barrier<0>();
-      load_k(i + 2);
-      load_v(i + 1);
+      if (KIND == kChunk) {
+        if (turns) {
+          if (i & 1) __builtin_amdgcn_s_setprio(1);
+          else __builtin_amdgcn_s_setprio(0);
+        }
+        load_k(i + 2, pk);
+        load_v(i + 1, pv);
+        pv = pk;
+        pk = page_at(tile(i + 3));
+      } else {
+        load_k(i + 2, page_at(tile(i + 2)));
+        load_v(i + 1, page_at(tile(i + 1)));
+      }
       step(slot_of(vt0 + i), kring + ((i + 1) & 1) * KB, vring + (i & 1) * KB);
     }
   }
+  if (KIND == kChunk) __builtin_amdgcn_s_setprio(0);
   ring_barrier<0>();   // (the rings are the output's buffer now)
   sum += __shfl_xor(sum, 32);
   rsum += __shfl_xor(rsum, 32);
