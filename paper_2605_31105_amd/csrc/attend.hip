@@ -260,7 +260,7 @@ hipError_t launch_ed(const AttendK& a, int rt, hipStream_t s) {
 
 // Marks of one call's splits: different for every call of a process, and unlike what
 // a workspace may hold.
-static uint64_t next_nonce() {
+uint64_t next_nonce() {
   static const uint64_t seed = (uint64_t)std::chrono::system_clock::now().time_since_epoch().count();
   static std::atomic<uint64_t> calls{0};
   uint64_t x = seed + 0x9e3779b97f4a7c15ull * ++calls;   // (splitmix64)

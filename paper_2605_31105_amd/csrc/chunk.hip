@@ -25,10 +25,13 @@ static_assert(kAtTh == kWTh, "one kernel holds both");
 
 // Rows of a job, and of those that the kernel of few rows takes.
 template <typename E>
-constexpr int kJobShift = sizeof(E) == 2 ? 7 : 4;
+constexpr int kJobShift = sizeof(E) == 2 ? 7 : 5;
 constexpr int kFewRows = 16;
 // Costs, in half tiles of 32 keys read for few rows: MEASURED
-constexpr int kFewFixed = 6, kFewTile = 2, kWideFixed = 15, kWideTile = 5;
+constexpr int kFewFixed = 6, kFewTile = 2, kWideFixed = 15, kWideTile = 5, kTwoFixed = 9, kTwoTile = 3;
+// Calls of so few jobs give every block a piece of one job (8 units of 2048 keys and one token: MEASURED);
+// pieces of few rows are joined by the block that ends last, up to kJoined of a job.
+constexpr int kAlignedJobs = 64, kJoined = 16;
 // Starts that a block keeps in LDS, where the searches of its threads read them.
 constexpr int kStartsHeld = 1024;
 
@@ -83,15 +86,12 @@ __device__ __forceinline__ bool shape_of(const AttendK& a, const int32_t* starts
   return true;
 }
 
-template <typename E>
-__device__ __forceinline__ bool few(const Shape& s) {
-  return sizeof(E) == 4 || s.rows <= kFewRows;
-}
+__device__ __forceinline__ bool few(const Shape& s) { return s.rows <= kFewRows; }
 
 template <typename E>
 __device__ __forceinline__ Span span_of(const AttendK& a, const Shape& s) {
   return make_span(a, false, s.len, s.len - s.t, s.t, group_of(a, s.r0), group_of(a, s.r0 + s.rows - 1),
-                   few<E>(s) ? Tile<E>::KEYS : kWideKeys);
+                   sizeof(E) == 4 || few(s) ? Tile<E>::KEYS : kWideKeys);
 }
 
 // What jobs cost: `fixed` for the rows themselves, then `tile` for each of `n` tiles (one at least, so that a job without keys is some block's too).
@@ -108,7 +108,8 @@ struct Cost {
 template <typename E>
 __device__ __forceinline__ Cost cost_of(const Shape& s, const Span& sn) {
   const int n = max(sn.nt, 1);
-  return few<E>(s) ? Cost{kFewFixed, kFewTile, n} : Cost{kWideFixed, kWideTile, n};
+  return few(s) ? Cost{kFewFixed, kFewTile, n}
+         : sizeof(E) == 4 ? Cost{kTwoFixed, kTwoTile, n} : Cost{kWideFixed, kWideTile, n};
 }
 template <typename E>
 __device__ __forceinline__ int job_cost(const AttendK& a, const int32_t* starts, int64_t j, int b, int tile, int next) {
@@ -144,7 +145,22 @@ struct Walk {
   }
 };
 
-template <typename E, int D>
+// Four values of a cut job's row, from its parts in blocks b ..  (JOINED: parts of blocks of this
+// launch.)
+template <typename E, int D, bool JOINED>
+__device__ __forceinline__ void combine_row(const AttendK& a, const CutJob& cut, int64_t b, int row, int ch) {
+  if (row >= cut.rows) return;
+  AttendK x = a;
+  x.o = (E*)a.o + cut.row0 * D;
+  x.lse = a.lse ? a.lse + cut.row0 : nullptr;
+  const int r = cut.r0 + row, i = group_of(a, r), g = r - i * a.group;
+  const Split o = add_splits<D, JOINED>(a, (size_t)2 * b * a.part_rows + row, a.part_rows, 2 * a.part_rows,
+                                        cut.parts, 0, 1, ch);
+  write_out<E, D>(x, row_at<kChunk>(x, 0, g, i), ch, o.x, o.m, o.l, o.lx);
+}
+
+// FEW: no job has more than kFewRows rows.
+template <typename E, int D, bool FEW>
 __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
   constexpr int BYTES = kStage<E, D>;
   static_assert(sizeof(E) == 4 || BYTES == kRing<D>, "both kinds take the same LDS");
@@ -152,6 +168,7 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
   __shared__ __attribute__((aligned(1024))) char v1_s[BYTES];
   __shared__ int64_t sum_s[kChunkTh / 64];
   __shared__ int64_t at_s, first_s;
+  __shared__ int pieces_s;
   __shared__ int32_t starts_s[kStartsHeld];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t blocks = gridDim.x, b = (blockIdx.x % kXcds) * (blocks / kXcds) + blockIdx.x / kXcds;
@@ -186,6 +203,38 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
       all += sum_s[k];
     }
     all = uniform64(all);
+    if (a.aligned) {
+      // (a job a thread) blocks of each job by what a part is to cost at most: the least, or so
+      // much that all jobs' blocks are there
+      auto blocks_for = [&](int64_t cost) {
+        const int k = (int)((own + cost - 1) / cost);
+        return a.flags ? min(k, kJoined) : k;
+      };
+      auto scan = [&](int k, int* total) {
+        int incl = k;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+          const int x = __shfl_up(incl, d);
+          if (lane >= d) incl += x;
+        }
+        *total = __shfl(incl, 63);
+        return incl - k;
+      };
+      if (wave == 0) {   // (kAlignedJobs at most)
+        int total, k = blocks_for(a.min_tiles), first = scan(k, &total);
+        if (total > blocks) {
+          k = blocks_for(max((int64_t)a.min_tiles, (all + blocks - a.jobs - 1) / (blocks - a.jobs)));
+          first = scan(k, &total);
+        }
+        if (lane == 0) pieces_s = 0;
+        if (first <= b && b < first + k) {
+          first_s = lane;
+          at_s = b - first;
+          pieces_s = k;
+        }
+      }
+      return;
+    }
     part = max((int64_t)a.min_tiles, (all + blocks - 1) / blocks);
     lo = b * part;
     hi = min(all, lo + part);
@@ -210,12 +259,18 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
     plan(a.starts);
   }
   if (tid == 0) a.ends[b].parts = 0;
-  if (lo >= hi) return;
+  if (!a.aligned && lo >= hi) return;
   __syncthreads();
+  // this block's piece of its one job
+  const int pieces = a.aligned ? __builtin_amdgcn_readfirstlane(pieces_s) : 0;
+  if (a.aligned) {
+    if (pieces == 0) return;
+    hi = 1;
+  }
   // whole jobs first: those of a unit, in blocks of one XCD, begin with the same keys at the
   // same time
   for (int pass = 0; pass < 2; ++pass) {
-    int64_t from = uniform64(at_s), j = uniform64(first_s);
+    int64_t from = a.aligned ? 0 : uniform64(at_s), j = uniform64(first_s);
     Walk<E> u{a.starts};
     u.start(a, j);
     for (; from < hi && j < a.jobs; ++j) {
@@ -227,8 +282,19 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
       const Span sn = span_of<E>(a, s);
       const Cost cost = cost_of<E>(s, sn);
       const int64_t at = from;
-      from = at + cost.all();
-      const int vt0 = cost.tiles(lo - at), vt1 = cost.tiles(hi - at);
+      int vt0, vt1, parts;
+      if (a.aligned) {
+        const int i = __builtin_amdgcn_readfirstlane((int)at_s);
+        vt0 = (int)((int64_t)cost.n * i / pieces);
+        vt1 = (int)((int64_t)cost.n * (i + 1) / pieces);
+        parts = pieces;
+        from = hi;
+      } else {
+        vt0 = cost.tiles(lo - at);
+        vt1 = cost.tiles(hi - at);
+        parts = (int)(min((at + cost.all() - cost.tile) / part, blocks - 1) - b) + 1;   // (the part that ends the job)
+        from = at + cost.all();
+      }
       const bool whole = vt0 == 0 && vt1 == cost.n;
       if (vt1 <= vt0 || whole != (pass == 0)) continue;
       AttendK x = a;   // the unit's own rows
@@ -239,17 +305,26 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
       x.tokens = s.t;
       // a part's two places: what it goes on with, and what it begins and leaves to others
       const int64_t rows_at = (2 * b + (vt0 == 0)) * a.part_rows - s.r0;   // partial row of row r: this + r
-      if (vt0 == 0 && !whole && tid == 0) {
-        const int64_t last = (at + cost.all() - cost.tile) / part;   // the part that ends the job
-        a.ends[b] = {row0, s.r0, s.rows, (int)(min(last, blocks - 1) - b) + 1};
-      }
+      if (vt0 == 0 && !whole && tid == 0) a.ends[b] = {row0, s.r0, s.rows, parts};
       const int end = min(vt1, sn.nt);
-      if (few<E>(s)) {
-        attend_rows<E, D, 1, kChunk>(x, sn, 0, s.r0, vt0, end, whole ? kWhole : rows_at, false, s.len, s.t, s.trow,
-                                     v0_s, v1_s);
-      } else if constexpr (sizeof(E) == 2) {
-        wide_rows<D, kChunk>(x, sn, 0, s.r0, vt0, end, [&] { return Part{!whole, rows_at}; }, s.len, s.t, s.trow,
-                             v0_s, v1_s);
+      const int64_t to = whole ? kWhole : rows_at;
+      if (FEW || few(s)) {
+        attend_rows<E, D, 1, kChunk>(x, sn, 0, s.r0, vt0, end, to, FEW && a.flags, s.len, s.t, s.trow, v0_s, v1_s);
+      } else if constexpr (!FEW) {
+        if constexpr (sizeof(E) == 4)
+          attend_rows<E, D, 2, kChunk>(x, sn, 0, s.r0, vt0, end, to, false, s.len, s.t, s.trow, v0_s, v1_s);
+        else
+          wide_rows<D, kChunk>(x, sn, 0, s.r0, vt0, end, [&] { return Part{!whole, rows_at}; }, s.len, s.t, s.trow,
+                               v0_s, v1_s);
+      }
+      if constexpr (FEW) {
+        const int i = (int)at_s;
+        if (a.flags && !whole && splits_done(a, j, i, pieces)) {
+          for (int c = tid; c < kFewRows * (D / 4); c += kChunkTh) {
+            const CutJob cut = {row0, s.r0, s.rows, pieces};
+            combine_row<E, D, true>(a, cut, b - i, c / (D / 4), c % (D / 4));
+          }
+        }
       }
       __syncthreads();   // (the next rows take the same stages)
     }
@@ -260,27 +335,19 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
 template <typename E, int D>
 __global__ __launch_bounds__(kChunkTh) void chunk_combine_kernel(AttendK a) {
   constexpr int CR = D / 4;
-  const CutJob p = a.ends[blockIdx.x];
-  if (p.parts < 2) return;
-  const int first = 16 * blockIdx.y;
-  AttendK x = a;
-  x.o = (E*)a.o + p.row0 * D;
-  x.lse = a.lse ? a.lse + p.row0 : nullptr;
-  for (int c = threadIdx.x; c < 16 * CR; c += kChunkTh) {
-    const int row = first + c / CR, ch = c % CR;
-    if (row >= p.rows) continue;
-    const int r = p.r0 + row, i = group_of(a, r), g = r - i * a.group;
-    const Split o = add_splits<D, false>(a, (size_t)2 * blockIdx.x * a.part_rows + row, a.part_rows, 2 * a.part_rows,
-                                         p.parts, 0, 1, ch);
-    write_out<E, D>(x, row_at<kChunk>(x, 0, g, i), ch, o.x, o.m, o.l, o.lx);
-  }
+  const CutJob cut = a.ends[blockIdx.x];
+  if (cut.parts < 2) return;
+  for (int c = threadIdx.x; c < 16 * CR; c += kChunkTh)
+    combine_row<E, D, false>(a, cut, blockIdx.x, 16 * blockIdx.y + c / CR, c % CR);
 }
 
 template <typename E, int D>
-hipError_t launch_ed(const AttendK& a, hipStream_t s) {
-  hipLaunchKernelGGL((chunk_kernel<E, D>), dim3((unsigned)a.blocks), dim3(kChunkTh), 0, s, a);
-  hipLaunchKernelGGL((chunk_combine_kernel<E, D>), dim3((unsigned)a.blocks, (a.part_rows + 15) / 16),
-                     dim3(kChunkTh), 0, s, a);
+hipError_t launch_ed(const AttendK& a, bool few, hipStream_t s) {
+  const dim3 grid((unsigned)a.blocks), th(kChunkTh);
+  if (few) hipLaunchKernelGGL((chunk_kernel<E, D, true>), grid, th, 0, s, a);
+  else hipLaunchKernelGGL((chunk_kernel<E, D, false>), grid, th, 0, s, a);
+  if (!a.flags)
+    hipLaunchKernelGGL((chunk_combine_kernel<E, D>), dim3((unsigned)a.blocks, (a.part_rows + 15) / 16), th, 0, s, a);
   return hipGetLastError();
 }
 
@@ -297,20 +364,28 @@ ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dty
   const int64_t keys = dtype == GRKV_BF16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
   const int64_t parts = (((slots + keys - 1) / keys) * kFewTile + kFewFixed + p.min_part - 1) / p.min_part;
   int64_t blocks = p.jobs < kChunkBlocks ? p.jobs * (parts < kChunkBlocks ? parts : kChunkBlocks) : kChunkBlocks;
+  p.aligned = p.jobs <= kAlignedJobs;
+  if (p.aligned && blocks < 2 * p.jobs) blocks = 2 * p.jobs;
   blocks = blocks < kChunkBlocks ? (blocks + kXcds - 1) / kXcds * kXcds : kChunkBlocks;
   p.blocks = (int)(blocks > kXcds ? blocks : kXcds);
+  p.few = rows <= kFewRows;
+  p.joined = p.aligned && p.few && p.blocks <= kJoined * p.jobs;
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   const size_t part = 2 * (size_t)p.blocks * p.part_rows;
   p.opart = 0;
   p.mpart = up(part * d * sizeof(float));
   p.ends = p.mpart + up(part * sizeof(float4));
-  p.total = p.ends + up((size_t)p.blocks * sizeof(CutJob));
+  p.flags = p.ends + up((size_t)p.blocks * sizeof(CutJob));
+  p.total = p.flags + (p.joined ? up((size_t)p.jobs * kJoined * sizeof(uint64_t)) : 0);
   return p;
 }
 
 hipError_t launch_chunk(AttendK a, const ChunkPlan& p, int d, int dtype, void* workspace, hipStream_t s) {
-  a.splits = 1;
+  a.splits = kJoined;   // (of the marks)
   a.split_shift = 0;
+  a.aligned = p.aligned;
+  a.flags = p.joined ? (uint64_t*)((char*)workspace + p.flags) : nullptr;
+  a.nonce = p.joined ? next_nonce() : 0;
   a.min_tiles = p.min_part;
   a.blocks = p.blocks;
   a.jobs = p.jobs;
@@ -320,8 +395,8 @@ hipError_t launch_chunk(AttendK a, const ChunkPlan& p, int d, int dtype, void* w
   a.mpart = (float4*)((char*)workspace + p.mpart);
   a.ends = (CutJob*)((char*)workspace + p.ends);
   set_group(a);
-  if (dtype == GRKV_BF16) return d == 64 ? launch_ed<u16, 64>(a, s) : launch_ed<u16, 128>(a, s);
-  return d == 64 ? launch_ed<float, 64>(a, s) : launch_ed<float, 128>(a, s);
+  if (dtype == GRKV_BF16) return d == 64 ? launch_ed<u16, 64>(a, p.few, s) : launch_ed<u16, 128>(a, p.few, s);
+  return d == 64 ? launch_ed<float, 64>(a, p.few, s) : launch_ed<float, 128>(a, p.few, s);
 }
 
 }  // namespace grkv

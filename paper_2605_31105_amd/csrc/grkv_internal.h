@@ -350,6 +350,7 @@ struct AttendK {
   int64_t unit_stride;
   int sequences, heads, q_heads, longest, step_tokens;
   int part_rows;      // rows of a partial result
+  int aligned;        // every block has a piece of one job
   int64_t jobs;
   struct CutJob* ends;   // [blocks]
 };
@@ -368,12 +369,14 @@ hipError_t launch_attend(AttendK a, const AttendPlan& p, int d, int dtype, void*
                          hipStream_t s);
 
 void set_group(AttendK& a);
+uint64_t next_nonce();
 
 // Attention of a step's new tokens (chunk.hip): blocks and workspace.
 struct ChunkPlan {
   int64_t jobs;       // row tiles of all units
   int blocks, min_part, part_rows;
-  size_t opart, mpart, ends, total;
+  int few, aligned, joined;
+  size_t opart, mpart, ends, flags, total;
 };
 ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dtype, int64_t slots);
 hipError_t launch_chunk(AttendK a, const ChunkPlan& p, int d, int dtype, void* workspace, hipStream_t s);

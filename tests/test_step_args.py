@@ -103,7 +103,7 @@ def test_bad_calls(L):
     assert L.grkv_chunk_attention_workspace_bytes(pg, _step(units=4096, unit_stride=64), ch) > 0
     assert L.grkv_chunk_attention_workspace_bytes(pg, _step(heads=1, tokens=(1 << 28) - 1), ch) > 0
     assert L.grkv_chunk_attention_workspace_bytes(pg, _step(heads=1, tokens=1 << 28), ch) == 0
-    # float32 rows come in tiles of 16: too many for a launch's index
+    # float32 rows come in tiles of 32: too many for a launch's index
     assert L.grkv_chunk_attention_workspace_bytes(_pool(dtype=1), _step(heads=1, tokens=(1 << 28) - 1), ch) == 0
 
 
