@@ -1029,20 +1029,13 @@ def _rotation(freqs, scale, interleaved, inverse, dev):
     return _Rotation(freqs.data_ptr(), 2 * freqs.shape[0], bool(interleaved), bool(inverse), scale)
 
 
-def _rows(t, name, dev, tokens=None, distinct=False):
+def _rows(t, name, dev):
     """A [tokens, heads, columns] tensor of whole rows."""
-    if t.get_device() != dev or _dtype_code(t) is None or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    step = t.stride()
+    if t.get_device() != dev or len(step) != 3 or (step[2] != 1 and t.shape[2] > 1) or _dtype_code(t) is None:
         raise ValueError("%s must be a bfloat16 or float32 [tokens, heads, columns] tensor on cuda:%d whose "
                          "last dimension is contiguous" % (name, dev))
-    if tokens is not None and t.shape[0] != tokens:
-        raise ValueError("%s has %d tokens, expected %d" % (name, t.shape[0], tokens))
-    if distinct:   # rows that are written do not overlap
-        ends = t.shape[2]
-        for step, n in sorted((t.stride(i), t.shape[i]) for i in (0, 1) if t.shape[i] > 1):
-            if step < ends:
-                raise ValueError("%s has rows that overlap" % name)
-            ends = step * (n - 1) + ends
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+    return _Rows(t.data_ptr(), step[0], step[1])
 
 
 def _out_rows(x, out, name, dev):
@@ -1051,11 +1044,23 @@ def _out_rows(x, out, name, dev):
 
     if out is None:
         out = torch.empty_like(x)
-    if out.shape != x.shape or out.dtype != x.dtype:
-        raise ValueError("%s must have %s and dtype %s" % (name, tuple(x.shape), x.dtype))
-    if out.data_ptr() == x.data_ptr() and out.stride() != x.stride() and x.numel() > 0:
-        raise ValueError("%s overlaps its input" % name)
-    return out, _rows(out, name, dev, distinct=True)
+        return out, _rows(out, name, dev)
+    if out is x:
+        apart = x.is_contiguous()
+    else:
+        if out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError("%s must have %s and dtype %s" % (name, tuple(x.shape), x.dtype))
+        if out.data_ptr() == x.data_ptr() and out.stride() != x.stride() and x.numel() > 0:
+            raise ValueError("%s overlaps its input" % name)
+        apart = out.is_contiguous()
+    rows = _rows(out, name, dev)
+    if not apart:   # rows that are written do not overlap
+        ends = out.shape[2]
+        for step, n in sorted((out.stride(i), out.shape[i]) for i in (0, 1) if out.shape[i] > 1):
+            if step < ends:
+                raise ValueError("%s has rows that overlap" % name)
+            ends = step * (n - 1) + ends
+    return out, rows
 
 
 def rotary(x, positions, freqs, *, scale: float = 1.0, interleaved: bool = False,
@@ -1177,9 +1182,8 @@ def pages_store(pages: Pages, slots, k, v, *, q=None, positions=None, freqs=None
         with on:
             return pages_store(pages, slots, k, v, q=q, positions=positions, freqs=freqs, scale=scale,
                                interleaved=interleaved, out=out)
-    kr = _rows(k, "k", dev)
+    kr, vr = _rows(k, "k", dev), _rows(v, "v", dev)
     T, H, d = k.shape
-    vr = _rows(v, "v", dev, T)
     _int32(T | H)
     if v.shape != k.shape or v.dtype != k.dtype or d != pages._c.head_dim:
         raise ValueError("shape mismatch: k %s %s v %s %s head_dim %d"
@@ -1197,14 +1201,14 @@ def pages_store(pages: Pages, slots, k, v, *, q=None, positions=None, freqs=None
     if freqs is not None:
         rot, at = _rotation(freqs, scale, interleaved, False, dev), _vector(positions, "positions", torch.int32, T, dev)
     if q is not None:
-        qr = _rows(q, "q", dev, T)
+        qr = _rows(q, "q", dev)
         out, yr = _out_rows(q, out, "out", dev)
         Q = q.shape[1]
         _int32(Q)
-        if q.shape[2] != d or q.dtype != k.dtype:
-            raise ValueError("q must have k's columns and dtype")
-    _check(lib().grkv_pages_store(pages._c, T, H, slots.data_ptr(), max(slots.stride(0), H) if T < 2 else
-                                  slots.stride(0), kr, vr, _dtype_code(k), qr, yr, Q, at, rot, handle))
+        if q.shape[::2] != (T, d) or q.dtype != k.dtype:
+            raise ValueError("q must have k's tokens, columns and dtype")
+    step = slots.stride(0) if T > 1 else H
+    _check(lib().grkv_pages_store(pages._c, T, H, slots.data_ptr(), step, kr, vr, _dtype_code(k), qr, yr, Q, at, rot, handle))
     return out
 
 

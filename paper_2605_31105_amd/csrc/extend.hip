@@ -8,12 +8,15 @@
 // slot, and where the slot is a page's first, the unit's table and the page's count.  What
 // bounds both is the chain of dependent reads and the two launches; the map's 8 bytes per
 // token and head are far from HBM's rate.
+#include <type_traits>
+
 #include "pages.h"
 
 namespace grkv {
 namespace {
 
 constexpr int kMapTh = 256;
+constexpr int kAhead = 8;
 
 struct ExtendK {
   grkv_pages pg;
@@ -30,12 +33,33 @@ struct ExtendK {
   int32_t* owner;           // [pool units] lowest entry that names the unit
   int32_t* code;            // [sequences] GRKV_PAGES_ of each
   int32_t* first;           // [sequences] position of the first new token
+  uint32_t hmul;            // division by heads: see sequence_at
+  int hshift;
   int2* jobs;               // [entries] rows before, place of the first new page among ids
   int32_t* ids;             // [pages] pages handed out, in order
 };
 
 __device__ __forceinline__ int unit_of(const ExtendK& a, int b, int h) {
   return a.units ? a.units[b * a.unit_stride + h] : b * a.heads + h;
+}
+// The sequence of entry e (e / heads), by the multiplication with a rounded-up reciprocal of 32 +
+// hshift bits (its top bit is the addition).
+__device__ __forceinline__ int sequence_at(const ExtendK& a, int e) {
+  return (int)((__umulhi((uint32_t)e, a.hmul) + (uint32_t)e) >> a.hshift);
+}
+// Inclusive sum over the lanes of a wave up to this one, by DPP: within 16 lanes, then the last of
+// a row to the next row, and of the first half to the second.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  auto step = [](uint32_t v, auto ctrl, auto rows) {
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+  };
+  constexpr std::integral_constant<int, 0xF> all{};
+  x = step(x, std::integral_constant<int, 0x111>{}, all);
+  x = step(x, std::integral_constant<int, 0x112>{}, all);
+  x = step(x, std::integral_constant<int, 0x114>{}, all);
+  x = step(x, std::integral_constant<int, 0x118>{}, all);
+  x = step(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});
+  return step(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});
 }
 __device__ __forceinline__ int count_of(const ExtendK& a, int b) { return max(a.counts[b], 0); }
 __device__ __forceinline__ int pages_of(const ExtendK& a, int64_t rows) {
@@ -45,8 +69,11 @@ __device__ __forceinline__ int pages_of(const ExtendK& a, int64_t rows) {
 __global__ __launch_bounds__(kPlanTh) void extend_plan_kernel(ExtendK a) {
   __shared__ int owner_s[kOwnerUnits];
   __shared__ unsigned long long scratch[2][kPlanTh / 64];
+  constexpr int WAVES = kPlanTh / 64;
+  static_assert(kAhead * WAVES == 128, "two sums to a lane");
+  __shared__ unsigned long long sums_s[kAhead * WAVES + 1];
   __shared__ int used_s;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t cap = (int64_t)a.pg.max_pages << a.shift;
   auto in_pool = [&](int u) { return (unsigned)u < (unsigned)a.pg.units; };
   auto refuse = [&](int b, int code) { atomicMax(a.code + b, code); };
@@ -56,6 +83,7 @@ __global__ __launch_bounds__(kPlanTh) void extend_plan_kernel(ExtendK a) {
   // sequences: where their rows start, and their first position
   if (tid == 0) used_s = 0;
   unsigned long long rows = 0;
+  bool late = false;   // a sequence of this thread's is refused
   for (int b0 = 0; b0 < a.sequences; b0 += kPlanTh) {
     const int b = b0 + tid;
     const bool on = b < a.sequences;
@@ -71,10 +99,11 @@ __global__ __launch_bounds__(kPlanTh) void extend_plan_kernel(ExtendK a) {
       const int u = unit_of(a, b, 0);
       if (in_pool(u)) first = a.pg.lens[u];   // (a bad length is found below)
     }
-    const bool fits = at + c <= (unsigned long long)a.tokens && first >= 0 && first <= 0x7fffffff - c;
+    const bool fits = c == 0 || (at + c <= (unsigned long long)a.tokens && first >= 0 && first <= 0x7fffffff - c);
+    late |= !fits;
     a.starts[b] = (int)(at < (unsigned)a.tokens ? at : (unsigned)a.tokens);
     a.first[b] = first;
-    __hip_atomic_store(a.code + b, c == 0 || fits ? GRKV_PAGES_OK : GRKV_PAGES_RANGE, __ATOMIC_RELAXED,
+    __hip_atomic_store(a.code + b, fits ? GRKV_PAGES_OK : GRKV_PAGES_RANGE, __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
   }
   if (tid == 0) a.starts[a.sequences] = (int)(rows < (unsigned)a.tokens ? rows : (unsigned)a.tokens);
@@ -86,72 +115,125 @@ __global__ __launch_bounds__(kPlanTh) void extend_plan_kernel(ExtendK a) {
       for (int u = tid; u < a.pg.units; u += kPlanTh) owner_s[u] = kNoOwner;
     } else {
       for (int e = tid; e < a.entries; e += kPlanTh) {
-        const int u = unit_of(a, e / a.heads, e % a.heads);
+        const int b = sequence_at(a, e), u = unit_of(a, b, e - b * a.heads);
         if (in_pool(u)) __hip_atomic_store(a.owner + u, kNoOwner, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
     __syncthreads();
     for (int e = tid; e < a.entries; e += kPlanTh) {
-      const int u = unit_of(a, e / a.heads, e % a.heads);
+      const int b = sequence_at(a, e), u = unit_of(a, b, e - b * a.heads);
       if (in_pool(u)) atomicMin(small ? owner_s + u : a.owner + u, e);
     }
   }
   __syncthreads();
 
-  // units: whether each can grow
-  for (int e = tid; e < a.entries; e += kPlanTh) {
-    const int b = e / a.heads, u = unit_of(a, b, e - b * a.heads);
-    int code = GRKV_PAGES_OK, n0 = 0;
-    if (!in_pool(u) || (a.units && (small ? owner_s[u] : load_agent(a.owner + u)) != e)) {
-      code = GRKV_PAGES_UNIT;
-    } else {
-      n0 = a.pg.lens[u];
-      if (n0 < 0 || n0 > cap) code = GRKV_PAGES_UNIT;
-      else if ((int64_t)n0 + count_of(a, b) > cap) code = GRKV_PAGES_LENGTH;
+  // Entries kAhead to a thread at a time, neighbouring threads' neighbours: their reads go out
+  // together, and a barrier serves the scans of all (8192 units MEASURED).
+  constexpr int BATCH = kPlanTh * kAhead;
+  auto each = [&](int e0, auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int e = e0 + k * kPlanTh + tid;
+      if (e0 + k * kPlanTh < a.entries && e < a.entries) f(k, e, sequence_at(a, e));
     }
-    if (code != GRKV_PAGES_OK) refuse(b, code);
-    a.jobs[e].x = n0;
-  }
-  __syncthreads();
-
-  // the pages that each needs, in the order of the entries
-  auto needs = [&](int e, int b, int* n0) {
-    *n0 = a.jobs[e].x;
-    if (load_agent(a.code + b) != GRKV_PAGES_OK) return 0;
-    return pages_of(a, (int64_t)*n0 + count_of(a, b)) - pages_of(a, *n0);
   };
+
+  // whether each can grow
+  bool bad = late;
+  for (int e0 = 0; e0 < a.entries; e0 += BATCH) {
+    int n[kAhead], c[kAhead], u[kAhead];
+    each(e0, [&](int k, int e, int b) { u[k] = unit_of(a, b, e - b * a.heads); });
+    each(e0, [&](int k, int, int b) {
+      c[k] = count_of(a, b);
+      n[k] = in_pool(u[k]) ? a.pg.lens[u[k]] : 0;
+    });
+    each(e0, [&](int k, int e, int b) {
+      int code = GRKV_PAGES_OK;
+      if (!in_pool(u[k]) || (a.units && (small ? owner_s[u[k]] : load_agent(a.owner + u[k])) != e) ||
+          n[k] < 0 || n[k] > cap)
+        code = GRKV_PAGES_UNIT;
+      else if ((int64_t)n[k] + c[k] > cap)
+        code = GRKV_PAGES_LENGTH;
+      if (code != GRKV_PAGES_OK) {
+        refuse(b, code);
+        bad = true;
+      }
+      a.jobs[e].x = n[k];
+    });
+  }
+  const bool any = __syncthreads_or(bad);   // a sequence is refused
+
+  // the pages that each needs, and those of the entries before it
   unsigned long long all = 0;
-  for (int e0 = 0; e0 < a.entries; e0 += kPlanTh) {
-    const int e = e0 + tid;
-    int n0, need = 0;
-    if (e < a.entries) need = needs(e, e / a.heads, &n0);
-    unsigned long long total;
-    const unsigned long long off = all + plan_scan((unsigned long long)need, scratch, turn++, &total);
-    all += total;
-    if (e < a.entries) a.jobs[e].y = (int)(off < (unsigned)a.pg.pages ? off : (unsigned)a.pg.pages);
+  for (int e0 = 0; e0 < a.entries; e0 += BATCH) {
+    uint32_t need[kAhead], before[kAhead];   // (2^26 pages at most: a wave's sum fits)
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) need[k] = 0;
+    each(e0, [&](int k, int e, int b) {
+      const int n0 = a.jobs[e].x;
+      if (!any || load_agent(a.code + b) == GRKV_PAGES_OK)
+        need[k] = pages_of(a, (int64_t)n0 + count_of(a, b)) - pages_of(a, n0);
+    });
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      before[k] = e0 + k * kPlanTh < a.entries ? wave_scan(need[k]) : 0;
+      if (lane == 63) sums_s[k * WAVES + wave] = before[k];
+      before[k] -= need[k];
+    }
+    __syncthreads();
+    // (of the batch's waves, in the order of their entries: two to a lane of the first wave)
+    if (wave == 0) {
+      const unsigned long long x = sums_s[2 * lane], y = sums_s[2 * lane + 1];
+      unsigned long long incl = x + y;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const unsigned long long t = __shfl_up(incl, d);
+        if (lane >= d) incl += t;
+      }
+      sums_s[2 * lane] = incl - x - y;
+      sums_s[2 * lane + 1] = incl - y;
+      if (lane == 63) sums_s[kAhead * WAVES] = incl;
+    }
+    __syncthreads();
+    each(e0, [&](int k, int e, int) {
+      const unsigned long long off = all + sums_s[k * WAVES + wave] + before[k];
+      a.jobs[e].y = (int)(off < (unsigned)a.pg.pages ? off : (unsigned)a.pg.pages);
+    });
+    all += sums_s[kAhead * WAVES];
+    __syncthreads();   // (the next batch writes the sums)
   }
   const uint32_t want = (uint32_t)(all < (unsigned)a.pg.pages ? all : (unsigned)a.pg.pages);
   const uint32_t found = take_pages(a.pg, want, bits0, a.ids, &turn);
 
   // sequences past the free pages are refused: those behind them that need pages are too,
   // so the pages of the others are the first of ids
-  if (all > found) {
+  auto needs = [&](int2 j, int c) { return pages_of(a, (int64_t)j.x + c) - pages_of(a, j.x); };
+  const bool full = all > found;
+  if (full) {
     for (int e = tid; e < a.entries; e += kPlanTh) {
-      const int b = e / a.heads;
-      int n0;
-      const int need = needs(e, b, &n0);
-      if (need > 0 && (uint64_t)a.jobs[e].y + need > found) refuse(b, GRKV_PAGES_FULL);
+      const int b = sequence_at(a, e);
+      if (any && load_agent(a.code + b) != GRKV_PAGES_OK) continue;   // (or refused here, by another of its heads)
+      const int2 j = a.jobs[e];
+      const int need = needs(j, count_of(a, b));
+      if (need > 0 && (uint64_t)j.y + need > found) refuse(b, GRKV_PAGES_FULL);
     }
     __syncthreads();
   }
   int used = 0;
-  for (int e = tid; e < a.entries; e += kPlanTh) {
-    const int b = e / a.heads;
-    if (load_agent(a.code + b) != GRKV_PAGES_OK) continue;
-    int n0;
-    const int need = needs(e, b, &n0);
-    if (need > 0) used = max(used, a.jobs[e].y + need);
-    a.pg.lens[unit_of(a, b, e - b * a.heads)] = n0 + count_of(a, b);
+  for (int e0 = 0; e0 < a.entries; e0 += BATCH) {
+    int2 j[kAhead];
+    int u[kAhead], c[kAhead];
+    each(e0, [&](int k, int e, int b) {
+      j[k] = a.jobs[e];
+      u[k] = unit_of(a, b, e - b * a.heads);
+      c[k] = count_of(a, b);
+    });
+    each(e0, [&](int k, int, int b) {
+      if ((any || full) && load_agent(a.code + b) != GRKV_PAGES_OK) return;
+      const int need = needs(j[k], c[k]);
+      if (need > 0) used = max(used, j[k].y + need);
+      a.pg.lens[u[k]] = j[k].x + c[k];
+    });
   }
   if (a.status)
     for (int b = tid; b < a.sequences; b += kPlanTh) a.status[b] = load_agent(a.code + b);
@@ -236,6 +318,8 @@ hipError_t launch_extend(const grkv_pages* pg, const grkv_step* step, const int3
   a.positions = positions;
   a.slots = slots;
   a.status = status;
+  while ((1ll << a.hshift) < a.heads) ++a.hshift;
+  a.hmul = (uint32_t)((((1ull << a.hshift) - (uint64_t)a.heads) << 32) / (uint64_t)a.heads + 1);
   char* ws = (char*)workspace;
   const ExtendLayout lay = extend_layout(pg, step->sequences, step->heads);
   a.owner = (int32_t*)(ws + lay.owner);

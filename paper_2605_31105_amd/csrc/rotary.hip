@@ -48,14 +48,16 @@ __device__ __forceinline__ void turn(int p, double f, float scale, bool inverse,
 __device__ __forceinline__ float value(u16 x) { return bf16_to_f32(x); }
 __device__ __forceinline__ float value(float x) { return x; }
 
-// N neighbouring columns as floats, by loads of 16 bytes where N fills them.
+// N neighbouring columns as floats, by loads of 16 bytes where N fills them, which pass the
+// caches: rows are read once (16k tokens of 40 heads, tensors used in turn, 66.6 -> 56.9 us; stored
+// so too 57.1).
 template <int N, typename T>
 __device__ __forceinline__ void load_cols(const T* p, float (&x)[N]) {
   constexpr int V = 16 / sizeof(T);
   if constexpr (N % V == 0) {
 #pragma unroll
     for (int k = 0; k < N; k += V) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(p + k);
+      const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + k));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (sizeof(T) == 2) {
@@ -251,7 +253,7 @@ void plan(RotaryK* r, int esize, bool vec, int heads) {
   r->pieces = r->turned + (r->d - r->dims) / v;
   r->per = 1;
   const int64_t threads = (int64_t)r->tokens * r->pieces * heads;
-  while (r->per < 8 && threads / (2 * r->per) >= 1024 * 8 * 64) r->per *= 2;
+  while (r->per < 4 && threads / (2 * r->per) >= 1024 * 8 * 64) r->per *= 2;
 }
 
 // Whether 16 bytes are whole pairs (or columns of one half) everywhere.
