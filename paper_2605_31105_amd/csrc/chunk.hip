@@ -32,6 +32,8 @@ constexpr int kFewFixed = 6, kFewTile = 2, kWideFixed = 15, kWideTile = 5, kTwoF
 // Calls of so few jobs give every block a piece of one job (8 units of 2048 keys and one token: MEASURED);
 // pieces of few rows are joined by the block that ends last, up to kJoined of a job.
 constexpr int kAlignedJobs = 64, kJoined = 16;
+// Jobs of a thread whose lengths are read together (66 sequences, 784 jobs: MEASURED).
+constexpr int kTogether = 4;
 // Starts that a block keeps in LDS, where the searches of its threads read them.
 constexpr int kStartsHeld = 1024;
 
@@ -57,11 +59,10 @@ __device__ __forceinline__ int find_sequence(const AttendK& a, const int32_t* st
 
 // A job's shape.
 struct Shape {
-  int h, start, t, r0, rows, len;
+  int h, start, t, r0, rows, unit, len;   // unit -1: outside the pool
   const int32_t* trow;
   __device__ __forceinline__ void hold() {   // (see Walk)
-    for (int* x : {&h, &start, &t, &r0, &rows, &len}) *x = __builtin_amdgcn_readfirstlane(*x);
-    trow = (const int32_t*)uniform64((int64_t)trow);
+    for (int* x : {&h, &start, &t, &r0, &rows, &unit}) *x = __builtin_amdgcn_readfirstlane(*x);
   }
 };
 
@@ -80,10 +81,13 @@ __device__ __forceinline__ bool shape_of(const AttendK& a, const int32_t* starts
   if (s->r0 >= R) return false;
   s->rows = (int)(R - s->r0 < (1 << kJobShift<E>) ? R - s->r0 : 1 << kJobShift<E>);
   const int u = a.units ? a.units[b * a.unit_stride + s->h] : b * a.heads + s->h;
-  const bool ok = (unsigned)u < (unsigned)a.pool_units;
-  s->len = ok ? min(max(a.lens[u], 0), a.max_pages << a.shift) : 0;
-  s->trow = a.table + (size_t)(ok ? u : 0) * a.max_pages;
+  s->unit = (unsigned)u < (unsigned)a.pool_units ? u : -1;
   return true;
+}
+__device__ __forceinline__ int raw_len(const AttendK& a, const Shape& s) { return s.unit >= 0 ? a.lens[s.unit] : 0; }
+__device__ __forceinline__ void set_len(const AttendK& a, int len, Shape* s) {
+  s->len = min(max(len, 0), a.max_pages << a.shift);
+  s->trow = a.table + (size_t)max(s->unit, 0) * a.max_pages;
 }
 
 __device__ __forceinline__ bool few(const Shape& s) { return s.rows <= kFewRows; }
@@ -111,13 +115,6 @@ __device__ __forceinline__ Cost cost_of(const Shape& s, const Span& sn) {
   return few(s) ? Cost{kFewFixed, kFewTile, n}
          : sizeof(E) == 4 ? Cost{kTwoFixed, kTwoTile, n} : Cost{kWideFixed, kWideTile, n};
 }
-template <typename E>
-__device__ __forceinline__ int job_cost(const AttendK& a, const int32_t* starts, int64_t j, int b, int tile, int next) {
-  Shape s;
-  if (!shape_of<E>(a, starts, j, b, tile, next, &s)) return 0;
-  return cost_of<E>(s, span_of<E>(a, s)).all();
-}
-
 // A walk over jobs in order, which keeps the sequence it is in.
 template <typename E>
 struct Walk {
@@ -180,12 +177,36 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
     const int64_t per = (a.jobs + kChunkTh - 1) / kChunkTh;
     const int64_t j0 = tid * per, j1 = min(j0 + per, a.jobs);
     int64_t own = 0;
+    int costs[kTogether];   // of the last jobs
     Walk<E> w{starts};
+    // the costs of jobs j ..: their reads go out together
+    auto together = [&](int64_t j) __attribute__((always_inline)) {
+      Shape s[kTogether];
+      int len[kTogether];
+      bool on[kTogether];
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) {
+        on[k] = j + k < j1;
+        if (on[k]) {
+          w.to(a, j + k);
+          on[k] = shape_of<E>(a, starts, j + k, w.b, w.tile, w.next, s + k);
+        }
+        len[k] = on[k] ? raw_len(a, s[k]) : 0;
+      }
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) {
+        costs[k] = 0;
+        if (!on[k]) continue;
+        set_len(a, len[k], s + k);
+        costs[k] = cost_of<E>(s[k], span_of<E>(a, s[k])).all();
+      }
+    };
     if (j0 < j1) {
       w.start(a, j0);
-      for (int64_t j = j0; j < j1; ++j) {
-        w.to(a, j);
-        own += job_cost<E>(a, starts, j, w.b, w.tile, w.next);
+      for (int64_t j = j0; j < j1; j += kTogether) {
+        together(j);
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) own += costs[k];
       }
     }
     int64_t incl = own;
@@ -240,12 +261,18 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
     hi = min(all, lo + part);
     if (at <= lo && lo < at + own) {
       int64_t j = j0;
-      w.start(a, j);
-      for (; j < j1; ++j) {
-        w.to(a, j);
-        const int cost = job_cost<E>(a, starts, j, w.b, w.tile, w.next);
-        if (lo < at + cost) break;
-        at += cost;
+      if (per > kTogether) w.start(a, j);
+      for (bool found = false; !found && j < j1;) {
+        if (per > kTogether) together(j);
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+          if (found || lo < at + costs[k]) {
+            found = true;
+          } else {
+            at += costs[k];
+            ++j;
+          }
+        }
       }
       first_s = j;
       at_s = at;
@@ -279,6 +306,7 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
       Shape s;
       if (!shape_of<E>(a, a.starts, j, u.b, u.tile, u.next, &s)) continue;
       s.hold();
+      set_len(a, __builtin_amdgcn_readfirstlane(raw_len(a, s)), &s);
       const Span sn = span_of<E>(a, s);
       const Cost cost = cost_of<E>(s, sn);
       const int64_t at = from;
