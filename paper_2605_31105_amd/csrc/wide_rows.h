@@ -154,7 +154,7 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
         vf[s][dm] = read_tr(tile + 16 * s * RB + (va ^ (dm << 6)), 8 * RB);
   };
 
-  f32x16 acc[DM], st[NK];
+  f32x16 acc[DM], s0[NK];
   float nref = kUnset;          // minus the reference
   float sum = 0.f, rsum = 0.f;  // weights' sums before and after their rounding (this lane's keys)
 #pragma unroll
@@ -172,7 +172,8 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
   };
   // One step: the 32 NK keys at slot0, whose logits are in st and whose V rows are at vt;
   // kt: K rows of the next step.
-  auto step = [&](int slot0, const char* kt, const char* vt) __attribute__((always_inline)) {
+  auto step = [&](int slot0, const char* kt, const char* vt, f32x16 (&st)[NK], f32x16 (&nx)[NK])
+                  __attribute__((always_inline)) {
     const bool full = slot0 + 32 * NK <= lim && (slot0 >= lo || slot0 + 32 * NK <= a.n_sink);
     if (!full) {
 #pragma unroll
@@ -183,7 +184,6 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
           if ((on >> (8 * (r / 4) + r % 4) & 1) == 0) st[n][r] = -__builtin_huge_valf();
       }
     }
-    f32x16 nx[NK];
     logits(kt, nx);
     bf16x8 p[NK][2];
     float s1, s2;   // this step's sums
@@ -238,7 +238,10 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
         for (int dm = 0; dm < DM; ++dm) acc[dm] = mfma32(vf[s][dm], p[n][s], acc[dm]);
     }
     if (KIND == kChunk) {
-      constexpr int ALL = NK * 2 * DM, AHEAD = 4;   // products of the step, operands read ahead
+      // products of the step, operands read ahead.  (Left to itself the compiler reads two ahead
+      // here, and the products wait for LDS: 4 chunks of 2048 over 4k to 14k 1620 -> 1500 us;
+      // three to eight ahead are equal.)
+      constexpr int ALL = NK * 2 * DM, AHEAD = 4;
       __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
       for (int k = 0; k < ALL - AHEAD; ++k) {
@@ -247,8 +250,6 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
       }
       __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
     }
-#pragma unroll
-    for (int n = 0; n < NK; ++n) st[n] = nx[n];
   };
 
   if (vt0 < vt1) {
@@ -260,34 +261,48 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
     auto load_k = [&](int i, int p) { load(a.k, tile(i), p, kr0 + (i & 1) * KB, ko, 64, false); };
     auto load_v = [&](int i, int p) { load(a.v, tile(i), p, vr0 + (i & 1) * KB, vo, 0, once); };
     const int p0 = page_at(tile(0));
-    // Pages are looked up a step before their keys are asked for (and values take those of
-    // the keys), so that no step waits for the table (MEASURED)
+    // A step's pages are looked up a step before their keys are asked for, and values take those
+    // of the keys, so that no step waits for the table (4 chunks of 2048 over 4k to 14k 1564 ->
+    // 1524 us).
     int pv = page_at(tile(1)), pk = 0;
-    const bool turns = KIND == kChunk && younger_block();
     load_k(0, p0);
     load_k(1, pv);
     load_v(0, p0);
     if (KIND == kChunk) pk = page_at(tile(2));
     ring_barrier<2 * NI>();
-    logits(kring, st);
-    for (int i = 0; i < vt1 - vt0; ++i) {
-      // K of tile i + 1 and V of tile i are here, and every wave is done with K of
-      // tile i and V of tile i - 1
-      ring_barrier<0>();
-      if (KIND == kChunk) {
-        if (turns) {
-          if (i & 1) __builtin_amdgcn_s_setprio(1);
-          else __builtin_amdgcn_s_setprio(0);
-        }
-        load_k(i + 2, pk);
-        load_v(i + 1, pv);
+    logits(kring, s0);
+    if (KIND == kChunk) {
+      f32x16 s1[NK];
+      const bool turns = younger_block();
+      // Two steps to a turn, so that logits are formed where the step after reads them
+      // (4 chunks of 2048 over 4k to 14k 1405 -> 1330 us).
+      auto turn = [&](int i, int odd, f32x16 (&st)[NK], f32x16 (&nx)[NK]) __attribute__((always_inline)) {
+        // K of tile i + 1 and V of tile i are here, and every wave is done with K of
+        // tile i and V of tile i - 1
+        ring_barrier<0>();
+        if (turns) odd ? __builtin_amdgcn_s_setprio(1) : __builtin_amdgcn_s_setprio(0);
+        load(a.k, tile(i + 2), pk, kr0 + odd * KB, ko, 64, false);
+        load(a.v, tile(i + 1), pv, vr0 + (1 - odd) * KB, vo, 0, false);
         pv = pk;
         pk = page_at(tile(i + 3));
-      } else {
+        step(slot_of(vt0 + i), kring + (1 - odd) * KB, vring + odd * KB, st, nx);
+      };
+      for (int i = 0;;) {
+        turn(i, 0, s0, s1);
+        if (++i >= vt1 - vt0) break;
+        turn(i, 1, s1, s0);
+        if (++i >= vt1 - vt0) break;
+      }
+    } else {
+      for (int i = 0; i < vt1 - vt0; ++i) {
+        ring_barrier<0>();
         load_k(i + 2, page_at(tile(i + 2)));
         load_v(i + 1, page_at(tile(i + 1)));
+        f32x16 nx[NK];
+        step(slot_of(vt0 + i), kring + ((i + 1) & 1) * KB, vring + (i & 1) * KB, s0, nx);
+#pragma unroll
+        for (int n = 0; n < NK; ++n) s0[n] = nx[n];
       }
-      step(slot_of(vt0 + i), kring + ((i + 1) & 1) * KB, vring + (i & 1) * KB);
     }
   }
   if (KIND == kChunk) __builtin_amdgcn_s_setprio(0);
