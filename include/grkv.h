@@ -649,8 +649,8 @@ size_t grkv_chunk_attention_workspace_bytes(const grkv_pages* pages, const grkv_
 
 /* These are asynchronous on stream, allocate nothing and may be captured.  Errors: those of the
  * calls on pages; GRKV_ERR_INVALID for null pointers and sizes out of range (sequences *
- * heads >= 2^24, tokens * heads or tokens * head_dim >= 2^31, heads or q_heads of a
- * store or a rotation > 65535, tokens * heads * group >= 2^30, a chunk call of 2^24
+ * heads >= 2^24, tokens * heads or tokens * head_dim >= 2^31, heads of a rotation,
+ * or 2 heads + q_heads of a store, > 65535, tokens * heads * group >= 2^30, a chunk call of 2^24
  * row tiles or more), a factor below 1 or other constants that are not finite and
  * positive; GRKV_ERR_UNSUPPORTED for head_dim > 32768 of grkv_rotary. */
 

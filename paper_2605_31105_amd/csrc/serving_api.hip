@@ -13,6 +13,9 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 // Blocks of 256 threads in a launch, which has fewer than 2^32 threads.
 constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
 
+// Heads of a launch of rotated rows (its grid's second size).
+constexpr int64_t kMostHeads = 65535;
+
 // Rows and elements of q within the kernels' indices.
 bool sizes_ok(int64_t entries, int64_t group, int64_t tokens, int64_t d) {
   return group * tokens < (int64_t(1) << 30) &&
@@ -371,7 +374,7 @@ int grkv_pages_extend(const grkv_pages* pages, const grkv_step* step, const int3
 int grkv_rotary(const grkv_rows* x, const grkv_rows* y, int32_t tokens, int32_t heads,
                 int32_t head_dim, int32_t dtype, const int32_t* positions,
                 const grkv_rotation* rotation, void* stream) {
-  if (tokens < 0 || heads < 0 || heads > 65535 || head_dim < 2) return GRKV_ERR_INVALID;
+  if (tokens < 0 || heads < 0 || heads > kMostHeads || head_dim < 2) return GRKV_ERR_INVALID;
   if (dtype != GRKV_BF16 && dtype != GRKV_F32) return GRKV_ERR_INVALID;
   if (head_dim > 32768) return GRKV_ERR_UNSUPPORTED;
   if ((int64_t)tokens * head_dim >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
@@ -412,8 +415,8 @@ int grkv_pages_store(const grkv_pages* pages, int32_t tokens, int32_t heads, con
                      const int32_t* positions, const grkv_rotation* rotation, void* stream) {
   int st = check_pages(pages);
   if (st != GRKV_OK) return st;
-  if (tokens < 0 || heads < 0 || heads > 65535 || q_heads < 0 || q_heads > 65535 || slot_stride < heads)
-    return GRKV_ERR_INVALID;
+  if (tokens < 0 || heads < 0 || q_heads < 0 || slot_stride < heads) return GRKV_ERR_INVALID;
+  if (2 * (int64_t)heads + q_heads > kMostHeads) return GRKV_ERR_INVALID;
   if (dtype != GRKV_BF16 && dtype != GRKV_F32) return GRKV_ERR_INVALID;
   if ((int64_t)tokens * pages->head_dim >= (int64_t(1) << 31)) return GRKV_ERR_INVALID;
   if (!rotation) q_heads = 0;

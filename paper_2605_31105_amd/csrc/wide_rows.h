@@ -237,19 +237,18 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
 #pragma unroll
         for (int dm = 0; dm < DM; ++dm) acc[dm] = mfma32(vf[s][dm], p[n][s], acc[dm]);
     }
-    if (KIND == kChunk) {
-      // products of the step, operands read ahead.  (Left to itself the compiler reads two ahead
-      // here, and the products wait for LDS: 4 chunks of 2048 over 4k to 14k 1620 -> 1500 us;
-      // three to eight ahead are equal.)
-      constexpr int ALL = NK * 2 * DM, AHEAD = 4;
-      __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
+    // products of the step, operands read ahead.  (Left to itself the compiler reads two ahead in
+    // a step's kernel, and the products wait for LDS: 4 chunks of 2048 over 4k to 14k 1620 -> 1500
+    // us; three to eight ahead are equal.  A 16k prompt with a 4k window 993 -> 985, trees of 32
+    // over 32k 106 -> 105.)
+    constexpr int ALL = NK * 2 * DM, AHEAD = 4;
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
-      for (int k = 0; k < ALL - AHEAD; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+    for (int k = 0; k < ALL - AHEAD; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
   };
 
   if (vt0 < vt1) {

@@ -128,7 +128,7 @@ def test_rotary_of_nothing(L):
         assert L.grkv_rotary(None, None, tokens, heads, 128, 0, None, None, None) == 0
 
 
-STORE = [(dict(tokens=-1), INV), (dict(heads=-1), INV), (dict(heads=65536, stride=65536), INV), (dict(stride=1), INV),
+STORE = [(dict(tokens=-1), INV), (dict(heads=-1), INV), (dict(heads=32764, stride=65536), INV), (dict(stride=1), INV),
          (dict(q_heads=-1), INV), (dict(q_heads=65536), INV), (dict(dtype=2), INV), (dict(slots=None), INV),
          (dict(k=None), INV), (dict(v=G._Rows(4097, 1, 1)), INV), (dict(q=None), INV), (dict(q_out=None), INV),
          (dict(positions=None), INV), (dict(rot=_rotation(dims=130)), INV), (dict(tokens=1 << 24), INV)]
