@@ -1151,11 +1151,12 @@ def pages_extend(pages: Pages, counts, tokens: int, *, heads=None, units=None, s
                    torch.empty(B, dtype=i32, device=dev))
     else:
         _given(out.slots, "out.slots", torch.int64, (tokens, st.heads), dev)
+        _vector(out.starts, "out.starts", i32, B + 1, dev)
+        _vector(out.positions, "out.positions", i32, tokens, dev)
+        _vector(out.status, "out.status", i32, B, dev)
     L = lib()
-    args = (_vector(counts, "counts", i32, B, dev), _vector(seen, "seen", i32, B, dev),
-            _vector(out.starts, "out.starts", i32, B + 1, dev),
-            _vector(out.positions, "out.positions", i32, tokens, dev), out.slots.data_ptr(),
-            _vector(out.status, "out.status", i32, B, dev))
+    args = (_vector(counts, "counts", i32, B, dev), _vector(seen, "seen", i32, B, dev), out.starts.data_ptr(),
+            out.positions.data_ptr(), out.slots.data_ptr(), out.status.data_ptr())
     workspace = _workspace(workspace, L.grkv_pages_extend_workspace_bytes(pages._c, st), dev)
     _check(L.grkv_pages_extend(pages._c, st, *args, handle, workspace.data_ptr(), workspace.numel()))
     if B == 0:   # (the call does nothing)

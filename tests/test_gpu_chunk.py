@@ -101,6 +101,13 @@ def test_many_sequences_of_one_token():
     _run("many", lens, [1] * 300, 3, 4, 16, 64, BF, heads=[1])
 
 
+def test_more_sequences_than_a_block_holds_starts_of():
+    lens = [[1 + (7 * b) % 40] for b in range(1500)]
+    _run("1500", lens, [1 if b % 7 else 0 for b in range(1500)], 1, 2, 16, 64, BF)
+    counts = [1 + (b % 600 == 5) * 70 for b in range(1200)]
+    _run("1200", [[c + (3 * b) % 20] for b, c in enumerate(counts)], counts, 1, 2, 16, 64, F32)
+
+
 def test_many_short_jobs_and_idle_sequences():
     counts = [(b * 7) % 23 if b % 3 else 0 for b in range(150)]
     lens = [[c + (13 * b) % 90 for _ in range(2)] for b, c in enumerate(counts)]

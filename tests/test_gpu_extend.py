@@ -170,7 +170,7 @@ def test_many_units_and_sequences(U, H, B):
     # more units than the plan's LDS holds, more sequences and entries than it has threads
     import paper_2605_31105_amd as G
     rng = random.Random(U + B)
-    ps, width, pages = 16, 6, 60000
+    ps, width, pages = 16, 6, 2 * U + 7
     pg, m = G.new_pages(U, width, pages, ps, 64), Model(U, width, pages, ps)
     for turn in range(2):
         counts = [rng.choice([0, 1, rng.randint(1, 40)]) for _ in range(B)]
@@ -178,6 +178,14 @@ def test_many_units_and_sequences(U, H, B):
         units = [flat[b * H:b * H + H] for b in range(B)]
         _both(pg, m, counts, sum(counts) + turn, units)
     _both(pg, m, counts, sum(counts), None, H)
+    # a unit that is not there, one named twice, rows past the step's and, in the end, no pages left
+    units[B // 2][H - 1], units[B - 1][0] = U, units[0][0]
+    bad = _both(pg, m, counts, sum(counts) - 1, units)
+    assert bad[B // 2] in (UNIT, RANGE) and bad[B - 1] in (UNIT, RANGE)   # (the largest of its codes)
+    for _ in range(4):
+        more = [max(c, 12) for c in counts]
+        codes = _both(pg, m, more, sum(more), None, H)
+    print(U, H, B, "codes", sorted(set(codes)), flush=True)
 
 
 def test_a_units_matrix_with_strides_and_a_step_used_again():
