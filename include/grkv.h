@@ -613,11 +613,11 @@ int grkv_rotary_freqs(int32_t dims, double base, int32_t method, double factor, 
 
 /* Stores the step's keys and values: row (t, h) of k and v goes to row slots[t * slot_stride + h]
  * of the pool's k and v, rounded to the pool's type; a negative slot, or one past the pool's
- * rows, stores nothing.  With a rotation (whose `inverse` is not read as a special case) keys
- * are rotated by positions, and so are q's `q_heads` rows into q_out (as in grkv_rotary);
- * rows of tokens at GRKV_NO_POSITION are left as they were.  rotation NULL: positions and q are
- * not read.  q_heads 0: no queries.  k, v and q have head_dim columns of one type, dtype.  Slots of
- * a call are different from one another (grkv_pages_extend's are). */
+ * rows, stores nothing.  With a rotation keys are rotated by positions, and so are q's `q_heads`
+ * rows into q_out (as in grkv_rotary); rows of tokens at GRKV_NO_POSITION are left as they were.
+ * rotation NULL: positions and q are not read.  q_heads 0: no queries.  k, v and q have head_dim
+ * columns of one type, dtype.  Slots of a call are different from one another
+ * (grkv_pages_extend's are). */
 int grkv_pages_store(const grkv_pages* pages, int32_t tokens, int32_t heads, const int64_t* slots,
                      int64_t slot_stride, const grkv_rows* k, const grkv_rows* v, int32_t dtype,
                      const grkv_rows* q, const grkv_rows* q_out, int32_t q_heads,
@@ -629,8 +629,10 @@ int grkv_pages_store(const grkv_pages* pages, int32_t tokens, int32_t heads, con
  * j > p - window or j < n_sink:
  *   q, o  pages' dtype [tokens][heads * group][head_dim], 16-byte aligned
  *   lse   float [tokens][heads * group], or NULL
- * as in grkv_tree_attention, also for queries that see nothing, values that are not seen, and
- * roundings.  Rows of no sequence, and those from a sequence's `longest` on, stay as they
+ * as in grkv_tree_attention, also for queries that see nothing and for values that are not
+ * seen.  Over bf16 values weights are held to 2^-15 of them for a sequence's rows (tokens times
+ * group) up to 16, and the last 16 or fewer past a multiple of 128; the others are rounded
+ * to bf16 (2^-8).  Rows of no sequence, and those from a sequence's `longest` on, stay as they
  * were.  `longest` bounds the workspace.  Of a refused sequence (grkv_pages_extend) the rows
  * mean nothing. */
 typedef struct {

@@ -38,12 +38,12 @@ constexpr int kFewRows = 16;
 // tiles more for a job's first reads and its outputs; a token of 64 sequences beside two chunks of
 // 512 with the latter tile at 4, 5 and 6: 285, 272 and 282 us.
 constexpr int kFewFixed = 6, kFewTile = 2, kWideFixed = 15, kWideTile = 5, kTwoFixed = 9, kTwoTile = 3;
-// Calls of so few jobs give every block a piece of one job (8 units of 2048 keys and one token 22 ->
-// 17 us, the joining in place among it);
-// pieces of few rows are joined by the block that ends last, up to kJoined of a job.
+// Calls of so few jobs give every block a piece of one job, and pieces of few rows, up to kJoined
+// of a job, are joined by the block that ends last (8 units of 2048 keys and one token, both
+// together 22 -> 17 us).
 constexpr int kAlignedJobs = 64, kJoined = 16;
-// Jobs of a thread whose lengths are read together (66 sequences, 784 jobs: a
-// call of 274 -> 272 us).
+// Jobs of a thread whose lengths are read together (66 sequences, 784 jobs: a call of 274 -> 272
+// us).
 constexpr int kTogether = 4;
 // Starts that a block keeps in LDS, where the searches of its threads read them.
 constexpr int kStartsHeld = 1024;
@@ -109,7 +109,8 @@ __device__ __forceinline__ Span span_of(const AttendK& a, const Shape& s) {
                    sizeof(E) == 4 || few(s) ? Tile<E>::KEYS : kWideKeys);
 }
 
-// What jobs cost: `fixed` for the rows themselves, then `tile` for each of `n` tiles (one at least, so that a job without keys is some block's too).
+// What jobs cost: `fixed` for the rows themselves, then `tile` for each of `n` tiles (one at
+// least, so that a job without keys is some block's too).
 struct Cost {
   int fixed, tile, n;
   __device__ __forceinline__ int all() const { return fixed + tile * n; }
@@ -126,6 +127,7 @@ __device__ __forceinline__ Cost cost_of(const Shape& s, const Span& sn) {
   return few(s) ? Cost{kFewFixed, kFewTile, n}
          : sizeof(E) == 4 ? Cost{kTwoFixed, kTwoTile, n} : Cost{kWideFixed, kWideTile, n};
 }
+
 // A walk over jobs in order, which keeps the sequence it is in.
 template <typename E>
 struct Walk {

@@ -6,6 +6,7 @@ import pytest
 
 from tests.attention_ref import check, sink_seen
 from tests.test_gpu_attention import BF, F32, _i32, _pool
+from tests.test_gpu_attention_values import _close, _ramp
 
 pytestmark = pytest.mark.gpu
 
@@ -153,6 +154,62 @@ def test_large_logits_and_values():
         o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32([0, c]), heads=1, return_lse=True))
         for g in {0, group - 1}:
             check("growing", o[:, g], lse[:, g], q[:, g], K[0], V[0], sink_seen(n, c, 0, 0))
+
+
+@pytest.mark.parametrize("d,group,counts,lens", [
+    (128, 4, [1, 3, 4], [300, 40, 2000]), (64, 3, [5, 1, 0], [129, 33, 7]), (128, 4, [1] * 90, [20 + 31 * b for b in range(90)]),
+    (64, 16, [1, 1], [9000, 20])])
+def test_weights_of_few_rows_are_held_to_two_parts(d, group, counts, lens):
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + group)
+    pg, K, V = _pool(lens, 16, d, BF, gen)
+    T, starts = sum(counts), [sum(counts[:b]) for b in range(len(counts) + 1)]
+    q = torch.randn((T, group, d), generator=gen).to(BF)
+    o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32(starts), heads=1, return_lse=True))
+    for b, c in enumerate(counts):
+        at = slice(starts[b], starts[b + 1])
+        for g in range(group if c else 0):
+            _close("seq %d head %d" % (b, g), o[at, g], lse[at, g], q[at, g], K[b], V[b], sink_seen(lens[b], c, 0, 0))
+
+
+@pytest.mark.parametrize("dtype,d,group,counts,lens", [
+    (BF, 128, 4, [1, 2], [300, 40]), (BF, 64, 4, [1, 1], [900, 20000]), (F32, 128, 4, [2, 20], [500, 90]),
+    (F32, 64, 1, [1, 1], [100, 17]), (BF, 128, 4, [100, 1], [700, 50]), (BF, 64, 5, [40, 60], [1500, 400])])
+def test_large_values_under_growing_logits(dtype, d, group, counts, lens):
+    # logits that rise by 39 (log2) along the keys under values of 1e36: no weight against an early
+    # reference may carry finite values past a float's range
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + group)
+    pg, K, V = _pool(lens, 64, d, dtype, gen)
+    T, starts = sum(counts), [sum(counts[:b]) for b in range(len(counts) + 1)]
+    q = torch.randn((T, group, d), generator=gen)
+    for u, n in enumerate(lens):
+        K[u], V[u] = K[u].float(), V[u].float()
+        _ramp(q, K[u], V[u], -19.5, 19.5)
+        K[u], V[u] = K[u].to(dtype), V[u].to(dtype)
+        slot = torch.arange(n, device="cuda")
+        pg.k[pg.table[u, slot // 64].long(), slot % 64] = K[u].cuda()
+        pg.v[pg.table[u, slot // 64].long(), slot % 64] = V[u].cuda()
+    q = q.to(dtype)
+    o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32(starts), heads=1, return_lse=True))
+    assert torch.isfinite(o).all()
+    for b, c in enumerate(counts):
+        at = slice(starts[b], starts[b + 1])
+        for g in range(group):
+            check("seq %d head %d" % (b, g), o[at, g], lse[at, g], q[at, g], K[b], V[b], sink_seen(lens[b], c, 0, 0))
+
+
+def test_infinities_that_every_row_sees_stay_infinities():
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(21)
+    for dtype, c in ((BF, 1), (BF, 30), (F32, 1), (F32, 30)):
+        pg, K, V = _pool([700], 64, 128, dtype, gen)
+        V[0][70, 7], V[0][70, 9] = torch.inf, -torch.inf
+        pg.v[int(pg.table[0, 1]), 6] = V[0][70].cuda()
+        q = torch.randn((c, 4, 128), generator=gen).to(dtype)
+        o = G.chunk_attention(q.cuda(), pg, _i32([0, c]), heads=1).cpu()
+        assert (o[..., 7] == torch.inf).all() and (o[..., 9] == -torch.inf).all()
+        assert torch.isfinite(o[..., [x for x in range(128) if x not in (7, 9)]]).all()
 
 
 def test_results_do_not_depend_on_the_workspace_or_the_run():
