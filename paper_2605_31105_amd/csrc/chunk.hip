@@ -5,7 +5,8 @@
 // of the group) of one unit: up to 16 rows take the kernel of few rows, whose four waves each
 // read keys of their own and which HBM bounds; more, up to 128, the one of many rows,
 // whose waves share tiles of 64 keys in LDS and which its exponentials and products bound.
-// float32 has jobs of 32 rows, by the kernel of few rows.
+// float32 has jobs of 32 rows, by the kernel of few rows.  Calls without longer sequences than one
+// or two 16-row tiles have kernels of their own, with the code of few rows alone.
 // How many rows and keys a job has only the device knows, and a batch holds one key beside
 // 100k and one row beside 128, so the costs of all jobs are put in a row and cut into equal
 // parts, one per block, two blocks per compute unit: no block waits for a longer one, and
@@ -33,7 +34,8 @@ static_assert(kAtTh == kWTh, "one kernel holds both");
 template <typename E>
 constexpr int kJobShift = sizeof(E) == 2 ? 7 : 5;
 constexpr int kFewRows = 16;
-// Costs, in half tiles of 32 keys read for few rows (bf16; float32 of two 16-row tiles: kTwo).
+// Costs, in half tiles of 32 keys read for few rows (kTwo: two
+// 16-row tiles of them, 32 keys of bf16 or 16 of float32).
 // Timed blocks take 1.05 us for such a tile, 2.4 to 2.8 for 64 keys of many rows and some two
 // tiles more for a job's first reads and its outputs; a token of 64 sequences beside two chunks of
 // 512 with the latter tile at 4, 5 and 6: 285, 272 and 282 us.
@@ -106,7 +108,7 @@ __device__ __forceinline__ bool few(const Shape& s) { return s.rows <= kFewRows;
 template <typename E>
 __device__ __forceinline__ Span span_of(const AttendK& a, const Shape& s) {
   return make_span(a, false, s.len, s.len - s.t, s.t, group_of(a, s.r0), group_of(a, s.r0 + s.rows - 1),
-                   sizeof(E) == 4 || few(s) ? Tile<E>::KEYS : kWideKeys);
+                   sizeof(E) == 4 || a.rt == 2 || few(s) ? Tile<E>::KEYS : kWideKeys);
 }
 
 // What jobs cost: `fixed` for the rows themselves, then `tile` for each of `n` tiles (one at
@@ -122,10 +124,10 @@ struct Cost {
   }
 };
 template <typename E>
-__device__ __forceinline__ Cost cost_of(const Shape& s, const Span& sn) {
+__device__ __forceinline__ Cost cost_of(const AttendK& a, const Shape& s, const Span& sn) {
   const int n = max(sn.nt, 1);
   return few(s) ? Cost{kFewFixed, kFewTile, n}
-         : sizeof(E) == 4 ? Cost{kTwoFixed, kTwoTile, n} : Cost{kWideFixed, kWideTile, n};
+         : sizeof(E) == 4 || a.rt == 2 ? Cost{kTwoFixed, kTwoTile, n} : Cost{kWideFixed, kWideTile, n};
 }
 
 // A walk over jobs in order, which keeps the sequence it is in.
@@ -169,9 +171,13 @@ __device__ __forceinline__ void combine_row(const AttendK& a, const CutJob& cut,
   write_out<E, D>(x, row_at<kChunk>(x, 0, g, i), ch, o.x, o.m, o.l, o.lx);
 }
 
-// FEW: no job has more than kFewRows rows.
-template <typename E, int D, bool FEW>
-__global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
+// RT: 16-row tiles that no job has more of (1, or 2 over bf16 values), 0: rows of any number.
+// Jobs of 17 to 32 rows alone are bound by HBM, which the kernel of few rows serves better (64
+// sequences of 500 to 8000 keys, 5 tokens of 4 heads each: 235 -> 211 us, one block for each compute
+// unit, whose registers hold no second of 128 columns; two in turn 227).
+template <typename E, int D, int RT>
+__global__ __launch_bounds__(kChunkTh, RT == 2 && D == 128 ? 1 : 2) void chunk_kernel(AttendK a) {
+  constexpr bool FEW = RT == 1;   // no job has more than kFewRows rows
   constexpr int BYTES = kStage<E, D>;
   static_assert(sizeof(E) == 4 || BYTES == kRing<D>, "both kinds take the same LDS");
   __shared__ __attribute__((aligned(1024))) char v0_s[BYTES];
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
         costs[k] = 0;
         if (!on[k]) continue;
         set_len(a, len[k], s + k);
-        costs[k] = cost_of<E>(s[k], span_of<E>(a, s[k])).all();
+        costs[k] = cost_of<E>(a, s[k], span_of<E>(a, s[k])).all();
       }
     };
     if (j0 < j1) {
@@ -321,7 +327,7 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
       s.hold();
       set_len(a, __builtin_amdgcn_readfirstlane(raw_len(a, s)), &s);
       const Span sn = span_of<E>(a, s);
-      const Cost cost = cost_of<E>(s, sn);
+      const Cost cost = cost_of<E>(a, s, sn);
       const int64_t at = from;
       int vt0, vt1, parts;
       if (a.aligned) {
@@ -352,7 +358,7 @@ __global__ __launch_bounds__(kChunkTh, 2) void chunk_kernel(AttendK a) {
       if (FEW || few(s)) {
         attend_rows<E, D, 1, kChunk>(x, sn, 0, s.r0, vt0, end, to, FEW && a.flags, s.len, s.t, s.trow, v0_s, v1_s);
       } else if constexpr (!FEW) {
-        if constexpr (sizeof(E) == 4)
+        if constexpr (sizeof(E) == 4 || RT == 2)
           attend_rows<E, D, 2, kChunk>(x, sn, 0, s.r0, vt0, end, to, false, s.len, s.t, s.trow, v0_s, v1_s);
         else
           wide_rows<D, kChunk>(x, sn, 0, s.r0, vt0, end, [&] { return Part{!whole, rows_at}; }, s.len, s.t, s.trow,
@@ -383,10 +389,15 @@ __global__ __launch_bounds__(kChunkTh) void chunk_combine_kernel(AttendK a) {
 }
 
 template <typename E, int D>
-hipError_t launch_ed(const AttendK& a, bool few, hipStream_t s) {
+hipError_t launch_ed(const AttendK& a, hipStream_t s) {
   const dim3 grid((unsigned)a.blocks), th(kChunkTh);
-  if (few) hipLaunchKernelGGL((chunk_kernel<E, D, true>), grid, th, 0, s, a);
-  else hipLaunchKernelGGL((chunk_kernel<E, D, false>), grid, th, 0, s, a);
+  if (a.rt == 1) {
+    hipLaunchKernelGGL((chunk_kernel<E, D, 1>), grid, th, 0, s, a);
+  } else if (a.rt == 0) {
+    hipLaunchKernelGGL((chunk_kernel<E, D, 0>), grid, th, 0, s, a);
+  } else if constexpr (sizeof(E) == 2) {
+    hipLaunchKernelGGL((chunk_kernel<E, D, 2>), grid, th, 0, s, a);
+  }
   if (!a.flags)
     hipLaunchKernelGGL((chunk_combine_kernel<E, D>), dim3((unsigned)a.blocks, (a.part_rows + 15) / 16), th, 0, s, a);
   return hipGetLastError();
@@ -404,13 +415,14 @@ ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dty
   // parts of the longest units, if all are
   const int64_t keys = dtype == GRKV_BF16 ? Tile<u16>::KEYS : Tile<float>::KEYS;
   const int64_t parts = (((slots + keys - 1) / keys) * kFewTile + kFewFixed + p.min_part - 1) / p.min_part;
-  int64_t blocks = p.jobs < kChunkBlocks ? p.jobs * (parts < kChunkBlocks ? parts : kChunkBlocks) : kChunkBlocks;
+  p.rt = rows <= kFewRows ? 1 : rows <= 2 * kFewRows && dtype == GRKV_BF16 ? 2 : 0;
+  const int most = p.rt == 2 && d == 128 ? kChunkBlocks / 2 : kChunkBlocks;   // (what the card holds at once)
+  int64_t blocks = p.jobs < most ? p.jobs * (parts < most ? parts : most) : most;
   p.aligned = p.jobs <= kAlignedJobs;
   if (p.aligned && blocks < 2 * p.jobs) blocks = 2 * p.jobs;
-  blocks = blocks < kChunkBlocks ? (blocks + kXcds - 1) / kXcds * kXcds : kChunkBlocks;
+  blocks = blocks < most ? (blocks + kXcds - 1) / kXcds * kXcds : most;
   p.blocks = (int)(blocks > kXcds ? blocks : kXcds);
-  p.few = rows <= kFewRows;
-  p.joined = p.aligned && p.few && p.blocks <= kJoined * p.jobs;
+  p.joined = p.aligned && p.rt == 1 && p.blocks <= kJoined * p.jobs;
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   const size_t part = 2 * (size_t)p.blocks * p.part_rows;
   p.opart = 0;
@@ -424,6 +436,7 @@ ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dty
 hipError_t launch_chunk(AttendK a, const ChunkPlan& p, int d, int dtype, void* workspace, hipStream_t s) {
   a.splits = kJoined;   // (of the marks)
   a.split_shift = 0;
+  a.rt = p.rt;
   a.aligned = p.aligned;
   a.flags = p.joined ? (uint64_t*)((char*)workspace + p.flags) : nullptr;
   a.nonce = p.joined ? next_nonce() : 0;
@@ -436,8 +449,8 @@ hipError_t launch_chunk(AttendK a, const ChunkPlan& p, int d, int dtype, void* w
   a.mpart = (float4*)((char*)workspace + p.mpart);
   a.ends = (CutJob*)((char*)workspace + p.ends);
   set_group(a);
-  if (dtype == GRKV_BF16) return d == 64 ? launch_ed<u16, 64>(a, p.few, s) : launch_ed<u16, 128>(a, p.few, s);
-  return d == 64 ? launch_ed<float, 64>(a, p.few, s) : launch_ed<float, 128>(a, p.few, s);
+  if (dtype == GRKV_BF16) return d == 64 ? launch_ed<u16, 64>(a, s) : launch_ed<u16, 128>(a, s);
+  return d == 64 ? launch_ed<float, 64>(a, s) : launch_ed<float, 128>(a, s);
 }
 
 }  // namespace grkv

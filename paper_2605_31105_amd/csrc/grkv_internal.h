@@ -350,6 +350,7 @@ struct AttendK {
   int64_t unit_stride;
   int sequences, heads, q_heads, longest, step_tokens;
   int part_rows;      // rows of a partial result
+  int rt;             // 16-row tiles that no entry has more of (1, 2), 0: rows of any number
   int aligned;        // every block has a piece of one job
   int64_t jobs;
   struct CutJob* ends;   // [blocks]
@@ -375,7 +376,7 @@ uint64_t next_nonce();
 struct ChunkPlan {
   int64_t jobs;       // row tiles of all units
   int blocks, min_part, part_rows;
-  int few, aligned, joined;
+  int rt, aligned, joined;
   size_t opart, mpart, ends, flags, total;
 };
 ChunkPlan chunk_plan(const grkv_step* step, const grkv_chunk* ch, int d, int dtype, int64_t slots);

@@ -158,14 +158,17 @@ def test_large_logits_and_values():
 
 @pytest.mark.parametrize("d,group,counts,lens", [
     (128, 4, [1, 3, 4], [300, 40, 2000]), (64, 3, [5, 1, 0], [129, 33, 7]), (128, 4, [1] * 90, [20 + 31 * b for b in range(90)]),
-    (64, 16, [1, 1], [9000, 20])])
+    (64, 16, [1, 1], [9000, 20]), (128, 4, [5, 8, 1, 6], [300, 40, 9000, 6]), (64, 3, [10, 9], [129, 33]),
+    (128, 7, [4, 3] * 40, [20 + 31 * b for b in range(80)])])
 def test_weights_of_few_rows_are_held_to_two_parts(d, group, counts, lens):
     import paper_2605_31105_amd as G
     gen = torch.Generator().manual_seed(d + group)
     pg, K, V = _pool(lens, 16, d, BF, gen)
     T, starts = sum(counts), [sum(counts[:b]) for b in range(len(counts) + 1)]
     q = torch.randn((T, group, d), generator=gen).to(BF)
-    o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32(starts), heads=1, return_lse=True))
+    assert max(counts) * group <= 32   # (calls that name their longest sequence)
+    o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32(starts), heads=1, longest=max(counts),
+                                                 return_lse=True))
     for b, c in enumerate(counts):
         at = slice(starts[b], starts[b + 1])
         for g in range(group if c else 0):
