@@ -102,10 +102,11 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
   const char* vb = (const char*)a.v;
   const int last = sn.kend - 1;
   auto slot_of = [&](int vt) { return (vt < sn.at ? vt : vt - sn.at + sn.bt) * TK; };
-  // the page of 16-row part h of tile vt, and the byte offset of its rows (uniform)
-  auto slot16 = [&](int vt, int h) { return __builtin_amdgcn_readfirstlane(min(slot_of(vt) + 16 * h, last)); };
-  auto page16 = [&](int vt, int h) -> int {
-    if (PAGED) return page_of<KIND>(trow, slot16(vt, h) >> a.shift);
+  // the first slot of 16-row part h of the tile at slot0, its page, and the byte offset of its rows
+  // (uniform)
+  auto slot16 = [&](int slot0, int h) { return __builtin_amdgcn_readfirstlane(min(slot0 + 16 * h, last)); };
+  auto page16 = [&](int slot) -> int {
+    if (PAGED) return page_of<KIND>(trow, slot >> a.shift);
     return 0;
   };
   auto rows16 = [&](int slot, int p) -> size_t {
@@ -136,8 +137,9 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     size_t rb[KT];
 #pragma unroll
     for (int h = 0; h < KT; ++h) {
-      rb[h] = rows16(slot16(vt, h), KIND == kChunk ? ahead[h] : page16(vt, h));
-      if (KIND == kChunk) ahead[h] = page16(next_tile(vt), h);
+      const int slot = slot16(slot0, h);
+      rb[h] = rows16(slot, KIND == kChunk ? ahead[h] : page16(slot));
+      if (KIND == kChunk) ahead[h] = page16(slot16(slot_of(next_tile(vt)), h));
     }
     const bool whole = slot0 + TK - 1 <= last;
     auto lane_row = [&](int row) { return min(slot0 + row, last) & 15; };
@@ -296,7 +298,7 @@ __device__ __forceinline__ void attend_rows(const AttendK& a, const Span& sn, in
     Frag ka[KT][DS], kc[KT][DS];
 #pragma unroll
     for (int h = 0; h < KT; ++h)
-      if (KIND == kChunk) ahead[h] = page16(vt, h);
+      if (KIND == kChunk) ahead[h] = page16(slot16(slot_of(vt), h));
     load(vt, va, ka);
     const bool turns = KIND == kChunk && younger_block();
     for (;;) {
