@@ -603,7 +603,10 @@ int grkv_rotary(const grkv_rows* x, const grkv_rows* y, int32_t tokens, int32_t 
  *                       as they are)
  *   GRKV_ROTARY_PARTS   f (1 - y + y factor) / factor with y = (length f / (2 pi) - low) / (high - low)
  *                       taken to 0 .. 1: pairs that make `high` turns or more over the length
- *                       stay, those of `low` or fewer are divided (arXiv 2309.00071, Sec. 3.2) */
+ *                       stay, those of `low` or fewer are divided (arXiv 2309.00071, Sec. 3.2)
+ * GRKV_ERR_INVALID for constants that are not finite, a base, factor or length not above zero, a
+ * factor below 1, low < 0 or high <= low (each where the method reads it), and where the scaled base or
+ * a frequency passes 64 bits or falls to zero; freqs then means nothing. */
 #define GRKV_ROTARY_PLAIN 0
 #define GRKV_ROTARY_LINEAR 1
 #define GRKV_ROTARY_BASE 2
@@ -653,8 +656,8 @@ size_t grkv_chunk_attention_workspace_bytes(const grkv_pages* pages, const grkv_
  * calls on pages; GRKV_ERR_INVALID for null pointers and sizes out of range (sequences *
  * heads >= 2^24, tokens * heads or tokens * head_dim >= 2^31, heads of a rotation,
  * or 2 heads + q_heads of a store, > 65535, tokens * heads * group >= 2^30, a chunk call of 2^24
- * row tiles or more), a factor below 1 or other constants that are not finite and
- * positive; GRKV_ERR_UNSUPPORTED for head_dim > 32768 of grkv_rotary. */
+ * row tiles or more); GRKV_ERR_UNSUPPORTED for head_dim > 32768 of grkv_rotary.  A rotation's scale
+ * and frequencies are taken as they are. */
 
 /* Workspace bytes grkv_compress needs for this shape; 0 if the shape is
  * invalid or unsupported. */

@@ -395,6 +395,7 @@ int grkv_rotary_freqs(int32_t dims, double base, int32_t method, double factor, 
       (!(length > 0.0) || !isfinite(length) || !(low >= 0.0) || !(high > low) || !isfinite(high)))
     return GRKV_ERR_INVALID;
   if (method == GRKV_ROTARY_BASE && dims > 2) base *= pow(factor, (double)dims / (dims - 2));
+  if (!isfinite(base)) return GRKV_ERR_INVALID;
   for (int i = 0; i < dims / 2; ++i) {
     double f = pow(base, -2.0 * i / dims);
     if (method == GRKV_ROTARY_LINEAR) f /= factor;
@@ -404,6 +405,8 @@ int grkv_rotary_freqs(int32_t dims, double base, int32_t method, double factor, 
       stay = stay < 0.0 ? 0.0 : stay > 1.0 ? 1.0 : stay;
       f = f * stay + f / factor * (1.0 - stay);
     }
+    // (constants far apart: a frequency of 0 would leave its pair without a position)
+    if (!(f > 0.0) || !isfinite(f)) return GRKV_ERR_INVALID;
     freqs[i] = f;
   }
   return GRKV_OK;

@@ -194,6 +194,26 @@ def test_bad_scaling(kw):
         G.rotary_freqs(8, **kw)
 
 
+@pytest.mark.parametrize("dims,base,kw", [
+    (128, 1e300, dict(method="base", factor=1e10)),      # the scaled base passes 64 bits: pairs without a turn
+    (4, 1e200, dict(method="base", factor=1e100)),       # base * factor^2
+    (64, 5e-324, {}),                                    # the highest frequency does (10^(323.3 * 62 / 64))
+    (64, 1e300, dict(method="linear", factor=1e300)),    # the lowest falls to zero
+    (64, 1e300, dict(method="parts", factor=1e300, length=100.0)),
+])
+def test_frequencies_that_64_bits_do_not_hold_are_refused(dims, base, kw):
+    with pytest.raises(G.GrkvError) as e:
+        G.rotary_freqs(dims, base, **kw)
+    assert e.value.status == INV
+
+
+@pytest.mark.parametrize("dims,base,kw", [(128, 1e300, {}), (128, 1e-300, {}), (128, 1e200, dict(method="base", factor=1e100)),
+                                          (2, 1e300, dict(method="base", factor=1e300)), (64, 1e4, dict(method="linear", factor=1e300))])
+def test_far_frequencies_that_64_bits_hold(dims, base, kw):
+    f = G.rotary_freqs(dims, base, **kw)
+    assert all(0 < x < math.inf for x in f.tolist())
+
+
 def test_an_unknown_scaling():
     with pytest.raises(ValueError):
         G.rotary_freqs(8, method="other")
