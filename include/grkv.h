@@ -619,8 +619,8 @@ int grkv_rotary_freqs(int32_t dims, double base, int32_t method, double factor, 
  * rows, stores nothing.  With a rotation keys are rotated by positions, and so are q's `q_heads`
  * rows into q_out (as in grkv_rotary); rows of tokens at GRKV_NO_POSITION are left as they were.
  * rotation NULL: positions and q are not read.  q_heads 0: no queries.  k, v and q have head_dim
- * columns of one type, dtype.  Slots of a call are different from one another
- * (grkv_pages_extend's are). */
+ * columns of one type, dtype.  q_out overlaps neither k and v nor the pool.  Slots of a call are
+ * different from one another (grkv_pages_extend's are). */
 int grkv_pages_store(const grkv_pages* pages, int32_t tokens, int32_t heads, const int64_t* slots,
                      int64_t slot_stride, const grkv_rows* k, const grkv_rows* v, int32_t dtype,
                      const grkv_rows* q, const grkv_rows* q_out, int32_t q_heads,

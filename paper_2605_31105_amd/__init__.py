@@ -1038,6 +1038,38 @@ def _rows(t, name, dev):
     return _Rows(t.data_ptr(), step[0], step[1])
 
 
+def _rows_meet(x, y):
+    """Whether rows of x [T, H, d] and of y, of the same shape and type, share an element without
+    being the same rows."""
+    import torch
+
+    T, H, d = x.shape
+    at = (y.data_ptr() - x.data_ptr()) // x.element_size()   # where y begins, in x's elements
+    (xt, xh, _), (yt, yh, _) = x.stride(), y.stride()
+    if not -((T - 1) * yt + (H - 1) * yh + d) < at < (T - 1) * xt + (H - 1) * xh + d or x.numel() == 0:
+        return False
+    if T == 1 or H == 1:   # (the other's stride alone counts)
+        xt, xh = (0, 0 if H == 1 else xh) if T == 1 else (xt, 0)
+        yt, yh = (0, 0 if H == 1 else yh) if T == 1 else (yt, 0)
+    if at == 0 and (xt, xh) == (yt, yh):   # the same rows
+        return False
+    if (xt, xh) != (yt, yh):   # any two sets of rows, which hardly ever lie among one another
+        t, h = torch.arange(T)[:, None], torch.arange(H)
+        a, b = (t * xt + h * xh).flatten().sort().values, (t * yt + h * yh).flatten() + at
+        i = torch.searchsorted(a, b)
+        return bool(((a[(i - 1).clamp(min=0)] - b).abs() < d).any() or ((a[i.clamp(max=a.numel() - 1)] - b).abs() < d).any())
+    if xh == d:            # heads side by side are one row
+        H, d, xh = 1, H * d, 0
+    (n, step), (m, far) = sorted([(T, xt), (H, xh)])
+    for i in range(1 - n, n):   # rows that lie i and j steps apart
+        r = at + i * step
+        j = -r // far if far else 0
+        for k in (j, j + 1):
+            if abs(r + max(1 - m, min(m - 1, k)) * far) < d:
+                return True
+    return False
+
+
 def _out_rows(x, out, name, dev):
     """The output of rotated rows: ``out``, or a tensor like x."""
     import torch
@@ -1050,10 +1082,10 @@ def _out_rows(x, out, name, dev):
     else:
         if out.shape != x.shape or out.dtype != x.dtype:
             raise ValueError("%s must have %s and dtype %s" % (name, tuple(x.shape), x.dtype))
-        if out.data_ptr() == x.data_ptr() and out.stride() != x.stride() and x.numel() > 0:
-            raise ValueError("%s overlaps its input" % name)
         apart = out.is_contiguous()
     rows = _rows(out, name, dev)
+    if out is not x and _rows_meet(x, out):
+        raise ValueError("%s overlaps its input" % name)
     if not apart:   # rows that are written do not overlap
         ends = out.shape[2]
         for step, n in sorted((out.stride(i), out.shape[i]) for i in (0, 1) if out.shape[i] > 1):
@@ -1069,7 +1101,8 @@ def rotary(x, positions, freqs, *, scale: float = 1.0, interleaved: bool = False
     float32, of any strides with whole rows (queries as ``compress`` takes them, [G, w, d], as
     ``x.transpose(0, 1)``); positions int32 [tokens]; freqs float64 [dims / 2] (``rotary_freqs``).
     Pairs are columns (i, i + dims / 2), or (2 i, 2 i + 1) with ``interleaved``; columns from
-    dims on stay.  ``inverse`` rotates back, which is the gradient of the call.  ``out`` may be x.
+    dims on stay.  ``inverse`` rotates back, which is the gradient of the call.  ``out`` may be x, and else
+    shares no element with it.
     Rows at NO_POSITION are left as they were.  Returns out."""
     import torch
 
@@ -1174,7 +1207,7 @@ def pages_store(pages: Pages, slots, k, v, *, q=None, positions=None, freqs=None
     [tokens, heads, d], bfloat16 or float32, of any strides with whole rows, rounded to the
     pool's type.  With ``freqs`` (float64 [dims / 2]) and ``positions`` (int32 [tokens]) keys are
     rotated as by ``rotary``, and so are queries q [tokens, query heads, d] of k's type into ``out``
-    (which may be q).  Returns out, None without q."""
+    (which may be q, and else overlaps none of the call's rows).  Returns out, None without q."""
     import torch
 
     dev = pages.k.get_device()

@@ -2,6 +2,7 @@
 is launched.  And the frequencies of rotary positions, which are formed there."""
 import math
 import os
+import random
 
 import pytest
 
@@ -217,3 +218,48 @@ def test_far_frequencies_that_64_bits_hold(dims, base, kw):
 def test_an_unknown_scaling():
     with pytest.raises(ValueError):
         G.rotary_freqs(8, method="other")
+
+
+def _sets(buf, view):
+    at = (view.data_ptr() - buf.data_ptr()) // buf.element_size()
+    T, H, d = view.shape
+    a, b, _ = view.stride()
+    return {at + t * a + h * b + c for t in range(T) for h in range(H) for c in range(d)}
+
+
+def test_whether_an_output_overlaps_its_input():
+    # views of one buffer against the sets of their elements, and their refusal as `out`
+    torch = pytest.importorskip("torch")
+    rng, counted = random.Random(5), [0, 0, 0]
+    buf = torch.zeros(4000)
+    for _ in range(4000):
+        T, H, d = rng.choice([1, 2, 3, 7]), rng.choice([1, 2, 3, 5]), rng.choice([2, 3, 8])
+        views, shared = [], rng.random() < 0.7
+        for k in range(2):
+            if k == 0 or not shared:
+                inner = rng.choice([d, d, d + 1, 2 * d, 3 * d, 0])
+                outer = rng.choice([H * inner, 2 * H * inner, 4 * d, d * T, H * inner + 2 * d, 1, 0])
+                step = (outer, inner) if rng.random() < 0.7 else (inner, outer)
+            views.append(torch.as_strided(buf, (T, H, d), step + (1,), rng.choice([0, 1, d, 3 * d, H * d, rng.randrange(300)])))
+        x, y = views
+        a, b = _sets(buf, x), _sets(buf, y)
+        same = x.data_ptr() == y.data_ptr() and all(x.stride(i) == y.stride(i) for i in (0, 1) if x.shape[i] > 1)
+        assert G._rows_meet(x, y) == (bool(a & b) and not same), (x.shape, x.stride(), y.stride(), x.storage_offset(), y.storage_offset())
+        counted[2 if same else bool(a & b)] += 1
+    assert min(counted) > 100, counted
+
+
+def test_an_output_among_the_rows_of_its_input():
+    torch = pytest.importorskip("torch")
+    wide = torch.zeros((6, 8, 16))
+    x = wide[:, :4]
+    for out in (wide[:, 2:6], wide[:, 1:5], torch.as_strided(wide, (6, 4, 16), (128, 16, 1), 8)):
+        with pytest.raises(ValueError):
+            G._out_rows(x, out, "out", -1)
+    for out in (wide[:, 4:], x, wide[:, :4], torch.zeros_like(x)):   # beside the input, in place, elsewhere
+        assert G._out_rows(x, out, "out", -1)[0] is out
+    ahead = torch.zeros((7, 4, 16))
+    with pytest.raises(ValueError):   # a token on
+        G._out_rows(ahead[:6], ahead[1:], "out", -1)
+    none = wide[:0]
+    assert G._out_rows(none, wide[:0], "out", -1)[0].shape == (0, 8, 16)
