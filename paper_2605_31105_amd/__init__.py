@@ -1103,7 +1103,8 @@ def rotary(x, positions, freqs, *, scale: float = 1.0, interleaved: bool = False
     Pairs are columns (i, i + dims / 2), or (2 i, 2 i + 1) with ``interleaved``; columns from
     dims on stay.  ``inverse`` rotates back, which is the gradient of the call.  ``out`` may be x, and else
     shares no element with it.
-    Rows at NO_POSITION are left as they were.  Returns out."""
+    Rows at NO_POSITION are left as they were.  Returns out, which carries x's gradient (those rows'
+    is zero; positions and freqs are to stay until then); a call whose x needs one takes no ``out``."""
     import torch
 
     dev = x.get_device()
@@ -1114,6 +1115,10 @@ def rotary(x, positions, freqs, *, scale: float = 1.0, interleaved: bool = False
         with on:
             return rotary(x, positions, freqs, scale=scale, interleaved=interleaved, inverse=inverse,
                           out=out)
+    if x.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            raise ValueError("rotary into out records no gradient, which x needs (torch.no_grad for none)")
+        return _rotated()(x, positions, freqs, scale, interleaved, inverse, False)
     xr = _rows(x, "x", dev)
     out, yr = _out_rows(x, out, "out", dev)
     T, H, d = x.shape
@@ -1121,6 +1126,36 @@ def rotary(x, positions, freqs, *, scale: float = 1.0, interleaved: bool = False
     _check(lib().grkv_rotary(xr, yr, T, H, d, _dtype_code(x), _vector(positions, "positions", torch.int32, T, dev),
                              _rotation(freqs, scale, interleaved, inverse, dev), handle))
     return out
+
+
+_ROTATED = None
+
+
+def _rotated():
+    """``rotary`` for autograd: the gradient is the call with ``inverse`` the other way round, and zero
+    in rows that the call did not write."""
+    global _ROTATED
+    if _ROTATED is None:
+        import torch
+
+        class Rotated(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x, positions, freqs, scale, interleaved, inverse, clear):
+                ctx.save_for_backward(positions, freqs)
+                ctx.how = scale, interleaved, inverse
+                out = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if clear else None
+                return rotary(x, positions, freqs, scale=scale, interleaved=interleaved, inverse=inverse, out=out)
+
+            @staticmethod
+            def backward(ctx, g):
+                positions, freqs = ctx.saved_tensors
+                scale, interleaved, inverse = ctx.how
+                if g.shape[2] > 1 and g.stride(2) != 1:   # (of a sum: one element as all)
+                    g = g.contiguous()
+                return (Rotated.apply(g, positions, freqs, scale, interleaved, not inverse, True),) + (None,) * 6
+
+        _ROTATED = Rotated.apply
+    return _ROTATED
 
 
 def _step(pages, B, T, heads, units):
