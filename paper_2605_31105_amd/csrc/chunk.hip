@@ -171,6 +171,16 @@ __device__ __forceinline__ void combine_row(const AttendK& a, const CutJob& cut,
   write_out<E, D>(x, row_at<kChunk>(x, 0, g, i), ch, o.x, o.m, o.l, o.lx);
 }
 
+// The kernel's arguments, read anew.  A job takes them this way, so that those of the plan and of the
+// jobs before are not held over it: the loop over its tiles needs the scalar registers, and what they do
+// not hold is kept in lanes of vector registers (scalars read back in two steps of many rows 19 -> 0; 4 chunks
+// of 2048 over 4k to 14k 1357 -> 1336 us, 2 of 512 124 -> 117, 4 prompts of 4096 with 64 columns 469 -> 465).
+__device__ __forceinline__ AttendK arguments() {
+  auto at = __builtin_amdgcn_kernarg_segment_ptr();   // (the first argument lies there)
+  asm volatile("" : "+s"(at));
+  return *(const AttendK*)at;
+}
+
 // RT: 16-row tiles that no job has more of (1, or 2 over bf16 values), 0: rows of any number.
 // Jobs of 17 to 32 rows alone are bound by HBM, which the kernel of few rows serves better (64
 // sequences of 500 to 8000 keys, 5 tokens of 4 heads each: 235 -> 211 us, one block for each compute
@@ -322,15 +332,16 @@ __global__ __launch_bounds__(kChunkTh, RT == 2 && D == 128 ? 1 : 2) void chunk_k
     for (; from < hi && j < a.jobs; ++j) {
       u.to(a, j);
       u.hold();
+      AttendK x = arguments();
       Shape s;
-      if (!shape_of<E>(a, a.starts, j, u.b, u.tile, u.next, &s)) continue;
+      if (!shape_of<E>(x, x.starts, j, u.b, u.tile, u.next, &s)) continue;
       s.hold();
-      set_len(a, __builtin_amdgcn_readfirstlane(raw_len(a, s)), &s);
-      const Span sn = span_of<E>(a, s);
-      const Cost cost = cost_of<E>(a, s, sn);
+      set_len(x, __builtin_amdgcn_readfirstlane(raw_len(x, s)), &s);
+      const Span sn = span_of<E>(x, s);
+      const Cost cost = cost_of<E>(x, s, sn);
       const int64_t at = from;
       int vt0, vt1, parts;
-      if (a.aligned) {
+      if (x.aligned) {
         const int i = __builtin_amdgcn_readfirstlane((int)at_s);
         vt0 = (int)((int64_t)cost.n * i / pieces);
         vt1 = (int)((int64_t)cost.n * (i + 1) / pieces);
@@ -344,19 +355,21 @@ __global__ __launch_bounds__(kChunkTh, RT == 2 && D == 128 ? 1 : 2) void chunk_k
       }
       const bool whole = vt0 == 0 && vt1 == cost.n;
       if (vt1 <= vt0 || whole != (pass == 0)) continue;
-      AttendK x = a;   // the unit's own rows
-      const size_t row0 = (size_t)s.start * a.q_heads + (size_t)s.h * a.group;
-      x.q = (const E*)a.q + row0 * D;
-      x.o = (E*)a.o + row0 * D;
-      x.lse = a.lse ? a.lse + row0 : nullptr;
+      // the unit's own rows
+      void* const o = x.o;
+      float* const lse = x.lse;
+      const size_t row0 = (size_t)s.start * x.q_heads + (size_t)s.h * x.group;
+      x.q = (const E*)x.q + row0 * D;
+      x.o = (E*)o + row0 * D;
+      x.lse = lse ? lse + row0 : nullptr;
       x.tokens = s.t;
       // a part's two places: what it goes on with, and what it begins and leaves to others
-      const int64_t rows_at = (2 * b + (vt0 == 0)) * a.part_rows - s.r0;   // partial row of row r: this + r
-      if (vt0 == 0 && !whole && tid == 0) a.ends[b] = {row0, s.r0, s.rows, parts};
+      const int64_t rows_at = (2 * b + (vt0 == 0)) * x.part_rows - s.r0;   // partial row of row r: this + r
+      if (vt0 == 0 && !whole && tid == 0) x.ends[b] = {row0, s.r0, s.rows, parts};
       const int end = min(vt1, sn.nt);
       const int64_t to = whole ? kWhole : rows_at;
       if (FEW || few(s)) {
-        attend_rows<E, D, 1, kChunk>(x, sn, 0, s.r0, vt0, end, to, FEW && a.flags, s.len, s.t, s.trow, v0_s, v1_s);
+        attend_rows<E, D, 1, kChunk>(x, sn, 0, s.r0, vt0, end, to, FEW && x.flags, s.len, s.t, s.trow, v0_s, v1_s);
       } else if constexpr (!FEW) {
         if constexpr (sizeof(E) == 4 || RT == 2)
           attend_rows<E, D, 2, kChunk>(x, sn, 0, s.r0, vt0, end, to, false, s.len, s.t, s.trow, v0_s, v1_s);
@@ -366,10 +379,13 @@ __global__ __launch_bounds__(kChunkTh, RT == 2 && D == 128 ? 1 : 2) void chunk_k
       }
       if constexpr (FEW) {
         const int i = (int)at_s;
-        if (a.flags && !whole && splits_done(a, j, i, pieces)) {
+        if (x.flags && !whole && splits_done(x, j, i, pieces)) {
           for (int c = tid; c < kFewRows * (D / 4); c += kChunkTh) {
             const CutJob cut = {row0, s.r0, s.rows, pieces};
-            combine_row<E, D, true>(a, cut, b - i, c / (D / 4), c % (D / 4));
+            AttendK y = x;
+            y.o = o;
+            y.lse = lse;
+            combine_row<E, D, true>(y, cut, b - i, c / (D / 4), c % (D / 4));
           }
         }
       }
