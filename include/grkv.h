@@ -633,11 +633,10 @@ int grkv_pages_store(const grkv_pages* pages, int32_t tokens, int32_t heads, con
  *   q, o  pages' dtype [tokens][heads * group][head_dim], 16-byte aligned
  *   lse   float [tokens][heads * group], or NULL
  * as in grkv_tree_attention, also for queries that see nothing and for values that are not
- * seen.  Over bf16 values weights are held to 2^-15 of them where `longest` times group is 32 or
- * less, else for a sequence's rows (tokens times group) up to 16 and the last 16 or fewer past a
- * multiple of 128; the others are rounded to bf16 (2^-8).  Rows of no sequence, and those from a sequence's `longest` on, stay as they
- * were.  `longest` bounds the workspace.  Of a refused sequence (grkv_pages_extend) the rows
- * mean nothing. */
+ * seen.  Over bf16 values weights are held to 2^-15 of them for a sequence's rows (tokens times
+ * group) up to 64, and for the last 64 or fewer past a multiple of 128; the others are rounded to bf16
+ * (2^-8).  Rows of no sequence, and those from a sequence's `longest` on, stay as they were.
+ * `longest` bounds the workspace.  Of a refused sequence (grkv_pages_extend) the rows mean nothing. */
 typedef struct {
   int32_t group;    /* query heads per unit, >= 1 */
   int32_t longest;  /* most new tokens of a sequence, >= 1 */

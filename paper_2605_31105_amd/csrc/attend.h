@@ -21,6 +21,8 @@ constexpr float kRefAbove = 8.f;
 constexpr float kMoveLog = 16.f, kMoveSum = 0x1p16f;   // log2 of it, and it
 constexpr uint32_t kOnes = 0x3f803f80u;   // two bf16 ones
 constexpr float kLn2 = 0.6931471805599453f;
+// Of a weight that enters its product in two bf16 parts, before its upper bits are taken away.
+constexpr float kPartUp = 1.f + 0x1p-18f;
 
 // What the rows of a call are: queries over contiguous keys, drafted tokens over pages, or
 // the new tokens of a step over pages (packed, each seeing the slots up to its own).

@@ -10,7 +10,6 @@ namespace grkv {
 
 constexpr int kAtWaves = 4;
 constexpr int kAtTh = 64 * kAtWaves;
-constexpr float kPartUp = 1.f + 0x1p-18f;   // of a weight, before its upper bits are taken away
 
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` (uniform), as
 // a non-temporal load: values are read once, and pass the caches faster so (over

@@ -34,6 +34,12 @@ static_assert(kAtTh == kWTh, "one kernel holds both");
 template <typename E>
 constexpr int kJobShift = sizeof(E) == 2 ? 7 : 5;
 constexpr int kFewRows = 16;
+// Jobs of so many rows have weights of two bf16 parts in the kernel of many rows too (2^-15 of a weight,
+// as a tree of as many rows has): their keys' bytes bound them, and a sequence of up to 64 rows has them
+// as exact whatever others the call holds.  (16 tokens of 64 sequences of 500 to 8000 keys, 64 rows
+// a unit: 257 us with rounded weights and two waves without rows, 254 so.  Longer jobs are bound by their products: see
+// attend_wide.hip.)
+constexpr int kTwoParts = 64;
 // Costs, in half tiles of 32 keys read for few rows (kTwo: two
 // 16-row tiles of them, 32 keys of bf16 or 16 of float32).
 // Timed blocks take 1.05 us for such a tile, 2.4 to 2.8 for 64 keys of many rows and some two
@@ -373,6 +379,9 @@ __global__ __launch_bounds__(kChunkTh, RT == 2 && D == 128 ? 1 : 2) void chunk_k
       } else if constexpr (!FEW) {
         if constexpr (sizeof(E) == 4 || RT == 2)
           attend_rows<E, D, 2, kChunk>(x, sn, 0, s.r0, vt0, end, to, false, s.len, s.t, s.trow, v0_s, v1_s);
+        else if (s.rows <= kTwoParts)
+          wide_rows<D, kChunk, true>(x, sn, 0, s.r0, vt0, end, [&] { return Part{!whole, rows_at}; }, s.len, s.t, s.trow,
+                                     v0_s, v1_s);
         else
           wide_rows<D, kChunk>(x, sn, 0, s.r0, vt0, end, [&] { return Part{!whole, rows_at}; }, s.len, s.t, s.trow,
                                v0_s, v1_s);

@@ -39,14 +39,16 @@ constexpr int kRing = 2 * kWideKeys * 2 * D;   // bytes of either ring
 
 // Rows r0 .. r0 + 127 of entry e over the tiles vt0 .. vt1 - 1 of its span, by a block: partial
 // rows from part_of() on or (kWhole) the outputs.  kring and vring: two tiles of keys and two of
-// values in LDS, 1 KB aligned.
-template <int D, Rows KIND, typename F>
+// values in LDS, 1 KB aligned.  TWO: 64 rows at most, whose weights enter their product in two bf16
+// parts, as in attend.hip.  Waves w and w + 2 hold the same 32 rows and take half of a tile's keys each
+// (two waves would have none), and their sums are added at the end.
+template <int D, Rows KIND, bool TWO = false, typename F>
 __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int e, int r0, int vt0, int vt1,
                                           F part_of, int len, int t, const int32_t* trow, char* kring,
                                           char* vring) {
   constexpr bool PAGED = KIND != kContiguous, TREE = KIND == kTree;
   constexpr int TK = kWideKeys;
-  constexpr int NK = TK / 32;          // 32-key parts of a step
+  constexpr int NK = TWO ? 1 : TK / 32;   // 32-key parts of a wave's step
   constexpr int RB = 2 * D;            // bytes of a row
   constexpr int CPR = RB / 16;         // chunks of a row
   constexpr int KB = TK * RB;          // bytes of a K (or V) tile
@@ -55,6 +57,7 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
   constexpr int KS = D / 16, DM = D / 32;
   static_assert(TK == 16 * kWWaves, "a wave brings 16 rows of a tile");
   static_assert(kWWaves * 32 * D * 4 == 2 * kRing<D>, "the waves' outputs fit the ring");
+  static_assert(!TWO || (KIND == kChunk && kWWaves == 4), "the jobs of a step");
 
   int tid = threadIdx.x;
   if (KIND == kChunk) asm volatile("" : "+v"(tid));   // (what follows from it is not held over jobs)
@@ -65,7 +68,8 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
   uint64_t family = 0;
   int depth = 0;
   if (TREE) draft_family(a, e, t, base, lane, &family, &depth);
-  const int w0 = r0 + 32 * wave;   // this wave's first row
+  const int w0 = r0 + 32 * (TWO ? wave & 1 : wave);   // this wave's first row
+  const int key0 = TWO ? 32 * (wave >> 1) : 0;           // its first key of a tile
   bf16x8 qf[KS];
   RowSight sight;
   {
@@ -164,16 +168,17 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
       bf16x8 kf[KS];
-      read_k(kt + n * 32 * RB, kf);
+      read_k(kt + (key0 + n * 32) * RB, kf);
       x[n] = f32x16{};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) x[n] = mfma32(kf[ks], qf[ks], x[n]);
     }
   };
-  // One step: the 32 NK keys at slot0, whose logits are in st and whose V rows are at vt;
-  // kt: K rows of the next step.
-  auto step = [&](int slot0, const char* kt, const char* vt, f32x16 (&st)[NK], f32x16 (&nx)[NK])
+  // One step: the 32 NK keys at key0 of the tile at `slot`, whose logits are in st and whose V rows are
+  // at vt; kt: K rows of the next step.
+  auto step = [&](int slot, const char* kt, const char* vt, f32x16 (&st)[NK], f32x16 (&nx)[NK])
                   __attribute__((always_inline)) {
+    const int slot0 = slot + key0;
     const bool full = slot0 + 32 * NK <= lim && (slot0 >= lo || slot0 + 32 * NK <= a.n_sink);
     if (!full) {
 #pragma unroll
@@ -185,7 +190,7 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
       }
     }
     logits(kt, nx);
-    bf16x8 p[NK][2];
+    bf16x8 p[NK][2], rest[TWO ? NK : 1][2];
     float s1, s2;   // this step's sums
     auto weights = [&]() __attribute__((always_inline)) {
       s1 = s2 = 0.f;
@@ -199,10 +204,21 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
             const float x1 = __builtin_amdgcn_exp2f(fmaf(st[n][8 * s + c + 1], a.scale_log2, nref));
             s1 += x0;
             s1 += x1;
-            const bf16x2 w = __builtin_convertvector((f32x2){x0, x1}, bf16x2);
+            bf16x2 w;
+            if constexpr (TWO) {
+              const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+              w = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(u1, u0, 0x07060302u));
+              const bf16x2 l = __builtin_convertvector((f32x2){fmaf(x0, kPartUp, -__uint_as_float(u0 & 0xffff0000u)),
+                                                               fmaf(x1, kPartUp, -__uint_as_float(u1 & 0xffff0000u))},
+                                                       bf16x2);
+              rest[n][s][c] = l[0];
+              rest[n][s][c + 1] = l[1];
+            } else {
+              w = __builtin_convertvector((f32x2){x0, x1}, bf16x2);
+              s2 = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, kOnes), s2, false);
+            }
             p[n][s][c] = w[0];
             p[n][s][c + 1] = w[1];
-            s2 = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, kOnes), s2, false);
           }
     };
     weights();
@@ -231,24 +247,27 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
       bf16x8 vf[2][DM];
-      read_v(vt + n * 32 * RB, vf);
+      read_v(vt + (key0 + n * 32) * RB, vf);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int dm = 0; dm < DM; ++dm) acc[dm] = mfma32(vf[s][dm], p[n][s], acc[dm]);
+        for (int dm = 0; dm < DM; ++dm) {
+          acc[dm] = mfma32(vf[s][dm], p[n][s], acc[dm]);
+          if constexpr (TWO) acc[dm] = mfma32(vf[s][dm], rest[n][s], acc[dm]);
+        }
     }
     // products of the step, operands read ahead.  (Left to itself the compiler reads two ahead in
     // a step's kernel, and the products wait for LDS: 4 chunks of 2048 over 4k to 14k 1620 -> 1500
     // us; three to eight ahead are equal.  A 16k prompt with a 4k window 993 -> 985, trees of 32
     // over 32k 106 -> 105.)
-    constexpr int ALL = NK * 2 * DM, AHEAD = 4;
+    constexpr int ALL = NK * 2 * DM, AHEAD = 4, EACH = TWO ? 2 : 1;
     __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
     for (int k = 0; k < ALL - AHEAD; ++k) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, EACH, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+    __builtin_amdgcn_sched_group_barrier(0x8, EACH * AHEAD, 0);
   };
 
   if (vt0 < vt1) {
@@ -315,6 +334,52 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
     for (int r = 0; r < 16; ++r) odd = fmaf(acc[dm][r], 0.f, odd);
   const Part to = part_of();
   const bool far = far_off(sum, nref);
+  if constexpr (TWO) {
+    __shared__ float m_s[2][64], l_s[2][64];   // references and sums of the rows over either half of the keys
+    if (__syncthreads_or(far || (odd != odd && sum == sum)) &&
+        (__syncthreads_or(far) || odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, sn.lim, sn.lo, trow) ||
+         !odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, 0, sn.lo, trow))) {
+      rows_by_key<u16, D, KIND>(a, sn, e, to.partial ? to.row : kWhole, r0 + 16 * wave, 16, vt0, vt1, TK, len, t, trow,
+                                family, depth);
+      return;
+    }
+    // the halves' rows, scaled to the larger reference, through the waves' parts of the rings (lane's
+    // four columns 32 dm + 8 c + 4 h of row l32, chunks permuted by row), added where they are read
+    constexpr int CR = D / 4;
+    const int my = 32 * (wave & 1) + l32;
+    if (h == 0) {
+      m_s[wave >> 1][my] = -nref;
+      l_s[wave >> 1][my] = sum;
+    }
+    __syncthreads();
+    // (of a part: weights of 1 at most, so that parts may be added)
+    const float f = __builtin_amdgcn_exp2f(-nref - fmaxf(m_s[0][my], m_s[1][my])) * (to.partial ? 1.f / kMoveSum : 1.f);
+    char* mine = (wave < 2 ? kring : vring) + (wave & 1) * KB;
+#pragma unroll
+    for (int dm = 0; dm < DM; ++dm)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<f32x4*>(mine + (l32 * CR + ((8 * dm + 2 * c + h) ^ (l32 & 15))) * 16) =
+            (f32x4){acc[dm][4 * c], acc[dm][4 * c + 1], acc[dm][4 * c + 2], acc[dm][4 * c + 3]} * f;
+    __syncthreads();
+#pragma unroll 4
+    for (int k = tid; k < 64 * CR; k += kWTh) {
+      const int row = k / CR, ch = k % CR, r = r0 + row, i = group_of(a, r);
+      if (r >= R || i >= t) continue;
+      const int at = (row >> 5) * KB + ((row & 31) * CR + (ch ^ (row & 15))) * 16;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(kring + at) + *reinterpret_cast<const f32x4*>(vring + at);
+      const float m = fmaxf(m_s[0][row], m_s[1][row]);
+      const float lx = l_s[0][row] * __builtin_amdgcn_exp2f(m_s[0][row] - m) + l_s[1][row] * __builtin_amdgcn_exp2f(m_s[1][row] - m);
+      if (to.partial) {
+        const float l = lx * (1.f / kMoveSum);
+        *reinterpret_cast<f32x4*>(a.opart + (to.row + r) * D + 4 * ch) = x;
+        if (ch == 0) a.mpart[to.row + r] = make_float4(m + kMoveLog, l * kPartUp, l, 0.f);
+      } else {
+        write_out<u16, D>(a, row_at<KIND>(a, e, r - i * a.group, i), ch, x, m, lx * kPartUp, lx);
+      }
+    }
+    return;
+  }
   if (__any(far || (odd != odd && sum == sum)) &&
       (__any(far) || odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, lim, lo, trow) ||
        !odd_values<u16, D, PAGED>(a, sn, e, vt0, vt1, TK, 0, lo, trow))) {

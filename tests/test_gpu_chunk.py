@@ -331,3 +331,66 @@ def test_binding_checks():
         assert e.value.status == G.GRKV_ERR_INVALID
     assert G.chunk_attention(q[:0], pg, _i32([0, 0]), heads=2).shape == (0, 4, 64)
     assert G.chunk_attention_workspace_bytes(pg, 2, 2, 3, 2, longest=0) == 0
+
+
+def _two_parts(c, group):
+    """Whether the weights of each (token, head of the group) of a sequence of c new tokens are held to two
+    parts: those of its last 64 rows or fewer past a multiple of 128, rows being token by token."""
+    r = torch.arange(c * group).view(c, group)
+    return (r >= c * group // 128 * 128) & (c * group % 128 <= 64)
+
+
+@pytest.mark.parametrize("d,group,counts,lens", [
+    (128, 4, [16, 300, 9, 1], [300, 520, 40, 2000]), (64, 3, [21, 5, 70, 0], [129, 33, 300, 4]),
+    (128, 7, [9] * 40, [30 + 31 * b for b in range(40)]), (64, 16, [4, 2, 3], [9000, 20, 700]),
+    (128, 1, [64, 33, 190, 65], [64, 1000, 250, 400]), (64, 5, [12] * 70 + [200], [40 + 17 * b for b in range(70)] + [900])])
+def test_weights_of_up_to_64_rows_are_held_to_two_parts(d, group, counts, lens):
+    # whatever the other sequences are, and whether the call names its longest or not
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + group)
+    pg, K, V = _pool(lens, 16, d, BF, gen)
+    T, starts = sum(counts), [sum(counts[:b]) for b in range(len(counts) + 1)]
+    q = torch.randn((T, group, d), generator=gen).to(BF)
+    for longest in (None, max(counts)):
+        o, lse = (x.cpu() for x in G.chunk_attention(q.cuda(), pg, _i32(starts), heads=1, longest=longest, return_lse=True))
+        done = 0
+        for b, c in enumerate(counts):
+            two = _two_parts(c, group)
+            for g in range(group):
+                at = two[:, g].nonzero().flatten() if c else torch.zeros(0, dtype=torch.long)
+                if at.numel() == 0:
+                    continue
+                done += at.numel()
+                x = starts[b] + at
+                _close("seq %d head %d" % (b, g), o[x, g], lse[x, g], q[x, g], K[b], V[b], sink_seen(lens[b], c, 0, 0)[at])
+        assert done >= 4 * group
+
+
+@pytest.mark.parametrize("d,window,n_sink", [(128, 50, 5), (64, 37, 70)])
+def test_up_to_64_rows_with_windows(d, window, n_sink):
+    counts, before = [16, 9, 40, 11], [900, 100, 3000, 0]
+    lens = [[b + 5 * h + c for h in range(2)] for b, c in zip(before, counts)]
+    _run("64", lens, counts, 2, 4, 16, d, BF, window, n_sink, pad=2)
+
+
+@pytest.mark.parametrize("group,counts", [(8, [6]), (16, [4, 1]), (5, [11, 20])])
+def test_what_up_to_64_rows_do_not_see_never_reaches_them(group, counts):
+    test_what_a_query_does_not_see_never_reaches_it(BF, group, counts)
+
+
+@pytest.mark.parametrize("d,group,counts,lens", [(128, 5, [12, 40], [700, 900]), (64, 16, [4, 3], [20000, 300]), (128, 1, [60], [1500])])
+def test_large_values_under_growing_logits_of_up_to_64_rows(d, group, counts, lens):
+    test_large_values_under_growing_logits(BF, d, group, counts, lens)
+
+
+def test_infinities_that_up_to_64_rows_see_stay_infinities():
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(22)
+    for d, n in ((128, 700), (64, 9000)):
+        pg, K, V = _pool([n], 64, d, BF, gen)
+        V[0][70, 7], V[0][70, 9] = torch.inf, -torch.inf
+        pg.v[int(pg.table[0, 1]), 6] = V[0][70].cuda()
+        q = torch.randn((13, 4, d), generator=gen).to(BF)
+        o = G.chunk_attention(q.cuda(), pg, _i32([0, 13]), heads=1).cpu()
+        assert (o[..., 7] == torch.inf).all() and (o[..., 9] == -torch.inf).all()
+        assert torch.isfinite(o[..., [x for x in range(d) if x not in (7, 9)]]).all()
