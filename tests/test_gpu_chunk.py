@@ -394,3 +394,53 @@ def test_infinities_that_up_to_64_rows_see_stay_infinities():
         o = G.chunk_attention(q.cuda(), pg, _i32([0, 13]), heads=1).cpu()
         assert (o[..., 7] == torch.inf).all() and (o[..., 9] == -torch.inf).all()
         assert torch.isfinite(o[..., [x for x in range(d) if x not in (7, 9)]]).all()
+
+
+@pytest.mark.parametrize("dtype,d,group,counts,before,window,n_sink", [
+    # up to 16 rows a unit: few units, whose blocks join their pieces, and many, cut into equal parts
+    (BF, 128, 4, [1, 3], [5000, 2070], 1000, 37), (BF, 64, 5, [2, 1, 0], [3001, 40, 900], 333, 5),
+    (BF, 128, 4, [1] * 50, [19 + 61 * b for b in range(50)], 77, 13), (BF, 64, 16, [1] * 70, [5 + 43 * b for b in range(70)], 100, 70),
+    # 17 to 32 rows: pieces of a job a block, and equal parts
+    (BF, 128, 4, [5, 8, 1], [4000, 333, 0], 1000, 37), (BF, 64, 3, [10, 6], [2100, 50], 333, 70),
+    (BF, 128, 7, [4, 3] * 25, [20 + 61 * b for b in range(50)], 77, 13), (BF, 64, 4, [8, 1] * 35, [5 + 43 * b for b in range(70)], 100, 5),
+    # float32: 16 rows a unit, and tiles of 32
+    (F32, 128, 4, [1, 3], [3000, 70], 333, 37), (F32, 64, 4, [8, 1] * 20, [5 + 43 * b for b in range(40)], 77, 13),
+    (F32, 128, 3, [10, 20], [2100, 50], 333, 5),
+    # windows of a slot or two, and shorter than the new tokens
+    (BF, 128, 4, [4, 1], [500, 70], 1, 0), (BF, 64, 2, [15, 9], [300, 2], 2, 33), (BF, 128, 4, [7, 2], [500, 70], 3, 1)])
+def test_windows_of_calls_that_name_their_longest(dtype, d, group, counts, before, window, n_sink):
+    lens = [[b + 3 * h + c for h in range(2)] for b, c in zip(before, counts)]
+    few = len(counts) < 10
+    _run("named", lens, counts, 2, group, 16, d, dtype, window, n_sink, pad=1, longest=max(counts), heads=None if few else [1])
+
+
+@pytest.mark.parametrize("d,dtype,sequences,longest", [(128, BF, 5, None), (64, BF, 90, None), (128, BF, 90, 4), (64, BF, 5, 4),
+                                                       (128, BF, 90, 8), (64, F32, 90, None), (128, F32, 5, 4)])
+def test_starts_that_fall_or_pass_the_rows_stay_inside_them(d, dtype, sequences, longest):
+    # q lies between rows of NaN, o, lse and the workspace between marks: nothing beside them is read
+    # or written
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(d + sequences)
+    group, T, edge = 4, 120, 40
+    pg, _, _ = _pool([10 + (37 * b) % 500 for b in range(sequences)], 16, d, dtype, gen)
+    pg.k.nan_to_num_(0.0)
+    pg.v.nan_to_num_(0.0)
+    q = torch.full((T + 2 * edge, group, d), math.nan, dtype=dtype, device="cuda")
+    q[edge:-edge] = torch.randn((T, group, d), generator=gen).to(dtype).cuda()
+    o, lse = torch.full_like(q, 5.0), torch.full(q.shape[:2], 6.0, device="cuda")
+    need = G.chunk_attention_workspace_bytes(pg, sequences, 1, T, group, longest)
+    ws = torch.full((need + 2 * 4096,), 165, dtype=torch.uint8, device="cuda")
+    at = slice(edge, T + edge)
+    some = torch.randint(-T, 2 * T, (6, sequences + 1), generator=gen).tolist()
+    far = [[(1 << 30) * (b % 3 - 1) for b in range(sequences + 1)], [2 ** 31 - 1 - b for b in range(sequences + 1)],
+           [T - b for b in range(sequences + 1)], [-(2 ** 31)] + [T] * sequences, [0] + [2 ** 31 - 1] * sequences]
+    for starts in some + far:
+        o.fill_(5.0)
+        lse.fill_(6.0)
+        G.chunk_attention(q[at], pg, _i32(starts), heads=1, longest=longest, out=o[at], lse=lse[at],
+                          workspace=ws[4096:4096 + need])
+        torch.cuda.synchronize()
+        for x, mark in ((o, 5.0), (lse, 6.0)):
+            assert (x[:edge] == mark).all() and (x[-edge:] == mark).all()
+        assert (ws[:4096] == 165).all() and (ws[4096 + need:] == 165).all()
+        assert torch.isfinite(o).all() and not torch.isnan(lse).any()

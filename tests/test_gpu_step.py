@@ -256,3 +256,9 @@ def test_streams_of_another_device_and_broken_sums():
         G.chunk_attention(q, pg, _i32(bad), heads=1, out=o, lse=lse)
     torch.cuda.synchronize()
     assert not torch.isnan(o.float()).any() and math.isfinite(float(o.float().sum()))
+
+
+@pytest.mark.parametrize("d,window", [(128, 50), (64, 33)])
+def test_compressed_caches_go_on_under_a_window_that_hides_slots(d, window):
+    # (units of 128 to 240 slots: all but the window and four sinks are out of sight)
+    test_compressed_caches_go_on_with_prompts_and_tokens(d, window)
