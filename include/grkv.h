@@ -556,10 +556,11 @@ typedef struct {
  * seen (int32 [sequences]): how many tokens a sequence had, which its units' lengths do not say
  * once they are compressed; NULL: the length of its first unit.  All units of a sequence
  * grow, or none: a sequence is refused for the largest of its units' GRKV_PAGES_ codes (_UNIT
- * also for a unit that an earlier head or sequence of the call names; _RANGE: its rows pass
- * `tokens`, or its positions leave 0 .. 2^31 - 1), and its rows, like those behind the
- * last sequence, have position GRKV_NO_POSITION and slots -1.  New pages are handed
- * out in the order of the sequences and their heads. */
+ * also for a unit that an earlier head or sequence of the call names; _RANGE: it has new tokens
+ * and their rows pass `tokens`, seen[b] is below 0, or what it has seen after the call, seen[b] +
+ * counts[b], passes 2^31 - 1), and its rows, like those behind the last sequence, have position
+ * GRKV_NO_POSITION and slots -1.  New pages are handed out in the order of the sequences and their
+ * heads. */
 int grkv_pages_extend(const grkv_pages* pages, const grkv_step* step, const int32_t* counts,
                       const int32_t* seen, int32_t* starts, int32_t* positions, int64_t* slots,
                       int32_t* status, void* stream, void* workspace, size_t workspace_bytes);

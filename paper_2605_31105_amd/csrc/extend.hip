@@ -167,7 +167,9 @@ __global__ __launch_bounds__(kPlanTh) void extend_plan_kernel(ExtendK a) {
   // the pages that each needs, and those of the entries before it
   unsigned long long all = 0;
   for (int e0 = 0; e0 < a.entries; e0 += BATCH) {
-    uint32_t need[kAhead], before[kAhead];   // (2^26 pages at most: a wave's sum fits)
+    // (32 bits hold all needs together: rows that are accepted are tokens * heads < 2^31 in all, in pages
+    // of 16 rows or more, and each of the 2^24 entries may begin one page besides)
+    uint32_t need[kAhead], before[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) need[k] = 0;
     each(e0, [&](int k, int e, int b) {

@@ -135,6 +135,7 @@ int check_step(const grkv_pages* pg, const grkv_step* st) {
   if (ok != GRKV_OK) return ok;
   if (!st || st->sequences < 0 || st->heads < 1 || st->tokens < 0) return GRKV_ERR_INVALID;
   if (st->units && st->unit_stride < st->heads) return GRKV_ERR_INVALID;
+  // (both limits: launches, and the sums of pages in extend.hip)
   if ((int64_t)st->sequences * st->heads > kMostBlocks) return GRKV_ERR_INVALID;
   return (int64_t)st->tokens * st->heads >= (int64_t(1) << 31) ? GRKV_ERR_INVALID : GRKV_OK;
 }
@@ -179,7 +180,7 @@ int make_chunk(const grkv_pages* pg, const grkv_step* st, const grkv_chunk* ch, 
   return GRKV_OK;
 }
 
-// A rotation of rows of d columns; with rows to rotate, their pieces fit a launch.
+// A rotation of rows of d columns.
 int check_rotation(const grkv_rotation* rot, const int32_t* positions, int32_t d) {
   if (!rot || !rot->freqs || !positions || !aligned(rot->freqs, 8)) return GRKV_ERR_INVALID;
   if (rot->dims < 2 || rot->dims > d || rot->dims % 2 != 0) return GRKV_ERR_INVALID;
