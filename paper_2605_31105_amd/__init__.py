@@ -1242,7 +1242,8 @@ def pages_store(pages: Pages, slots, k, v, *, q=None, positions=None, freqs=None
     [tokens, heads, d], bfloat16 or float32, of any strides with whole rows, rounded to the
     pool's type.  With ``freqs`` (float64 [dims / 2]) and ``positions`` (int32 [tokens]) keys are
     rotated as by ``rotary``, and so are queries q [tokens, query heads, d] of k's type into ``out``
-    (which may be q, and else overlaps none of the call's rows).  Returns out, None without q."""
+    (which may be q, and else overlaps none of the call's rows).  No gradient is recorded.  Returns out,
+    None without q."""
     import torch
 
     dev = pages.k.get_device()
@@ -1299,7 +1300,7 @@ def chunk_attention(q, pages: Pages, starts, *, heads=None, units=None, longest=
     last slots of the sequence's units.  ``units``: int32 [B, heads] (default: unit b * heads +
     h).  ``longest``: the most new tokens of a sequence (default: all rows), which bounds the
     workspace.  ``window`` > 0: only the last ``window`` slots and the first ``n_sink``.  Rows of no
-    sequence stay as they were.  Returns o, with ``return_lse`` (o, lse float32 [tokens, heads *
+    sequence stay as they were.  No gradient is recorded.  Returns o, with ``return_lse`` (o, lse float32 [tokens, heads *
     G])."""
     import torch
 

@@ -205,6 +205,37 @@ def test_autograd_takes_the_inverse(dtype, interleaved):
             G.rotary(x, pos, f, out=out)
 
 
+def test_a_captured_gradient_is_replayed():
+    # forward and backward in one graph, replayed with other rows and positions, eager calls between
+    import paper_2605_31105_amd as G
+    gen = torch.Generator().manual_seed(28)
+    x = torch.randn((33, 4, 64), generator=gen).cuda().requires_grad_()
+    w, pos, f = torch.randn((33, 4, 64), generator=gen).cuda(), _positions(33, 900, gen), G.rotary_freqs(48, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            torch.autograd.grad(G.rotary(x, pos, f, scale=1.5), x, w)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = G.rotary(x, pos, f, scale=1.5)
+        g, = torch.autograd.grad(y, x, w)
+        y = y.detach()
+    for turn in range(4):
+        with torch.no_grad():
+            x.copy_(torch.randn(x.shape, generator=gen))
+            w.copy_(torch.randn(x.shape, generator=gen))
+            pos.copy_(torch.randint(-50, 7000, (33,), generator=gen))
+            pos[turn] = G.NO_POSITION
+        graph.replay()
+        torch.cuda.synchronize()
+        on = torch.arange(33) != turn
+        want, = torch.autograd.grad(G.rotary(x, pos, f, scale=1.5), x, w)
+        assert torch.equal(g, want) and not g[turn].any()
+        assert torch.equal(y[on], G.rotary(x.detach(), pos, f, scale=1.5)[on])
+
+
 def test_there_and_back():
     import paper_2605_31105_amd as G
     gen = torch.Generator().manual_seed(2)
