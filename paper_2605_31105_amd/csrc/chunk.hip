@@ -18,8 +18,8 @@
 // come first).
 //
 // Measured (bf16, 8 KV heads of 128 columns, 4 query heads each): a token of 64 sequences of 500 to
-// 8000 keys 195 us (1.11 GB, 5.7 TB/s); beside two chunks of 512, 273; four chunks of 2048 over 4k to
-// 14k 1330 to 1370 (0.98 PFLOP/s, the clock at 2.0 GHz); one token over 2048 keys 16.5, a chain of reads.
+// 8000 keys 195 us (1.11 GB, 5.7 TB/s); beside two chunks of 512, 275; four chunks of 2048 over 4k to
+// 14k 1320 to 1350 (1.0 PFLOP/s, the clock at 1.8 GHz); one token over 2048 keys 16.5, a chain of reads.
 #include "attend_rows.h"
 #include "wide_rows.h"
 

@@ -12,8 +12,8 @@
 //  * A thread holds the sines and cosines of one group of pairs (16 bytes of a row, 32 with
 //    halves) of one token and goes over some heads with them, so that angles cost little
 //    beside the rows.  What bounds the call is HBM, or the launch.  (16k tokens of 40 heads of 128
-//    bf16 columns, 336 MB, 57 to 69 us by where its tensors lie, 4.9 to 5.9 TB/s; a chunk of 4096
-//    tokens stored, 101 MB, 20.7 us, 4.9; a large copy 4.9.)
+//    bf16 columns, 336 MB, 57 to 69 us by where its tensors lie, 4.9 to 5.9 TB/s, the kernel over one set
+//    of tensors 55, 6.1; a chunk of 4096 tokens stored, 101 MB, 20.6 us, 4.9; a large copy 4.9.)
 #include <type_traits>
 
 #include "grkv_device.h"
@@ -51,8 +51,8 @@ __device__ __forceinline__ float value(u16 x) { return bf16_to_f32(x); }
 __device__ __forceinline__ float value(float x) { return x; }
 
 // N neighbouring columns as floats, by loads of 16 bytes where N fills them, which pass the
-// caches: rows are read once (16k tokens of 40 heads, six tensors used in turn, 66.6 -> 56.9 us;
-// stored so too 57.1).
+// caches: rows are read once (16k tokens of 40 heads, six tensors used in turn, 66.6 -> 56.9 us
+// where those lay, 67 to 69 where others do; stored so too 57.1).
 template <int N, typename T>
 __device__ __forceinline__ void load_cols(const T* p, float (&x)[N]) {
   constexpr int V = 16 / sizeof(T);

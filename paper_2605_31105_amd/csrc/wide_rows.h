@@ -258,8 +258,8 @@ __device__ __forceinline__ void wide_rows(const AttendK& a, const Span& sn, int 
     }
     // products of the step, operands read ahead.  (Left to itself the compiler reads two ahead in
     // a step's kernel, and the products wait for LDS: 4 chunks of 2048 over 4k to 14k 1620 -> 1500
-    // us; three to eight ahead are equal.  A 16k prompt with a 4k window 993 -> 985, trees of 32
-    // over 32k 106 -> 105.)
+    // us; three to eight ahead are equal.  A 16k prompt over 8 units 2274 -> 2248; trees are as fast
+    // without.)
     constexpr int ALL = NK * 2 * DM, AHEAD = 4, EACH = TWO ? 2 : 1;
     __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
 #pragma unroll
