@@ -1103,8 +1103,9 @@ def rotary(x, positions, freqs, *, scale: float = 1.0, interleaved: bool = False
     Pairs are columns (i, i + dims / 2), or (2 i, 2 i + 1) with ``interleaved``; columns from
     dims on stay.  ``inverse`` rotates back, which is the gradient of the call.  ``out`` may be x, and else
     shares no element with it.
-    Rows at NO_POSITION are left as they were.  Returns out, which carries x's gradient (those rows'
-    is zero; positions and freqs are to stay until then); a call whose x needs one takes no ``out``."""
+    Rows at NO_POSITION are left as they were.  Returns out, which carries x's gradient (zero in those
+    rows; positions and freqs are to stay until then, freqs have none); a call whose x needs one takes no
+    ``out``."""
     import torch
 
     dev = x.get_device()
